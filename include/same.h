@@ -56,7 +56,9 @@
  *         s takes word r&3 of the block at counter {g, i, r>>2, s} (one block
  *         per column and quad of replicas; g < 2^32); the Gamma
  *         attempt t of CPT entry e at update q uses counter {e, t, 1<<24, q};
- *         the initial latent state uses {g>>2, i, r | 2<<24, 0}.
+ *         the initial latent state uses {g>>2, i, r | 2<<24, 0}; attention
+ *         dropout and dropout use {.., .., 3<<24, call} and {.., .., 4<<24,
+ *         call} (see same_cross_attention and same_dropout).
  */
 #ifndef SAME_H
 #define SAME_H
@@ -542,6 +544,113 @@ int same_step_graph(same_ctx *ctx, void *states, const uint8_t *obs, float *cpts
                     int32_t steps, void *workspace, same_graph **out);
 int same_graph_launch(same_graph *graph, void *stream);
 void same_graph_destroy(same_graph *graph);
+
+/*
+ * Operators of an amortised imputer.  same_predict answers a column's missing
+ * entries by n frozen-CPT sweeps; a network that attends from the missing
+ * entries to the same column's known entries answers them in one pass, and
+ * its answers can start the latent states.  Its two operators with state of
+ * their own are here: cross attention over ragged columns with gradients, and
+ * dropout whose mask is made again wherever it is needed.
+ */
+enum {
+    SAME_F32 = 0,
+    SAME_F16 = 1,
+    SAME_BF16 = 2
+};
+
+/*
+ * A plan of cross attention over n_segs segments (columns).  Segment s has
+ * the query tokens [q_ptr[s], q_ptr[s+1]) and the key tokens
+ * [k_ptr[s], k_ptr[s+1]) (host arrays of n_segs + 1, starting at 0; copied);
+ * either may be empty.  heads_q query heads share heads_kv key heads, query
+ * head h reading key head h / (heads_q / heads_kv).  head_dim is a multiple
+ * of 8 up to 128, dtype SAME_F16 or SAME_BF16.  Host only; the work lists are
+ * uploaded synchronously on the first device call per device, so make one
+ * before capturing a graph.  A plan serves any number of calls, one host
+ * thread at a time; calls on different streams need workspaces of their own.
+ * Errors: SAME_EINVAL, SAME_ESIZE (a segment with 2^30 keys, or 2^30 query
+ * rows of one key head; over 2^30 blocks), SAME_ENOMEM.
+ */
+typedef struct same_cross_plan same_cross_plan;
+
+int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr, int32_t heads_q,
+                      int32_t heads_kv, int32_t head_dim, int32_t dtype, same_cross_plan **out);
+/* Waits for the device (it frees device memory); null is a no-op. */
+void same_cross_destroy(same_cross_plan *plan);
+/* Workspace bytes of same_cross_attention (backward = 0) or
+ * same_cross_attention_backward (1); 0: the call takes a null workspace. */
+int same_cross_workspace_size(const same_cross_plan *plan, int32_t backward, size_t *bytes);
+
+/*
+ * out_i = sum_j D_ij P_ij v_j, P_i = softmax over the segment's visible keys
+ * of scale q_i . k_j.
+ *
+ * q [tokens][heads_q][head_dim], k and v [tokens][heads_kv][head_dim] have
+ * unit stride in the last axis and the given element strides of a token (row)
+ * and a head, multiples of 8 (0 repeats one); base pointers are 16-byte
+ * aligned.  key_mask (device, one byte per key token; null: all visible): 0
+ * hides the key from every query, and what k and v hold there, NaN included,
+ * is not used.  A query without a visible key gets out = 0, lse = -inf.
+ * scale is positive.  out is contiguous [tokens][heads_q][head_dim]; lse
+ * (null: not wanted) is contiguous [tokens][heads_q] fp32, the logarithm of
+ * the softmax's sum; the gradient needs it.
+ *
+ * Scores, maxima, sums and the weighted sum of values are fp32; probabilities
+ * are rounded to dtype before the product with v, out once at the end.
+ *
+ * drop in [0, 1) is taken to the nearest of 256 parts t (SAME_EINVAL where a
+ * positive drop rounds to 0 or 256): D_ij = 0 where the 8-bit number of
+ * (i, j) is below t, else 256 / (256 - t).  Key j of query row
+ * r = token * heads_q + head takes byte j % 4 of word (j / 8) % 4 of the
+ * Philox block at counter {2 (j / 32) + (j / 4) % 2, r mod 2^32,
+ * 3<<24 | r >> 32, call_id}, j counted within the segment.  The mask depends
+ * on nothing else and is not stored.
+ *
+ * out, lse and workspace must not overlap each other or an input.  Results do
+ * not depend on the device's scheduling (no atomics).  SAME_EINVAL,
+ * SAME_EALIGN, SAME_ESIZE (strides that pass 2^62 elements), SAME_EHIP,
+ * SAME_ENOMEM.
+ */
+int same_cross_attention(same_cross_plan *plan, const void *q, int64_t q_row, int64_t q_head,
+                         const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                         int64_t v_head, const uint8_t *key_mask, double scale, double drop,
+                         uint64_t seed, uint32_t call_id, void *out, float *lse, void *workspace,
+                         void *stream);
+
+/*
+ * Gradients of same_cross_attention: dq, dk and dv (contiguous, shaped like
+ * q, k and v) from dout (shaped like out, strides as for q), with the
+ * forward's arguments and its out and lse.  The gradient of a key head is the
+ * sum over the query heads that share it; inputs repeated by a zero stride
+ * get one gradient per repetition, which the caller sums.  Hidden keys get
+ * zeros.  Sums are fp32; P and dS are rounded to dtype before their products
+ * (in SAME_F16 dS must stay in its range, as with any loss scaling).
+ */
+int same_cross_attention_backward(same_cross_plan *plan, const void *q, int64_t q_row,
+                                  int64_t q_head, const void *k, int64_t k_row, int64_t k_head,
+                                  const void *v, int64_t v_row, int64_t v_head,
+                                  const uint8_t *key_mask, double scale, double drop, uint64_t seed,
+                                  uint32_t call_id, const void *out, const float *lse,
+                                  const void *dout, int64_t dout_row, int64_t dout_head, void *dq,
+                                  void *dk, void *dv, void *workspace, void *stream);
+
+/*
+ * y = residual + x * keep / (1 - drop) over a [rows][cols] matrix of dtype,
+ * with the given element strides of a row (residual may be null: zeros).
+ * The gradient with respect to x is the same call on dy with the same drop,
+ * seed and call_id and no residual.  drop is taken to the nearest of 65536
+ * parts t (SAME_EINVAL where a positive drop rounds to 0 or 65536): element
+ * e = row * cols + column is dropped where its 16-bit number is below t, half
+ * e % 2 (low first) of word (e / 2) % 4 of the Philox block at counter
+ * {(e / 8) mod 2^32, e / 8 >> 32, 4<<24, call_id}, and else scaled by
+ * 65536 / (65536 - t), in fp32, rounded once.  A dropped element does not use
+ * x (NaN included).  y may be x or residual itself (same strides) and must
+ * not overlap them otherwise.
+ */
+int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residual,
+                 int64_t residual_row, int64_t rows, int64_t cols, double drop, uint64_t seed,
+                 uint32_t call_id, void *y, int64_t y_row, void *stream);
 
 /* Message for the calling thread's last failed call ("" if none). */
 const char *same_last_error(void);

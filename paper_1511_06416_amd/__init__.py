@@ -23,6 +23,8 @@ __all__ = [
     "same_accumulate_hits", "same_predict", "same_counts_ema", "same_sample_cpts_ema", "same_stream_pass_ema",
     "same_grow_replicas", "same_debug_thresholds", "same_counts_noalloc", "same_stream_compact_layout",
     "same_stream_pass_compact", "same_step_graph", "same_graph_launch", "same_graph_destroy", "StepGraph",
+    "CrossPlan", "same_cross_create", "same_cross_destroy", "same_cross_workspace_size", "same_cross_attention",
+    "same_cross_attention_backward", "same_dropout",
     "pack_states", "unpack_states", "state_shape",
     "library_path", "load_library",
 ]
@@ -35,6 +37,7 @@ _lib = None
 SAME_OK, SAME_EINVAL, SAME_EGRAPH, SAME_ECARD, SAME_ESIZE, SAME_ENOMEM, SAME_EHIP, SAME_EALIGN = (
     0, -1, -2, -3, -4, -5, -6, -7)
 SAME_STREAM_COUNTS_ONLY = 1
+SAME_F32, SAME_F16, SAME_BF16 = 0, 1, 2
 _NAMES = {0: "SAME_OK", -1: "SAME_EINVAL", -2: "SAME_EGRAPH", -3: "SAME_ECARD",
           -4: "SAME_ESIZE", -5: "SAME_ENOMEM", -6: "SAME_EHIP", -7: "SAME_EALIGN"}
 
@@ -108,6 +111,15 @@ def load_library():
         L.same_graph_launch.argtypes = [P, P]
         L.same_graph_destroy.argtypes = [P]
         L.same_graph_destroy.restype = None
+        D = C.c_double
+        kv = [P, I64, I64] * 3 + [P, D, D, U64, U32]
+        L.same_cross_create.argtypes = [I64, P, P, I32, I32, I32, I32, C.POINTER(P)]
+        L.same_cross_destroy.argtypes = [P]
+        L.same_cross_destroy.restype = None
+        L.same_cross_workspace_size.argtypes = [P, I32, C.POINTER(C.c_size_t)]
+        L.same_cross_attention.argtypes = [P] + kv + [P, P, P, P]
+        L.same_cross_attention_backward.argtypes = [P] + kv + [P, P, P, I64, I64, P, P, P, P, P]
+        L.same_dropout.argtypes = [I32, P, I64, P, I64, I64, I64, D, U64, U32, P, I64, P]
         L.same_last_error.argtypes = []
         L.same_last_error.restype = C.c_char_p
         for f in ("same_create", "same_create_ex", "same_layout", "same_workspace_size", "same_sweep",
@@ -117,7 +129,8 @@ def load_library():
                   "same_accumulate_hits", "same_predict", "same_counts_ema", "same_sample_cpts_ema",
                   "same_stream_pass_ema", "same_grow_replicas", "same_debug_thresholds",
                   "same_counts_noalloc", "same_stream_compact_layout", "same_stream_pass_compact",
-                  "same_step_graph", "same_graph_launch"):
+                  "same_step_graph", "same_graph_launch", "same_cross_create", "same_cross_workspace_size",
+                  "same_cross_attention", "same_cross_attention_backward", "same_dropout"):
             getattr(L, f).restype = C.c_int
         _lib = L
         return L
@@ -523,3 +536,146 @@ def same_stream_pass_compact(ctx, lat_host, lat_off, obs_dev, data_dev, ld_dev, 
                                                    _ptr(data_dev), int(ld_dev), int(n_cols), int(nb), int(m),
                                                    _ptr(cpts), _ptr(mb_counts), _ptr(totals), int(seed), int(pass_id),
                                                    int(flags), _ptr(slots), _ptr(workspace), _stream(stream)))
+
+
+def _dtype(dtype):
+    """SAME_F32, SAME_F16 or SAME_BF16 of a torch dtype."""
+    code = {"torch.float32": SAME_F32, "torch.float16": SAME_F16, "torch.bfloat16": SAME_BF16}.get(str(dtype))
+    if code is None:
+        raise SameError(SAME_EINVAL, "dtype must be torch.float32, torch.float16 or torch.bfloat16, got %s" % dtype)
+    return code
+
+
+def _on_device(name, t):
+    if not t.is_cuda:
+        raise SameError(SAME_EINVAL, "%s must be a device tensor" % name)
+
+
+class CrossPlan:
+    """Owns one same_cross_plan: the ragged structure of a set of columns, the
+    heads and the type of same_cross_attention."""
+
+    def __init__(self, q_ptr, k_ptr, heads_q, heads_kv, head_dim, dtype):
+        qp = np.ascontiguousarray(q_ptr, dtype=np.int64)
+        kp = np.ascontiguousarray(k_ptr, dtype=np.int64)
+        if qp.ndim != 1 or qp.shape != kp.shape or len(qp) < 1:
+            raise SameError(SAME_EINVAL, "q_ptr and k_ptr must be one-dimensional and of one length, n_segs + 1")
+        h = C.c_void_p()
+        _check(load_library().same_cross_create(len(qp) - 1, qp.ctypes.data, kp.ctypes.data, int(heads_q),
+                                                int(heads_kv), int(head_dim), _dtype(dtype), C.byref(h)))
+        self._h = h
+        self.heads_q, self.heads_kv, self.head_dim, self.dtype = int(heads_q), int(heads_kv), int(head_dim), dtype
+        self.n_q, self.n_k = int(qp[-1]), int(kp[-1])
+
+    @property
+    def handle(self):
+        return self._h
+
+    def workspace_bytes(self, backward=False) -> int:
+        out = C.c_size_t()
+        _check(load_library().same_cross_workspace_size(self._h, 1 if backward else 0, C.byref(out)))
+        return int(out.value)
+
+    def new_workspace(self, backward=False, device="cuda"):
+        """A workspace of the forward pass, or (backward) one that serves both."""
+        import torch
+        size = self.workspace_bytes(False)
+        if backward:
+            size = max(size, self.workspace_bytes(True))
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            load_library().same_cross_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _tensor(self, name, t, tokens, heads, contiguous=False):
+        """Shape, type and layout of a [tokens][heads][head_dim] tensor; its
+        address and the element strides of a token and a head."""
+        want = (tokens, heads, self.head_dim)
+        _on_device(name, t)
+        if tuple(t.shape) != want or t.dtype != self.dtype:
+            raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
+                            % (name, self.dtype, want, t.dtype, tuple(t.shape)))
+        if contiguous and not t.is_contiguous():
+            raise SameError(SAME_EINVAL, "%s must be contiguous" % name)
+        if t.numel() and t.stride(2) != 1:
+            raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+        return [_ptr(t), t.stride(0) if tokens > 1 else 0, t.stride(1) if heads > 1 else 0]
+
+    def _inputs(self, q, k, v, key_mask, workspace, backward):
+        args = (self._tensor("q", q, self.n_q, self.heads_q) + self._tensor("k", k, self.n_k, self.heads_kv)
+                + self._tensor("v", v, self.n_k, self.heads_kv))
+        if key_mask is not None:
+            _on_device("key_mask", key_mask)
+            if tuple(key_mask.shape) != (self.n_k,) or key_mask.element_size() != 1 or not key_mask.is_contiguous():
+                raise SameError(SAME_EINVAL, "key_mask must be a contiguous byte per key token")
+        need = self.workspace_bytes(backward)
+        if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+            raise SameError(SAME_EINVAL, "workspace must have at least %d bytes" % need)
+        return args + [_ptr(key_mask)]
+
+    def _lse(self, lse):
+        import torch
+        _on_device("lse", lse)
+        if tuple(lse.shape) != (self.n_q, self.heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise SameError(SAME_EINVAL, "lse must be contiguous torch.float32 of shape %s" % ((self.n_q, self.heads_q),))
+        return _ptr(lse)
+
+
+def same_cross_create(q_ptr, k_ptr, heads_q, heads_kv, head_dim, dtype) -> CrossPlan:
+    return CrossPlan(q_ptr, k_ptr, heads_q, heads_kv, head_dim, dtype)
+
+
+def same_cross_destroy(plan: CrossPlan) -> None:
+    plan.close()
+
+
+def same_cross_workspace_size(plan: CrossPlan, backward=False) -> int:
+    return plan.workspace_bytes(backward)
+
+
+def same_cross_attention(plan, q, k, v, out, lse, workspace, key_mask=None, scale=None, drop=0.0, seed=0, call_id=0,
+                         stream=None):
+    """lse may be None; scale defaults to head_dim ** -0.5."""
+    args = plan._inputs(q, k, v, key_mask, workspace, False)
+    _check(load_library().same_cross_attention(
+        plan.handle, *args, float(plan.head_dim ** -0.5 if scale is None else scale), float(drop), int(seed),
+        int(call_id), plan._tensor("out", out, plan.n_q, plan.heads_q, True)[0], None if lse is None else plan._lse(lse),
+        _ptr(workspace), _stream(stream)))
+
+
+def same_cross_attention_backward(plan, q, k, v, out, lse, dout, dq, dk, dv, workspace, key_mask=None, scale=None,
+                                  drop=0.0, seed=0, call_id=0, stream=None):
+    args = plan._inputs(q, k, v, key_mask, workspace, True)
+    _check(load_library().same_cross_attention_backward(
+        plan.handle, *args, float(plan.head_dim ** -0.5 if scale is None else scale), float(drop), int(seed),
+        int(call_id), plan._tensor("out", out, plan.n_q, plan.heads_q, True)[0], plan._lse(lse),
+        *plan._tensor("dout", dout, plan.n_q, plan.heads_q),
+        plan._tensor("dq", dq, plan.n_q, plan.heads_q, True)[0],
+        plan._tensor("dk", dk, plan.n_k, plan.heads_kv, True)[0],
+        plan._tensor("dv", dv, plan.n_k, plan.heads_kv, True)[0], _ptr(workspace), _stream(stream)))
+
+
+def same_dropout(x, y, drop, seed, call_id, residual=None, stream=None):
+    """Two-dimensional tensors of one type with unit stride in the last axis."""
+    dtype = _dtype(x.dtype)
+    rows = []
+    for name, t in (("x", x), ("y", y), ("residual", residual)):
+        if t is None:
+            rows.append(0)
+            continue
+        _on_device(name, t)
+        if t.dim() != 2 or t.shape != x.shape or t.dtype != x.dtype:
+            raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like x" % name)
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+        rows.append(t.stride(0))
+    _check(load_library().same_dropout(dtype, _ptr(x), rows[0], _ptr(residual), rows[2], x.shape[0], x.shape[1],
+                                       float(drop), int(seed), int(call_id), _ptr(y), rows[1], _stream(stream)))

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "../../include/same.h"
+#include "errors.hpp"
 #include "graph.hpp"
 #include "launch.hpp"
 
@@ -517,6 +518,12 @@ SlotGeom slot_geom(const same_ctx *ctx, int32_t m, int64_t nb) {
 }
 
 }  // namespace
+
+namespace same {
+
+int record_error(int code, const std::string &msg) { return set_error(code, msg); }
+
+}  // namespace same
 
 extern "C" {
 

@@ -1,0 +1,126 @@
+// Dropout with the residual sum, for gfx950: y = residual + x * keep * gain.
+// The mask is never stored: element e of the matrix (row * cols + column)
+// takes 16 bits, number e % 8 of the Philox block at counter
+// {e / 8, high word, 4 << 24, call}, so any later pass makes it again.
+#include "cross.hpp"
+#include "philox.hpp"
+
+namespace same {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 2;  // groups of eight elements a thread has in flight
+
+template <typename T>
+struct alignas(sizeof(T) == 4 ? 32 : 16) Group {
+    T v[8];
+};
+
+__device__ __forceinline__ dev::Philox4 group_bits(const DropoutParams &p, int64_t g) {
+    return dev::philox4x32_10((uint32_t)g, (uint32_t)((uint64_t)g >> 32), 4u << 24, p.call_id, p.seed_lo, p.seed_hi);
+}
+
+__device__ __forceinline__ float dropped(const DropoutParams &p, const dev::Philox4 &w, int e, float x, float base) {
+    const uint32_t h = (w.w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu;
+    return h >= p.drop_below ? __builtin_fmaf(x, p.keep_gain, base) : base;
+}
+
+// Groups that lie whole in a row (or in a contiguous matrix), 16-byte
+// accesses; per_row groups a row, the last n % 8 elements of a contiguous
+// matrix by their own thread.
+template <typename T, bool RES, bool DROP>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p, int64_t n_groups, int64_t per_row,
+                                                           int tail) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kPer) + threadIdx.x;
+    Group<T> x[kPer], r[kPer];
+    int64_t row[kPer], off[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int64_t g = first + k * kThreads;
+        if (g >= n_groups) continue;
+        row[k] = per_row == n_groups ? 0 : n_groups <= 0xFFFFFFFFll ? (uint32_t)g / (uint32_t)per_row : g / per_row;
+        off[k] = (g - row[k] * per_row) * 8;
+        x[k] = *(const Group<T> *)((const T *)p.x + row[k] * p.x_row + off[k]);
+        if (RES) r[k] = *(const Group<T> *)((const T *)p.residual + row[k] * p.r_row + off[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int64_t g = first + k * kThreads;
+        if (g >= n_groups) continue;
+        dev::Philox4 w;
+        if (DROP) w = group_bits(p, g);
+        Group<T> y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float base = RES ? (float)r[k].v[e] : 0.0f;
+            y.v[e] = (T)(DROP ? dropped(p, w, e, (float)x[k].v[e], base) : (float)x[k].v[e] + base);
+        }
+        *(Group<T> *)((T *)p.y + row[k] * p.y_row + off[k]) = y;
+    }
+    if (tail && first == 0) {
+        dev::Philox4 w;
+        if (DROP) w = group_bits(p, n_groups);
+        for (int e = 0; e < tail; ++e) {
+            const int64_t at = n_groups * 8 + e;
+            const float v = (float)((const T *)p.x)[at], base = RES ? (float)((const T *)p.residual)[at] : 0.0f;
+            ((T *)p.y)[at] = (T)(DROP ? dropped(p, w, e, v, base) : v + base);
+        }
+    }
+}
+
+// Any strides and alignment: a thread takes a group of eight, element by element.
+template <typename T, bool RES, bool DROP>
+__global__ __launch_bounds__(kThreads) void dropout_any_kernel(DropoutParams p, int64_t n) {
+    const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (g * 8 >= n) return;
+    dev::Philox4 w;
+    if (DROP) w = group_bits(p, g);
+    int64_t row = g * 8 / p.cols, col = g * 8 - row * p.cols;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (g * 8 + e < n) {
+            const float v = (float)((const T *)p.x)[row * p.x_row + col];
+            const float base = RES ? (float)((const T *)p.residual)[row * p.r_row + col] : 0.0f;
+            ((T *)p.y)[row * p.y_row + col] = (T)(DROP ? dropped(p, w, e, v, base) : v + base);
+            if (++col == p.cols) {
+                col = 0;
+                ++row;
+            }
+        }
+    }
+}
+
+template <typename T, bool RES, bool DROP>
+hipError_t launch(const DropoutParams &p, hipStream_t s) {
+    const int64_t n = p.rows * p.cols;
+    const bool whole = p.x_row == p.cols && p.y_row == p.cols && (!RES || p.r_row == p.cols);
+    const uintptr_t mix = (uintptr_t)p.x | (uintptr_t)p.y | (RES ? (uintptr_t)p.residual : 0);
+    const int64_t steps = p.x_row | p.y_row | (RES ? p.r_row : 0) | p.cols;
+    if (mix % 16 == 0 && (whole || steps % 8 == 0)) {
+        const int64_t groups = n / 8, per_block = kThreads * kPer;
+        const dim3 grid((uint32_t)((groups + per_block - 1) / per_block + (groups == 0)));
+        dropout_kernel<T, RES, DROP><<<grid, kThreads, 0, s>>>(p, groups, whole ? groups : p.cols / 8,
+                                                               whole ? (int)(n % 8) : 0);
+    } else {
+        const int64_t groups = (n + 7) / 8;
+        dropout_any_kernel<T, RES, DROP><<<dim3((uint32_t)((groups + kThreads - 1) / kThreads)), kThreads, 0, s>>>(p, n);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_typed(const DropoutParams &p, hipStream_t s) {
+    if (p.drop_below)
+        return p.residual ? launch<T, true, true>(p, s) : launch<T, false, true>(p, s);
+    return p.residual ? launch<T, true, false>(p, s) : launch<T, false, false>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutParams &p, int dtype, hipStream_t s) {
+    if (dtype == kCrossBf16) return launch_typed<__bf16>(p, s);
+    if (dtype == kCrossF16) return launch_typed<_Float16>(p, s);
+    return launch_typed<float>(p, s);
+}
+
+}  // namespace same

@@ -1,0 +1,513 @@
+// C ABI of the imputer's operators (declared in include/same.h): cross
+// attention over ragged segments with its gradients, and dropout.  Argument
+// checks, the work lists of a plan, its workspace and the launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/same.h"
+#include "cross.hpp"
+#include "errors.hpp"
+
+namespace {
+
+using same::CrossItem;
+using same::CrossJoin;
+using same::record_error;
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxAxis = (int64_t)1 << 30;  // rows or keys of one segment
+constexpr int64_t kMaxBlocks = (int64_t)1 << 30;
+
+inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p) % a == 0; }
+
+// The work list of one pass on the host.
+struct PassPlan {
+    std::vector<CrossItem> items;
+    std::vector<CrossJoin> joins;
+    int32_t own_waves = 1, cut_waves = 1, n_slots = 0;
+};
+
+struct DeviceLists {
+    int device = -1;
+    char *base = nullptr;
+    CrossItem *rows = nullptr, *keys = nullptr;
+    CrossJoin *row_joins = nullptr, *key_joins = nullptr;
+};
+
+}  // namespace
+
+struct same_cross_plan {
+    int32_t heads_q = 0, heads_kv = 0, dim = 0, dtype = 0;
+    int64_t n_q = 0, n_k = 0;  // tokens
+    PassPlan rows, keys;       // owners: query rows (forward, dQ); keys (dK, dV)
+    // workspace: parts and their statistics (forward); delta, then parts (gradient)
+    size_t ws_ml = 0, ws_forward = 0, ws_part = 0, ws_backward = 0;
+    std::vector<DeviceLists> dev;
+    std::mutex mu;
+};
+
+namespace {
+
+// Splits the owners of every segment into tiles and, where the tiles alone
+// leave the chip idle, the other axis into parts.
+int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vector<int64_t> &k_ptr, int32_t group,
+               int32_t heads_kv, bool own_keys) {
+    const int64_t n = (int64_t)q_ptr.size() - 1;
+    auto rows_of = [&](int64_t s) { return (q_ptr[s + 1] - q_ptr[s]) * group; };
+    auto keys_of = [&](int64_t s) { return k_ptr[s + 1] - k_ptr[s]; };
+    int64_t max_own = 0, max_cut = 0;
+    for (int64_t s = 0; s < n; ++s) {
+        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
+        if (own == 0) continue;
+        max_own = std::max(max_own, own);
+        max_cut = std::max(max_cut, cut);
+    }
+    pp.own_waves = max_own > 32 ? 4 : 1;
+    pp.cut_waves = pp.own_waves == 1 && max_cut > 64 ? 4 : 1;
+    const int64_t tile = 32 * pp.own_waves;
+    int64_t blocks = 0;
+    double work = 0.0;
+    for (int64_t s = 0; s < n; ++s) {
+        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
+        const int64_t t = (own + tile - 1) / tile * heads_kv;
+        blocks += t;
+        work += (double)t * (double)cut;
+    }
+    int64_t part = kMaxAxis;
+    if (blocks < 512) part = std::max<int64_t>(256, (int64_t)std::ceil(work / 512.0 / 128.0) * 128);
+    // longest first; the tiles of a segment stay together
+    std::vector<int64_t> order;
+    for (int64_t s = 0; s < n; ++s)
+        if ((own_keys ? keys_of(s) : rows_of(s)) > 0) order.push_back(s);
+    std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) {
+        return (own_keys ? rows_of(a) : keys_of(a)) > (own_keys ? rows_of(b) : keys_of(b));
+    });
+    for (int64_t s : order) {
+        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
+        const int64_t parts = std::max<int64_t>(1, (cut + part - 1) / part);
+        const int64_t step = parts == 1 ? std::max<int64_t>(cut, 1) : ((cut + parts - 1) / parts + 127) / 128 * 128;
+        for (int64_t o = 0; o < own; o += tile) {
+            CrossItem it;
+            it.q0 = q_ptr[s];
+            it.k0 = k_ptr[s];
+            it.own0 = (int32_t)o;
+            it.n_own = (int32_t)std::min(tile, own - o);
+            it.slot = -1;
+            it.pad = 0;
+            const int32_t first = pp.n_slots;
+            int64_t b = 0;
+            do {
+                it.beg = (int32_t)b;
+                it.end = (int32_t)std::min(cut, b + step);
+                if (step < cut) it.slot = pp.n_slots++;
+                pp.items.push_back(it);
+                b += step;
+            } while (b < cut);
+            if (step < cut) pp.joins.push_back(CrossJoin{it.q0, it.k0, it.own0, it.n_own, first, pp.n_slots - first});
+            if ((int64_t)pp.items.size() * heads_kv > kMaxBlocks)
+                return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
+        }
+    }
+    return SAME_OK;
+}
+
+template <typename T>
+size_t bytes_of(const std::vector<T> &v) {
+    return align_up(v.size() * sizeof(T));
+}
+
+// The plan's lists on the current device, uploaded on first use (synchronous).
+int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
+    int device = -1;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return record_error(SAME_EHIP, std::string("hipGetDevice: ") + hipGetErrorString(e));
+    std::lock_guard<std::mutex> lock(pl->mu);
+    if ((int)pl->dev.size() <= device) pl->dev.resize(device + 1);
+    DeviceLists &d = pl->dev[device];
+    if (d.device != device) {
+        const size_t at[5] = {0, bytes_of(pl->rows.items), bytes_of(pl->rows.joins), bytes_of(pl->keys.items),
+                              bytes_of(pl->keys.joins)};
+        size_t off[5] = {0, 0, 0, 0, 0};
+        for (int i = 1; i < 5; ++i) off[i] = off[i - 1] + at[i];
+        std::vector<char> host(std::max<size_t>(off[4], 1));
+        auto put = [&](size_t o, const void *src, size_t bytes) {
+            if (bytes) std::memcpy(host.data() + o, src, bytes);
+        };
+        put(off[0], pl->rows.items.data(), pl->rows.items.size() * sizeof(CrossItem));
+        put(off[1], pl->rows.joins.data(), pl->rows.joins.size() * sizeof(CrossJoin));
+        put(off[2], pl->keys.items.data(), pl->keys.items.size() * sizeof(CrossItem));
+        put(off[3], pl->keys.joins.data(), pl->keys.joins.size() * sizeof(CrossJoin));
+        char *base = nullptr;
+        e = hipMalloc((void **)&base, host.size());
+        if (e == hipSuccess) e = hipMemcpy(base, host.data(), host.size(), hipMemcpyHostToDevice);
+        if (e != hipSuccess) {
+            if (base) (void)hipFree(base);
+            return record_error(e == hipErrorOutOfMemory ? SAME_ENOMEM : SAME_EHIP,
+                                std::string("uploading the plan's lists: ") + hipGetErrorString(e));
+        }
+        d.base = base;
+        d.rows = (CrossItem *)(base + off[0]);
+        d.row_joins = (CrossJoin *)(base + off[1]);
+        d.keys = (CrossItem *)(base + off[2]);
+        d.key_joins = (CrossJoin *)(base + off[3]);
+        d.device = device;
+    }
+    *out = d;
+    return SAME_OK;
+}
+
+struct Extent {
+    uintptr_t lo = 0, hi = 0;
+};
+
+inline Extent extent(const void *p, int64_t bytes) { return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}; }
+inline bool overlap(const Extent &a, const Extent &b) {
+    return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
+}
+
+// A strided input [tokens][heads][dim] of 16-bit elements.
+int check_input(const char *name, const void *p, int64_t tokens, int64_t heads, int64_t dim, int64_t row, int64_t head,
+                Extent *ext) {
+    if (tokens == 0) return SAME_OK;
+    if (!p) return record_error(SAME_EINVAL, std::string(name) + " is null");
+    if (row < 0 || head < 0) return record_error(SAME_EINVAL, std::string(name) + ": strides must not be negative");
+    if (!aligned(p, 16) || row % 8 != 0 || head % 8 != 0)
+        return record_error(SAME_EALIGN,
+                            std::string(name) + " must be 16-byte aligned, with strides that are multiples of 8");
+    const double last = (double)(tokens - 1) * (double)row + (double)(heads - 1) * (double)head + (double)dim;
+    if (last >= 4.6e18) return record_error(SAME_ESIZE, std::string(name) + ": strides pass 2^62 elements");
+    *ext = extent(p, 2 * ((tokens - 1) * row + (heads - 1) * head + dim));
+    return SAME_OK;
+}
+
+int check_output(const char *name, const void *p, int64_t elements, int64_t size, Extent *ext) {
+    if (elements == 0) return SAME_OK;
+    if (!p) return record_error(SAME_EINVAL, std::string(name) + " is null");
+    if (!aligned(p, 16)) return record_error(SAME_EALIGN, std::string(name) + " must be 16-byte aligned");
+    *ext = extent(p, elements * size);
+    return SAME_OK;
+}
+
+// Writable buffers must not overlap each other or what is read.
+int check_apart(const std::vector<Extent> &writes, const std::vector<Extent> &reads) {
+    for (size_t i = 0; i < writes.size(); ++i) {
+        for (size_t j = i + 1; j < writes.size(); ++j)
+            if (overlap(writes[i], writes[j])) return record_error(SAME_EINVAL, "two outputs overlap");
+        for (const Extent &r : reads)
+            if (overlap(writes[i], r)) return record_error(SAME_EINVAL, "an output overlaps an input");
+    }
+    return SAME_OK;
+}
+
+// drop as a number of `steps`: what lies below it is dropped.
+int drop_threshold(double drop, uint32_t steps, uint32_t *below) {
+    *below = 0;
+    if (!(drop >= 0.0 && drop < 1.0)) return record_error(SAME_EINVAL, "drop must lie in [0, 1)");
+    if (drop == 0.0) return SAME_OK;
+    *below = (uint32_t)std::nearbyint(drop * steps);
+    if (*below == 0 || *below >= steps)
+        return record_error(SAME_EINVAL, "drop must be 0 or round to 1 .. " + std::to_string(steps - 1) +
+                                             " parts of " + std::to_string(steps));
+    return SAME_OK;
+}
+
+int check_hip(hipError_t e, const char *what) {
+    if (e == hipSuccess) return SAME_OK;
+    return record_error(SAME_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// What both passes share: plan, inputs, scale, dropout, workspace.
+struct Call {
+    same::CrossParams p;
+    DeviceLists d;
+    std::vector<Extent> reads;
+};
+
+int prepare_call(same_cross_plan *pl, Call &c, const void *q, int64_t q_row, int64_t q_head, const void *k,
+                 int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head, const uint8_t *key_mask,
+                 double scale, double drop, uint64_t seed, uint32_t call_id, void *workspace, size_t need) {
+    if (!(scale > 0.0) || !std::isfinite(scale) || !std::isfinite((float)scale))
+        return record_error(SAME_EINVAL, "scale must be positive and finite");
+    Extent e;
+    int rc = check_input("q", q, pl->n_q, pl->heads_q, pl->dim, q_row, q_head, &e);
+    if (rc) return rc;
+    c.reads.push_back(e);
+    e = Extent();
+    rc = check_input("k", k, pl->n_k, pl->heads_kv, pl->dim, k_row, k_head, &e);
+    if (rc) return rc;
+    c.reads.push_back(e);
+    e = Extent();
+    rc = check_input("v", v, pl->n_k, pl->heads_kv, pl->dim, v_row, v_head, &e);
+    if (rc) return rc;
+    c.reads.push_back(e);
+    if (key_mask) c.reads.push_back(extent(key_mask, pl->n_k));
+    std::memset((void *)&c.p, 0, sizeof(c.p));
+    rc = drop_threshold(drop, 256, &c.p.drop_below);
+    if (rc) return rc;
+    if (need && !workspace) return record_error(SAME_EINVAL, "workspace is null");
+    if (!aligned(workspace, kAlign)) return record_error(SAME_EALIGN, "workspace must be 256-byte aligned");
+    c.p.q = {q, q_row, q_head};
+    c.p.k = {k, k_row, k_head};
+    c.p.v = {v, v_row, v_head};
+    c.p.key_mask = key_mask;
+    c.p.heads_q = pl->heads_q;
+    c.p.heads_kv = pl->heads_kv;
+    c.p.group = pl->heads_q / pl->heads_kv;
+    c.p.dim = pl->dim;
+    c.p.scale = (float)scale;
+    c.p.keep_gain = 256.0f / (256.0f - (float)c.p.drop_below);
+    c.p.seed_lo = (uint32_t)seed;
+    c.p.seed_hi = (uint32_t)(seed >> 32);
+    c.p.call_id = call_id;
+    return SAME_OK;
+}
+
+same::CrossPass pass_of(const PassPlan &pp, const CrossItem *items, const CrossJoin *joins) {
+    same::CrossPass w;
+    w.items = items;
+    w.joins = joins;
+    w.n_items = (int32_t)pp.items.size();
+    w.n_joins = (int32_t)pp.joins.size();
+    w.n_slots = pp.n_slots;
+    w.own_waves = pp.own_waves;
+    w.cut_waves = pp.cut_waves;
+    return w;
+}
+
+int check_ptr(const char *name, int64_t n_segs, const int64_t *ptr, std::vector<int64_t> &out) {
+    if (!ptr) return record_error(SAME_EINVAL, std::string(name) + " is null");
+    out.assign(ptr, ptr + n_segs + 1);
+    if (out[0] != 0) return record_error(SAME_EINVAL, std::string(name) + "[0] must be 0");
+    for (int64_t s = 0; s < n_segs; ++s) {
+        if (out[s + 1] < out[s]) return record_error(SAME_EINVAL, std::string(name) + " must not decrease");
+        if (out[s + 1] - out[s] >= kMaxAxis)
+            return record_error(SAME_ESIZE, std::string(name) + ": a segment has 2^30 entries or more");
+    }
+    return SAME_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr, int32_t heads_q, int32_t heads_kv,
+                      int32_t head_dim, int32_t dtype, same_cross_plan **out) {
+    if (!out) return record_error(SAME_EINVAL, "out is null");
+    *out = nullptr;
+    if (n_segs < 0) return record_error(SAME_EINVAL, "n_segs must not be negative");
+    if (heads_q < 1 || heads_kv < 1 || heads_q % heads_kv != 0)
+        return record_error(SAME_EINVAL, "heads_q must be a positive multiple of heads_kv");
+    if (heads_q > 65536) return record_error(SAME_ESIZE, "heads_q must be at most 65536");
+    if (head_dim < 8 || head_dim > 128 || head_dim % 8 != 0)
+        return record_error(SAME_EINVAL, "head_dim must be a multiple of 8 in [8, 128]");
+    if (dtype != SAME_F16 && dtype != SAME_BF16) return record_error(SAME_EINVAL, "dtype must be SAME_F16 or SAME_BF16");
+    same_cross_plan *pl = new (std::nothrow) same_cross_plan();
+    if (!pl) return record_error(SAME_ENOMEM, "out of host memory");
+    int rc;
+    try {
+        std::vector<int64_t> qp, kp;
+        rc = check_ptr("q_ptr", n_segs, q_ptr, qp);
+        if (!rc) rc = check_ptr("k_ptr", n_segs, k_ptr, kp);
+        const int32_t group = heads_q / heads_kv;
+        for (int64_t s = 0; !rc && s < n_segs; ++s)
+            if ((qp[s + 1] - qp[s]) * group >= kMaxAxis)
+                rc = record_error(SAME_ESIZE, "a segment has 2^30 query rows of one key head or more");
+        if (!rc) rc = build_pass(pl->rows, qp, kp, group, heads_kv, false);
+        if (!rc) rc = build_pass(pl->keys, qp, kp, group, heads_kv, true);
+        if (!rc) {
+            pl->heads_q = heads_q;
+            pl->heads_kv = heads_kv;
+            pl->dim = head_dim;
+            pl->dtype = dtype;
+            pl->n_q = qp[n_segs];
+            pl->n_k = kp[n_segs];
+            auto owners = [&](const PassPlan &pp) {
+                return (size_t)pp.n_slots * (size_t)heads_kv * 32 * (size_t)pp.own_waves;
+            };
+            const size_t row = (size_t)head_dim * sizeof(float);
+            pl->ws_ml = align_up(owners(pl->rows) * row);
+            pl->ws_forward = pl->ws_ml + align_up(owners(pl->rows) * 2 * sizeof(float));
+            pl->ws_part = align_up((size_t)pl->n_q * (size_t)heads_q * sizeof(float));
+            pl->ws_backward = pl->ws_part + align_up(std::max(owners(pl->rows), 2 * owners(pl->keys)) * row);
+        }
+    } catch (const std::bad_alloc &) {
+        rc = record_error(SAME_ENOMEM, "out of host memory");
+    }
+    if (rc) {
+        delete pl;
+        return rc;
+    }
+    *out = pl;
+    return SAME_OK;
+}
+
+void same_cross_destroy(same_cross_plan *pl) {
+    if (!pl) return;
+    int cur = -1;
+    for (DeviceLists &d : pl->dev)
+        if (d.device >= 0) {
+            if (cur < 0) (void)hipGetDevice(&cur);
+            (void)hipSetDevice(d.device);
+            (void)hipFree(d.base);
+        }
+    if (cur >= 0) (void)hipSetDevice(cur);
+    delete pl;
+}
+
+int same_cross_workspace_size(const same_cross_plan *pl, int32_t backward, size_t *bytes) {
+    if (!pl || !bytes) return record_error(SAME_EINVAL, "plan and bytes must be non-null");
+    *bytes = backward ? pl->ws_backward : pl->ws_forward;
+    return SAME_OK;
+}
+
+int same_cross_attention(same_cross_plan *pl, const void *q, int64_t q_row, int64_t q_head, const void *k,
+                         int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                         const uint8_t *key_mask, double scale, double drop, uint64_t seed, uint32_t call_id,
+                         void *out, float *lse, void *workspace, void *stream) {
+    if (!pl) return record_error(SAME_EINVAL, "plan is null");
+    try {
+        Call c;
+        int rc = prepare_call(pl, c, q, q_row, q_head, k, k_row, k_head, v, v_row, v_head, key_mask, scale, drop, seed,
+                              call_id, workspace, pl->ws_forward);
+        if (rc) return rc;
+        const int64_t rows = pl->n_q * pl->heads_q;
+        std::vector<Extent> writes(3);
+        rc = check_output("out", out, rows * pl->dim, 2, &writes[0]);
+        if (rc) return rc;
+        if (lse) {
+            if (!aligned(lse, 4)) return record_error(SAME_EALIGN, "lse must be 4-byte aligned");
+            writes[1] = extent(lse, rows * 4);
+        }
+        writes[2] = extent(workspace, (int64_t)pl->ws_forward);
+        rc = check_apart(writes, c.reads);
+        if (rc) return rc;
+        if (rows == 0) return SAME_OK;
+        rc = lists_for_current_device(pl, &c.d);
+        if (rc) return rc;
+        c.p.out = out;
+        c.p.lse = lse;
+        c.p.part = (float *)workspace;
+        c.p.part_ml = (float *)((char *)workspace + pl->ws_ml);
+        return check_hip(same::launch_cross_forward(c.p, pass_of(pl->rows, c.d.rows, c.d.row_joins), pl->dtype,
+                                                    (hipStream_t)stream),
+                         "cross attention launch");
+    } catch (const std::bad_alloc &) {
+        return record_error(SAME_ENOMEM, "out of host memory");
+    }
+}
+
+int same_cross_attention_backward(same_cross_plan *pl, const void *q, int64_t q_row, int64_t q_head, const void *k,
+                                  int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                                  const uint8_t *key_mask, double scale, double drop, uint64_t seed, uint32_t call_id,
+                                  const void *out, const float *lse, const void *dout, int64_t dout_row,
+                                  int64_t dout_head, void *dq, void *dk, void *dv, void *workspace, void *stream) {
+    if (!pl) return record_error(SAME_EINVAL, "plan is null");
+    try {
+        Call c;
+        int rc = prepare_call(pl, c, q, q_row, q_head, k, k_row, k_head, v, v_row, v_head, key_mask, scale, drop, seed,
+                              call_id, workspace, pl->ws_backward);
+        if (rc) return rc;
+        const int64_t rows = pl->n_q * pl->heads_q, keys = pl->n_k * pl->heads_kv;
+        Extent e;
+        rc = check_input("dout", dout, pl->n_q, pl->heads_q, pl->dim, dout_row, dout_head, &e);
+        if (rc) return rc;
+        c.reads.push_back(e);
+        e = Extent();
+        rc = check_output("out", out, rows * pl->dim, 2, &e);
+        if (rc) return rc;
+        c.reads.push_back(e);
+        if (rows) {
+            if (!lse) return record_error(SAME_EINVAL, "lse is null");
+            if (!aligned(lse, 4)) return record_error(SAME_EALIGN, "lse must be 4-byte aligned");
+            c.reads.push_back(extent(lse, rows * 4));
+        }
+        std::vector<Extent> writes(4);
+        rc = check_output("dq", dq, rows * pl->dim, 2, &writes[0]);
+        if (!rc) rc = check_output("dk", dk, keys * pl->dim, 2, &writes[1]);
+        if (!rc) rc = check_output("dv", dv, keys * pl->dim, 2, &writes[2]);
+        if (rc) return rc;
+        writes[3] = extent(workspace, (int64_t)pl->ws_backward);
+        rc = check_apart(writes, c.reads);
+        if (rc) return rc;
+        if (rows == 0 && keys == 0) return SAME_OK;
+        rc = lists_for_current_device(pl, &c.d);
+        if (rc) return rc;
+        c.p.delta = (float *)workspace;
+        c.p.part = (float *)((char *)workspace + pl->ws_part);
+        c.p.dout = {dout, dout_row, dout_head};
+        c.p.out_in = out;
+        c.p.lse = (float *)lse;
+        c.p.dq = dq;
+        c.p.dk = dk;
+        c.p.dv = dv;
+        hipStream_t s = (hipStream_t)stream;
+        // dQ first: it leaves delta for the other pass
+        rc = check_hip(same::launch_cross_dq(c.p, pass_of(pl->rows, c.d.rows, c.d.row_joins), pl->dtype, s),
+                       "query gradient launch");
+        if (rc) return rc;
+        return check_hip(same::launch_cross_dkv(c.p, pass_of(pl->keys, c.d.keys, c.d.key_joins), pl->dtype, s),
+                         "key gradient launch");
+    } catch (const std::bad_alloc &) {
+        return record_error(SAME_ENOMEM, "out of host memory");
+    }
+}
+
+int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residual, int64_t residual_row, int64_t rows,
+                 int64_t cols, double drop, uint64_t seed, uint32_t call_id, void *y, int64_t y_row, void *stream) {
+    if (dtype != SAME_F32 && dtype != SAME_F16 && dtype != SAME_BF16)
+        return record_error(SAME_EINVAL, "dtype must be SAME_F32, SAME_F16 or SAME_BF16");
+    if (rows < 0 || cols < 0) return record_error(SAME_EINVAL, "rows and cols must not be negative");
+    same::DropoutParams p;
+    int rc = drop_threshold(drop, 65536, &p.drop_below);
+    if (rc) return rc;
+    if (rows == 0 || cols == 0) return SAME_OK;
+    if (!x || !y) return record_error(SAME_EINVAL, "x and y must be non-null");
+    if (x_row < 0 || (residual && residual_row < 0))
+        return record_error(SAME_EINVAL, "row strides must not be negative");
+    if (rows > 1 && y_row < cols) return record_error(SAME_EINVAL, "y_row must be at least cols");
+    const int64_t size = dtype == SAME_F32 ? 4 : 2;
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(residual, size))
+        return record_error(SAME_EALIGN, "x, residual and y must be aligned to their elements");
+    if ((double)rows * (double)cols >= 1e12) return record_error(SAME_ESIZE, "rows * cols must stay below 10^12");
+    const double far = (double)(rows - 1) * (double)std::max(x_row, std::max(y_row, residual ? residual_row : 0));
+    if (far >= 1e18) return record_error(SAME_ESIZE, "row strides pass 10^18 elements");
+    if (rows == 1) x_row = y_row = residual_row = cols;
+    // y may be x or residual itself, or lie apart; column blocks of one wider
+    // buffer lie apart although their extents overlap
+    auto apart = [&](const void *a, int64_t a_row) {
+        if (a == y && a_row == y_row) return true;
+        if (!overlap(extent(a, ((rows - 1) * a_row + cols) * size), extent(y, ((rows - 1) * y_row + cols) * size)))
+            return true;
+        if (a_row != y_row) return false;
+        const int64_t step = y_row * size;
+        const int64_t d = (((int64_t)((uintptr_t)a - (uintptr_t)y)) % step + step) % step;
+        return d >= cols * size && d <= step - cols * size;
+    };
+    if (!apart(x, x_row)) return record_error(SAME_EINVAL, "y overlaps x without being x");
+    if (residual && !apart(residual, residual_row))
+        return record_error(SAME_EINVAL, "y overlaps residual without being residual");
+    p.x = x;
+    p.residual = residual;
+    p.y = y;
+    p.rows = rows;
+    p.cols = cols;
+    p.x_row = x_row;
+    p.r_row = residual_row;
+    p.y_row = y_row;
+    p.keep_gain = 65536.0f / (65536.0f - (float)p.drop_below);
+    p.seed_lo = (uint32_t)seed;
+    p.seed_hi = (uint32_t)(seed >> 32);
+    p.call_id = call_id;
+    return check_hip(same::launch_dropout(p, dtype, (hipStream_t)stream), "dropout launch");
+}
+
+}  // extern "C"

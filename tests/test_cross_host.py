@@ -1,0 +1,53 @@
+"""Plans of cross attention: host checks, no device."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1511_06416_amd as same
+
+
+@pytest.mark.parametrize("code,args", [
+    (same.SAME_EINVAL, dict(heads_q=3, heads_kv=2)),
+    (same.SAME_EINVAL, dict(heads_q=0)),
+    (same.SAME_EINVAL, dict(head_dim=0)),
+    (same.SAME_EINVAL, dict(head_dim=12)),
+    (same.SAME_EINVAL, dict(head_dim=136)),
+    (same.SAME_EINVAL, dict(dtype=torch.float32)),
+    (same.SAME_EINVAL, dict(dtype=torch.int8)),
+    (same.SAME_EINVAL, dict(q_ptr=[1, 3])),
+    (same.SAME_EINVAL, dict(q_ptr=[0, 3, 2], k_ptr=[0, 1, 1])),
+    (same.SAME_EINVAL, dict(q_ptr=[0, 3, 4])),
+    (same.SAME_ESIZE, dict(k_ptr=[0, 1 << 30])),
+    (same.SAME_ESIZE, dict(q_ptr=[0, 1 << 28])),
+    (same.SAME_ESIZE, dict(heads_q=1 << 17)),
+])
+def test_refused_plans(code, args):
+    ok = dict(q_ptr=[0, 3], k_ptr=[0, 5], heads_q=4, heads_kv=1, head_dim=64, dtype=torch.bfloat16)
+    with pytest.raises(same.SameError) as e:
+        same.same_cross_create(**dict(ok, **args))
+    assert e.value.code == code and str(e.value)
+
+
+def test_workspace():
+    """The gradient keeps delta; parts are needed where few rows meet many keys."""
+    p = same.same_cross_create([0, 3], [0, 5], 4, 1, 64, torch.bfloat16)
+    assert p.workspace_bytes() == 0 and p.workspace_bytes(True) >= 3 * 4 * 4
+    p = same.same_cross_create([0, 1], [0, 100_000], 4, 1, 64, torch.bfloat16)
+    assert p.workspace_bytes() > 0
+    p = same.same_cross_create([0, 100_000], [0, 3], 4, 1, 64, torch.bfloat16)
+    assert p.workspace_bytes(True) > 100_000 * 4 * 4
+
+
+def test_empty_plans():
+    for q_ptr, k_ptr in (([0], [0]), ([0, 0], [0, 0]), ([0, 0, 0], [0, 4, 4])):
+        p = same.same_cross_create(q_ptr, k_ptr, 1, 1, 8, torch.float16)
+        assert p.workspace_bytes() == 0
+        same.same_cross_destroy(p)
+        same.same_cross_destroy(p)
+
+
+def test_pointers_are_copied():
+    q_ptr = np.array([0, 5], dtype=np.int64)
+    p = same.same_cross_create(q_ptr, [0, 7], 1, 1, 8, torch.float16)
+    q_ptr[1] = 1 << 40
+    assert p.n_q == 5 and p.workspace_bytes(True) < 1 << 20
