@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsame.so")
-SOURCES = ["kernels.hip", "cross.hip", "dropout.hip", "api.cpp", "graph.cpp", "operators.cpp"]
+SOURCES = ["kernels.hip", "cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "dropout.hip", "api.cpp", "graph.cpp", "operators.cpp"]
 ARCH = os.environ.get("SAME_OFFLOAD_ARCH", "gfx950")
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 instructions.

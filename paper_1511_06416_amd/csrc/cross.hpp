@@ -1,5 +1,5 @@
 // Internal interface between the cross-attention and dropout entry points
-// (operators.cpp) and their gfx950 kernels (cross.hip, dropout.hip).
+// (operators.cpp) and their gfx950 kernels (cross_*.hip, dropout.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -1,0 +1,164 @@
+// Cross attention: the gradients of keys and values (gfx950).
+#include "cross_join.hpp"
+
+namespace same {
+namespace {
+
+using namespace cross;
+
+// -------------------------------------------------------- gradient: dK and dV
+//
+// The mirror image: a wave owns 32 keys of a key head (a lane one key) and
+// walks the query rows of every head that shares it, so that the sum over
+// those heads stays in its accumulators.  S = Q K^T (rows x keys),
+// dV^T += dO^T (D P), dK^T += Q^T dS.
+template <typename T, int NS, int OW, int CW, bool DROP>
+__global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams p) {
+    constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
+    constexpr int kTile = QT * Tile<NS>::kRowBytes;
+    constexpr int kBufs = CW > 1 ? 1 : 2;
+    constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ f32x4 stat[kBufs][2][QT / 4];
+    const int64_t lb = logical_block(p.chunk);
+    if (lb >= (int64_t)p.n_items * p.heads_kv) return;
+    const int hk = (int)(lb / p.n_items);
+    const CrossItem it = p.items[lb - (int64_t)hk * p.n_items];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int ow = wave % OW, cw = wave / OW;
+    const int own = ow * 32 + col;
+    const bool valid = own < it.n_own;
+    const int64_t tok = it.k0 + it.own0 + (valid ? own : 0);
+    const bool visible = valid && (!p.key_mask || p.key_mask[tok] != 0);
+    typename Vec<T>::x8 kf[NS], vf[NS];
+    load_own<T, NS>(kf, (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head, visible, half, p.dim);
+    load_own<T, NS>(vf, (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head, visible, half, p.dim);
+    f32x16 ok[ND], ov[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
+    const float c = p.scale * kLog2e;
+    const float gain = DROP ? p.keep_gain : 1.0f;
+
+    QueryStage<T, NS, QT, NT> st(p, it, hk);
+    auto stats = [&](int buf, int row) {
+        for (int i = threadIdx.x; i < QT; i += NT) {
+            float l = kInf, d = 0.0f;
+            if (row + i < it.end) {
+                const int64_t id = row_id(p, it.q0, row + i, hk);
+                l = p.lse[id];
+                l = l == -kInf ? kInf : l * kLog2e;
+                d = p.delta[id];
+            }
+            ((float *)stat[buf][0])[i] = l;
+            ((float *)stat[buf][1])[i] = d;
+        }
+    };
+    if (it.beg < it.end) {
+        st.load(p);
+        st.store(lds, lds + kTile);
+        stats(0, it.beg);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int row = it.beg; row < it.end; row += QT) {
+        const bool more = row + QT < it.end;
+        if (more) st.load(p);
+        const char *tq = lds + buf * 2 * kTile, *tg = tq + kTile;
+        const int base = cw * 32;
+        f32x16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            s = mfma(read_rows<T, NS>(tq, base + col, 2 * t + half), kf[t], s);
+            dp = mfma(read_rows<T, NS>(tg, base + col, 2 * t + half), vf[t], dp);
+        }
+        uint32_t keep = 0xFFFFFFFF;  // bit i: the block's row i keeps this lane's key
+        if (DROP) {
+            // the flags are made row by row, as in the other passes (a lane a
+            // row, 16 keys); a ballot per element turns them into one word of
+            // 32 rows per key, and lane l takes the word of key l % 32
+            const int rr = row + base + col;
+            const int64_t id = row_id(p, it.q0, rr < it.end ? rr : it.end - 1, hk);
+            const uint32_t mine = keep_bits(p, id, (it.own0 + ow * 32) >> 5, half);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint64_t b = __ballot((mine >> e) & 1);
+                if (col == acc_row(e, 0)) keep = (uint32_t)b;
+                if (col == acc_row(e, 1)) keep = (uint32_t)(b >> 32);
+            }
+        }
+        f32x16 w;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 l4 = stat[buf][0][(base + 8 * g + 4 * half) >> 2];
+            const f32x4 d4 = stat[buf][1][(base + 8 * g + 4 * half) >> 2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 4 * g + i;
+                float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -l4[i]));
+                x = visible ? x : 0.0f;
+                float d = dp[e];
+                w[e] = x;
+                if (DROP) {
+                    const bool kept = (keep >> acc_row(e, half)) & 1;
+                    d = kept ? d * gain : 0.0f;
+                    w[e] = kept ? x : 0.0f;
+                }
+                s[e] = x * (d - d4[i]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const typename Vec<T>::x8 wf = round8<T>(w, 8 * t), df = round8<T>(s, 8 * t);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                ov[dt] = mfma(read_columns<T, NS>(tg, base + 16 * t, dt, lane), wf, ov[dt]);
+                ok[dt] = mfma(read_columns<T, NS>(tq, base + 16 * t, dt, lane), df, ok[dt]);
+            }
+        }
+        if (kBufs == 1) __syncthreads();
+        if (more) {
+            const int nb = kBufs == 1 ? 0 : buf ^ 1;
+            st.store(lds + nb * 2 * kTile, lds + nb * 2 * kTile + kTile);
+            stats(nb, row + QT);
+            buf = nb;
+        }
+        __syncthreads();
+    }
+    if (CW > 1) {
+        join_waves<ND, OW, CW>(ok, lds, ow, cw, lane);
+        join_waves<ND, OW, CW>(ov, lds, ow, cw, lane);
+        if (cw != 0) return;
+    }
+    if (!valid) return;
+    if (!visible)  // whatever the queries hold, a hidden key's gradients are zero
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
+    if (it.slot >= 0) {
+        const int64_t at = ((int64_t)it.slot * p.heads_kv + hk) * (32 * OW) + own;
+        write_part<ND>(p.part + 2 * at * p.dim, ok, half, p.dim);
+        write_part<ND>(p.part + (2 * at + 1) * p.dim, ov, half, p.dim);
+        return;
+    }
+    const int64_t at = (tok * p.heads_kv + hk) * p.dim;
+    write_owner<T, ND>((T *)p.dk + at, ok, p.scale, half, p.dim);
+    write_owner<T, ND>((T *)p.dv + at, ov, gain, half, p.dim);
+}
+
+struct Pass {
+    template <typename T, int NS, int OW, int CW, bool DROP>
+    static void run(const CrossParams &p, hipStream_t s) {
+        cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+    }
+    template <typename T>
+    static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
+        cross_join_grad_kernel<T, 2><<<grid, 256, 0, s>>>(p, w.joins, w.n_joins, 32 * w.own_waves);
+    }
+};
+
+}  // namespace
+
+hipError_t launch_cross_dkv(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s) {
+    return cross::launch_pass<Pass>(p, w, dtype, s);
+}
+
+}  // namespace same

@@ -1,0 +1,142 @@
+// Cross attention: the gradient of the queries (gfx950).
+#include "cross_join.hpp"
+
+namespace same {
+namespace {
+
+using namespace cross;
+
+// ------------------------------------------------------------- gradient: dQ
+//
+// A wave owns 32 query rows and walks the keys as the forward does:
+// P = exp(S - lse), dP^T = V dO^T, dS = P (D dP - delta),
+// dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV.
+template <typename T, int NS, int OW, int CW, bool DROP>
+__global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p) {
+    constexpr int NT = 64 * OW * CW, KT = 32 * CW, ND = (NS + 1) / 2;
+    constexpr int kTile = KT * Tile<NS>::kRowBytes;
+    constexpr int kBufs = CW > 1 ? 1 : 2;
+    constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ uint32_t seen[kBufs][KT / 4];
+    const int64_t lb = logical_block(p.chunk);
+    if (lb >= (int64_t)p.n_items * p.heads_kv) return;
+    const int hk = (int)(lb / p.n_items);
+    const CrossItem it = p.items[lb - (int64_t)hk * p.n_items];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int ow = wave % OW, cw = wave / OW;
+    const int own = ow * 32 + col;
+    const bool valid = own < it.n_own;
+    const int r = valid ? it.own0 + own : it.own0;
+    const int64_t row = row_id(p, it.q0, r, hk);
+    typename Vec<T>::x8 qf[NS], gf[NS];
+    load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
+    load_own<T, NS>(gf, (const T *)p.dout.p + row_at(p.dout, it.q0, r, p.group, hk), valid, half, p.dim);
+    float delta = 0.0f;
+    {
+        typename Vec<T>::x8 of[NS];
+        load_own<T, NS>(of, (const T *)p.out_in + row * p.dim, valid, half, p.dim);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
+        delta += other_half(delta);
+    }
+    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
+    f32x16 o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
+    const float c = p.scale * kLog2e;
+    const float lse = valid ? p.lse[row] : -kInf;
+    const float base2 = lse == -kInf ? kInf : lse * kLog2e;
+    const float gain = DROP ? p.keep_gain : 1.0f;
+
+    KeyStage<T, NS, KT, NT> st(p, it, hk);
+    auto flags = [&](int buf, int key) {
+        for (int i = threadIdx.x; i < KT; i += NT) {
+            bool in = key + i < it.end;
+            if (in && p.key_mask) in = p.key_mask[it.k0 + key + i] != 0;
+            ((uint8_t *)seen[buf])[i] = in;
+        }
+    };
+    if (it.beg < it.end) {
+        st.load(p);
+        st.store(lds, lds + kTile);
+        flags(0, it.beg);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int key = it.beg; key < it.end; key += KT) {
+        const bool more = key + KT < it.end;
+        if (more) st.load(p);
+        const char *tk = lds + buf * 2 * kTile, *tv = tk + kTile;
+        const int base = cw * 32;
+        f32x16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            s = mfma(read_rows<T, NS>(tk, base + col, 2 * t + half), qf[t], s);
+            dp = mfma(read_rows<T, NS>(tv, base + col, 2 * t + half), gf[t], dp);
+        }
+        uint32_t keep = 0xFFFF;
+        if (DROP) keep = keep_bits(p, row, (key + base) >> 5, half);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+            const float d = DROP ? ((keep >> e) & 1 ? dp[e] * gain : 0.0f) : dp[e];
+            s[e] = w * (d - delta);
+        }
+        if (p.key_mask || key + KT > it.end) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t f = seen[buf][(base + 8 * g + 4 * half) >> 2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!((f >> (8 * i)) & 1)) s[4 * g + i] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(read_columns<T, NS>(tk, base + 16 * t, dt, lane), df, o[dt]);
+        }
+        if (kBufs == 1) __syncthreads();
+        if (more) {
+            const int nb = kBufs == 1 ? 0 : buf ^ 1;
+            st.store(lds + nb * 2 * kTile, lds + nb * 2 * kTile + kTile);
+            flags(nb, key + KT);
+            buf = nb;
+        }
+        __syncthreads();
+    }
+    if (CW > 1) {
+        join_waves<ND, OW, CW>(o, lds, ow, cw, lane);
+        if (cw != 0) return;
+    }
+    if (!valid) return;
+    if (it.slot >= 0) {
+        const int64_t at = ((int64_t)it.slot * p.heads_kv + hk) * (32 * OW) + own;
+        write_part<ND>(p.part + at * p.dim, o, half, p.dim);
+        return;
+    }
+    write_owner<T, ND>((T *)p.dq + row * p.dim, o, p.scale, half, p.dim);
+}
+
+struct Pass {
+    template <typename T, int NS, int OW, int CW, bool DROP>
+    static void run(const CrossParams &p, hipStream_t s) {
+        cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+    }
+    template <typename T>
+    static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
+        cross_join_grad_kernel<T, 1><<<grid, 256, 0, s>>>(p, w.joins, w.n_joins, 32 * w.own_waves);
+    }
+};
+
+}  // namespace
+
+hipError_t launch_cross_dq(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s) {
+    return cross::launch_pass<Pass>(p, w, dtype, s);
+}
+
+}  // namespace same

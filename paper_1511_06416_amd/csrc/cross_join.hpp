@@ -1,0 +1,39 @@
+// The join of a gradient's parts.
+#pragma once
+
+#include "cross_common.hpp"
+
+namespace same {
+namespace cross {
+
+// Sums the parts of dQ (SIDES = 1) or of dK and dV (SIDES = 2), in order.
+template <typename T, int SIDES>
+__global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, const CrossJoin *joins, int32_t n_joins,
+                                                              int tile) {
+    const int hk = blockIdx.x / n_joins;
+    const CrossJoin j = joins[blockIdx.x - hk * n_joins];
+    const int quads = p.dim / 4;
+    for (int idx = threadIdx.x; idx < j.n_own * quads * SIDES; idx += blockDim.x) {
+        const int own = idx / (quads * SIDES), side = (idx / quads) % SIDES, d = (idx % quads) * 4;
+        f32x4 acc = 0.0f;
+        for (int s = 0; s < j.n_parts; ++s) {
+            const int64_t at = ((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own;
+            acc += *(const f32x4 *)(p.part + (SIDES * at + side) * p.dim + d);
+        }
+        T *dst;
+        float gain = p.scale;
+        if (SIDES == 1) {
+            dst = (T *)p.dq + row_id(p, j.q0, j.own0 + own, hk) * p.dim;
+        } else {
+            dst = (T *)(side ? p.dv : p.dk) + ((j.k0 + j.own0 + own) * p.heads_kv + hk) * p.dim;
+            gain = side ? p.keep_gain : p.scale;
+        }
+        typename Vec<T>::x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (T)(acc[i] * gain);
+        *(typename Vec<T>::x4 *)(dst + d) = w;
+    }
+}
+
+}  // namespace cross
+}  // namespace same
