@@ -588,8 +588,8 @@ int same_cross_workspace_size(const same_cross_plan *plan, int32_t backward, siz
  *
  * q [tokens][heads_q][head_dim], k and v [tokens][heads_kv][head_dim] have
  * unit stride in the last axis and the given element strides of a token (row)
- * and a head, multiples of 8 (0 repeats one); base pointers are 16-byte
- * aligned.  key_mask (device, one byte per key token; null: all visible): 0
+ * and a head, multiples of 8 (0 repeats one), a token's below 2^25; base
+ * pointers are 16-byte aligned.  key_mask (device, one byte per key token; null: all visible): 0
  * hides the key from every query, and what k and v hold there, NaN included,
  * is not used.  A query without a visible key gets out = 0, lse = -inf.
  * scale is positive.  out is contiguous [tokens][heads_q][head_dim]; lse
@@ -609,7 +609,7 @@ int same_cross_workspace_size(const same_cross_plan *plan, int32_t backward, siz
  *
  * out, lse and workspace must not overlap each other or an input.  Results do
  * not depend on the device's scheduling (no atomics).  SAME_EINVAL,
- * SAME_EALIGN, SAME_ESIZE (strides that pass 2^62 elements), SAME_EHIP,
+ * SAME_EALIGN, SAME_ESIZE (a token's stride), SAME_EHIP,
  * SAME_ENOMEM.
  */
 int same_cross_attention(same_cross_plan *plan, const void *q, int64_t q_row, int64_t q_head,

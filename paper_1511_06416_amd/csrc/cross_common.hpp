@@ -31,34 +31,47 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
-// LDS tiles hold rows of kPitch 16-byte chunks.  Chunk c of row r sits at
-// c ^ turn(r), so that both reads are free of bank conflicts: a chunk of 16
-// consecutive rows (matrix operand, 16 bytes a lane) and 64 bytes of four
-// consecutive rows (transposed operand).
+// Rows of a head's width in LDS, 16-byte chunks, so that a read meets no bank
+// twice.  Two reads occur: "rows", a chunk of 16 consecutive rows (matrix
+// operand, 16 bytes a lane), and "columns", 64 bytes of each of four
+// consecutive rows (transposed operand, 8 bytes a lane).  A tile that is read
+// in one way only is padded (addresses are one register and constants); one
+// that is read in both has its chunks turned by the row number instead.
+constexpr int lanes_per_row(int ns) { return ns <= 2 ? 4 : ns <= 4 ? 8 : 16; }
+
 template <int NS>
-struct Tile {
-    static constexpr int kChunks = 2 * NS;
-    static constexpr int kPitch = NS <= 2 ? 4 : NS <= 4 ? 8 : 16;
-    static constexpr int kRowBytes = kPitch * 16;
+struct RowTile {
+    static constexpr int kRowBytes = 32 * NS + 16;
+    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + c * 16; }
+};
+template <int NS>
+struct ColumnTile {
+    // four consecutive rows 64 bytes apart modulo 256
+    static constexpr int kRowBytes = NS == 4 || NS == 8 ? 32 * NS + 64 : 32 * NS;
+    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + c * 16; }
+};
+template <int NS>
+struct BothTile {
+    static constexpr int kRowBytes = lanes_per_row(NS) * 16;
     __device__ static __forceinline__ int turn(int r) {
-        if (kPitch == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
-        if (kPitch == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+        if (NS > 4) return ((r & 3) << 2) | ((r >> 2) & 3);
+        if (NS > 2) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
         return (r >> 2) & 3;
     }
     __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ turn(r)) << 4); }
 };
 
 // Matrix operand: chunk c of row r.
-template <typename T, int NS>
+template <typename T, typename Tile>
 __device__ __forceinline__ typename Vec<T>::x8 read_rows(const char *tile, int r, int c) {
-    return *(const typename Vec<T>::x8 *)(tile + Tile<NS>::at(r, c));
+    return *(const typename Vec<T>::x8 *)(tile + Tile::at(r, c));
 }
 
 // Transposed operand of 16 rows from row0 on (a multiple of 16) and columns
 // 32 dt .. 32 dt + 31: lane l gets column 32 dt + l % 32 of rows
 // row0 + 4 (l / 32) + {0..3} and the same eight rows further: the rows that
 // the accumulator layout of a 32x32 product gives a lane.
-template <typename T, int NS>
+template <typename T, typename Tile>
 __device__ __forceinline__ typename Vec<T>::x8 read_columns(const char *tile, int row0, int dt, int lane) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int t = lane & 15;
@@ -68,8 +81,8 @@ __device__ __forceinline__ typename Vec<T>::x8 read_columns(const char *tile, in
         s16x4 h[2];
         typename Vec<T>::x8 v;
     } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile<NS>::at(r, c) + (t & 1) * 8));
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile<NS>::at(r + 8, c) + (t & 1) * 8));
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile::at(r, c) + (t & 1) * 8));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile::at(r + 8, c) + (t & 1) * 8));
     return u.v;
 }
 
@@ -92,16 +105,23 @@ __device__ __forceinline__ int64_t row_id(const CrossParams &p, int64_t q0, int 
     return (q0 + i) * p.heads_q + hk * p.group + r - i * p.group;
 }
 
-// Keep flags of query row `row` and the 16 keys a lane holds of the 32-key
-// block kb, bit e = accumulator element e.
+// The 16 numbers of query row `row` and the keys a lane holds of the 32-key
+// block kb: byte e % 4 of word e / 4 belongs to accumulator element e.
+__device__ __forceinline__ dev::Philox4 keep_words(const CrossParams &p, int64_t row, int kb, int half) {
+    return dev::philox4x32_10((uint32_t)(2 * kb + half), (uint32_t)row, (3u << 24) | (uint32_t)((uint64_t)row >> 32),
+                              p.call_id, p.seed_lo, p.seed_hi);
+}
+__device__ __forceinline__ bool kept(const dev::Philox4 &w, int e, uint32_t below) {
+    return ((w.w[e >> 2] >> (8 * (e & 3))) & 255u) >= below;
+}
+
+// The same as flags, bit e = accumulator element e.
 __device__ __forceinline__ uint32_t keep_bits(const CrossParams &p, int64_t row, int kb, int half) {
-    const dev::Philox4 w = dev::philox4x32_10((uint32_t)(2 * kb + half), (uint32_t)row,
-                                              (3u << 24) | (uint32_t)((uint64_t)row >> 32), p.call_id,
-                                              p.seed_lo, p.seed_hi);
+    const dev::Philox4 w = keep_words(p, row, kb, half);
     uint32_t bits = 0;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-        bits |= (((w.w[e >> 2] >> (8 * (e & 3))) & 255u) >= p.drop_below ? 1u : 0u) << e;
+        bits |= (kept(w, e, p.drop_below) ? 1u : 0u) << e;
     return bits;
 }
 
@@ -113,88 +133,142 @@ __device__ __forceinline__ typename Vec<T>::x8 zero8() {
     return z;
 }
 
-// ROWS rows of two tensors on their way from global memory to LDS, 16 bytes a
-// lane: a thread takes the same chunk of every kStep-th row, so that one
-// address per tensor and a uniform step serve all of them.
+// ROWS rows on their way from global memory to LDS, 16 bytes a lane: a thread
+// takes the same chunk of every kStep-th row.
 template <typename T, int NS, int ROWS, int NT>
-struct Stage {
-    static constexpr int kSlots = Tile<NS>::kPitch;  // lanes per row (three in four work for NS = 6)
+struct Lanes {
+    static constexpr int kSlots = lanes_per_row(NS);  // three in four work for NS = 6
     static constexpr int kStep = NT / kSlots;
     static constexpr int kN = (ROWS + kStep - 1) / kStep;
     static_assert(NT % kSlots == 0 && (ROWS % kStep == 0 || kN == 1), "whole rows per thread");
-    typename Vec<T>::x8 a[kN], b[kN];
     __device__ static __forceinline__ int row() { return threadIdx.x / kSlots; }
     __device__ static __forceinline__ int slot() { return threadIdx.x % kSlots; }
     // lanes without a chunk of the tile, or past the width
     __device__ static __forceinline__ bool idle() { return slot() >= 2 * NS || row() >= ROWS; }
-
-    __device__ __forceinline__ void store(char *ta, char *tb) const {
-        const int r = row(), c = slot();
+    template <typename Tile>
+    __device__ static __forceinline__ void store(char *tile, const typename Vec<T>::x8 (&a)[kN]) {
         if (idle()) return;
 #pragma unroll
-        for (int n = 0; n < kN; ++n) {
-            *(typename Vec<T>::x8 *)(ta + Tile<NS>::at(r + n * kStep, c)) = a[n];
-            *(typename Vec<T>::x8 *)(tb + Tile<NS>::at(r + n * kStep, c)) = b[n];
-        }
+        for (int n = 0; n < kN; ++n) *(typename Vec<T>::x8 *)(tile + Tile::at(row() + n * kStep, slot())) = a[n];
     }
 };
 
-// Tiles of keys and values.  Rows past `end`, hidden keys and chunks past the
-// head's width become zeros, so that nothing a hidden key holds (infinities,
-// NaN) reaches a product.
+// Tiles of one of k and v.  The tile's base is uniform and a lane's part of
+// the address 32 bits (row strides are below 2^25 elements).  Rows past the
+// end, hidden keys and chunks past the head's width become zeros, so that
+// nothing a hidden key holds (infinities, NaN) reaches a product.  The mask
+// travels with the rows and is applied on the way into LDS, so that no load
+// waits for it.
 template <typename T, int NS, int ROWS, int NT>
-struct KeyStage : Stage<T, NS, ROWS, NT> {
-    typedef Stage<T, NS, ROWS, NT> Base;
-    const T *kp, *vp;
-    const uint8_t *mp;
-    int left;   // rows from this thread's first one to the end; 0 for idle lanes
-    __device__ __forceinline__ KeyStage(const CrossParams &p, const CrossItem &it, int hk) {
-        const int64_t tok = it.k0 + it.beg + Base::row();
-        kp = (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head + Base::slot() * 8;
-        vp = (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head + Base::slot() * 8;
-        mp = p.key_mask ? p.key_mask + tok : nullptr;
-        left = Base::slot() * 8 < p.dim && !Base::idle() ? it.end - it.beg - Base::row() : 0;
+struct KeyStage {
+    typedef Lanes<T, NS, ROWS, NT> L;
+    typename Vec<T>::x8 a[L::kN];
+    uint8_t m[L::kN];
+    const char *base;
+    const uint8_t *mask;
+    int64_t step;      // bytes of a row
+    uint32_t lane_at;  // bytes
+    int left;          // rows from the tile's first one to the end (uniform)
+    bool used;
+    __device__ __forceinline__ KeyStage(const CrossTensor &t, const CrossParams &p, const CrossItem &it, int hk,
+                                        int ahead = 0) {
+        const int64_t tok = it.k0 + it.beg + ahead;
+        step = 2 * t.row;
+        base = (const char *)t.p + tok * step + 2 * (int64_t)hk * t.head;
+        mask = p.key_mask ? p.key_mask + tok : nullptr;
+        lane_at = (uint32_t)L::row() * (uint32_t)step + (uint32_t)L::slot() * 16;
+        left = it.end - it.beg - ahead;
+        used = L::slot() * 8 < p.dim && !L::idle();
     }
-    __device__ __forceinline__ void load(const CrossParams &p) {
+    __device__ __forceinline__ void load() {
 #pragma unroll
-        for (int n = 0; n < Base::kN; ++n) {
-            bool in = n * Base::kStep < left;
-            if (in && p.key_mask) in = mp[n * Base::kStep] != 0;
-            this->a[n] = in ? *(const typename Vec<T>::x8 *)(kp + n * Base::kStep * p.k.row) : zero8<T>();
-            this->b[n] = in ? *(const typename Vec<T>::x8 *)(vp + n * Base::kStep * p.v.row) : zero8<T>();
+        for (int n = 0; n < L::kN; ++n) {
+            const bool in = used && L::row() + n * L::kStep < left;
+            a[n] = zero8<T>();
+            if (in) a[n] = *(const typename Vec<T>::x8 *)(base + n * L::kStep * step + lane_at);
+            if (mask) {
+                m[n] = 1;
+                if (in) m[n] = mask[n * L::kStep + L::row()];
+            }
         }
-        kp += ROWS * p.k.row;
-        vp += ROWS * p.v.row;
-        mp += ROWS;
+        base += ROWS * step;
+        if (mask) mask += ROWS;
         left -= ROWS;
     }
+    template <typename Tile>
+    __device__ __forceinline__ void store(char *tile) {
+        if (mask)
+#pragma unroll
+            for (int n = 0; n < L::kN; ++n)
+                if (!m[n]) a[n] = zero8<T>();
+        L::template store<Tile>(tile, a);
+    }
 };
 
-// Tiles of query rows of q and dout.
+// Which keys of a tile are there and visible: one bit a key in LDS.
+template <int KT>
+struct SeenStage {
+    static constexpr int kWords = (KT + 63) / 64;
+    const uint8_t *mask;
+    int left;
+    uint8_t m;
+    __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it) {
+        mask = p.key_mask ? p.key_mask + it.k0 + it.beg + threadIdx.x : nullptr;
+        left = (int)threadIdx.x < KT ? it.end - it.beg - (int)threadIdx.x : 0;
+        m = 0;
+    }
+    __device__ __forceinline__ void load() {
+        m = left > 0;
+        if (mask) {
+            if (left > 0) m = *mask;
+            mask += KT;
+        }
+        left -= KT;
+    }
+    __device__ __forceinline__ void store(uint64_t *words) const {
+        if (threadIdx.x < 64 * kWords) {
+            const uint64_t b = __ballot(m != 0);
+            if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = b;
+        }
+    }
+};
+
+// Accumulator elements whose bit is not set become `hidden`.
+__device__ __forceinline__ void hide(f32x16 &s, uint32_t bits, int half, float hidden) {
+    const uint32_t mine = bits >> (4 * half);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const uint32_t keep = (uint32_t)((int32_t)(mine << (31 - (8 * (e >> 2) + (e & 3)))) >> 31);
+        s[e] = __uint_as_float((__float_as_uint(s[e]) & keep) | (__float_as_uint(hidden) & ~keep));
+    }
+}
+
+// Tiles of query rows of q or dout.
 template <typename T, int NS, int ROWS, int NT>
-struct QueryStage : Stage<T, NS, ROWS, NT> {
-    typedef Stage<T, NS, ROWS, NT> Base;
+struct QueryStage {
+    typedef Lanes<T, NS, ROWS, NT> L;
+    typename Vec<T>::x8 a[L::kN];
     int64_t q0;
     int hk, r, end;
     __device__ __forceinline__ QueryStage(const CrossParams &p, const CrossItem &it, int head) {
         q0 = it.q0;
         hk = head;
-        r = it.beg + Base::row();
-        end = Base::slot() * 8 < p.dim && !Base::idle() ? it.end : 0;
+        r = it.beg + L::row();
+        end = L::slot() * 8 < p.dim && !L::idle() ? it.end : 0;
     }
-    __device__ __forceinline__ void load(const CrossParams &p) {
+    __device__ __forceinline__ void load(const CrossTensor &t, int group) {
 #pragma unroll
-        for (int n = 0; n < Base::kN; ++n) {
-            const int rr = r + n * Base::kStep;
-            const bool in = rr < end;
-            this->a[n] = in ? *(const typename Vec<T>::x8 *)((const T *)p.q.p + row_at(p.q, q0, rr, p.group, hk) +
-                                                             Base::slot() * 8)
-                            : zero8<T>();
-            this->b[n] = in ? *(const typename Vec<T>::x8 *)((const T *)p.dout.p +
-                                                             row_at(p.dout, q0, rr, p.group, hk) + Base::slot() * 8)
-                            : zero8<T>();
+        for (int n = 0; n < L::kN; ++n) {
+            const int rr = r + n * L::kStep;
+            a[n] = zero8<T>();
+            if (rr < end)
+                a[n] = *(const typename Vec<T>::x8 *)((const T *)t.p + row_at(t, q0, rr, group, hk) + L::slot() * 8);
         }
         r += ROWS;
+    }
+    template <typename Tile>
+    __device__ __forceinline__ void store(char *tile) const {
+        L::template store<Tile>(tile, a);
     }
 };
 
@@ -208,7 +282,15 @@ __device__ __forceinline__ void load_own(typename Vec<T>::x8 (&f)[NS], const T *
     }
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// A lane's value and that of the lane 32 away.
+__device__ __forceinline__ float both_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // Accumulator element e of a lane is row 8 (e / 4) + 4 half + e % 4.
 __device__ __forceinline__ int acc_row(int e, int half) { return 8 * (e >> 2) + 4 * half + (e & 3); }

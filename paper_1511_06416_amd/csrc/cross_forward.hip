@@ -16,14 +16,21 @@ using namespace cross;
 // the keys in accumulator order, and V^T is read transposed from LDS in the
 // same order.
 template <typename T, int NS, int OW, int CW, int KS, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, 2) void cross_forward_kernel(CrossParams p) {
+__global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross_forward_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, KT = 32 * KS * CW, ND = (NS + 1) / 2;
-    constexpr int kTile = KT * Tile<NS>::kRowBytes;
-    constexpr int kBufs = CW > 1 ? 1 : 2;
-    constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    typedef RowTile<NS> KTile;
+    typedef ColumnTile<NS> VTile;
+    constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
+    // With the rows split over waves, the scores of the next 32 keys are
+    // formed beside the softmax of the present ones; the tiles of k then begin
+    // 32 keys after those of v.  Otherwise one buffer each.
+    constexpr bool kAhead = OW > 1;
+    constexpr int kBufs = kAhead ? 2 : 1;
+    constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    __shared__ uint32_t seen[kBufs][KT / 4];
+    __shared__ uint64_t seen[2][SeenStage<KT>::kWords];
     __shared__ float stat[2][OW * CW * 32];
+    char *const lds_v = lds + kBufs * kTileK;
     const int64_t lb = logical_block(p.chunk);
     if (lb >= (int64_t)p.n_items * p.heads_kv) return;
     const int hk = (int)(lb / p.n_items);
@@ -34,6 +41,13 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_forward_kernel(CrossPar
     const bool valid = own < it.n_own;
     const int r = valid ? it.own0 + own : it.own0;
     const int64_t row = row_id(p, it.q0, r, hk);
+    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk, kAhead ? 32 : 0), sv(p.v, p, it, hk);
+    SeenStage<KT> ss(p, it);
+    KeyStage<T, NS, 32, NT> first(p.k, p, it, hk);
+    if (kAhead) first.load();
+    sk.load();
+    sv.load();
+    ss.load();
     typename Vec<T>::x8 qf[NS];
     load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
     f32x16 o[ND];
@@ -42,91 +56,99 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_forward_kernel(CrossPar
     float top = -kInf, sum = 0.0f;
     const float c = p.scale * kLog2e;
 
-    KeyStage<T, NS, KT, NT> st(p, it, hk);
-    auto flags = [&](int buf, int key) {
-        for (int i = threadIdx.x; i < KT; i += NT) {
-            bool in = key + i < it.end;
-            if (in && p.key_mask) in = p.key_mask[it.k0 + key + i] != 0;
-            ((uint8_t *)seen[buf])[i] = in;
-        }
+    auto scores = [&](const char *tk, int ks) {
+        f32x16 s = 0.0f;
+        const int base = (cw * KS + ks) * 32;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
+        return s;
     };
-    if (it.beg < it.end) {
-        st.load(p);
-        st.store(lds, lds + kTile);
-        flags(0, it.beg);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int key = it.beg; key < it.end; key += KT) {
-        const bool more = key + KT < it.end;
-        if (more) st.load(p);
-        const char *tk = lds + buf * 2 * kTile, *tv = tk + kTile;
-        f32x16 s[KS];
+    // The maximum that the exponentials refer to follows the running one only
+    // when that has grown by more than 2^8: until then the probabilities stay
+    // within 2^8, exact in the sums and in range for either type, and the
+    // accumulators need no rescaling.
+    auto raise = [&](const f32x16 &s) {
+        float mx = s[0];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            s[ks] = 0.0f;
-            const int base = (cw * KS + ks) * 32;
-#pragma unroll
-            for (int t = 0; t < NS; ++t) s[ks] = mfma(read_rows<T, NS>(tk, base + col, 2 * t + half), qf[t], s[ks]);
-        }
-        if (p.key_mask || key + KT > it.end) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const uint32_t f = seen[buf][((cw * KS + ks) * 32 + 8 * g + 4 * half) >> 2];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!((f >> (8 * i)) & 1)) s[ks][4 * g + i] = -kInf;
-                }
-        }
-        float mx = top;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[ks][e]);
-        mx = fmaxf(mx, other_half(mx));
-        if (__any(mx > top)) {
-            // a row whose keys are all hidden so far keeps -inf; 0 stands in for it below
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+        mx = both_max(mx);
+        if (__any(mx * c > __builtin_fmaf(top, c, 8.0f))) {
+            mx = fmaxf(mx, top);
+            // a row whose keys are all hidden so far keeps -inf; 0 stands in for it
             const float from = top == -kInf ? 0.0f : top, to = mx == -kInf ? 0.0f : mx;
-            const float f = __builtin_amdgcn_exp2f((from - to) * c);
-            const float g = top == -kInf ? 0.0f : f;
-            sum *= g;
+            const float f = top == -kInf ? 0.0f : __builtin_amdgcn_exp2f((from - to) * c);
+            sum *= f;
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) o[dt] *= g;
+            for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
             top = mx;
         }
+    };
+    auto weigh = [&](f32x16 &s, const char *tv, int key, int ks) {
         const float base2 = (top == -kInf ? 0.0f : top) * c;
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[ks][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks][e], c, -base2));
-                sum += s[ks][e];
-            }
-            if (DROP) {
-                const uint32_t keep = keep_bits(p, row, ((key + (cw * KS + ks) * 32)) >> 5, half);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[ks][e] = (keep >> e) & 1 ? s[ks][e] : 0.0f;
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const typename Vec<T>::x8 pf = round8<T>(s[ks], 8 * t);
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-                    o[dt] = mfma(read_columns<T, NS>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf, o[dt]);
-            }
+        for (int e = 0; e < 16; ++e) {
+            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+            part[e & 3] += s[e];
         }
-        if (kBufs == 1) __syncthreads();
-        if (more) {
-            const int nb = kBufs == 1 ? 0 : buf ^ 1;
-            st.store(lds + nb * 2 * kTile, lds + nb * 2 * kTile + kTile);
-            flags(nb, key + KT);
-            buf = nb;
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
+        if (DROP) {
+            const dev::Philox4 w = keep_words(p, row, (key + (cw * KS + ks) * 32) >> 5, half);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = kept(w, e, p.drop_below) ? s[e] : 0.0f;
         }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const typename Vec<T>::x8 pf = round8<T>(s, 8 * t);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+                o[dt] = mfma(read_columns<T, VTile>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf, o[dt]);
+        }
+    };
+    auto bits_of = [&](int buf, int ks) {
+        const int sub = cw * KS + ks;
+        return (uint32_t)(seen[buf][sub >> 1] >> (32 * (sub & 1)));
+    };
+
+    if (it.beg < it.end) {
+        f32x16 s;
+        sk.template store<KTile>(lds);
+        sv.template store<VTile>(lds_v);
+        ss.store(seen[0]);
+        if (kAhead) first.template store<KTile>(lds + kTileK);
         __syncthreads();
+        if (kAhead) {
+            s = scores(lds + kTileK, -cw * KS);
+            __syncthreads();
+        }
+        int buf = 0;
+        for (int key = it.beg; key < it.end; key += KT) {
+            sk.load();
+            sv.load();
+            ss.load();
+            const bool masked = p.key_mask || key + KT > it.end;
+            const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (!kAhead) s = scores(tk, ks);
+                if (masked) hide(s, bits_of(buf, ks), half, -kInf);
+                raise(s);
+                f32x16 next;
+                if (kAhead) next = scores(tk, ks);
+                weigh(s, tv, key, ks);
+                if (kAhead) s = next;
+            }
+            if (kAhead)
+                buf ^= 1;
+            else
+                __syncthreads();
+            sk.template store<KTile>(lds + buf * kTileK);
+            sv.template store<VTile>(lds_v + buf * kTileV);
+            ss.store(seen[buf]);
+            __syncthreads();
+        }
     }
-    sum += other_half(sum);
+    sum = both_sum(sum);
     if (CW > 1) {
         // the waves that share these rows bring their sums to the common maximum
         if (half == 0) {
@@ -201,7 +223,7 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
 struct Pass {
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_forward_kernel<T, NS, OW, CW, (OW > 1 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+        cross_forward_kernel<T, NS, OW, CW, (OW > 1 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

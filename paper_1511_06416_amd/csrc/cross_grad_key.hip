@@ -15,7 +15,8 @@ using namespace cross;
 template <typename T, int NS, int OW, int CW, bool DROP>
 __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
-    constexpr int kTile = QT * Tile<NS>::kRowBytes;
+    typedef BothTile<NS> Tile;
+    constexpr int kTile = QT * Tile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     const float c = p.scale * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
 
-    QueryStage<T, NS, QT, NT> st(p, it, hk);
+    QueryStage<T, NS, QT, NT> sq(p, it, hk), sg(p, it, hk);
     auto stats = [&](int buf, int row) {
         for (int i = threadIdx.x; i < QT; i += NT) {
             float l = kInf, d = 0.0f;
@@ -54,22 +55,27 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
         }
     };
     if (it.beg < it.end) {
-        st.load(p);
-        st.store(lds, lds + kTile);
+        sq.load(p.q, p.group);
+        sg.load(p.dout, p.group);
+        sq.template store<Tile>(lds);
+        sg.template store<Tile>(lds + kTile);
         stats(0, it.beg);
     }
     __syncthreads();
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
         const bool more = row + QT < it.end;
-        if (more) st.load(p);
+        if (more) {
+            sq.load(p.q, p.group);
+            sg.load(p.dout, p.group);
+        }
         const char *tq = lds + buf * 2 * kTile, *tg = tq + kTile;
         const int base = cw * 32;
         f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
-            s = mfma(read_rows<T, NS>(tq, base + col, 2 * t + half), kf[t], s);
-            dp = mfma(read_rows<T, NS>(tg, base + col, 2 * t + half), vf[t], dp);
+            s = mfma(read_rows<T, Tile>(tq, base + col, 2 * t + half), kf[t], s);
+            dp = mfma(read_rows<T, Tile>(tg, base + col, 2 * t + half), vf[t], dp);
         }
         uint32_t keep = 0xFFFFFFFF;  // bit i: the block's row i keeps this lane's key
         if (DROP) {
@@ -111,14 +117,15 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
             const typename Vec<T>::x8 wf = round8<T>(w, 8 * t), df = round8<T>(s, 8 * t);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
-                ov[dt] = mfma(read_columns<T, NS>(tg, base + 16 * t, dt, lane), wf, ov[dt]);
-                ok[dt] = mfma(read_columns<T, NS>(tq, base + 16 * t, dt, lane), df, ok[dt]);
+                ov[dt] = mfma(read_columns<T, Tile>(tg, base + 16 * t, dt, lane), wf, ov[dt]);
+                ok[dt] = mfma(read_columns<T, Tile>(tq, base + 16 * t, dt, lane), df, ok[dt]);
             }
         }
         if (kBufs == 1) __syncthreads();
         if (more) {
             const int nb = kBufs == 1 ? 0 : buf ^ 1;
-            st.store(lds + nb * 2 * kTile, lds + nb * 2 * kTile + kTile);
+            sq.template store<Tile>(lds + nb * 2 * kTile);
+            sg.template store<Tile>(lds + nb * 2 * kTile + kTile);
             stats(nb, row + QT);
             buf = nb;
         }

@@ -14,11 +14,14 @@ using namespace cross;
 template <typename T, int NS, int OW, int CW, bool DROP>
 __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, KT = 32 * CW, ND = (NS + 1) / 2;
-    constexpr int kTile = KT * Tile<NS>::kRowBytes;
+    typedef BothTile<NS> KTile;
+    typedef RowTile<NS> VTile;
+    constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
-    constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    __shared__ uint32_t seen[kBufs][KT / 4];
+    __shared__ uint64_t seen[kBufs][SeenStage<KT>::kWords];
+    char *const lds_v = lds + kBufs * kTileK;
     const int64_t lb = logical_block(p.chunk);
     if (lb >= (int64_t)p.n_items * p.heads_kv) return;
     const int hk = (int)(lb / p.n_items);
@@ -40,7 +43,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
-        delta += other_half(delta);
+        delta = both_sum(delta);
     }
     if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
     f32x16 o[ND];
@@ -51,31 +54,29 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
     const float base2 = lse == -kInf ? kInf : lse * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
 
-    KeyStage<T, NS, KT, NT> st(p, it, hk);
-    auto flags = [&](int buf, int key) {
-        for (int i = threadIdx.x; i < KT; i += NT) {
-            bool in = key + i < it.end;
-            if (in && p.key_mask) in = p.key_mask[it.k0 + key + i] != 0;
-            ((uint8_t *)seen[buf])[i] = in;
-        }
-    };
+    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
+    SeenStage<KT> ss(p, it);
     if (it.beg < it.end) {
-        st.load(p);
-        st.store(lds, lds + kTile);
-        flags(0, it.beg);
+        sk.load();
+        sv.load();
+        ss.load();
+        sk.template store<KTile>(lds);
+        sv.template store<VTile>(lds_v);
+        ss.store(seen[0]);
     }
     __syncthreads();
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
-        const bool more = key + KT < it.end;
-        if (more) st.load(p);
-        const char *tk = lds + buf * 2 * kTile, *tv = tk + kTile;
+        sk.load();
+        sv.load();
+        ss.load();
+        const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
         const int base = cw * 32;
         f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
-            s = mfma(read_rows<T, NS>(tk, base + col, 2 * t + half), qf[t], s);
-            dp = mfma(read_rows<T, NS>(tv, base + col, 2 * t + half), gf[t], dp);
+            s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
+            dp = mfma(read_rows<T, VTile>(tv, base + col, 2 * t + half), gf[t], dp);
         }
         uint32_t keep = 0xFFFF;
         if (DROP) keep = keep_bits(p, row, (key + base) >> 5, half);
@@ -85,28 +86,20 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
             const float d = DROP ? ((keep >> e) & 1 ? dp[e] * gain : 0.0f) : dp[e];
             s[e] = w * (d - delta);
         }
-        if (p.key_mask || key + KT > it.end) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint32_t f = seen[buf][(base + 8 * g + 4 * half) >> 2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!((f >> (8 * i)) & 1)) s[4 * g + i] = 0.0f;
-            }
-        }
+        if (p.key_mask || key + KT > it.end) hide(s, (uint32_t)(seen[buf][cw >> 1] >> (32 * (cw & 1))), half, 0.0f);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(read_columns<T, NS>(tk, base + 16 * t, dt, lane), df, o[dt]);
+            for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(read_columns<T, KTile>(tk, base + 16 * t, dt, lane), df, o[dt]);
         }
-        if (kBufs == 1) __syncthreads();
-        if (more) {
-            const int nb = kBufs == 1 ? 0 : buf ^ 1;
-            st.store(lds + nb * 2 * kTile, lds + nb * 2 * kTile + kTile);
-            flags(nb, key + KT);
-            buf = nb;
-        }
+        if (kBufs == 1)
+            __syncthreads();
+        else
+            buf ^= 1;
+        sk.template store<KTile>(lds + buf * kTileK);
+        sv.template store<VTile>(lds_v + buf * kTileV);
+        ss.store(seen[buf]);
         __syncthreads();
     }
     if (CW > 1) {

@@ -183,6 +183,8 @@ int check_input(const char *name, const void *p, int64_t tokens, int64_t heads, 
     if (!aligned(p, 16) || row % 8 != 0 || head % 8 != 0)
         return record_error(SAME_EALIGN,
                             std::string(name) + " must be 16-byte aligned, with strides that are multiples of 8");
+    if (tokens > 1 && row >= (int64_t)1 << 25)
+        return record_error(SAME_ESIZE, std::string(name) + ": a token's stride must stay below 2^25 elements");
     const double last = (double)(tokens - 1) * (double)row + (double)(heads - 1) * (double)head + (double)dim;
     if (last >= 4.6e18) return record_error(SAME_ESIZE, std::string(name) + ": strides pass 2^62 elements");
     *ext = extent(p, 2 * ((tokens - 1) * row + (heads - 1) * head + dim));

@@ -159,7 +159,7 @@ def test_repeated_inputs():
 
 def test_offsets_past_32_bits():
     """Key tokens more than 2^31 elements apart."""
-    n, d, row = 70, 64, 1 << 26
+    n, d, row = 140, 64, 1 << 24
     buf = torch.empty((n - 1) * row + 2 * d, dtype=BF, device="cuda")
     q, k, v, dout = inputs([5], [n], 2, 1, d, BF)
     far_k, far_v = (torch.as_strided(buf, (n, 1, d), (row, d, 1), o) for o in (0, d))
@@ -287,6 +287,8 @@ def test_refusals():
     odd = torch.zeros(90 * 2 * 64 + 1, dtype=BF, device="cuda")[1:].view(90, 2, 64)
     refuse(same.SAME_EALIGN, k=odd)
     refuse(same.SAME_EALIGN, k=torch.zeros(90, 2, 68, dtype=BF, device="cuda")[:, :, :64])
+    far = torch.empty(89 * (1 << 25) + 128, dtype=BF, device="cuda")
+    refuse(same.SAME_ESIZE, k=torch.as_strided(far, (90, 2, 64), (1 << 25, 64, 1)))
     need = plan.workspace_bytes(True)
     assert need > 0
     with pytest.raises(same.SameError):
