@@ -45,7 +45,7 @@ struct CrossParams {
     float *lse, *delta;        // [tokens][heads]
     float *part, *part_ml;     // parts: [slot][key head][owner][head_dim], (max, sum)
     const CrossItem *items;
-    int32_t n_items, chunk;    // chunk: consecutive blocks kept on one XCD
+    int32_t n_items;
     int32_t heads_q, heads_kv, group, dim;
     float scale;
     uint32_t drop_below;       // bytes below this are dropped (0: no dropout)

@@ -61,6 +61,43 @@ struct BothTile {
     __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ turn(r)) << 4); }
 };
 
+// Reads of BothTile tiles by one lane.  A turned chunk number is a fixed one
+// exclusive-or a constant of the read, so a lane needs two addresses; renew()
+// keeps the compiler from holding every combination in a register.
+template <typename T, int NS>
+struct BothReader {
+    typedef BothTile<NS> Tile;
+    typedef __attribute__((address_space(3))) const typename Vec<T>::x8 lds_x8;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    uint32_t rows, columns;
+    __device__ __forceinline__ BothReader(const char *lds, int lane) {
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
+        const int t = lane & 15, r = 4 * (lane >> 5) + (t >> 2);
+        rows = base + (uint32_t)Tile::at(lane & 31, lane >> 5);
+        columns = base + (uint32_t)Tile::at(r, 2 * ((lane >> 4) & 1) + ((t & 3) >> 1)) + (t & 1) * 8;
+    }
+    __device__ __forceinline__ void renew() {
+        asm volatile("" : "+v"(rows), "+v"(columns));
+    }
+    // chunk 2 t + lane / 32 of row lane % 32, `at` bytes (whole tiles) on
+    __device__ __forceinline__ typename Vec<T>::x8 row(uint32_t at, int t) const {
+        return *(lds_x8 *)(uintptr_t)((rows ^ (uint32_t)(t << 5)) + at);
+    }
+    // as read_columns, rows 16 half .. 16 half + 15
+    __device__ __forceinline__ typename Vec<T>::x8 column(uint32_t at, int half, int dt) const {
+        constexpr uint32_t kEight = 2 << 4;  // turn(r + 8) = turn(r) ^ 2
+        const uint32_t a = (columns ^ (uint32_t)(dt << 6)) + at + half * 16 * Tile::kRowBytes;
+        const uint32_t b = (columns ^ (uint32_t)(dt << 6) ^ kEight) + at + (half * 16 + 8) * Tile::kRowBytes;
+        union {
+            s16x4 h[2];
+            typename Vec<T>::x8 v;
+        } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)a);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)b);
+        return u.v;
+    }
+};
+
 // Matrix operand: chunk c of row r.
 template <typename T, typename Tile>
 __device__ __forceinline__ typename Vec<T>::x8 read_rows(const char *tile, int r, int c) {
@@ -84,15 +121,6 @@ __device__ __forceinline__ typename Vec<T>::x8 read_columns(const char *tile, in
     u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile::at(r, c) + (t & 1) * 8));
     u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + Tile::at(r + 8, c) + (t & 1) * 8));
     return u.v;
-}
-
-// Logical block of a launch: `chunk` consecutive ones run on one XCD (blocks
-// are dealt to the eight XCDs in turn), so that tiles which read the same
-// keys share an L2.
-__device__ __forceinline__ int64_t logical_block(int chunk) {
-    const int64_t b = blockIdx.x;
-    const int64_t slot = b >> 3;
-    return ((slot / chunk) * 8 + (b & 7)) * chunk + slot % chunk;
 }
 
 // A query row of a segment: its tensors' element offset.
@@ -243,32 +271,80 @@ __device__ __forceinline__ void hide(f32x16 &s, uint32_t bits, int half, float h
     }
 }
 
-// Tiles of query rows of q or dout.
+// Tiles of query rows: q and dout, and the softmax sums and deltas of the
+// rows.  Row numbers run over tokens and the heads of a group; the addresses
+// step by whole tiles, so that no division is left in the loop.
 template <typename T, int NS, int ROWS, int NT>
 struct QueryStage {
     typedef Lanes<T, NS, ROWS, NT> L;
-    typename Vec<T>::x8 a[L::kN];
-    int64_t q0;
-    int hk, r, end;
-    __device__ __forceinline__ QueryStage(const CrossParams &p, const CrossItem &it, int head) {
-        q0 = it.q0;
-        hk = head;
-        r = it.beg + L::row();
-        end = L::slot() * 8 < p.dim && !L::idle() ? it.end : 0;
-    }
-    __device__ __forceinline__ void load(const CrossTensor &t, int group) {
+    typename Vec<T>::x8 a[L::kN], b[L::kN];
+    const T *pq[L::kN], *pg[L::kN];
+    int g[L::kN];
+    int left;                          // rows from this thread's first one to the end; 0 for idle lanes
+    int64_t step_q, wrap_q, step_g, wrap_g;
+    int step, group;
+    int64_t id, step_id;               // this thread's row of the statistics
+    int id_g, id_left, heads;
+    float lse, delta;
+    __device__ __forceinline__ QueryStage(const CrossParams &p, const CrossItem &it, int hk) {
+        group = p.group;
+        heads = p.heads_q;
+        const int tokens = ROWS / group;
+        step = ROWS - tokens * group;
+        step_q = tokens * p.q.row + step * p.q.head;
+        wrap_q = p.q.row - group * p.q.head;
+        step_g = tokens * p.dout.row + step * p.dout.head;
+        wrap_g = p.dout.row - group * p.dout.head;
+        step_id = (int64_t)tokens * heads + step;
 #pragma unroll
         for (int n = 0; n < L::kN; ++n) {
-            const int rr = r + n * L::kStep;
-            a[n] = zero8<T>();
-            if (rr < end)
-                a[n] = *(const typename Vec<T>::x8 *)((const T *)t.p + row_at(t, q0, rr, group, hk) + L::slot() * 8);
+            const int r = it.beg + L::row() + n * L::kStep;
+            g[n] = r % group;
+            pq[n] = (const T *)p.q.p + row_at(p.q, it.q0, r, group, hk) + L::slot() * 8;
+            pg[n] = (const T *)p.dout.p + row_at(p.dout, it.q0, r, group, hk) + L::slot() * 8;
         }
-        r += ROWS;
+        left = L::slot() * 8 < p.dim && !L::idle() ? it.end - it.beg - L::row() : 0;
+        const int r = it.beg + (int)threadIdx.x;
+        id = row_id(p, it.q0, r, hk);
+        id_g = r % group;
+        id_left = (int)threadIdx.x < ROWS ? it.end - r : 0;
     }
+    __device__ __forceinline__ void load(const CrossParams &p) {
+#pragma unroll
+        for (int n = 0; n < L::kN; ++n) {
+            a[n] = b[n] = zero8<T>();
+            if (n * L::kStep < left) {
+                a[n] = *(const typename Vec<T>::x8 *)pq[n];
+                b[n] = *(const typename Vec<T>::x8 *)pg[n];
+            }
+            g[n] += step;
+            const bool over = g[n] >= group;
+            g[n] -= over ? group : 0;
+            pq[n] += step_q + (over ? wrap_q : 0);
+            pg[n] += step_g + (over ? wrap_g : 0);
+        }
+        left -= ROWS;
+        lse = -kInf;
+        delta = 0.0f;
+        if (id_left > 0) {
+            lse = p.lse[id];
+            delta = p.delta[id];
+        }
+        id_g += step;
+        const bool over = id_g >= group;
+        id_g -= over ? group : 0;
+        id += step_id + (over ? heads - group : 0);
+        id_left -= ROWS;
+    }
+    // A row without a visible key, or past the end, gets exponent -inf.
     template <typename Tile>
-    __device__ __forceinline__ void store(char *tile) const {
-        L::template store<Tile>(tile, a);
+    __device__ __forceinline__ void store(char *tq, char *tg, float *stat_lse, float *stat_delta) const {
+        L::template store<Tile>(tq, a);
+        L::template store<Tile>(tg, b);
+        if ((int)threadIdx.x < ROWS) {
+            stat_lse[threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e;
+            stat_delta[threadIdx.x] = delta;
+        }
     }
 };
 
@@ -360,16 +436,18 @@ __device__ __forceinline__ void join_waves(f32x16 (&o)[ND], char *lds, int ow, i
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
 
-inline uint32_t grid_of(const CrossParams &p) {
-    const int64_t n = (int64_t)p.n_items * p.heads_kv, unit = 8 * (int64_t)p.chunk;
-    return (uint32_t)((n + unit - 1) / unit * unit);
-}
+// Blocks: a work item's key heads are neighbours.  Blocks go to the eight
+// XCDs in turn, so that with 1, 2, 4 or 8 m key heads an XCD's L2 holds the
+// keys of one (or m) of them.
+inline uint32_t grid_of(const CrossParams &p) { return (uint32_t)p.n_items * (uint32_t)p.heads_kv; }
 
 // One launch of Pass::run<T, NS, OW, CW, DROP>, then the join of its parts.
 template <typename Pass, typename T, int NS>
 void launch_shape(const CrossParams &p, const CrossPass &w, hipStream_t s) {
     const bool drop = p.drop_below != 0;
-    if (w.own_waves == 4)
+    if (w.own_waves == 2)
+        drop ? Pass::template run<T, NS, 2, 1, true>(p, s) : Pass::template run<T, NS, 2, 1, false>(p, s);
+    else if (w.own_waves == 4)
         drop ? Pass::template run<T, NS, 4, 1, true>(p, s) : Pass::template run<T, NS, 4, 1, false>(p, s);
     else if (w.cut_waves == 4)
         drop ? Pass::template run<T, NS, 1, 4, true>(p, s) : Pass::template run<T, NS, 1, 4, false>(p, s);
@@ -382,7 +460,6 @@ hipError_t launch_typed(CrossParams p, const CrossPass &w, hipStream_t s) {
     if (w.n_items == 0) return hipSuccess;
     p.items = w.items;
     p.n_items = w.n_items;
-    p.chunk = 4;
     if (p.dim <= 32)
         launch_shape<Pass, T, 2>(p, w, s);
     else if (p.dim <= 64)
@@ -393,7 +470,7 @@ hipError_t launch_typed(CrossParams p, const CrossPass &w, hipStream_t s) {
         launch_shape<Pass, T, 8>(p, w, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || w.n_joins == 0) return e;
-    Pass::template join<T>(p, w, dim3((uint32_t)w.n_joins * p.heads_kv), s);
+    Pass::template join<T>(p, w, dim3((uint32_t)w.n_joins, p.heads_kv, w.own_waves), s);
     return hipGetLastError();
 }
 

@@ -21,20 +21,21 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     typedef RowTile<NS> KTile;
     typedef ColumnTile<NS> VTile;
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
-    // With the rows split over waves, the scores of the next 32 keys are
-    // formed beside the softmax of the present ones; the tiles of k then begin
-    // 32 keys after those of v.  Otherwise one buffer each.
-    constexpr bool kAhead = OW > 1;
+    // Wide heads leave room for two waves a SIMD: the scores of the next 32
+    // keys are then formed beside the softmax of the present ones (the tiles of
+    // k begin 32 keys after those of v, in two buffers each).  Up to 64 wide,
+    // four waves a SIMD do the same for each other with one buffer: 71 against
+    // 83 us for 256 columns of 330 nodes, 8 heads of 64; at 128 wide 744 with
+    // the scores ahead against 770 us without (4,099 x 7,951, 16 heads).
+    constexpr bool kAhead = OW > 1 && NS > 4;
     constexpr int kBufs = kAhead ? 2 : 1;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ uint64_t seen[2][SeenStage<KT>::kWords];
     __shared__ float stat[2][OW * CW * 32];
     char *const lds_v = lds + kBufs * kTileK;
-    const int64_t lb = logical_block(p.chunk);
-    if (lb >= (int64_t)p.n_items * p.heads_kv) return;
-    const int hk = (int)(lb / p.n_items);
-    const CrossItem it = p.items[lb - (int64_t)hk * p.n_items];
+    const int hk = blockIdx.x % p.heads_kv;
+    const CrossItem it = p.items[blockIdx.x / p.heads_kv];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
@@ -188,16 +189,16 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
         p.lse[row] = sum == 0.0f ? -kInf : top * p.scale + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
-// Joins the parts of split rows: one block per tile of rows and key head.
+// Joins the parts of split rows: a block per tile, key head and 32 rows.
 template <typename T>
-__global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, const CrossJoin *joins, int32_t n_joins,
-                                                                 int tile) {
-    const int hk = blockIdx.x / n_joins;
-    const CrossJoin j = joins[blockIdx.x - hk * n_joins];
+__global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, const CrossJoin *joins) {
+    const int hk = blockIdx.y, tile = 32 * gridDim.z;
+    const CrossJoin j = joins[blockIdx.x];
     const float c = p.scale * kLog2e;
     const int quads = p.dim / 4;
-    for (int idx = threadIdx.x; idx < j.n_own * quads; idx += blockDim.x) {
-        const int own = idx / quads, d = (idx % quads) * 4;
+    const int rows = min(32, j.n_own - 32 * (int)blockIdx.z);
+    for (int idx = threadIdx.x; idx < rows * quads; idx += blockDim.x) {
+        const int own = 32 * blockIdx.z + idx / quads, d = (idx % quads) * 4;
         float mx = -kInf;
         for (int s = 0; s < j.n_parts; ++s)
             mx = fmaxf(mx, p.part_ml[2 * (((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own)]);
@@ -223,11 +224,11 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
 struct Pass {
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_forward_kernel<T, NS, OW, CW, (OW > 1 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+        cross_forward_kernel<T, NS, OW, CW, (OW == 4 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
-        cross_join_forward_kernel<T><<<grid, 256, 0, s>>>(p, w.joins, w.n_joins, 32 * w.own_waves);
+        cross_join_forward_kernel<T><<<grid, 256, 0, s>>>(p, w.joins);
     }
 };
 

@@ -19,12 +19,10 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     constexpr int kTile = QT * Tile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ __attribute__((aligned(256))) char lds[kLds];
     __shared__ f32x4 stat[kBufs][2][QT / 4];
-    const int64_t lb = logical_block(p.chunk);
-    if (lb >= (int64_t)p.n_items * p.heads_kv) return;
-    const int hk = (int)(lb / p.n_items);
-    const CrossItem it = p.items[lb - (int64_t)hk * p.n_items];
+    const int hk = blockIdx.x % p.heads_kv;
+    const CrossItem it = p.items[blockIdx.x / p.heads_kv];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
@@ -40,42 +38,24 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     const float c = p.scale * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
 
-    QueryStage<T, NS, QT, NT> sq(p, it, hk), sg(p, it, hk);
-    auto stats = [&](int buf, int row) {
-        for (int i = threadIdx.x; i < QT; i += NT) {
-            float l = kInf, d = 0.0f;
-            if (row + i < it.end) {
-                const int64_t id = row_id(p, it.q0, row + i, hk);
-                l = p.lse[id];
-                l = l == -kInf ? kInf : l * kLog2e;
-                d = p.delta[id];
-            }
-            ((float *)stat[buf][0])[i] = l;
-            ((float *)stat[buf][1])[i] = d;
-        }
-    };
+    QueryStage<T, NS, QT, NT> sq(p, it, hk);
     if (it.beg < it.end) {
-        sq.load(p.q, p.group);
-        sg.load(p.dout, p.group);
-        sq.template store<Tile>(lds);
-        sg.template store<Tile>(lds + kTile);
-        stats(0, it.beg);
+        sq.load(p);
+        sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1]);
     }
     __syncthreads();
+    BothReader<T, NS> rd(lds, lane);
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
-        const bool more = row + QT < it.end;
-        if (more) {
-            sq.load(p.q, p.group);
-            sg.load(p.dout, p.group);
-        }
-        const char *tq = lds + buf * 2 * kTile, *tg = tq + kTile;
+        sq.load(p);
         const int base = cw * 32;
+        const uint32_t at_q = buf * 2 * kTile + base * Tile::kRowBytes, at_g = at_q + kTile;
+        rd.renew();
         f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
-            s = mfma(read_rows<T, Tile>(tq, base + col, 2 * t + half), kf[t], s);
-            dp = mfma(read_rows<T, Tile>(tg, base + col, 2 * t + half), vf[t], dp);
+            s = mfma(rd.row(at_q, t), kf[t], s);
+            dp = mfma(rd.row(at_g, t), vf[t], dp);
         }
         uint32_t keep = 0xFFFFFFFF;  // bit i: the block's row i keeps this lane's key
         if (DROP) {
@@ -117,18 +97,16 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
             const typename Vec<T>::x8 wf = round8<T>(w, 8 * t), df = round8<T>(s, 8 * t);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
-                ov[dt] = mfma(read_columns<T, Tile>(tg, base + 16 * t, dt, lane), wf, ov[dt]);
-                ok[dt] = mfma(read_columns<T, Tile>(tq, base + 16 * t, dt, lane), df, ok[dt]);
+                ov[dt] = mfma(rd.column(at_g, t, dt), wf, ov[dt]);
+                ok[dt] = mfma(rd.column(at_q, t, dt), df, ok[dt]);
             }
         }
-        if (kBufs == 1) __syncthreads();
-        if (more) {
-            const int nb = kBufs == 1 ? 0 : buf ^ 1;
-            sq.template store<Tile>(lds + nb * 2 * kTile);
-            sg.template store<Tile>(lds + nb * 2 * kTile + kTile);
-            stats(nb, row + QT);
-            buf = nb;
-        }
+        if (kBufs == 1)
+            __syncthreads();
+        else
+            buf ^= 1;
+        sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
+                                (float *)stat[buf][1]);
         __syncthreads();
     }
     if (CW > 1) {
@@ -158,7 +136,7 @@ struct Pass {
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
-        cross_join_grad_kernel<T, 2><<<grid, 256, 0, s>>>(p, w.joins, w.n_joins, 32 * w.own_waves);
+        cross_join_grad_kernel<T, 2><<<grid, 256, 0, s>>>(p, w.joins);
     }
 };
 

@@ -19,13 +19,11 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ __attribute__((aligned(256))) char lds[kLds];
     __shared__ uint64_t seen[kBufs][SeenStage<KT>::kWords];
     char *const lds_v = lds + kBufs * kTileK;
-    const int64_t lb = logical_block(p.chunk);
-    if (lb >= (int64_t)p.n_items * p.heads_kv) return;
-    const int hk = (int)(lb / p.n_items);
-    const CrossItem it = p.items[lb - (int64_t)hk * p.n_items];
+    const int hk = blockIdx.x % p.heads_kv;
+    const CrossItem it = p.items[blockIdx.x / p.heads_kv];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
@@ -45,7 +43,9 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
             for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
         delta = both_sum(delta);
     }
-    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
+    // Up to 32 keys lie in one wave, which then forms delta from P and dP in fp32:
+    // with so few keys out's rounding would cost dS a good part of its digits.
+    const bool short_row = it.slot < 0 && it.end - it.beg <= 32;
     f32x16 o[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
@@ -65,33 +65,43 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         ss.store(seen[0]);
     }
     __syncthreads();
+    BothReader<T, NS> rk(lds, lane);
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
         sk.load();
         sv.load();
         ss.load();
-        const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
         const int base = cw * 32;
+        const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
+        const char *tv = lds_v + buf * kTileV;
+        rk.renew();
         f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
-            s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
+            s = mfma(rk.row(at_k, t), qf[t], s);
             dp = mfma(read_rows<T, VTile>(tv, base + col, 2 * t + half), gf[t], dp);
         }
+        if (p.key_mask || key + KT > it.end) hide(s, (uint32_t)(seen[buf][cw >> 1] >> (32 * (cw & 1))), half, -kInf);
         uint32_t keep = 0xFFFF;
         if (DROP) keep = keep_bits(p, row, (key + base) >> 5, half);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
-            const float d = DROP ? ((keep >> e) & 1 ? dp[e] * gain : 0.0f) : dp[e];
-            s[e] = w * (d - delta);
+            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+            if (DROP) dp[e] = (keep >> e) & 1 ? dp[e] * gain : 0.0f;
         }
-        if (p.key_mask || key + KT > it.end) hide(s, (uint32_t)(seen[buf][cw >> 1] >> (32 * (cw & 1))), half, 0.0f);
+        if (short_row) {
+            float d = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) d = __builtin_fmaf(s[e], dp[e], d);
+            delta = both_sum(d);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(read_columns<T, KTile>(tk, base + 16 * t, dt, lane), df, o[dt]);
+            for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(rk.column(at_k, t, dt), df, o[dt]);
         }
         if (kBufs == 1)
             __syncthreads();
@@ -102,6 +112,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         ss.store(seen[buf]);
         __syncthreads();
     }
+    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
     if (CW > 1) {
         join_waves<ND, OW, CW>(o, lds, ow, cw, lane);
         if (cw != 0) return;
@@ -122,7 +133,7 @@ struct Pass {
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
-        cross_join_grad_kernel<T, 1><<<grid, 256, 0, s>>>(p, w.joins, w.n_joins, 32 * w.own_waves);
+        cross_join_grad_kernel<T, 1><<<grid, 256, 0, s>>>(p, w.joins);
     }
 };
 

@@ -8,13 +8,13 @@ namespace cross {
 
 // Sums the parts of dQ (SIDES = 1) or of dK and dV (SIDES = 2), in order.
 template <typename T, int SIDES>
-__global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, const CrossJoin *joins, int32_t n_joins,
-                                                              int tile) {
-    const int hk = blockIdx.x / n_joins;
-    const CrossJoin j = joins[blockIdx.x - hk * n_joins];
+__global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, const CrossJoin *joins) {
+    const int hk = blockIdx.y, tile = 32 * gridDim.z;
+    const CrossJoin j = joins[blockIdx.x];
     const int quads = p.dim / 4;
-    for (int idx = threadIdx.x; idx < j.n_own * quads * SIDES; idx += blockDim.x) {
-        const int own = idx / (quads * SIDES), side = (idx / quads) % SIDES, d = (idx % quads) * 4;
+    const int owners = min(32, j.n_own - 32 * (int)blockIdx.z);
+    for (int idx = threadIdx.x; idx < owners * quads * SIDES; idx += blockDim.x) {
+        const int own = 32 * blockIdx.z + idx / (quads * SIDES), side = (idx / quads) % SIDES, d = (idx % quads) * 4;
         f32x4 acc = 0.0f;
         for (int s = 0; s < j.n_parts; ++s) {
             const int64_t at = ((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own;

@@ -39,8 +39,8 @@ struct PassPlan {
 struct DeviceLists {
     int device = -1;
     char *base = nullptr;
-    CrossItem *rows = nullptr, *keys = nullptr;
-    CrossJoin *row_joins = nullptr, *key_joins = nullptr;
+    CrossItem *items[3] = {nullptr, nullptr, nullptr};
+    CrossJoin *joins[3] = {nullptr, nullptr, nullptr};
 };
 
 }  // namespace
@@ -48,7 +48,7 @@ struct DeviceLists {
 struct same_cross_plan {
     int32_t heads_q = 0, heads_kv = 0, dim = 0, dtype = 0;
     int64_t n_q = 0, n_k = 0;  // tokens
-    PassPlan rows, keys;       // owners: query rows (forward, dQ); keys (dK, dV)
+    PassPlan pass[3];          // by PassKind
     // workspace: parts and their statistics (forward); delta, then parts (gradient)
     size_t ws_ml = 0, ws_forward = 0, ws_part = 0, ws_backward = 0;
     std::vector<DeviceLists> dev;
@@ -57,45 +57,83 @@ struct same_cross_plan {
 
 namespace {
 
+enum PassKind { kForward, kGradQuery, kGradKey };
+
+// Waves of a pass's kernel that a SIMD holds (registers).
+int waves_per_simd(PassKind kind, int32_t dim) { return kind == kForward && dim <= 64 ? 4 : 2; }
+
 // Splits the owners of every segment into tiles and, where the tiles alone
-// leave the chip idle, the other axis into parts.
+// leave compute units idle, the other axis into parts.
 int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vector<int64_t> &k_ptr, int32_t group,
-               int32_t heads_kv, bool own_keys) {
+               int32_t heads_kv, int32_t dim, PassKind kind) {
     const int64_t n = (int64_t)q_ptr.size() - 1;
-    auto rows_of = [&](int64_t s) { return (q_ptr[s + 1] - q_ptr[s]) * group; };
-    auto keys_of = [&](int64_t s) { return k_ptr[s + 1] - k_ptr[s]; };
+    const bool own_keys = kind == kGradKey;
+    auto own_of = [&](int64_t s) { return own_keys ? k_ptr[s + 1] - k_ptr[s] : (q_ptr[s + 1] - q_ptr[s]) * group; };
+    auto cut_of = [&](int64_t s) { return own_keys ? (q_ptr[s + 1] - q_ptr[s]) * group : k_ptr[s + 1] - k_ptr[s]; };
     int64_t max_own = 0, max_cut = 0;
+    double by4 = 0.0, by2 = 0.0;
+    std::vector<int64_t> order;  // longest first; the tiles of a segment stay together
     for (int64_t s = 0; s < n; ++s) {
-        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
+        const int64_t own = own_of(s), cut = cut_of(s);
         if (own == 0) continue;
+        order.push_back(s);
         max_own = std::max(max_own, own);
         max_cut = std::max(max_cut, cut);
+        by4 += (double)((own + 127) / 128 * 128) * (double)cut;
+        by2 += (double)((own + 63) / 64 * 64) * (double)cut;
     }
-    pp.own_waves = max_own > 32 ? 4 : 1;
+    if (order.empty()) return SAME_OK;
+    std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return cut_of(a) > cut_of(b); });
+    // Tiles of 128 owners, of 64 where those leave much less of a tile empty,
+    // of 32 where no segment has more (then four waves share the other axis,
+    // if it is long enough to).
+    pp.own_waves = max_own <= 32 ? 1 : by2 < 0.85 * by4 ? 2 : 4;
     pp.cut_waves = pp.own_waves == 1 && max_cut > 64 ? 4 : 1;
     const int64_t tile = 32 * pp.own_waves;
-    int64_t blocks = 0;
-    double work = 0.0;
-    for (int64_t s = 0; s < n; ++s) {
-        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
-        const int64_t t = (own + tile - 1) / tile * heads_kv;
-        blocks += t;
-        work += (double)t * (double)cut;
+    const double room = 1024.0 * waves_per_simd(kind, dim) / (pp.own_waves * pp.cut_waves);  // blocks the chip holds
+    int64_t tiles = 0;
+    for (int64_t s : order) tiles += (own_of(s) + tile - 1) / tile;
+    if (tiles * heads_kv > kMaxBlocks) return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
+
+    // Whole rounds of blocks are left whole; the tiles of the last, partly
+    // filled round are cut into parts that fill it.  With many rounds the last
+    // one does not matter.  A block costs about as much as kBlock entries of
+    // the axis before it begins, a join about kJoin.
+    constexpr double kBlock = 128.0, kJoin = 384.0;
+    int64_t whole = tiles, part = kMaxAxis;
+    if (pp.own_waves * pp.cut_waves > 1 && (double)tiles * heads_kv <= 16.0 * room) {
+        whole = (int64_t)(std::floor((double)tiles * heads_kv / room) * room / heads_kv);
+        std::vector<int64_t> cuts;
+        int64_t at = 0, longest = 0;
+        double work = 0.0;
+        for (int64_t s : order)
+            for (int64_t o = 0; o < own_of(s); o += tile, ++at)
+                if (at >= whole) {
+                    cuts.push_back(cut_of(s));
+                    longest = std::max(longest, cuts.back());
+                    work += (double)cuts.back() * heads_kv;
+                }
+        double best = 0.0;
+        for (int64_t k = 1; k <= 64; ++k) {
+            const int64_t p = k == 1 ? std::max<int64_t>(longest, 1) : ((longest + k - 1) / k + 127) / 128 * 128;
+            if (k > 1 && p < 256) break;
+            double blocks = 0.0;
+            for (int64_t c : cuts) blocks += (double)std::max<int64_t>(1, (c + p - 1) / p);
+            blocks *= heads_kv;
+            double cost = blocks <= room ? p + kBlock : (work + kBlock * blocks) / room + 0.5 * (p + kBlock);
+            if (k > 1) cost += kJoin;
+            if (k == 1 || cost < best) {
+                best = cost;
+                part = k == 1 ? kMaxAxis : p;
+            }
+        }
     }
-    int64_t part = kMaxAxis;
-    if (blocks < 512) part = std::max<int64_t>(256, (int64_t)std::ceil(work / 512.0 / 128.0) * 128);
-    // longest first; the tiles of a segment stay together
-    std::vector<int64_t> order;
-    for (int64_t s = 0; s < n; ++s)
-        if ((own_keys ? keys_of(s) : rows_of(s)) > 0) order.push_back(s);
-    std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) {
-        return (own_keys ? rows_of(a) : keys_of(a)) > (own_keys ? rows_of(b) : keys_of(b));
-    });
+    int64_t at = 0;
     for (int64_t s : order) {
-        const int64_t own = own_keys ? keys_of(s) : rows_of(s), cut = own_keys ? rows_of(s) : keys_of(s);
-        const int64_t parts = std::max<int64_t>(1, (cut + part - 1) / part);
-        const int64_t step = parts == 1 ? std::max<int64_t>(cut, 1) : ((cut + parts - 1) / parts + 127) / 128 * 128;
-        for (int64_t o = 0; o < own; o += tile) {
+        const int64_t own = own_of(s), cut = cut_of(s);
+        for (int64_t o = 0; o < own; o += tile, ++at) {
+            const int64_t parts = at < whole ? 1 : std::max<int64_t>(1, (cut + part - 1) / part);
+            const int64_t step = parts == 1 ? std::max<int64_t>(cut, 1) : ((cut + parts - 1) / parts + 127) / 128 * 128;
             CrossItem it;
             it.q0 = q_ptr[s];
             it.k0 = k_ptr[s];
@@ -113,8 +151,6 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
                 b += step;
             } while (b < cut);
             if (step < cut) pp.joins.push_back(CrossJoin{it.q0, it.k0, it.own0, it.n_own, first, pp.n_slots - first});
-            if ((int64_t)pp.items.size() * heads_kv > kMaxBlocks)
-                return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
         }
     }
     return SAME_OK;
@@ -134,18 +170,19 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
     if ((int)pl->dev.size() <= device) pl->dev.resize(device + 1);
     DeviceLists &d = pl->dev[device];
     if (d.device != device) {
-        const size_t at[5] = {0, bytes_of(pl->rows.items), bytes_of(pl->rows.joins), bytes_of(pl->keys.items),
-                              bytes_of(pl->keys.joins)};
-        size_t off[5] = {0, 0, 0, 0, 0};
-        for (int i = 1; i < 5; ++i) off[i] = off[i - 1] + at[i];
-        std::vector<char> host(std::max<size_t>(off[4], 1));
+        size_t off[7] = {0};
+        for (int k = 0; k < 3; ++k) {
+            off[2 * k + 1] = off[2 * k] + bytes_of(pl->pass[k].items);
+            off[2 * k + 2] = off[2 * k + 1] + bytes_of(pl->pass[k].joins);
+        }
+        std::vector<char> host(std::max<size_t>(off[6], 1));
         auto put = [&](size_t o, const void *src, size_t bytes) {
             if (bytes) std::memcpy(host.data() + o, src, bytes);
         };
-        put(off[0], pl->rows.items.data(), pl->rows.items.size() * sizeof(CrossItem));
-        put(off[1], pl->rows.joins.data(), pl->rows.joins.size() * sizeof(CrossJoin));
-        put(off[2], pl->keys.items.data(), pl->keys.items.size() * sizeof(CrossItem));
-        put(off[3], pl->keys.joins.data(), pl->keys.joins.size() * sizeof(CrossJoin));
+        for (int k = 0; k < 3; ++k) {
+            put(off[2 * k], pl->pass[k].items.data(), pl->pass[k].items.size() * sizeof(CrossItem));
+            put(off[2 * k + 1], pl->pass[k].joins.data(), pl->pass[k].joins.size() * sizeof(CrossJoin));
+        }
         char *base = nullptr;
         e = hipMalloc((void **)&base, host.size());
         if (e == hipSuccess) e = hipMemcpy(base, host.data(), host.size(), hipMemcpyHostToDevice);
@@ -155,10 +192,10 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
                                 std::string("uploading the plan's lists: ") + hipGetErrorString(e));
         }
         d.base = base;
-        d.rows = (CrossItem *)(base + off[0]);
-        d.row_joins = (CrossJoin *)(base + off[1]);
-        d.keys = (CrossItem *)(base + off[2]);
-        d.key_joins = (CrossJoin *)(base + off[3]);
+        for (int k = 0; k < 3; ++k) {
+            d.items[k] = (CrossItem *)(base + off[2 * k]);
+            d.joins[k] = (CrossJoin *)(base + off[2 * k + 1]);
+        }
         d.device = device;
     }
     *out = d;
@@ -273,10 +310,11 @@ int prepare_call(same_cross_plan *pl, Call &c, const void *q, int64_t q_row, int
     return SAME_OK;
 }
 
-same::CrossPass pass_of(const PassPlan &pp, const CrossItem *items, const CrossJoin *joins) {
+same::CrossPass pass_of(const same_cross_plan *pl, const DeviceLists &d, PassKind kind) {
+    const PassPlan &pp = pl->pass[kind];
     same::CrossPass w;
-    w.items = items;
-    w.joins = joins;
+    w.items = d.items[kind];
+    w.joins = d.joins[kind];
     w.n_items = (int32_t)pp.items.size();
     w.n_joins = (int32_t)pp.joins.size();
     w.n_slots = pp.n_slots;
@@ -323,8 +361,7 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
         for (int64_t s = 0; !rc && s < n_segs; ++s)
             if ((qp[s + 1] - qp[s]) * group >= kMaxAxis)
                 rc = record_error(SAME_ESIZE, "a segment has 2^30 query rows of one key head or more");
-        if (!rc) rc = build_pass(pl->rows, qp, kp, group, heads_kv, false);
-        if (!rc) rc = build_pass(pl->keys, qp, kp, group, heads_kv, true);
+        for (int k = 0; !rc && k < 3; ++k) rc = build_pass(pl->pass[k], qp, kp, group, heads_kv, head_dim, (PassKind)k);
         if (!rc) {
             pl->heads_q = heads_q;
             pl->heads_kv = heads_kv;
@@ -336,10 +373,10 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
                 return (size_t)pp.n_slots * (size_t)heads_kv * 32 * (size_t)pp.own_waves;
             };
             const size_t row = (size_t)head_dim * sizeof(float);
-            pl->ws_ml = align_up(owners(pl->rows) * row);
-            pl->ws_forward = pl->ws_ml + align_up(owners(pl->rows) * 2 * sizeof(float));
+            pl->ws_ml = align_up(owners(pl->pass[kForward]) * row);
+            pl->ws_forward = pl->ws_ml + align_up(owners(pl->pass[kForward]) * 2 * sizeof(float));
             pl->ws_part = align_up((size_t)pl->n_q * (size_t)heads_q * sizeof(float));
-            pl->ws_backward = pl->ws_part + align_up(std::max(owners(pl->rows), 2 * owners(pl->keys)) * row);
+            pl->ws_backward = pl->ws_part + align_up(std::max(owners(pl->pass[kGradQuery]), 2 * owners(pl->pass[kGradKey])) * row);
         }
     } catch (const std::bad_alloc &) {
         rc = record_error(SAME_ENOMEM, "out of host memory");
@@ -399,7 +436,7 @@ int same_cross_attention(same_cross_plan *pl, const void *q, int64_t q_row, int6
         c.p.lse = lse;
         c.p.part = (float *)workspace;
         c.p.part_ml = (float *)((char *)workspace + pl->ws_ml);
-        return check_hip(same::launch_cross_forward(c.p, pass_of(pl->rows, c.d.rows, c.d.row_joins), pl->dtype,
+        return check_hip(same::launch_cross_forward(c.p, pass_of(pl, c.d, kForward), pl->dtype,
                                                     (hipStream_t)stream),
                          "cross attention launch");
     } catch (const std::bad_alloc &) {
@@ -453,10 +490,10 @@ int same_cross_attention_backward(same_cross_plan *pl, const void *q, int64_t q_
         c.p.dv = dv;
         hipStream_t s = (hipStream_t)stream;
         // dQ first: it leaves delta for the other pass
-        rc = check_hip(same::launch_cross_dq(c.p, pass_of(pl->rows, c.d.rows, c.d.row_joins), pl->dtype, s),
+        rc = check_hip(same::launch_cross_dq(c.p, pass_of(pl, c.d, kGradQuery), pl->dtype, s),
                        "query gradient launch");
         if (rc) return rc;
-        return check_hip(same::launch_cross_dkv(c.p, pass_of(pl->keys, c.d.keys, c.d.key_joins), pl->dtype, s),
+        return check_hip(same::launch_cross_dkv(c.p, pass_of(pl, c.d, kGradKey), pl->dtype, s),
                          "key gradient launch");
     } catch (const std::bad_alloc &) {
         return record_error(SAME_ENOMEM, "out of host memory");
