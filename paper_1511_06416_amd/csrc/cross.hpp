@@ -18,7 +18,7 @@ struct CrossItem {
     int32_t slot, pad;
 };
 
-// Parts [slot, slot + n_parts) of one tile of owners.
+// Parts [slot, slot + n_parts) of one tile of owners, at most kMaxParts.
 struct CrossJoin {
     int64_t q0, k0;
     int32_t own0, n_own;
@@ -54,6 +54,8 @@ struct CrossParams {
 };
 
 constexpr int kCrossF16 = 1, kCrossBf16 = 2;
+constexpr int kJoinOwners = 8;  // owners that a join's block takes
+constexpr int kMaxParts = 64;   // of one tile
 
 hipError_t launch_cross_forward(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);
 hipError_t launch_cross_dq(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);

@@ -470,7 +470,7 @@ hipError_t launch_typed(CrossParams p, const CrossPass &w, hipStream_t s) {
         launch_shape<Pass, T, 8>(p, w, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || w.n_joins == 0) return e;
-    Pass::template join<T>(p, w, dim3((uint32_t)w.n_joins, p.heads_kv, w.own_waves), s);
+    Pass::template join<T>(p, w, dim3((uint32_t)w.n_joins, p.heads_kv, 32 * w.own_waves / kJoinOwners), s);
     return hipGetLastError();
 }
 

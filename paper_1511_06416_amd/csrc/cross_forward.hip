@@ -189,35 +189,63 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
         p.lse[row] = sum == 0.0f ? -kInf : top * p.scale + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
-// Joins the parts of split rows: a block per tile, key head and 32 rows.
+// Joins the parts of split rows: a block per tile, key head and kJoinOwners
+// rows.  The parts' weights are formed once per row, then the loads of several
+// parts are in flight together.
 template <typename T>
 __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, const CrossJoin *joins) {
-    const int hk = blockIdx.y, tile = 32 * gridDim.z;
+    __shared__ float weight[kJoinOwners][kMaxParts], gain[kJoinOwners];
     const CrossJoin j = joins[blockIdx.x];
+    const int hk = blockIdx.y, tile = kJoinOwners * gridDim.z, first = kJoinOwners * blockIdx.z;
+    const int rows = min(kJoinOwners, j.n_own - first);
     const float c = p.scale * kLog2e;
-    const int quads = p.dim / 4;
-    const int rows = min(32, j.n_own - 32 * (int)blockIdx.z);
-    for (int idx = threadIdx.x; idx < rows * quads; idx += blockDim.x) {
-        const int own = 32 * blockIdx.z + idx / quads, d = (idx % quads) * 4;
-        float mx = -kInf;
-        for (int s = 0; s < j.n_parts; ++s)
-            mx = fmaxf(mx, p.part_ml[2 * (((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own)]);
+    {
+        const int own = threadIdx.x / 32, l = threadIdx.x % 32;
+        float top[kMaxParts / 32], sum[kMaxParts / 32], mx = -kInf;
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; ++k) {
+            const int s = l + 32 * k;
+            top[k] = -kInf;
+            sum[k] = 0.0f;
+            if (own < rows && s < j.n_parts) {
+                const int64_t at = ((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + first + own;
+                top[k] = p.part_ml[2 * at];
+                sum[k] = p.part_ml[2 * at + 1];
+            }
+            mx = fmaxf(mx, top[k]);
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 32));
         const float to = mx == -kInf ? 0.0f : mx;
         float total = 0.0f;
-        f32x4 acc = 0.0f;
-        for (int s = 0; s < j.n_parts; ++s) {
-            const int64_t at = ((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own;
-            const float f = __builtin_amdgcn_exp2f((p.part_ml[2 * at] - to) * c);
-            total += f * p.part_ml[2 * at + 1];
-            acc += *(const f32x4 *)(p.part + at * p.dim + d) * f;
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; ++k) {
+            const float f = __builtin_amdgcn_exp2f((top[k] - to) * c);
+            if (own < kJoinOwners && l + 32 * k < j.n_parts) weight[own][l + 32 * k] = f;
+            total += f * sum[k];
         }
-        const int64_t row = row_id(p, j.q0, j.own0 + own, hk);
-        const float gain = total > 0.0f ? p.keep_gain / total : (total == 0.0f ? 0.0f : total);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) total += __shfl_xor(total, d, 32);
+        if (own < rows && l == 0) {
+            gain[own] = total > 0.0f ? p.keep_gain / total : (total == 0.0f ? 0.0f : total);
+            if (p.lse)
+                p.lse[row_id(p, j.q0, j.own0 + first + own, hk)] =
+                    total == 0.0f ? -kInf : mx * p.scale + __builtin_amdgcn_logf(total) * kLn2;
+        }
+    }
+    __syncthreads();
+    const int quads = p.dim / 4;
+    for (int idx = threadIdx.x; idx < rows * quads; idx += blockDim.x) {
+        const int own = idx / quads, d = (idx - own * quads) * 4;
+        const int64_t step = (int64_t)p.heads_kv * tile * p.dim;
+        const float *src = p.part + (((int64_t)j.slot * p.heads_kv + hk) * tile + first + own) * p.dim + d;
+        f32x4 acc = 0.0f;
+#pragma unroll 8
+        for (int s = 0; s < j.n_parts; ++s) acc += *(const f32x4 *)(src + s * step) * weight[own][s];
         typename Vec<T>::x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (T)(acc[i] * gain);
-        *(typename Vec<T>::x4 *)((T *)p.out + row * p.dim + d) = w;
-        if (p.lse && d == 0) p.lse[row] = total == 0.0f ? -kInf : mx * p.scale + __builtin_amdgcn_logf(total) * kLn2;
+        for (int i = 0; i < 4; ++i) w[i] = (T)(acc[i] * gain[own]);
+        *(typename Vec<T>::x4 *)((T *)p.out + row_id(p, j.q0, j.own0 + first + own, hk) * p.dim + d) = w;
     }
 }
 

@@ -9,17 +9,17 @@ namespace cross {
 // Sums the parts of dQ (SIDES = 1) or of dK and dV (SIDES = 2), in order.
 template <typename T, int SIDES>
 __global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, const CrossJoin *joins) {
-    const int hk = blockIdx.y, tile = 32 * gridDim.z;
     const CrossJoin j = joins[blockIdx.x];
-    const int quads = p.dim / 4;
-    const int owners = min(32, j.n_own - 32 * (int)blockIdx.z);
+    const int hk = blockIdx.y, tile = kJoinOwners * gridDim.z, first = kJoinOwners * blockIdx.z;
+    const int quads = p.dim / 4, owners = min(kJoinOwners, j.n_own - first);
     for (int idx = threadIdx.x; idx < owners * quads * SIDES; idx += blockDim.x) {
-        const int own = 32 * blockIdx.z + idx / (quads * SIDES), side = (idx / quads) % SIDES, d = (idx % quads) * 4;
+        const int line = idx / quads, d = (idx - line * quads) * 4;
+        const int own = first + line / SIDES, side = line % SIDES;
+        const int64_t step = (int64_t)p.heads_kv * tile * SIDES * p.dim;
+        const float *src = p.part + ((((int64_t)j.slot * p.heads_kv + hk) * tile + own) * SIDES + side) * p.dim + d;
         f32x4 acc = 0.0f;
-        for (int s = 0; s < j.n_parts; ++s) {
-            const int64_t at = ((int64_t)(j.slot + s) * p.heads_kv + hk) * tile + own;
-            acc += *(const f32x4 *)(p.part + (SIDES * at + side) * p.dim + d);
-        }
+#pragma unroll 8
+        for (int s = 0; s < j.n_parts; ++s) acc += *(const f32x4 *)(src + s * step);
         T *dst;
         float gain = p.scale;
         if (SIDES == 1) {

@@ -114,7 +114,7 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
                     work += (double)cuts.back() * heads_kv;
                 }
         double best = 0.0;
-        for (int64_t k = 1; k <= 64; ++k) {
+        for (int64_t k = 1; k <= same::kMaxParts; ++k) {
             const int64_t p = k == 1 ? std::max<int64_t>(longest, 1) : ((longest + k - 1) / k + 127) / 128 * 128;
             if (k > 1 && p < 256) break;
             double blocks = 0.0;
