@@ -166,13 +166,13 @@ __device__ __forceinline__ typename Vec<T>::x8 zero8() {
 template <typename T, int NS, int ROWS, int NT>
 struct Lanes {
     static constexpr int kSlots = lanes_per_row(NS);  // three in four work for NS = 6
-    static constexpr int kStep = NT / kSlots;
+    static constexpr int kStep = (NT >= 512 ? 512 : NT >= 256 ? 256 : NT >= 128 ? 128 : 64) / kSlots;
     static constexpr int kN = (ROWS + kStep - 1) / kStep;
-    static_assert(NT % kSlots == 0 && (ROWS % kStep == 0 || kN == 1), "whole rows per thread");
+    static_assert(ROWS % kStep == 0 || kN == 1, "whole rows per thread");
     __device__ static __forceinline__ int row() { return threadIdx.x / kSlots; }
     __device__ static __forceinline__ int slot() { return threadIdx.x % kSlots; }
     // lanes without a chunk of the tile, or past the width
-    __device__ static __forceinline__ bool idle() { return slot() >= 2 * NS || row() >= ROWS; }
+    __device__ static __forceinline__ bool idle() { return slot() >= 2 * NS || row() >= (kN == 1 ? ROWS : kStep); }
     template <typename Tile>
     __device__ static __forceinline__ void store(char *tile, const typename Vec<T>::x8 (&a)[kN]) {
         if (idle()) return;
@@ -239,7 +239,7 @@ struct SeenStage {
     static constexpr int kWords = (KT + 63) / 64;
     const uint8_t *mask;
     int left;
-    uint8_t m;
+    uint32_t m;
     __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it) {
         mask = p.key_mask ? p.key_mask + it.k0 + it.beg + threadIdx.x : nullptr;
         left = (int)threadIdx.x < KT ? it.end - it.beg - (int)threadIdx.x : 0;
@@ -255,7 +255,9 @@ struct SeenStage {
     }
     __device__ __forceinline__ void store(uint64_t *words) const {
         if (threadIdx.x < 64 * kWords) {
-            const uint64_t b = __ballot(m != 0);
+            uint32_t v = m;
+            asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
+            const uint64_t b = __ballot(v != 0);
             if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = b;
         }
     }
@@ -266,7 +268,7 @@ __device__ __forceinline__ void hide(f32x16 &s, uint32_t bits, int half, float h
     const uint32_t mine = bits >> (4 * half);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const uint32_t keep = (uint32_t)((int32_t)(mine << (31 - (8 * (e >> 2) + (e & 3)))) >> 31);
+        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)mine, 8 * (e >> 2) + (e & 3), 1);
         s[e] = __uint_as_float((__float_as_uint(s[e]) & keep) | (__float_as_uint(hidden) & ~keep));
     }
 }
@@ -445,7 +447,11 @@ inline uint32_t grid_of(const CrossParams &p) { return (uint32_t)p.n_items * (ui
 template <typename Pass, typename T, int NS>
 void launch_shape(const CrossParams &p, const CrossPass &w, hipStream_t s) {
     const bool drop = p.drop_below != 0;
-    if (w.own_waves == 2)
+    if (w.own_waves == 8)
+        drop ? Pass::template run<T, NS, 8, 1, true>(p, s) : Pass::template run<T, NS, 8, 1, false>(p, s);
+    else if (w.own_waves == 6)
+        drop ? Pass::template run<T, NS, 6, 1, true>(p, s) : Pass::template run<T, NS, 6, 1, false>(p, s);
+    else if (w.own_waves == 2)
         drop ? Pass::template run<T, NS, 2, 1, true>(p, s) : Pass::template run<T, NS, 2, 1, false>(p, s);
     else if (w.own_waves == 4)
         drop ? Pass::template run<T, NS, 4, 1, true>(p, s) : Pass::template run<T, NS, 4, 1, false>(p, s);

@@ -51,6 +51,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     ss.load();
     typename Vec<T>::x8 qf[NS];
     load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
+    const bool works = ow * 32 < it.n_own;  // waves without rows only help to load
     f32x16 o[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
             ss.load();
             const bool masked = p.key_mask || key + KT > it.end;
             const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
+            if (works)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 if (!kAhead) s = scores(tk, ks);
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
 struct Pass {
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_forward_kernel<T, NS, OW, CW, (OW == 4 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+        cross_forward_kernel<T, NS, OW, CW, (OW >= 4 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

@@ -48,6 +48,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
         sq.load(p);
+        if (ow * 32 < it.n_own) {  // waves without keys only help to load
         const int base = cw * 32;
         const uint32_t at_q = buf * 2 * kTile + base * Tile::kRowBytes, at_g = at_q + kTile;
         rd.renew();
@@ -100,6 +101,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
                 ov[dt] = mfma(rd.column(at_g, t, dt), wf, ov[dt]);
                 ok[dt] = mfma(rd.column(at_q, t, dt), df, ok[dt]);
             }
+        }
         }
         if (kBufs == 1)
             __syncthreads();

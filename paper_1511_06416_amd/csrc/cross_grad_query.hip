@@ -71,6 +71,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         sk.load();
         sv.load();
         ss.load();
+        if (ow * 32 < it.n_own) {  // waves without rows only help to load
         const int base = cw * 32;
         const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
         const char *tv = lds_v + buf * kTileV;
@@ -102,6 +103,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
             const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] = mfma(rk.column(at_k, t, dt), df, o[dt]);
+        }
         }
         if (kBufs == 1)
             __syncthreads();

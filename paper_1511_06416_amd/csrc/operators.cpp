@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <cstdlib>
 #include <mutex>
 #include <new>
 #include <string>
@@ -88,6 +89,7 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     // of 32 where no segment has more (then four waves share the other axis,
     // if it is long enough to).
     pp.own_waves = max_own <= 32 ? 1 : by2 < 0.85 * by4 ? 2 : 4;
+    if (getenv("OWX") && max_own > 32) pp.own_waves = getenv("OWX")[kind] - '0';
     pp.cut_waves = pp.own_waves == 1 && max_cut > 64 ? 4 : 1;
     const int64_t tile = 32 * pp.own_waves;
     const double room = 1024.0 * waves_per_simd(kind, dim) / (pp.own_waves * pp.cut_waves);  // blocks the chip holds
