@@ -143,6 +143,21 @@ __device__ __forceinline__ bool kept(const dev::Philox4 &w, int e, uint32_t belo
     return ((w.w[e >> 2] >> (8 * (e & 3))) & 255u) >= below;
 }
 
+// The same for probabilities already rounded and packed in pairs: masks of
+// the four numbers of one word, of elements (0, 1) and (2, 3).  Each byte's
+// comparison with the threshold comes out in its top bit: that of the low
+// seven bits by a subtraction that cannot borrow, then the top bits' own.
+__device__ __forceinline__ void keep_pairs(uint32_t w, uint32_t below, uint32_t (&m)[2]) {
+    const uint32_t t = below * 0x01010101u, tops = 0x80808080u;
+    const uint32_t low = (w | tops) - (t & ~tops);
+    // top bit of w above that of t, or equal and the rest no less: (w & low) | ((w | low) & ~t)
+    const uint32_t ge = __builtin_amdgcn_bitop3_b32(w, low, t, 0xD4);
+    const uint32_t up = ge << 8;
+    // the top bits of bytes 1 and 3 of (up, ge), spread over 16 bits each
+    m[0] = __builtin_amdgcn_perm(up, ge, 0x08080A0Au);
+    m[1] = __builtin_amdgcn_perm(up, ge, 0x09090B0Bu);
+}
+
 // The same as flags, bit e = accumulator element e.
 __device__ __forceinline__ uint32_t keep_bits(const CrossParams &p, int64_t row, int kb, int half) {
     const dev::Philox4 w = keep_words(p, row, kb, half);
@@ -181,8 +196,24 @@ struct Lanes {
     }
 };
 
+// A resource over `bytes` from a uniform address on (almost 4 GiB unless
+// said); a load past it, as at kOutside, returns zeros.
+constexpr uint32_t kRange = 0xFFFFFF00u, kOutside = 0xFFFFFFF0u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void *base, uint32_t bytes = kRange) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), (short)0, (int)bytes, 0x00020000);
+}
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::x8 load8(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    union {
+        u32x4 w;
+        typename Vec<T>::x8 v;
+    } u;
+    u.w = __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0);
+    return u.v;
+}
+
 // Tiles of one of k and v.  The tile's base is uniform and a lane's part of
-// the address 32 bits (row strides are below 2^25 elements).  Rows past the
+// the address 32 bits (64 rows of less than 2^25 elements).  Rows past the
 // end, hidden keys and chunks past the head's width become zeros, so that
 // nothing a hidden key holds (infinities, NaN) reaches a product.  The mask
 // travels with the rows and is applied on the way into LDS, so that no load
@@ -190,34 +221,34 @@ struct Lanes {
 template <typename T, int NS, int ROWS, int NT>
 struct KeyStage {
     typedef Lanes<T, NS, ROWS, NT> L;
+    static_assert(L::kStep <= 64, "a lane's row is below 64");
     typename Vec<T>::x8 a[L::kN];
-    uint8_t m[L::kN];
+    uint32_t m[L::kN];
     const char *base;
     const uint8_t *mask;
     int64_t step;      // bytes of a row
     uint32_t lane_at;  // bytes
     int left;          // rows from the tile's first one to the end (uniform)
-    bool used;
     __device__ __forceinline__ KeyStage(const CrossTensor &t, const CrossParams &p, const CrossItem &it, int hk,
                                         int ahead = 0) {
         const int64_t tok = it.k0 + it.beg + ahead;
         step = 2 * t.row;
         base = (const char *)t.p + tok * step + 2 * (int64_t)hk * t.head;
         mask = p.key_mask ? p.key_mask + tok : nullptr;
-        lane_at = (uint32_t)L::row() * (uint32_t)step + (uint32_t)L::slot() * 16;
+        lane_at = L::slot() * 8 < p.dim && !L::idle() ? (uint32_t)L::row() * (uint32_t)step + (uint32_t)L::slot() * 16
+                                                      : kOutside;
         left = it.end - it.beg - ahead;
-        used = L::slot() * 8 < p.dim && !L::idle();
     }
     __device__ __forceinline__ void load() {
 #pragma unroll
         for (int n = 0; n < L::kN; ++n) {
-            const bool in = used && L::row() + n * L::kStep < left;
-            a[n] = zero8<T>();
-            if (in) a[n] = *(const typename Vec<T>::x8 *)(base + n * L::kStep * step + lane_at);
-            if (mask) {
-                m[n] = 1;
-                if (in) m[n] = mask[n * L::kStep + L::row()];
-            }
+            uint32_t at = lane_at;
+            if (left < ROWS) at = L::row() + n * L::kStep < left ? lane_at : kOutside;
+            a[n] = load8<T>(resource(base + n * L::kStep * step), at);
+            // rows past the end read as hidden
+            if (mask)
+                m[n] = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)),
+                                                           L::row() + n * L::kStep, 0, 0);
         }
         base += ROWS * step;
         if (mask) mask += ROWS;
@@ -237,25 +268,25 @@ struct KeyStage {
 template <int KT>
 struct SeenStage {
     static constexpr int kWords = (KT + 63) / 64;
-    const uint8_t *mask;
-    int left;
+    const uint8_t *mask;  // of the tile (uniform)
+    int left;             // keys from the tile's first one to the end (uniform)
     uint32_t m;
     __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it) {
-        mask = p.key_mask ? p.key_mask + it.k0 + it.beg + threadIdx.x : nullptr;
-        left = (int)threadIdx.x < KT ? it.end - it.beg - (int)threadIdx.x : 0;
-        m = 0;
+        mask = p.key_mask ? p.key_mask + it.k0 + it.beg : nullptr;
+        left = it.end - it.beg;
     }
     __device__ __forceinline__ void load() {
-        m = left > 0;
         if (mask) {
-            if (left > 0) m = *mask;
+            m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), threadIdx.x, 0, 0);
             mask += KT;
+        } else {
+            m = (int)threadIdx.x < left;
         }
         left -= KT;
     }
     __device__ __forceinline__ void store(uint64_t *words) const {
         if (threadIdx.x < 64 * kWords) {
-            uint32_t v = m;
+            uint32_t v = (int)threadIdx.x < KT ? m : 0u;
             asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
             const uint64_t b = __ballot(v != 0);
             if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = b;
@@ -438,27 +469,34 @@ __device__ __forceinline__ void join_waves(f32x16 (&o)[ND], char *lds, int ow, i
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
 
+// The second choice of owner waves beside 4 (see build_pass).
+template <bool FORWARD, int NS>
+constexpr int kWide = FORWARD ? (NS > 4 ? 8 : 4) : (NS > 4 ? 4 : 2);
+
 // Blocks: a work item's key heads are neighbours.  Blocks go to the eight
 // XCDs in turn, so that with 1, 2, 4 or 8 m key heads an XCD's L2 holds the
 // keys of one (or m) of them.
 inline uint32_t grid_of(const CrossParams &p) { return (uint32_t)p.n_items * (uint32_t)p.heads_kv; }
 
-// One launch of Pass::run<T, NS, OW, CW, DROP>, then the join of its parts.
+template <typename Pass, typename T, int NS, int OW, int CW>
+void launch_drop(const CrossParams &p, hipStream_t s) {
+    if (p.drop_below)
+        Pass::template run<T, NS, OW, CW, true>(p, s);
+    else
+        Pass::template run<T, NS, OW, CW, false>(p, s);
+}
+
+// The geometries that a plan may choose for a pass and a width.
 template <typename Pass, typename T, int NS>
 void launch_shape(const CrossParams &p, const CrossPass &w, hipStream_t s) {
-    const bool drop = p.drop_below != 0;
-    if (w.own_waves == 8)
-        drop ? Pass::template run<T, NS, 8, 1, true>(p, s) : Pass::template run<T, NS, 8, 1, false>(p, s);
-    else if (w.own_waves == 6)
-        drop ? Pass::template run<T, NS, 6, 1, true>(p, s) : Pass::template run<T, NS, 6, 1, false>(p, s);
-    else if (w.own_waves == 2)
-        drop ? Pass::template run<T, NS, 2, 1, true>(p, s) : Pass::template run<T, NS, 2, 1, false>(p, s);
+    if (w.own_waves == kWide<Pass::kForward, NS>)
+        launch_drop<Pass, T, NS, kWide<Pass::kForward, NS>, 1>(p, s);
     else if (w.own_waves == 4)
-        drop ? Pass::template run<T, NS, 4, 1, true>(p, s) : Pass::template run<T, NS, 4, 1, false>(p, s);
+        launch_drop<Pass, T, NS, 4, 1>(p, s);
     else if (w.cut_waves == 4)
-        drop ? Pass::template run<T, NS, 1, 4, true>(p, s) : Pass::template run<T, NS, 1, 4, false>(p, s);
+        launch_drop<Pass, T, NS, 1, 4>(p, s);
     else
-        drop ? Pass::template run<T, NS, 1, 1, true>(p, s) : Pass::template run<T, NS, 1, 1, false>(p, s);
+        launch_drop<Pass, T, NS, 1, 1>(p, s);
 }
 
 template <typename Pass, typename T>

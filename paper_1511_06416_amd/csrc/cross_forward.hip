@@ -94,17 +94,26 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
             part[e & 3] += s[e];
         }
         sum += (part[0] + part[1]) + (part[2] + part[3]);
-        if (DROP) {
-            const dev::Philox4 w = keep_words(p, row, (key + (cw * KS + ks) * 32) >> 5, half);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = kept(w, e, p.drop_below) ? s[e] : 0.0f;
-        }
+        dev::Philox4 w;
+        if (DROP) w = keep_words(p, row, (key + (cw * KS + ks) * 32) >> 5, half);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const typename Vec<T>::x8 pf = round8<T>(s, 8 * t);
+            union {
+                typename Vec<T>::x8 v;
+                uint32_t w[4];
+            } pf;
+            pf.v = round8<T>(s, 8 * t);
+            if (DROP)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t m[2];
+                    keep_pairs(w.w[2 * t + i], p.drop_below, m);
+                    pf.w[2 * i] &= m[0];
+                    pf.w[2 * i + 1] &= m[1];
+                }
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
-                o[dt] = mfma(read_columns<T, VTile>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf, o[dt]);
+                o[dt] = mfma(read_columns<T, VTile>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf.v, o[dt]);
         }
     };
     auto bits_of = [&](int buf, int ks) {
@@ -252,6 +261,7 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
 }
 
 struct Pass {
+    static constexpr bool kForward = true;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
         cross_forward_kernel<T, NS, OW, CW, (OW >= 4 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);

@@ -18,7 +18,12 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     typedef BothTile<NS> Tile;
     constexpr int kTile = QT * Tile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
-    constexpr int kLds = max_of(2 * kTile * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    // Wide heads: a wave's own rows of v stay in LDS, for the registers that
+    // its two accumulators and its rows of k leave do not hold them.
+    constexpr bool kOwnLds = NS > 4;
+    typedef RowTile<NS> OwnTile;
+    constexpr int kOwn = kOwnLds ? 32 * OW * CW * OwnTile::kRowBytes : 0;
+    constexpr int kLds = max_of(2 * kTile * kBufs + kOwn, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(256))) char lds[kLds];
     __shared__ f32x4 stat[kBufs][2][QT / 4];
     const int hk = blockIdx.x % p.heads_kv;
@@ -32,6 +37,10 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     typename Vec<T>::x8 kf[NS], vf[NS];
     load_own<T, NS>(kf, (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head, visible, half, p.dim);
     load_own<T, NS>(vf, (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head, visible, half, p.dim);
+    char *const own_v = lds + 2 * kTile * kBufs + (threadIdx.x >> 6) * 32 * OwnTile::kRowBytes;
+    if (kOwnLds)
+#pragma unroll
+        for (int t = 0; t < NS; ++t) *(typename Vec<T>::x8 *)(own_v + OwnTile::at(col, 2 * t + half)) = vf[t];
     f32x16 ok[ND], ov[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
@@ -56,7 +65,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
             s = mfma(rd.row(at_q, t), kf[t], s);
-            dp = mfma(rd.row(at_g, t), vf[t], dp);
+            dp = mfma(rd.row(at_g, t), kOwnLds ? read_rows<T, OwnTile>(own_v, col, 2 * t + half) : vf[t], dp);
         }
         uint32_t keep = 0xFFFFFFFF;  // bit i: the block's row i keeps this lane's key
         if (DROP) {
@@ -132,6 +141,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
 }
 
 struct Pass {
+    static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
         cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);

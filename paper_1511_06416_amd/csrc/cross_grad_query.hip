@@ -129,6 +129,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
 }
 
 struct Pass {
+    static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
         cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);

@@ -7,7 +7,6 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
-#include <cstdlib>
 #include <mutex>
 #include <new>
 #include <string>
@@ -85,11 +84,17 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     }
     if (order.empty()) return SAME_OK;
     std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return cut_of(a) > cut_of(b); });
-    // Tiles of 128 owners, of 64 where those leave much less of a tile empty,
-    // of 32 where no segment has more (then four waves share the other axis,
-    // if it is long enough to).
-    pp.own_waves = max_own <= 32 ? 1 : by2 < 0.85 * by4 ? 2 : 4;
-    if (getenv("OWX") && max_own > 32) pp.own_waves = getenv("OWX")[kind] - '0';
+    // Tiles of 128 owners.  Gradients up to 64 wide: 64 owners where that leaves
+    // much less of a tile empty (128 columns of 330 nodes, 8 heads of 64, a
+    // training step 150 against 170 us).  Forward above 64 wide: 256 owners, so
+    // that a key read from LDS serves more waves (4,099 x 7,951, 16 heads of
+    // 128, 582 against 628 us; 64 wide it loses, 139 against 132 us for 64
+    // columns of 1000 nodes).  Where no segment has more than 32 owners one
+    // wave has them, and four share the other axis if it is long enough.
+    pp.own_waves = 4;
+    if (kind == kForward && dim > 64 && max_own > 128) pp.own_waves = 8;
+    if (kind != kForward && dim <= 64 && by2 < 0.85 * by4) pp.own_waves = 2;
+    if (max_own <= 32) pp.own_waves = 1;
     pp.cut_waves = pp.own_waves == 1 && max_cut > 64 ? 4 : 1;
     const int64_t tile = 32 * pp.own_waves;
     const double room = 1024.0 * waves_per_simd(kind, dim) / (pp.own_waves * pp.cut_waves);  // blocks the chip holds
