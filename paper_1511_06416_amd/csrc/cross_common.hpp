@@ -279,16 +279,18 @@ struct SeenStage {
         if (mask) {
             m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), threadIdx.x, 0, 0);
             mask += KT;
-        } else {
-            m = (int)threadIdx.x < left;
         }
         left -= KT;
     }
     __device__ __forceinline__ void store(uint64_t *words) const {
         if (threadIdx.x < 64 * kWords) {
-            uint32_t v = (int)threadIdx.x < KT ? m : 0u;
-            asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
-            const uint64_t b = __ballot(v != 0);
+            bool in = (int)threadIdx.x < KT && (int)threadIdx.x < left + KT;
+            if (mask) {
+                uint32_t v = m;
+                asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
+                in = (int)threadIdx.x < KT && v != 0;
+            }
+            const uint64_t b = __ballot(in);
             if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = b;
         }
     }
