@@ -13,8 +13,9 @@ using namespace cross;
 // those heads stays in its accumulators.  S = Q K^T (rows x keys),
 // dV^T += dO^T (D P), dK^T += Q^T dS.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams p) {
-    constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
+__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
+    typedef Unit<NS, OW, CW> U;
+    constexpr int NT = U::kThreads, QT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> Tile;
     constexpr int kTile = QT * Tile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
@@ -24,11 +25,15 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     typedef RowTile<NS> OwnTile;
     constexpr int kOwn = kOwnLds ? 32 * OW * CW * OwnTile::kRowBytes : 0;
     constexpr int kLds = max_of(2 * kTile * kBufs + kOwn, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(256))) char lds[kLds];
-    __shared__ f32x4 stat[kBufs][2][QT / 4];
-    const int hk = blockIdx.x % p.heads_kv;
-    const CrossItem it = p.items[blockIdx.x / p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    __shared__ __attribute__((aligned(256))) char lds_all[U::kPerBlock][kLds];
+    __shared__ f32x4 stat_all[U::kPerBlock][kBufs][2][QT / 4];
+    char *const lds = lds_all[U::number()];
+    auto &stat = stat_all[U::number()];
+    const uint32_t index = U::index();
+    if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
+    const int hk = (int)(index % (uint32_t)p.heads_kv);
+    const CrossItem it = p.items[index / (uint32_t)p.heads_kv];
+    const int lane = threadIdx.x & 63, wave = unit_thread<NT>() >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -37,7 +42,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
     typename Vec<T>::x8 kf[NS], vf[NS];
     load_own<T, NS>(kf, (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head, visible, half, p.dim);
     load_own<T, NS>(vf, (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head, visible, half, p.dim);
-    char *const own_v = lds + 2 * kTile * kBufs + (threadIdx.x >> 6) * 32 * OwnTile::kRowBytes;
+    char *const own_v = lds + 2 * kTile * kBufs + (unit_thread<NT>() >> 6) * 32 * OwnTile::kRowBytes;
     if (kOwnLds)
 #pragma unroll
         for (int t = 0; t < NS; ++t) *(typename Vec<T>::x8 *)(own_v + OwnTile::at(col, 2 * t + half)) = vf[t];
@@ -52,11 +57,12 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
         sq.load(p);
         sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1]);
     }
-    __syncthreads();
+    unit_sync<NT>();
     BothReader<T, NS> rd(lds, lane);
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
-        sq.load(p);
+        const bool more = OW * CW > 1 || row + QT < it.end;
+        if (more) sq.load(p);
         if (ow * 32 < it.n_own) {  // waves without keys only help to load
         const int base = cw * 32;
         const uint32_t at_q = buf * 2 * kTile + base * Tile::kRowBytes, at_g = at_q + kTile;
@@ -113,12 +119,13 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dkv_kernel(CrossParams 
         }
         }
         if (kBufs == 1)
-            __syncthreads();
+            unit_sync<NT>();
         else
             buf ^= 1;
-        sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
-                                (float *)stat[buf][1]);
-        __syncthreads();
+        if (more)
+            sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
+                                    (float *)stat[buf][1]);
+        unit_sync<NT>();
     }
     if (CW > 1) {
         join_waves<ND, OW, CW>(ok, lds, ow, cw, lane);
@@ -144,7 +151,7 @@ struct Pass {
     static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+        cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(Unit<NS, OW, CW>::grid(p)), Unit<NS, OW, CW>::kBlock, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

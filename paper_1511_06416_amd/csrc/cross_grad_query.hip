@@ -12,19 +12,24 @@ using namespace cross;
 // P = exp(S - lse), dP^T = V dO^T, dS = P (D dP - delta),
 // dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p) {
-    constexpr int NT = 64 * OW * CW, KT = 32 * CW, ND = (NS + 1) / 2;
+__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void cross_dq_kernel(CrossParams p) {
+    typedef Unit<NS, OW, CW> U;
+    constexpr int NT = U::kThreads, KT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> KTile;
     typedef RowTile<NS> VTile;
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(256))) char lds[kLds];
-    __shared__ uint64_t seen[kBufs][SeenStage<KT>::kWords];
+    __shared__ __attribute__((aligned(256))) char lds_all[U::kPerBlock][kLds];
+    __shared__ uint64_t seen_all[U::kPerBlock][kBufs][SeenStage<KT, NT>::kWords];
+    char *const lds = lds_all[U::number()];
+    auto &seen = seen_all[U::number()];
     char *const lds_v = lds + kBufs * kTileK;
-    const int hk = blockIdx.x % p.heads_kv;
-    const CrossItem it = p.items[blockIdx.x / p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const uint32_t index = U::index();
+    if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
+    const int hk = (int)(index % (uint32_t)p.heads_kv);
+    const CrossItem it = p.items[index / (uint32_t)p.heads_kv];
+    const int lane = threadIdx.x & 63, wave = unit_thread<NT>() >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -55,7 +60,7 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
     const float gain = DROP ? p.keep_gain : 1.0f;
 
     KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
-    SeenStage<KT> ss(p, it);
+    SeenStage<KT, NT> ss(p, it);
     if (it.beg < it.end) {
         sk.load();
         sv.load();
@@ -64,13 +69,16 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         sv.template store<VTile>(lds_v);
         ss.store(seen[0]);
     }
-    __syncthreads();
+    unit_sync<NT>();
     BothReader<T, NS> rk(lds, lane);
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
-        sk.load();
-        sv.load();
-        ss.load();
+        const bool more = OW * CW > 1 || key + KT < it.end;
+        if (more) {
+            sk.load();
+            sv.load();
+            ss.load();
+        }
         if (ow * 32 < it.n_own) {  // waves without rows only help to load
         const int base = cw * 32;
         const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
@@ -106,13 +114,15 @@ __global__ __launch_bounds__(64 * OW * CW, 2) void cross_dq_kernel(CrossParams p
         }
         }
         if (kBufs == 1)
-            __syncthreads();
+            unit_sync<NT>();
         else
             buf ^= 1;
-        sk.template store<KTile>(lds + buf * kTileK);
-        sv.template store<VTile>(lds_v + buf * kTileV);
-        ss.store(seen[buf]);
-        __syncthreads();
+        if (more) {
+            sk.template store<KTile>(lds + buf * kTileK);
+            sv.template store<VTile>(lds_v + buf * kTileV);
+            ss.store(seen[buf]);
+        }
+        unit_sync<NT>();
     }
     if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
     if (CW > 1) {
@@ -132,7 +142,7 @@ struct Pass {
     static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
+        cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(Unit<NS, OW, CW>::grid(p)), Unit<NS, OW, CW>::kBlock, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {
