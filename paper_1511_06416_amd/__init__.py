@@ -234,6 +234,9 @@ def _st(ctx, t, m, ld, what="states"):
 def _stream(stream):
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:  # the same handle without a Stream object: 0.5 against 2.7 us
+            return C.c_void_p(raw(torch.cuda.current_device()))
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return C.c_void_p(stream)
@@ -538,9 +541,12 @@ def same_stream_pass_compact(ctx, lat_host, lat_off, obs_dev, data_dev, ld_dev, 
                                                    int(flags), _ptr(slots), _ptr(workspace), _stream(stream)))
 
 
+_DTYPES = {"torch.float32": SAME_F32, "torch.float16": SAME_F16, "torch.bfloat16": SAME_BF16}
+
+
 def _dtype(dtype):
     """SAME_F32, SAME_F16 or SAME_BF16 of a torch dtype."""
-    code = {"torch.float32": SAME_F32, "torch.float16": SAME_F16, "torch.bfloat16": SAME_BF16}.get(str(dtype))
+    code = _DTYPES.get(str(dtype))
     if code is None:
         raise SameError(SAME_EINVAL, "dtype must be torch.float32, torch.float16 or torch.bfloat16, got %s" % dtype)
     return code
@@ -566,15 +572,19 @@ class CrossPlan:
         self._h = h
         self.heads_q, self.heads_kv, self.head_dim, self.dtype = int(heads_q), int(heads_kv), int(head_dim), dtype
         self.n_q, self.n_k = int(qp[-1]), int(kp[-1])
+        self._q_shape, self._k_shape = (self.n_q, self.heads_q, self.head_dim), (self.n_k, self.heads_kv, self.head_dim)
+        out = C.c_size_t()
+        _check(load_library().same_cross_workspace_size(self._h, 0, C.byref(out)))
+        self._ws_forward = int(out.value)
+        _check(load_library().same_cross_workspace_size(self._h, 1, C.byref(out)))
+        self._ws_backward = int(out.value)
 
     @property
     def handle(self):
         return self._h
 
     def workspace_bytes(self, backward=False) -> int:
-        out = C.c_size_t()
-        _check(load_library().same_cross_workspace_size(self._h, 1 if backward else 0, C.byref(out)))
-        return int(out.value)
+        return self._ws_backward if backward else self._ws_forward
 
     def new_workspace(self, backward=False, device="cuda"):
         """A workspace of the forward pass, or (backward) one that serves both."""
@@ -595,38 +605,48 @@ class CrossPlan:
         except Exception:
             pass
 
-    def _tensor(self, name, t, tokens, heads, contiguous=False):
-        """Shape, type and layout of a [tokens][heads][head_dim] tensor; its
-        address and the element strides of a token and a head."""
-        want = (tokens, heads, self.head_dim)
-        _on_device(name, t)
-        if tuple(t.shape) != want or t.dtype != self.dtype:
-            raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
-                            % (name, self.dtype, want, t.dtype, tuple(t.shape)))
-        if contiguous and not t.is_contiguous():
-            raise SameError(SAME_EINVAL, "%s must be contiguous" % name)
-        if t.numel() and t.stride(2) != 1:
+    # Argument checks run before every call, so they read each property once.
+    def _strided(self, name, t, want):
+        """Address and element strides of a token and a head of an input
+        [tokens][heads][head_dim]."""
+        if t.shape != want or t.dtype != self.dtype or not t.is_cuda:
+            self._refuse(name, t, want)
+        row, head, unit = t.stride()
+        if unit != 1 and t.numel():
             raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-        return [_ptr(t), t.stride(0) if tokens > 1 else 0, t.stride(1) if heads > 1 else 0]
+        return t.data_ptr(), row if want[0] > 1 else 0, head if want[1] > 1 else 0
 
-    def _inputs(self, q, k, v, key_mask, workspace, backward):
-        args = (self._tensor("q", q, self.n_q, self.heads_q) + self._tensor("k", k, self.n_k, self.heads_kv)
-                + self._tensor("v", v, self.n_k, self.heads_kv))
+    def _whole(self, name, t, want):
+        """Address of a contiguous output (or the forward's output)."""
+        if t.shape != want or t.dtype != self.dtype or not t.is_cuda:
+            self._refuse(name, t, want)
+        if not t.is_contiguous():
+            raise SameError(SAME_EINVAL, "%s must be contiguous" % name)
+        return t.data_ptr()
+
+    def _refuse(self, name, t, want):
+        _on_device(name, t)
+        raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
+                        % (name, self.dtype, want, t.dtype, tuple(t.shape)))
+
+    def _inputs(self, q, k, v, key_mask, workspace, need):
         if key_mask is not None:
             _on_device("key_mask", key_mask)
-            if tuple(key_mask.shape) != (self.n_k,) or key_mask.element_size() != 1 or not key_mask.is_contiguous():
+            if key_mask.shape != (self.n_k,) or key_mask.element_size() != 1 or not key_mask.is_contiguous():
                 raise SameError(SAME_EINVAL, "key_mask must be a contiguous byte per key token")
-        need = self.workspace_bytes(backward)
-        if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-            raise SameError(SAME_EINVAL, "workspace must have at least %d bytes" % need)
-        return args + [_ptr(key_mask)]
+            key_mask = key_mask.data_ptr()
+        if need:
+            if workspace is None or workspace.numel() * workspace.element_size() < need:
+                raise SameError(SAME_EINVAL, "workspace must have at least %d bytes" % need)
+            _on_device("workspace", workspace)
+        return (*self._strided("q", q, self._q_shape), *self._strided("k", k, self._k_shape),
+                *self._strided("v", v, self._k_shape), key_mask)
 
     def _lse(self, lse):
-        import torch
+        if lse.shape != self._q_shape[:2] or str(lse.dtype) != "torch.float32" or not lse.is_contiguous():
+            raise SameError(SAME_EINVAL, "lse must be contiguous torch.float32 of shape %s" % (self._q_shape[:2],))
         _on_device("lse", lse)
-        if tuple(lse.shape) != (self.n_q, self.heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise SameError(SAME_EINVAL, "lse must be contiguous torch.float32 of shape %s" % ((self.n_q, self.heads_q),))
-        return _ptr(lse)
+        return lse.data_ptr()
 
 
 def same_cross_create(q_ptr, k_ptr, heads_q, heads_kv, head_dim, dtype) -> CrossPlan:
@@ -644,38 +664,40 @@ def same_cross_workspace_size(plan: CrossPlan, backward=False) -> int:
 def same_cross_attention(plan, q, k, v, out, lse, workspace, key_mask=None, scale=None, drop=0.0, seed=0, call_id=0,
                          stream=None):
     """lse may be None; scale defaults to head_dim ** -0.5."""
-    args = plan._inputs(q, k, v, key_mask, workspace, False)
-    _check(load_library().same_cross_attention(
-        plan.handle, *args, float(plan.head_dim ** -0.5 if scale is None else scale), float(drop), int(seed),
-        int(call_id), plan._tensor("out", out, plan.n_q, plan.heads_q, True)[0], None if lse is None else plan._lse(lse),
-        _ptr(workspace), _stream(stream)))
+    _check((_lib or load_library()).same_cross_attention(
+        plan.handle, *plan._inputs(q, k, v, key_mask, workspace, plan._ws_forward),
+        plan.head_dim ** -0.5 if scale is None else float(scale), float(drop), int(seed), int(call_id), plan._whole("out", out, plan._q_shape),
+        None if lse is None else plan._lse(lse), None if workspace is None else workspace.data_ptr(), _stream(stream)))
 
 
 def same_cross_attention_backward(plan, q, k, v, out, lse, dout, dq, dk, dv, workspace, key_mask=None, scale=None,
                                   drop=0.0, seed=0, call_id=0, stream=None):
-    args = plan._inputs(q, k, v, key_mask, workspace, True)
-    _check(load_library().same_cross_attention_backward(
-        plan.handle, *args, float(plan.head_dim ** -0.5 if scale is None else scale), float(drop), int(seed),
-        int(call_id), plan._tensor("out", out, plan.n_q, plan.heads_q, True)[0], plan._lse(lse),
-        *plan._tensor("dout", dout, plan.n_q, plan.heads_q),
-        plan._tensor("dq", dq, plan.n_q, plan.heads_q, True)[0],
-        plan._tensor("dk", dk, plan.n_k, plan.heads_kv, True)[0],
-        plan._tensor("dv", dv, plan.n_k, plan.heads_kv, True)[0], _ptr(workspace), _stream(stream)))
+    _check((_lib or load_library()).same_cross_attention_backward(
+        plan.handle, *plan._inputs(q, k, v, key_mask, workspace, plan._ws_backward),
+        plan.head_dim ** -0.5 if scale is None else float(scale), float(drop), int(seed), int(call_id), plan._whole("out", out, plan._q_shape),
+        plan._lse(lse), *plan._strided("dout", dout, plan._q_shape), plan._whole("dq", dq, plan._q_shape),
+        plan._whole("dk", dk, plan._k_shape), plan._whole("dv", dv, plan._k_shape),
+        None if workspace is None else workspace.data_ptr(), _stream(stream)))
+
+
+def _matrix(name, t, like):
+    """Address and row stride of a matrix shaped and typed like another."""
+    if t.dim() != 2 or t.shape != like.shape or t.dtype != like.dtype or not t.is_cuda:
+        _on_device(name, t)
+        raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like x" % name)
+    row, unit = t.stride()
+    if unit != 1 and t.shape[1] > 1:
+        raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+    return t.data_ptr(), row
 
 
 def same_dropout(x, y, drop, seed, call_id, residual=None, stream=None):
     """Two-dimensional tensors of one type with unit stride in the last axis."""
     dtype = _dtype(x.dtype)
-    rows = []
-    for name, t in (("x", x), ("y", y), ("residual", residual)):
-        if t is None:
-            rows.append(0)
-            continue
-        _on_device(name, t)
-        if t.dim() != 2 or t.shape != x.shape or t.dtype != x.dtype:
-            raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like x" % name)
-        if t.shape[1] > 1 and t.stride(1) != 1:
-            raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-        rows.append(t.stride(0))
-    _check(load_library().same_dropout(dtype, _ptr(x), rows[0], _ptr(residual), rows[2], x.shape[0], x.shape[1],
-                                       float(drop), int(seed), int(call_id), _ptr(y), rows[1], _stream(stream)))
+    px, x_row = _matrix("x", x, x)
+    pr, r_row = (None, 0) if residual is None else _matrix("residual", residual, x)
+    py, y_row = _matrix("y", y, x)
+    rows, cols = x.shape
+    _check((_lib or load_library()).same_dropout(dtype, px, x_row, pr, r_row, rows, cols, float(drop), int(seed),
+                                                 int(call_id), py, y_row,
+                                                 _stream(stream)))

@@ -158,16 +158,6 @@ __device__ __forceinline__ void keep_pairs(uint32_t w, uint32_t below, uint32_t 
     m[1] = __builtin_amdgcn_perm(up, ge, 0x09090B0Bu);
 }
 
-// The same as flags, bit e = accumulator element e.
-__device__ __forceinline__ uint32_t keep_bits(const CrossParams &p, int64_t row, int kb, int half) {
-    const dev::Philox4 w = keep_words(p, row, kb, half);
-    uint32_t bits = 0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-        bits |= (kept(w, e, p.drop_below) ? 1u : 0u) << e;
-    return bits;
-}
-
 template <typename T>
 __device__ __forceinline__ typename Vec<T>::x8 zero8() {
     typename Vec<T>::x8 z;
@@ -355,7 +345,7 @@ struct QueryStage {
     int left;                          // rows from this thread's first one to the end; 0 for idle lanes
     int64_t step_q, wrap_q, step_g, wrap_g;
     int step, group;
-    int64_t id, step_id;               // this thread's row of the statistics
+    int64_t id, step_id, loaded_id;    // this thread's row of the statistics
     int id_g, id_left, heads;
     float lse, delta;
     __device__ __forceinline__ QueryStage(const CrossParams &p, const CrossItem &it, int hk) {
@@ -398,6 +388,7 @@ struct QueryStage {
         left -= ROWS;
         lse = -kInf;
         delta = 0.0f;
+        loaded_id = id;
         if (id_left > 0) {
             lse = p.lse[id];
             delta = p.delta[id];
@@ -408,14 +399,17 @@ struct QueryStage {
         id += step_id + (over ? heads - group : 0);
         id_left -= ROWS;
     }
-    // A row without a visible key, or past the end, gets exponent -inf.
+    // A row without a visible key, or past the end, gets exponent -inf.  Its
+    // number is that of the tile just loaded.
     template <typename Tile>
-    __device__ __forceinline__ void store(char *tq, char *tg, float *stat_lse, float *stat_delta) const {
+    __device__ __forceinline__ void store(char *tq, char *tg, float *stat_lse, float *stat_delta,
+                                          int64_t *stat_id) const {
         L::template store<Tile>(tq, a);
         L::template store<Tile>(tg, b);
         if (unit_thread<NT>() < ROWS) {
             stat_lse[unit_thread<NT>()] = lse == -kInf ? kInf : lse * kLog2e;
             stat_delta[unit_thread<NT>()] = delta;
+            if (stat_id) stat_id[unit_thread<NT>()] = loaded_id;
         }
     }
 };

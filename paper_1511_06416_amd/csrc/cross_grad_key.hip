@@ -29,6 +29,10 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     __shared__ f32x4 stat_all[U::kPerBlock][kBufs][2][QT / 4];
     char *const lds = lds_all[U::number()];
     auto &stat = stat_all[U::number()];
+    __shared__ int64_t id_all[U::kPerBlock][kBufs][DROP ? QT : 1];
+    __shared__ __attribute__((aligned(256))) char turn_all[DROP ? U::kBlock / 64 : 1][2048];
+    auto &stat_id = id_all[U::number()];
+    char *const turn = turn_all[DROP ? threadIdx.x >> 6 : 0];
     const uint32_t index = U::index();
     if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
     const int hk = (int)(index % (uint32_t)p.heads_kv);
@@ -55,7 +59,8 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     QueryStage<T, NS, QT, NT> sq(p, it, hk);
     if (it.beg < it.end) {
         sq.load(p);
-        sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1]);
+        sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1],
+                                DROP ? stat_id[0] : nullptr);
     }
     unit_sync<NT>();
     BothReader<T, NS> rd(lds, lane);
@@ -73,20 +78,35 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
             s = mfma(rd.row(at_q, t), kf[t], s);
             dp = mfma(rd.row(at_g, t), kOwnLds ? read_rows<T, OwnTile>(own_v, col, 2 * t + half) : vf[t], dp);
         }
-        uint32_t keep = 0xFFFFFFFF;  // bit i: the block's row i keeps this lane's key
+        // The keep numbers are made as in the other passes, a lane a row and 16
+        // keys of it; as 16-bit masks they are turned in LDS like an operand,
+        // so that a lane gets those of its key and accumulator rows.
+        uint32_t mask[8];
         if (DROP) {
-            // the flags are made row by row, as in the other passes (a lane a
-            // row, 16 keys); a ballot per element turns them into one word of
-            // 32 rows per key, and lane l takes the word of key l % 32
-            const int rr = row + base + col;
-            const int64_t id = row_id(p, it.q0, rr < it.end ? rr : it.end - 1, hk);
-            const uint32_t mine = keep_bits(p, id, (it.own0 + ow * 32) >> 5, half);
+            const dev::Philox4 bits = keep_words(p, stat_id[buf][base + col], (it.own0 + ow * 32) >> 5, half);
+            uint32_t *const mine = (uint32_t *)(turn + col * 64 + half * 8);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint64_t b = __ballot((mine >> e) & 1);
-                if (col == acc_row(e, 0)) keep = (uint32_t)b;
-                if (col == acc_row(e, 1)) keep = (uint32_t)(b >> 32);
+            for (int g = 0; g < 4; ++g) {
+                uint32_t m[2];
+                keep_pairs(bits.w[g], p.drop_below, m);
+                mine[4 * g] = m[0];
+                mine[4 * g + 1] = m[1];
             }
+            unit_sync<64>();
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const int t = lane & 15;
+            const char *from = turn + (4 * half + (t >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (t & 3) * 8;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                union {
+                    s16x4 h;
+                    uint32_t w[2];
+                } u;
+                u.h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 8 * g * 64));
+                mask[2 * g] = u.w[0];
+                mask[2 * g + 1] = u.w[1];
+            }
+            unit_sync<64>();
         }
         f32x16 w;
 #pragma unroll
@@ -96,16 +116,15 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int e = 4 * g + i;
-                float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -l4[i]));
-                x = visible ? x : 0.0f;
-                float d = dp[e];
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -l4[i]));
                 w[e] = x;
                 if (DROP) {
-                    const bool kept = (keep >> acc_row(e, half)) & 1;
-                    d = kept ? d * gain : 0.0f;
-                    w[e] = kept ? x : 0.0f;
+                    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)mask[e >> 1], 16 * (e & 1), 16);
+                    w[e] = __uint_as_float(__float_as_uint(x) & m);
+                    s[e] = __builtin_fmaf(w[e], dp[e], -x * d4[i]);   // dS / gain
+                } else {
+                    s[e] = x * (dp[e] - d4[i]);
                 }
-                s[e] = x * (d - d4[i]);
             }
         }
 #pragma unroll
@@ -124,7 +143,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
             buf ^= 1;
         if (more)
             sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
-                                    (float *)stat[buf][1]);
+                                    (float *)stat[buf][1], DROP ? stat_id[buf] : nullptr);
         unit_sync<NT>();
     }
     if (CW > 1) {
@@ -143,7 +162,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
         return;
     }
     const int64_t at = (tok * p.heads_kv + hk) * p.dim;
-    write_owner<T, ND>((T *)p.dk + at, ok, p.scale, half, p.dim);
+    write_owner<T, ND>((T *)p.dk + at, ok, p.scale * gain, half, p.dim);
     write_owner<T, ND>((T *)p.dv + at, ov, gain, half, p.dim);
 }
 

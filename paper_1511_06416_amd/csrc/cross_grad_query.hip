@@ -10,7 +10,8 @@ using namespace cross;
 //
 // A wave owns 32 query rows and walks the keys as the forward does:
 // P = exp(S - lse), dP^T = V dO^T, dS = P (D dP - delta),
-// dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV.
+// dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV
+// divided by D's value, which every gradient takes at its end.
 template <typename T, int NS, int OW, int CW, bool DROP>
 __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void cross_dq_kernel(CrossParams p) {
     typedef Unit<NS, OW, CW> U;
@@ -91,21 +92,26 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void c
             dp = mfma(read_rows<T, VTile>(tv, base + col, 2 * t + half), gf[t], dp);
         }
         if (p.key_mask || key + KT > it.end) hide(s, (uint32_t)(seen[buf][cw >> 1] >> (32 * (cw & 1))), half, -kInf);
-        uint32_t keep = 0xFFFF;
-        if (DROP) keep = keep_bits(p, row, (key + base) >> 5, half);
+        dev::Philox4 bits;
+        if (DROP) bits = keep_words(p, row, (key + base) >> 5, half);
+        // dS / gain = (keep P) dP - P delta / gain
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
-            if (DROP) dp[e] = (keep >> e) & 1 ? dp[e] * gain : 0.0f;
-        }
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
         if (short_row) {
             float d = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) d = __builtin_fmaf(s[e], dp[e], d);
-            delta = both_sum(d);
+            for (int e = 0; e < 16; ++e)
+                d = __builtin_fmaf(!DROP || kept(bits, e, p.drop_below) ? s[e] : 0.0f, dp[e], d);
+            delta = both_sum(d) * gain;
         }
+        const float rest = DROP ? delta / gain : delta;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
+        for (int e = 0; e < 16; ++e) {
+            if (DROP)
+                s[e] = __builtin_fmaf(kept(bits, e, p.drop_below) ? s[e] : 0.0f, dp[e], -s[e] * rest);
+            else
+                s[e] *= dp[e] - rest;
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
@@ -124,7 +130,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void c
         }
         unit_sync<NT>();
     }
-    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = delta;
+    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = DROP ? delta / gain : delta;
     if (CW > 1) {
         join_waves<ND, OW, CW>(o, lds, ow, cw, lane);
         if (cw != 0) return;
@@ -135,7 +141,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void c
         write_part<ND>(p.part + at * p.dim, o, half, p.dim);
         return;
     }
-    write_owner<T, ND>((T *)p.dq + row * p.dim, o, p.scale, half, p.dim);
+    write_owner<T, ND>((T *)p.dq + row * p.dim, o, p.scale * gain, half, p.dim);
 }
 
 struct Pass {

@@ -21,12 +21,12 @@ __global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, con
 #pragma unroll 8
         for (int s = 0; s < j.n_parts; ++s) acc += *(const f32x4 *)(src + s * step);
         T *dst;
-        float gain = p.scale;
+        float gain = p.scale * p.keep_gain;
         if (SIDES == 1) {
             dst = (T *)p.dq + row_id(p, j.q0, j.own0 + own, hk) * p.dim;
         } else {
             dst = (T *)(side ? p.dv : p.dk) + ((j.k0 + j.own0 + own) * p.heads_kv + hk) * p.dim;
-            gain = side ? p.keep_gain : p.scale;
+            if (side) gain = p.keep_gain;
         }
         typename Vec<T>::x4 w;
 #pragma unroll
