@@ -13,7 +13,7 @@ using namespace cross;
 // dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV
 // divided by D's value, which every gradient takes at its end.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 4 : 2) void cross_dq_kernel(CrossParams p) {
+__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
     typedef Unit<NS, OW, CW> U;
     constexpr int NT = U::kThreads, KT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> KTile;
