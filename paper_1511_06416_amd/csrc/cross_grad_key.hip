@@ -42,26 +42,33 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
     const int64_t tok = it.k0 + it.own0 + (valid ? own : 0);
-    const bool visible = valid && (!p.key_mask || p.key_mask[tok] != 0);
+    // every load of the prologue is under way before the first is waited for
     typename Vec<T>::x8 kf[NS], vf[NS];
-    load_own<T, NS>(kf, (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head, visible, half, p.dim);
-    load_own<T, NS>(vf, (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head, visible, half, p.dim);
+    load_own<T, NS>(kf, (const T *)p.k.p + tok * p.k.row + (int64_t)hk * p.k.head, valid, half, p.dim);
+    load_own<T, NS>(vf, (const T *)p.v.p + tok * p.v.row + (int64_t)hk * p.v.head, valid, half, p.dim);
+    uint32_t byte = 1;
+    if (p.key_mask) byte = p.key_mask[tok];
+    QueryStage<T, NS, QT, NT> sq(p, it, hk);
+    if (it.beg < it.end) sq.load(p);
+    const bool visible = valid && byte != 0;
+    if (p.key_mask)
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            kf[t] = visible ? kf[t] : zero8<T>();
+            vf[t] = visible ? vf[t] : zero8<T>();
+        }
     char *const own_v = lds + 2 * kTile * kBufs + (unit_thread<NT>() >> 6) * 32 * OwnTile::kRowBytes;
     if (kOwnLds)
 #pragma unroll
         for (int t = 0; t < NS; ++t) *(typename Vec<T>::x8 *)(own_v + OwnTile::at(col, 2 * t + half)) = vf[t];
+    if (it.beg < it.end)
+        sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1],
+                                DROP ? stat_id[0] : nullptr);
     f32x16 ok[ND], ov[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
     const float c = p.scale * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
-
-    QueryStage<T, NS, QT, NT> sq(p, it, hk);
-    if (it.beg < it.end) {
-        sq.load(p);
-        sq.template store<Tile>(lds, lds + kTile, (float *)stat[0][0], (float *)stat[0][1],
-                                DROP ? stat_id[0] : nullptr);
-    }
     unit_sync<NT>();
     BothReader<T, NS> rd(lds, lane);
     int buf = 0;

@@ -13,7 +13,7 @@ using namespace cross;
 // dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV
 // divided by D's value, which every gradient takes at its end.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
+__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), OW == 1 && CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
     typedef Unit<NS, OW, CW> U;
     constexpr int NT = U::kThreads, KT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> KTile;
@@ -36,19 +36,30 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     const bool valid = own < it.n_own;
     const int r = valid ? it.own0 + own : it.own0;
     const int64_t row = row_id(p, it.q0, r, hk);
-    typename Vec<T>::x8 qf[NS], gf[NS];
-    load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
-    load_own<T, NS>(gf, (const T *)p.dout.p + row_at(p.dout, it.q0, r, p.group, hk), valid, half, p.dim);
-    float delta = 0.0f;
-    {
-        typename Vec<T>::x8 of[NS];
-        load_own<T, NS>(of, (const T *)p.out_in + row * p.dim, valid, half, p.dim);
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
-        delta = both_sum(delta);
+    // every load of the prologue is under way before the first is waited for
+    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
+    SeenStage<KT, NT> ss(p, it);
+    if (it.beg < it.end) {
+        sk.load();
+        sv.load();
+        ss.load();
     }
+    typename Vec<T>::x8 qf[NS], gf[NS], of[NS];
+    load_own<T, NS>(gf, (const T *)p.dout.p + row_at(p.dout, it.q0, r, p.group, hk), valid, half, p.dim);
+    load_own<T, NS>(of, (const T *)p.out_in + row * p.dim, valid, half, p.dim);
+    load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
+    const float lse = valid ? p.lse[row] : -kInf;
+    if (it.beg < it.end) {
+        sk.template store<KTile>(lds);
+        sv.template store<VTile>(lds_v);
+        ss.store(seen[0]);
+    }
+    float delta = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
+    delta = both_sum(delta);
     // Up to 32 keys lie in one wave, which then forms delta from P and dP in fp32:
     // with so few keys out's rounding would cost dS a good part of its digits.
     const bool short_row = it.slot < 0 && it.end - it.beg <= 32;
@@ -56,20 +67,9 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
     const float c = p.scale * kLog2e;
-    const float lse = valid ? p.lse[row] : -kInf;
     const float base2 = lse == -kInf ? kInf : lse * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
 
-    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
-    SeenStage<KT, NT> ss(p, it);
-    if (it.beg < it.end) {
-        sk.load();
-        sv.load();
-        ss.load();
-        sk.template store<KTile>(lds);
-        sv.template store<VTile>(lds_v);
-        ss.store(seen[0]);
-    }
     unit_sync<NT>();
     BothReader<T, NS> rk(lds, lane);
     int buf = 0;
