@@ -25,6 +25,14 @@ struct CrossJoin {
     int32_t slot, n_parts;
 };
 
+// One wave's work where segments are small: neighbouring segments with at most
+// 32 query rows (of one key head) and 32 keys together.
+struct CrossSmallItem {
+    int64_t q0, k0;           // first query token and first key
+    int32_t n_rows, n_keys;
+    uint16_t range[32];       // a row's keys in the tile: first | (last + 1) << 8
+};
+
 struct CrossPass {
     const CrossItem *items;
     const CrossJoin *joins;
@@ -45,6 +53,7 @@ struct CrossParams {
     float *lse, *delta;        // [tokens][heads]
     float *part, *part_ml;     // parts: [slot][key head][owner][head_dim], (max, sum)
     const CrossItem *items;
+    const CrossSmallItem *small;
     int32_t n_items;
     int32_t heads_q, heads_kv, group, dim;
     float scale;
@@ -58,6 +67,7 @@ constexpr int kJoinOwners = 8;  // owners that a join's block takes
 constexpr int kMaxParts = 64;   // of one tile
 
 hipError_t launch_cross_forward(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);
+hipError_t launch_cross_small(const CrossParams &p, bool grad, int dtype, hipStream_t s);
 hipError_t launch_cross_dq(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);
 hipError_t launch_cross_dkv(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);
 

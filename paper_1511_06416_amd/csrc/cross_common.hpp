@@ -166,43 +166,13 @@ __device__ __forceinline__ typename Vec<T>::x8 zero8() {
     return z;
 }
 
-// A unit is the waves that work on one item of a work list: a block, or,
-// where one wave has the item alone, one wave of a block of several (a block
-// is dispatched in about the time that such an item takes).
-template <int NS, int OW, int CW>
-struct Unit {
-    static constexpr int kThreads = 64 * OW * CW;
-    static constexpr int kPerBlock = OW * CW > 1 ? 1 : NS <= 4 ? 4 : 2;
-    static constexpr int kBlock = kThreads * kPerBlock;
-    __device__ static __forceinline__ int number() { return kPerBlock == 1 ? 0 : (int)threadIdx.x / kThreads; }
-    __device__ static __forceinline__ uint32_t index() {
-        if (kPerBlock == 1) return blockIdx.x;
-        return blockIdx.x * kPerBlock + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
-    }
-    static uint32_t grid(const CrossParams &p) {
-        return (uint32_t)(((int64_t)p.n_items * p.heads_kv + kPerBlock - 1) / kPerBlock);
-    }
-};
-
-// Threads of a unit of NT, and the wait for all of them.
-template <int NT>
-__device__ __forceinline__ int unit_thread() {
-    return NT == 64 ? (int)threadIdx.x & 63 : (int)threadIdx.x;
-}
-template <int NT>
-__device__ __forceinline__ void unit_sync() {
-    if (NT == 64) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    } else {
-        __syncthreads();
-    }
+// Orders a wave's own LDS traffic, for the compiler too.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// Blocks: a work item's key heads are neighbours.  Blocks go to the eight
-// XCDs in turn, so that with 1, 2, 4 or 8 m key heads an XCD's L2 holds the
-// keys of one (or m) of them.
 // ROWS rows on their way from global memory to LDS, 16 bytes a lane: a thread
 // takes the same chunk of every kStep-th row.
 template <typename T, int NS, int ROWS, int NT>
@@ -211,8 +181,8 @@ struct Lanes {
     static constexpr int kStep = (NT >= 512 ? 512 : NT >= 256 ? 256 : NT >= 128 ? 128 : 64) / kSlots;
     static constexpr int kN = (ROWS + kStep - 1) / kStep;
     static_assert(ROWS % kStep == 0 || kN == 1, "whole rows per thread");
-    __device__ static __forceinline__ int row() { return unit_thread<NT>() / kSlots; }
-    __device__ static __forceinline__ int slot() { return unit_thread<NT>() % kSlots; }
+    __device__ static __forceinline__ int row() { return (int)threadIdx.x / kSlots; }
+    __device__ static __forceinline__ int slot() { return (int)threadIdx.x % kSlots; }
     // lanes without a chunk of the tile, or past the width
     __device__ static __forceinline__ bool idle() { return slot() >= 2 * NS || row() >= (kN == 1 ? ROWS : kStep); }
     template <typename Tile>
@@ -304,21 +274,21 @@ struct SeenStage {
     }
     __device__ __forceinline__ void load() {
         if (mask) {
-            m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), unit_thread<NT>(), 0, 0);
+            m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), (int)threadIdx.x, 0, 0);
             mask += KT;
         }
         left -= KT;
     }
     __device__ __forceinline__ void store(uint64_t *words) const {
-        if (unit_thread<NT>() < 64 * kWords) {
-            bool in = unit_thread<NT>() < KT && unit_thread<NT>() < left + KT;
+        if ((int)threadIdx.x < 64 * kWords) {
+            bool in = (int)threadIdx.x < KT && (int)threadIdx.x < left + KT;
             if (mask) {
                 uint32_t v = m;
                 asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
-                in = unit_thread<NT>() < KT && v != 0;
+                in = (int)threadIdx.x < KT && v != 0;
             }
             const uint64_t b = __ballot(in);
-            if ((unit_thread<NT>() & 63) == 0) words[unit_thread<NT>() >> 6] = b;
+            if (((int)threadIdx.x & 63) == 0) words[(int)threadIdx.x >> 6] = b;
         }
     }
 };
@@ -366,10 +336,10 @@ struct QueryStage {
             pg[n] = (const T *)p.dout.p + row_at(p.dout, it.q0, r, group, hk) + L::slot() * 8;
         }
         left = L::slot() * 8 < p.dim && !L::idle() ? it.end - it.beg - L::row() : 0;
-        const int r = it.beg + unit_thread<NT>();
+        const int r = it.beg + (int)threadIdx.x;
         id = row_id(p, it.q0, r, hk);
         id_g = r % group;
-        id_left = unit_thread<NT>() < ROWS ? it.end - r : 0;
+        id_left = (int)threadIdx.x < ROWS ? it.end - r : 0;
     }
     __device__ __forceinline__ void load(const CrossParams &p) {
 #pragma unroll
@@ -406,10 +376,10 @@ struct QueryStage {
                                           int64_t *stat_id) const {
         L::template store<Tile>(tq, a);
         L::template store<Tile>(tg, b);
-        if (unit_thread<NT>() < ROWS) {
-            stat_lse[unit_thread<NT>()] = lse == -kInf ? kInf : lse * kLog2e;
-            stat_delta[unit_thread<NT>()] = delta;
-            if (stat_id) stat_id[unit_thread<NT>()] = loaded_id;
+        if ((int)threadIdx.x < ROWS) {
+            stat_lse[(int)threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e;
+            stat_delta[(int)threadIdx.x] = -delta;
+            if (stat_id) stat_id[(int)threadIdx.x] = loaded_id;
         }
     }
 };
@@ -506,6 +476,8 @@ constexpr int max_of(int a, int b) { return a > b ? a : b; }
 template <bool FORWARD, int NS>
 constexpr int kWide = FORWARD ? (NS > 4 ? 8 : 4) : (NS > 4 ? 4 : 2);
 
+inline uint32_t grid_of(const CrossParams &p) { return (uint32_t)p.n_items * (uint32_t)p.heads_kv; }
+
 template <typename Pass, typename T, int NS, int OW, int CW>
 void launch_drop(const CrossParams &p, hipStream_t s) {
     if (p.drop_below)
@@ -521,10 +493,8 @@ void launch_shape(const CrossParams &p, const CrossPass &w, hipStream_t s) {
         launch_drop<Pass, T, NS, kWide<Pass::kForward, NS>, 1>(p, s);
     else if (w.own_waves == 4)
         launch_drop<Pass, T, NS, 4, 1>(p, s);
-    else if (w.cut_waves == 4)
-        launch_drop<Pass, T, NS, 1, 4>(p, s);
     else
-        launch_drop<Pass, T, NS, 1, 1>(p, s);
+        launch_drop<Pass, T, NS, 1, 4>(p, s);
 }
 
 template <typename Pass, typename T>

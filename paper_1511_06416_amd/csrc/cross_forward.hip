@@ -16,9 +16,8 @@ using namespace cross;
 // the keys in accumulator order, and V^T is read transposed from LDS in the
 // same order.
 template <typename T, int NS, int OW, int CW, int KS, bool DROP>
-__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS <= 4 && OW > 1 ? 4 : 2) void cross_forward_kernel(CrossParams p) {
-    typedef Unit<NS, OW, CW> U;
-    constexpr int NT = U::kThreads, KT = 32 * KS * CW, ND = (NS + 1) / 2;
+__global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross_forward_kernel(CrossParams p) {
+    constexpr int NT = 64 * OW * CW, KT = 32 * KS * CW, ND = (NS + 1) / 2;
     typedef RowTile<NS> KTile;
     typedef ColumnTile<NS> VTile;
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
@@ -31,17 +30,13 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS <= 4 && OW > 1 ? 4 :
     constexpr bool kAhead = OW > 1 && NS > 4;
     constexpr int kBufs = kAhead ? 2 : 1;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(16))) char lds_all[U::kPerBlock][kLds];
-    __shared__ uint64_t seen_all[U::kPerBlock][2][SeenStage<KT, NT>::kWords];
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    __shared__ uint64_t seen[2][SeenStage<KT, NT>::kWords];
     __shared__ float stat[2][OW * CW * 32];
-    char *const lds = lds_all[U::number()];
-    auto &seen = seen_all[U::number()];
     char *const lds_v = lds + kBufs * kTileK;
-    const uint32_t index = U::index();
-    if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
-    const int hk = (int)(index % (uint32_t)p.heads_kv);
-    const CrossItem it = p.items[index / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = unit_thread<NT>() >> 6, half = lane >> 5, col = lane & 31;
+    const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
+    const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
+    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -132,19 +127,16 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS <= 4 && OW > 1 ? 4 :
         sv.template store<VTile>(lds_v);
         ss.store(seen[0]);
         if (kAhead) first.template store<KTile>(lds + kTileK);
-        unit_sync<NT>();
+        __syncthreads();
         if (kAhead) {
             s = scores(lds + kTileK, -cw * KS);
-            unit_sync<NT>();
+            __syncthreads();
         }
         int buf = 0;
         for (int key = it.beg; key < it.end; key += KT) {
-            const bool more = OW * CW > 1 || key + KT < it.end;
-            if (more) {
-                sk.load();
-                sv.load();
-                ss.load();
-            }
+            sk.load();
+            sv.load();
+            ss.load();
             const bool masked = p.key_mask || key + KT > it.end;
             const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
             if (works)
@@ -161,13 +153,11 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS <= 4 && OW > 1 ? 4 :
             if (kAhead)
                 buf ^= 1;
             else
-                unit_sync<NT>();
-            if (more) {
-                sk.template store<KTile>(lds + buf * kTileK);
-                sv.template store<VTile>(lds_v + buf * kTileV);
-                ss.store(seen[buf]);
-            }
-            unit_sync<NT>();
+                __syncthreads();
+            sk.template store<KTile>(lds + buf * kTileK);
+            sv.template store<VTile>(lds_v + buf * kTileV);
+            ss.store(seen[buf]);
+            __syncthreads();
         }
     }
     sum = both_sum(sum);
@@ -274,7 +264,7 @@ struct Pass {
     static constexpr bool kForward = true;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_forward_kernel<T, NS, OW, CW, (OW >= 4 && NS > 4 ? 2 : 1), DROP><<<dim3(Unit<NS, OW, CW>::grid(p)), Unit<NS, OW, CW>::kBlock, 0, s>>>(p);
+        cross_forward_kernel<T, NS, OW, CW, (OW >= 4 && NS > 4 ? 2 : 1), DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

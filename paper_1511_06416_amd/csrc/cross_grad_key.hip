@@ -13,9 +13,8 @@ using namespace cross;
 // those heads stays in its accumulators.  S = Q K^T (rows x keys),
 // dV^T += dO^T (D P), dK^T += Q^T dS.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
-    typedef Unit<NS, OW, CW> U;
-    constexpr int NT = U::kThreads, QT = 32 * CW, ND = (NS + 1) / 2;
+__global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
+    constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> Tile;
     constexpr int kTile = QT * Tile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
@@ -25,19 +24,14 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     typedef RowTile<NS> OwnTile;
     constexpr int kOwn = kOwnLds ? 32 * OW * CW * OwnTile::kRowBytes : 0;
     constexpr int kLds = max_of(2 * kTile * kBufs + kOwn, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(256))) char lds_all[U::kPerBlock][kLds];
-    __shared__ f32x4 stat_all[U::kPerBlock][kBufs][2][QT / 4];
-    char *const lds = lds_all[U::number()];
-    auto &stat = stat_all[U::number()];
-    __shared__ int64_t id_all[U::kPerBlock][kBufs][DROP ? QT : 1];
-    __shared__ __attribute__((aligned(256))) char turn_all[DROP ? U::kBlock / 64 : 1][2048];
-    auto &stat_id = id_all[U::number()];
+    __shared__ __attribute__((aligned(256))) char lds[kLds];
+    __shared__ f32x4 stat[kBufs][2][QT / 4];
+    __shared__ int64_t stat_id[kBufs][DROP ? QT : 1];
+    __shared__ __attribute__((aligned(256))) char turn_all[DROP ? OW * CW : 1][2048];
     char *const turn = turn_all[DROP ? threadIdx.x >> 6 : 0];
-    const uint32_t index = U::index();
-    if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
-    const int hk = (int)(index % (uint32_t)p.heads_kv);
-    const CrossItem it = p.items[index / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = unit_thread<NT>() >> 6, half = lane >> 5, col = lane & 31;
+    const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
+    const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
+    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -57,7 +51,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
             kf[t] = visible ? kf[t] : zero8<T>();
             vf[t] = visible ? vf[t] : zero8<T>();
         }
-    char *const own_v = lds + 2 * kTile * kBufs + (unit_thread<NT>() >> 6) * 32 * OwnTile::kRowBytes;
+    char *const own_v = lds + 2 * kTile * kBufs + ((int)threadIdx.x >> 6) * 32 * OwnTile::kRowBytes;
     if (kOwnLds)
 #pragma unroll
         for (int t = 0; t < NS; ++t) *(typename Vec<T>::x8 *)(own_v + OwnTile::at(col, 2 * t + half)) = vf[t];
@@ -69,12 +63,11 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
     for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
     const float c = p.scale * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
-    unit_sync<NT>();
+    __syncthreads();
     BothReader<T, NS> rd(lds, lane);
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
-        const bool more = OW * CW > 1 || row + QT < it.end;
-        if (more) sq.load(p);
+        sq.load(p);
         if (ow * 32 < it.n_own) {  // waves without keys only help to load
         const int base = cw * 32;
         const uint32_t at_q = buf * 2 * kTile + base * Tile::kRowBytes, at_g = at_q + kTile;
@@ -99,7 +92,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
                 mine[4 * g] = m[0];
                 mine[4 * g + 1] = m[1];
             }
-            unit_sync<64>();
+            wave_sync();
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const int t = lane & 15;
             const char *from = turn + (4 * half + (t >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (t & 3) * 8;
@@ -113,7 +106,7 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
                 mask[2 * g] = u.w[0];
                 mask[2 * g + 1] = u.w[1];
             }
-            unit_sync<64>();
+            wave_sync();
         }
         f32x16 w;
 #pragma unroll
@@ -128,9 +121,9 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
                 if (DROP) {
                     const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)mask[e >> 1], 16 * (e & 1), 16);
                     w[e] = __uint_as_float(__float_as_uint(x) & m);
-                    s[e] = __builtin_fmaf(w[e], dp[e], -x * d4[i]);   // dS / gain
+                    s[e] = __builtin_fmaf(w[e], dp[e], x * d4[i]);   // dS / gain
                 } else {
-                    s[e] = x * (dp[e] - d4[i]);
+                    s[e] = x * (dp[e] + d4[i]);
                 }
             }
         }
@@ -145,13 +138,12 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), NS == 2 ? 3 : 2) void c
         }
         }
         if (kBufs == 1)
-            unit_sync<NT>();
+            __syncthreads();
         else
             buf ^= 1;
-        if (more)
-            sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
-                                    (float *)stat[buf][1], DROP ? stat_id[buf] : nullptr);
-        unit_sync<NT>();
+        sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
+                                (float *)stat[buf][1], DROP ? stat_id[buf] : nullptr);
+        __syncthreads();
     }
     if (CW > 1) {
         join_waves<ND, OW, CW>(ok, lds, ow, cw, lane);
@@ -177,7 +169,7 @@ struct Pass {
     static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(Unit<NS, OW, CW>::grid(p)), Unit<NS, OW, CW>::kBlock, 0, s>>>(p);
+        cross_dkv_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

@@ -13,24 +13,19 @@ using namespace cross;
 // dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV
 // divided by D's value, which every gradient takes at its end.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), OW == 1 && CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
-    typedef Unit<NS, OW, CW> U;
-    constexpr int NT = U::kThreads, KT = 32 * CW, ND = (NS + 1) / 2;
+__global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
+    constexpr int NT = 64 * OW * CW, KT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> KTile;
     typedef RowTile<NS> VTile;
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
-    __shared__ __attribute__((aligned(256))) char lds_all[U::kPerBlock][kLds];
-    __shared__ uint64_t seen_all[U::kPerBlock][kBufs][SeenStage<KT, NT>::kWords];
-    char *const lds = lds_all[U::number()];
-    auto &seen = seen_all[U::number()];
+    __shared__ __attribute__((aligned(256))) char lds[kLds];
+    __shared__ uint64_t seen[kBufs][SeenStage<KT, NT>::kWords];
     char *const lds_v = lds + kBufs * kTileK;
-    const uint32_t index = U::index();
-    if (U::kPerBlock > 1 && index >= (uint32_t)p.n_items * (uint32_t)p.heads_kv) return;
-    const int hk = (int)(index % (uint32_t)p.heads_kv);
-    const CrossItem it = p.items[index / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = unit_thread<NT>() >> 6, half = lane >> 5, col = lane & 31;
+    const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
+    const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
+    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -70,16 +65,13 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), OW == 1 && CW > 1 && NS
     const float base2 = lse == -kInf ? kInf : lse * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
 
-    unit_sync<NT>();
+    __syncthreads();
     BothReader<T, NS> rk(lds, lane);
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
-        const bool more = OW * CW > 1 || key + KT < it.end;
-        if (more) {
-            sk.load();
-            sv.load();
-            ss.load();
-        }
+        sk.load();
+        sv.load();
+        ss.load();
         if (ow * 32 < it.n_own) {  // waves without rows only help to load
         const int base = cw * 32;
         const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
@@ -104,13 +96,13 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), OW == 1 && CW > 1 && NS
                 d = __builtin_fmaf(!DROP || kept(bits, e, p.drop_below) ? s[e] : 0.0f, dp[e], d);
             delta = both_sum(d) * gain;
         }
-        const float rest = DROP ? delta / gain : delta;
+        const float rest = DROP ? -delta / gain : -delta;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             if (DROP)
-                s[e] = __builtin_fmaf(kept(bits, e, p.drop_below) ? s[e] : 0.0f, dp[e], -s[e] * rest);
+                s[e] = __builtin_fmaf(s[e], rest, (kept(bits, e, p.drop_below) ? s[e] : 0.0f) * dp[e]);
             else
-                s[e] *= dp[e] - rest;
+                s[e] *= dp[e] + rest;
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -120,15 +112,13 @@ __global__ __launch_bounds__((Unit<NS, OW, CW>::kBlock), OW == 1 && CW > 1 && NS
         }
         }
         if (kBufs == 1)
-            unit_sync<NT>();
+            __syncthreads();
         else
             buf ^= 1;
-        if (more) {
-            sk.template store<KTile>(lds + buf * kTileK);
-            sv.template store<VTile>(lds_v + buf * kTileV);
-            ss.store(seen[buf]);
-        }
-        unit_sync<NT>();
+        sk.template store<KTile>(lds + buf * kTileK);
+        sv.template store<VTile>(lds_v + buf * kTileV);
+        ss.store(seen[buf]);
+        __syncthreads();
     }
     if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = DROP ? delta / gain : delta;
     if (CW > 1) {
@@ -148,7 +138,7 @@ struct Pass {
     static constexpr bool kForward = false;
     template <typename T, int NS, int OW, int CW, bool DROP>
     static void run(const CrossParams &p, hipStream_t s) {
-        cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(Unit<NS, OW, CW>::grid(p)), Unit<NS, OW, CW>::kBlock, 0, s>>>(p);
+        cross_dq_kernel<T, NS, OW, CW, DROP><<<dim3(grid_of(p)), 64 * OW * CW, 0, s>>>(p);
     }
     template <typename T>
     static void join(const CrossParams &p, const CrossPass &w, dim3 grid, hipStream_t s) {

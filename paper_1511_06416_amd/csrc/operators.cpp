@@ -20,6 +20,7 @@ namespace {
 
 using same::CrossItem;
 using same::CrossJoin;
+using same::CrossSmallItem;
 using same::record_error;
 
 constexpr size_t kAlign = 256;
@@ -41,6 +42,7 @@ struct DeviceLists {
     char *base = nullptr;
     CrossItem *items[3] = {nullptr, nullptr, nullptr};
     CrossJoin *joins[3] = {nullptr, nullptr, nullptr};
+    CrossSmallItem *small = nullptr;
 };
 
 }  // namespace
@@ -48,7 +50,9 @@ struct DeviceLists {
 struct same_cross_plan {
     int32_t heads_q = 0, heads_kv = 0, dim = 0, dtype = 0;
     int64_t n_q = 0, n_k = 0;  // tokens
-    PassPlan pass[3];          // by PassKind
+    // Small segments: items of several; otherwise a work list for each PassKind.
+    std::vector<CrossSmallItem> small;
+    PassPlan pass[3];
     // workspace: parts and their statistics (forward); delta, then parts (gradient)
     size_t ws_ml = 0, ws_forward = 0, ws_part = 0, ws_backward = 0;
     std::vector<DeviceLists> dev;
@@ -62,6 +66,40 @@ enum PassKind { kForward, kGradQuery, kGradKey };
 // Waves of a pass's kernel that a SIMD holds (registers).
 int waves_per_simd(PassKind kind, int32_t dim) { return kind == kForward && dim <= 64 ? 4 : 2; }
 
+constexpr int64_t kSmall = 32;  // query rows and keys that a wave takes
+
+// Neighbouring segments into items of at most kSmall rows and keys; false if a
+// segment has more.
+bool build_small(std::vector<CrossSmallItem> &items, const std::vector<int64_t> &q_ptr,
+                 const std::vector<int64_t> &k_ptr, int32_t group) {
+    const int64_t n = (int64_t)q_ptr.size() - 1;
+    for (int64_t s = 0; s < n; ++s)
+        if ((q_ptr[s + 1] - q_ptr[s]) * group > kSmall || k_ptr[s + 1] - k_ptr[s] > kSmall) return false;
+    CrossSmallItem it;
+    auto start = [&](int64_t s) {
+        std::memset((void *)&it, 0, sizeof(it));
+        it.q0 = q_ptr[s];
+        it.k0 = k_ptr[s];
+    };
+    auto flush = [&]() {
+        if (it.n_rows || it.n_keys) items.push_back(it);
+    };
+    start(0);
+    for (int64_t s = 0; s < n; ++s) {
+        const int64_t rows = (q_ptr[s + 1] - q_ptr[s]) * group, keys = k_ptr[s + 1] - k_ptr[s];
+        if (it.n_rows + rows > kSmall || it.n_keys + keys > kSmall) {
+            flush();
+            start(s);
+        }
+        for (int64_t r = 0; r < rows; ++r)
+            it.range[it.n_rows + r] = (uint16_t)(it.n_keys | (it.n_keys + keys) << 8);
+        it.n_rows += (int32_t)rows;
+        it.n_keys += (int32_t)keys;
+    }
+    if (n) flush();
+    return true;
+}
+
 // Splits the owners of every segment into tiles and, where the tiles alone
 // leave compute units idle, the other axis into parts.
 int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vector<int64_t> &k_ptr, int32_t group,
@@ -70,7 +108,7 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     const bool own_keys = kind == kGradKey;
     auto own_of = [&](int64_t s) { return own_keys ? k_ptr[s + 1] - k_ptr[s] : (q_ptr[s + 1] - q_ptr[s]) * group; };
     auto cut_of = [&](int64_t s) { return own_keys ? (q_ptr[s + 1] - q_ptr[s]) * group : k_ptr[s + 1] - k_ptr[s]; };
-    int64_t max_own = 0, max_cut = 0;
+    int64_t max_own = 0;
     double by4 = 0.0, by2 = 0.0;
     std::vector<int64_t> order;  // longest first; the tiles of a segment stay together
     for (int64_t s = 0; s < n; ++s) {
@@ -78,7 +116,6 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
         if (own == 0) continue;
         order.push_back(s);
         max_own = std::max(max_own, own);
-        max_cut = std::max(max_cut, cut);
         by4 += (double)((own + 127) / 128 * 128) * (double)cut;
         by2 += (double)((own + 63) / 64 * 64) * (double)cut;
     }
@@ -90,12 +127,12 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     // that a key read from LDS serves more waves (4,099 x 7,951, 16 heads of
     // 128, 582 against 628 us; 64 wide it loses, 139 against 132 us for 64
     // columns of 1000 nodes).  Where no segment has more than 32 owners one
-    // wave has them, and four share the other axis if it is long enough.
+    // wave has them, and four share the other axis.
     pp.own_waves = 4;
     if (kind == kForward && dim > 64 && max_own > 128) pp.own_waves = 8;
     if (kind != kForward && dim <= 64 && by2 < 0.85 * by4) pp.own_waves = 2;
     if (max_own <= 32) pp.own_waves = 1;
-    pp.cut_waves = pp.own_waves == 1 && max_cut > 64 ? 4 : 1;
+    pp.cut_waves = pp.own_waves == 1 ? 4 : 1;
     const int64_t tile = 32 * pp.own_waves;
     const double room = 1024.0 * waves_per_simd(kind, dim) / (pp.own_waves * pp.cut_waves);  // blocks the chip holds
     int64_t tiles = 0;
@@ -108,7 +145,7 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     // the axis before it begins, a join about kJoin.
     constexpr double kBlock = 128.0, kJoin = 384.0;
     int64_t whole = tiles, part = kMaxAxis;
-    if (pp.own_waves * pp.cut_waves > 1 && (double)tiles * heads_kv <= 16.0 * room) {
+    if ((double)tiles * heads_kv <= 16.0 * room) {
         whole = (int64_t)(std::floor((double)tiles * heads_kv / room) * room / heads_kv);
         std::vector<int64_t> cuts;
         int64_t at = 0, longest = 0;
@@ -182,7 +219,7 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
             off[2 * k + 1] = off[2 * k] + bytes_of(pl->pass[k].items);
             off[2 * k + 2] = off[2 * k + 1] + bytes_of(pl->pass[k].joins);
         }
-        std::vector<char> host(std::max<size_t>(off[6], 1));
+        std::vector<char> host(off[6] + std::max<size_t>(bytes_of(pl->small), 1));
         auto put = [&](size_t o, const void *src, size_t bytes) {
             if (bytes) std::memcpy(host.data() + o, src, bytes);
         };
@@ -190,6 +227,7 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
             put(off[2 * k], pl->pass[k].items.data(), pl->pass[k].items.size() * sizeof(CrossItem));
             put(off[2 * k + 1], pl->pass[k].joins.data(), pl->pass[k].joins.size() * sizeof(CrossJoin));
         }
+        put(off[6], pl->small.data(), pl->small.size() * sizeof(CrossSmallItem));
         char *base = nullptr;
         e = hipMalloc((void **)&base, host.size());
         if (e == hipSuccess) e = hipMemcpy(base, host.data(), host.size(), hipMemcpyHostToDevice);
@@ -203,6 +241,7 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
             d.items[k] = (CrossItem *)(base + off[2 * k]);
             d.joins[k] = (CrossJoin *)(base + off[2 * k + 1]);
         }
+        d.small = (CrossSmallItem *)(base + off[6]);
         d.device = device;
     }
     *out = d;
@@ -368,7 +407,10 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
         for (int64_t s = 0; !rc && s < n_segs; ++s)
             if ((qp[s + 1] - qp[s]) * group >= kMaxAxis)
                 rc = record_error(SAME_ESIZE, "a segment has 2^30 query rows of one key head or more");
-        for (int k = 0; !rc && k < 3; ++k) rc = build_pass(pl->pass[k], qp, kp, group, heads_kv, head_dim, (PassKind)k);
+        if (!rc && !build_small(pl->small, qp, kp, group))
+            for (int k = 0; !rc && k < 3; ++k) rc = build_pass(pl->pass[k], qp, kp, group, heads_kv, head_dim, (PassKind)k);
+        if (!rc && (int64_t)pl->small.size() * heads_kv > kMaxBlocks)
+            rc = record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
         if (!rc) {
             pl->heads_q = heads_q;
             pl->heads_kv = heads_kv;
@@ -380,9 +422,10 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
                 return (size_t)pp.n_slots * (size_t)heads_kv * 32 * (size_t)pp.own_waves;
             };
             const size_t row = (size_t)head_dim * sizeof(float);
+            const int64_t delta = pl->small.empty() ? pl->n_q : 0;  // small segments form theirs on the way
             pl->ws_ml = align_up(owners(pl->pass[kForward]) * row);
             pl->ws_forward = pl->ws_ml + align_up(owners(pl->pass[kForward]) * 2 * sizeof(float));
-            pl->ws_part = align_up((size_t)pl->n_q * (size_t)heads_q * sizeof(float));
+            pl->ws_part = align_up((size_t)delta * (size_t)heads_q * sizeof(float));
             pl->ws_backward = pl->ws_part + align_up(std::max(owners(pl->pass[kGradQuery]), 2 * owners(pl->pass[kGradKey])) * row);
         }
     } catch (const std::bad_alloc &) {
@@ -443,6 +486,11 @@ int same_cross_attention(same_cross_plan *pl, const void *q, int64_t q_row, int6
         c.p.lse = lse;
         c.p.part = (float *)workspace;
         c.p.part_ml = (float *)((char *)workspace + pl->ws_ml);
+        c.p.small = c.d.small;
+        c.p.n_items = (int32_t)pl->small.size();
+        if (c.p.n_items)
+            return check_hip(same::launch_cross_small(c.p, false, pl->dtype, (hipStream_t)stream),
+                             "cross attention launch");
         return check_hip(same::launch_cross_forward(c.p, pass_of(pl, c.d, kForward), pl->dtype,
                                                     (hipStream_t)stream),
                          "cross attention launch");
@@ -496,6 +544,10 @@ int same_cross_attention_backward(same_cross_plan *pl, const void *q, int64_t q_
         c.p.dk = dk;
         c.p.dv = dv;
         hipStream_t s = (hipStream_t)stream;
+        c.p.small = c.d.small;
+        c.p.n_items = (int32_t)pl->small.size();
+        if (c.p.n_items)
+            return check_hip(same::launch_cross_small(c.p, true, pl->dtype, s), "gradient launch");
         // dQ first: it leaves delta for the other pass
         rc = check_hip(same::launch_cross_dq(c.p, pass_of(pl, c.d, kGradQuery), pl->dtype, s),
                        "query gradient launch");

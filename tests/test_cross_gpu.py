@@ -115,6 +115,36 @@ def test_hidden_keys_may_hold_anything(ql, kl):
     assert torch.equal(got["dk"], clean["dk"]) and torch.equal(got["dv"], clean["dv"])
 
 
+@pytest.mark.parametrize("d", [32, 96])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (6, 2)])
+def test_packed_segments_keep_apart(d, hq, hkv):
+    """Small segments, some empty on either side, whatever the others hold."""
+    rng = np.random.default_rng(d + hq)
+    ql, kl = rng.integers(0, 6, 60), rng.integers(0, 6, 60)
+    ql[7], kl[7], ql[20], kl[20] = 5, 32, 10, 31
+    q_ptr, k_ptr = ptrs(ql), ptrs(kl)
+    q, k, v, dout = inputs(ql, kl, hq, hkv, d, BF, seed=d)
+    mask = torch.from_numpy((rng.random(sum(kl)) >= 0.2).astype(np.uint8)).cuda()
+    for m, drop in ((None, 0.0), (mask, 0.25)):
+        want = ref.attention(q, k, v, q_ptr, k_ptr, d ** -0.5, m, drop, 11, 3, dout)
+        got = run(q, k, v, q_ptr, k_ptr, dout, m, drop=drop)
+        for n in got:
+            ref.check(n, got[n], *want[n])
+        for s in (3, 7, 20, 33):
+            for fill in (float("nan"), float("inf")):
+                bad = [x.clone() for x in (q, k, v, dout)]
+                bad[0][q_ptr[s]:q_ptr[s + 1]] = fill
+                bad[3][q_ptr[s]:q_ptr[s + 1]] = -fill
+                for x in bad[1:3]:
+                    x[k_ptr[s]:k_ptr[s + 1]] = fill
+                other = run(*bad[:3], q_ptr, k_ptr, bad[3], m, drop=drop)
+                for n in got:
+                    lo, hi = (k_ptr if n in ("dk", "dv") else q_ptr)[s:s + 2]
+                    apart = torch.ones(got[n].shape[0], dtype=torch.bool)
+                    apart[lo:hi] = False
+                    assert torch.equal(other[n][apart.cuda()], got[n][apart.cuda()]), (n, s, fill)
+
+
 def test_non_finite_values_stay_in_their_rows():
     ql, kl = [70, 3], [130, 40]
     q_ptr, k_ptr = ptrs(ql), ptrs(kl)

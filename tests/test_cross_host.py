@@ -29,8 +29,11 @@ def test_refused_plans(code, args):
 
 
 def test_workspace():
-    """The gradient keeps delta; parts are needed where few rows meet many keys."""
+    """The gradient keeps delta, except of small segments; parts are needed
+    where few rows meet many keys."""
     p = same.same_cross_create([0, 3], [0, 5], 4, 1, 64, torch.bfloat16)
+    assert p.workspace_bytes() == p.workspace_bytes(True) == 0
+    p = same.same_cross_create([0, 3], [0, 50], 4, 1, 64, torch.bfloat16)
     assert p.workspace_bytes() == 0 and p.workspace_bytes(True) >= 3 * 4 * 4
     p = same.same_cross_create([0, 1], [0, 100_000], 4, 1, 64, torch.bfloat16)
     assert p.workspace_bytes() > 0
