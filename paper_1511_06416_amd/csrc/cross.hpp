@@ -59,6 +59,7 @@ struct CrossParams {
     float scale;
     uint32_t drop_below;       // bytes below this are dropped (0: no dropout)
     float keep_gain;           // 256 / (256 - drop_below)
+    float keep_part;           // its inverse
     uint32_t seed_lo, seed_hi, call_id;
 };
 

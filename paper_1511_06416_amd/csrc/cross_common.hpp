@@ -261,37 +261,50 @@ struct KeyStage {
     }
 };
 
-// Which keys of a tile are there and visible: one bit a key in LDS.
-template <int KT, int NT>
+// What the scores of a tile's keys begin at: 0, or -inf for keys that are past
+// the end or hidden, as the accumulator of the first product of a score.
+// `any` (may be null) tells whether an item has a visible key at all.
+template <int KT>
 struct SeenStage {
-    static constexpr int kWords = (KT + 63) / 64;
     const uint8_t *mask;  // of the tile (uniform)
     int left;             // keys from the tile's first one to the end (uniform)
     uint32_t m;
-    __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it) {
-        mask = p.key_mask ? p.key_mask + it.k0 + it.beg : nullptr;
-        left = it.end - it.beg;
+    __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it, int ahead = 0) {
+        mask = p.key_mask ? p.key_mask + it.k0 + it.beg + ahead : nullptr;
+        left = it.end - it.beg - ahead;
     }
     __device__ __forceinline__ void load() {
         if (mask) {
-            m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), (int)threadIdx.x, 0, 0);
+            m = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)), threadIdx.x, 0, 0);
             mask += KT;
         }
         left -= KT;
     }
-    __device__ __forceinline__ void store(uint64_t *words) const {
-        if ((int)threadIdx.x < 64 * kWords) {
-            bool in = (int)threadIdx.x < KT && (int)threadIdx.x < left + KT;
+    __device__ __forceinline__ void store(float *start, uint32_t *any) const {
+        if ((int)threadIdx.x < KT) {
+            bool in = (int)threadIdx.x < left + KT;
             if (mask) {
                 uint32_t v = m;
                 asm volatile("" : "+v"(v));  // the comparison, and the wait for the load, stay here
-                in = (int)threadIdx.x < KT && v != 0;
+                in = v != 0;
             }
-            const uint64_t b = __ballot(in);
-            if (((int)threadIdx.x & 63) == 0) words[(int)threadIdx.x >> 6] = b;
+            start[threadIdx.x] = in ? 0.0f : -kInf;
+            if (any && in) *any = 1;
         }
     }
 };
+
+// The accumulator that a lane's 16 scores of 32 keys begin with.
+__device__ __forceinline__ f32x16 start_of(const float *start, int half) {
+    f32x16 s;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const f32x4 *)(start + 8 * g + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * g + i] = v[i];
+    }
+    return s;
+}
 
 // Accumulator elements whose bit is not set become `hidden`.
 __device__ __forceinline__ void hide(f32x16 &s, uint32_t bits, int half, float hidden) {

@@ -31,7 +31,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     constexpr int kBufs = kAhead ? 2 : 1;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    __shared__ uint64_t seen[2][SeenStage<KT, NT>::kWords];
+    __shared__ __attribute__((aligned(16))) float start[2][KT];
+    __shared__ uint32_t any;
     __shared__ float stat[2][OW * CW * 32];
     char *const lds_v = lds + kBufs * kTileK;
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
@@ -43,9 +44,14 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     const int r = valid ? it.own0 + own : it.own0;
     const int64_t row = row_id(p, it.q0, r, hk);
     KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk, kAhead ? 32 : 0), sv(p.v, p, it, hk);
-    SeenStage<KT, NT> ss(p, it);
+    SeenStage<KT> ss(p, it, kAhead ? 32 : 0);
+    SeenStage<32> first_seen(p, it);
     KeyStage<T, NS, 32, NT> first(p.k, p, it, hk);
-    if (kAhead) first.load();
+    if (kAhead) {
+        first.load();
+        first_seen.load();
+    }
+    if (threadIdx.x == 0) any = 0;
     sk.load();
     sv.load();
     ss.load();
@@ -58,11 +64,16 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     float top = -kInf, sum = 0.0f;
     const float c = p.scale * kLog2e;
 
-    auto scores = [&](const char *tk, int ks) {
-        f32x16 s = 0.0f;
+    auto scores = [&](const char *tk, int ks, bool partial, const float *from) {
+        f32x16 s;
         const int base = (cw * KS + ks) * 32;
+        const typename Vec<T>::x8 k0 = read_rows<T, KTile>(tk, base + col, half);
+        if (partial)
+            s = mfma(k0, qf[0], start_of(from + base, half));
+        else
+            s = mfma(k0, qf[0], f32x16(0.0f));
 #pragma unroll
-        for (int t = 0; t < NS; ++t) s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
+        for (int t = 1; t < NS; ++t) s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
         return s;
     };
     // The maximum that the exponentials refer to follows the running one only
@@ -116,20 +127,19 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
                 o[dt] = mfma(read_columns<T, VTile>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf.v, o[dt]);
         }
     };
-    auto bits_of = [&](int buf, int ks) {
-        const int sub = cw * KS + ks;
-        return (uint32_t)(seen[buf][sub >> 1] >> (32 * (sub & 1)));
-    };
-
     if (it.beg < it.end) {
         f32x16 s;
+        __syncthreads();
         sk.template store<KTile>(lds);
         sv.template store<VTile>(lds_v);
-        ss.store(seen[0]);
-        if (kAhead) first.template store<KTile>(lds + kTileK);
+        ss.store(start[0], &any);
+        if (kAhead) {
+            first.template store<KTile>(lds + kTileK);
+            first_seen.store(start[1], &any);
+        }
         __syncthreads();
         if (kAhead) {
-            s = scores(lds + kTileK, -cw * KS);
+            s = scores(lds + kTileK, -cw * KS, p.key_mask || it.beg + 32 > it.end, start[1]);
             __syncthreads();
         }
         int buf = 0;
@@ -137,16 +147,15 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
             sk.load();
             sv.load();
             ss.load();
-            const bool masked = p.key_mask || key + KT > it.end;
+            const bool partial = p.key_mask || key + KT + (kAhead ? 32 : 0) > it.end;
             const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
             if (works)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                if (!kAhead) s = scores(tk, ks);
-                if (masked) hide(s, bits_of(buf, ks), half, -kInf);
+                if (!kAhead) s = scores(tk, ks, partial, start[buf]);
                 raise(s);
                 f32x16 next;
-                if (kAhead) next = scores(tk, ks);
+                if (kAhead) next = scores(tk, ks, partial, start[buf]);
                 weigh(s, tv, key, ks);
                 if (kAhead) s = next;
             }
@@ -156,8 +165,14 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
                 __syncthreads();
             sk.template store<KTile>(lds + buf * kTileK);
             sv.template store<VTile>(lds_v + buf * kTileV);
-            ss.store(seen[buf]);
+            ss.store(start[buf], &any);
             __syncthreads();
+        }
+        if (!any) {  // whatever the queries hold, nothing was seen
+            top = -kInf;
+            sum = 0.0f;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
         }
     }
     sum = both_sum(sum);

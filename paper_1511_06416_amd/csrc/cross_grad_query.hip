@@ -21,7 +21,7 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
     constexpr int kBufs = CW > 1 ? 1 : 2;
     constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(256))) char lds[kLds];
-    __shared__ uint64_t seen[kBufs][SeenStage<KT, NT>::kWords];
+    __shared__ __attribute__((aligned(16))) float start[kBufs][KT];
     char *const lds_v = lds + kBufs * kTileK;
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
     const int64_t row = row_id(p, it.q0, r, hk);
     // every load of the prologue is under way before the first is waited for
     KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
-    SeenStage<KT, NT> ss(p, it);
+    SeenStage<KT> ss(p, it);
     if (it.beg < it.end) {
         sk.load();
         sv.load();
@@ -47,14 +47,14 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
     if (it.beg < it.end) {
         sk.template store<KTile>(lds);
         sv.template store<VTile>(lds_v);
-        ss.store(seen[0]);
+        ss.store(start[0], nullptr);
     }
     float delta = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)of[s][i], (float)gf[s][i], delta);
-    delta = both_sum(delta);
+    float rest = -both_sum(delta) * (DROP ? p.keep_part : 1.0f);
     // Up to 32 keys lie in one wave, which then forms delta from P and dP in fp32:
     // with so few keys out's rounding would cost dS a good part of its digits.
     const bool short_row = it.slot < 0 && it.end - it.beg <= 32;
@@ -77,33 +77,34 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
         const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
         const char *tv = lds_v + buf * kTileV;
         rk.renew();
-        f32x16 s = 0.0f, dp = 0.0f;
+        f32x16 s, dp = 0.0f;
+        if (p.key_mask || key + KT > it.end)
+            s = mfma(rk.row(at_k, 0), qf[0], start_of(start[buf] + base, half));
+        else
+            s = mfma(rk.row(at_k, 0), qf[0], f32x16(0.0f));
+        dp = mfma(read_rows<T, VTile>(tv, base + col, half), gf[0], dp);
 #pragma unroll
-        for (int t = 0; t < NS; ++t) {
+        for (int t = 1; t < NS; ++t) {
             s = mfma(rk.row(at_k, t), qf[t], s);
             dp = mfma(read_rows<T, VTile>(tv, base + col, 2 * t + half), gf[t], dp);
         }
-        if (p.key_mask || key + KT > it.end) hide(s, (uint32_t)(seen[buf][cw >> 1] >> (32 * (cw & 1))), half, -kInf);
         dev::Philox4 bits;
         if (DROP) bits = keep_words(p, row, (key + base) >> 5, half);
         // dS / gain = (keep P) dP - P delta / gain
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+        f32x16 w = s;
+        if (DROP)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = kept(bits, e, p.drop_below) ? s[e] : 0.0f;
         if (short_row) {
             float d = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                d = __builtin_fmaf(!DROP || kept(bits, e, p.drop_below) ? s[e] : 0.0f, dp[e], d);
-            delta = both_sum(d) * gain;
+            for (int e = 0; e < 16; ++e) d = __builtin_fmaf(w[e], dp[e], d);
+            rest = -both_sum(d);
         }
-        const float rest = DROP ? -delta / gain : -delta;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            if (DROP)
-                s[e] = __builtin_fmaf(s[e], rest, (kept(bits, e, p.drop_below) ? s[e] : 0.0f) * dp[e]);
-            else
-                s[e] *= dp[e] + rest;
-        }
+        for (int e = 0; e < 16; ++e) s[e] = DROP ? __builtin_fmaf(s[e], rest, w[e] * dp[e]) : s[e] * (dp[e] + rest);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const typename Vec<T>::x8 df = round8<T>(s, 8 * t);
@@ -117,14 +118,17 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
             buf ^= 1;
         sk.template store<KTile>(lds + buf * kTileK);
         sv.template store<VTile>(lds_v + buf * kTileV);
-        ss.store(seen[buf]);
+        ss.store(start[buf], nullptr);
         __syncthreads();
     }
-    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = DROP ? delta / gain : delta;
+    if (valid && half == 0 && cw == 0 && it.beg == 0) p.delta[row] = -rest;
     if (CW > 1) {
         join_waves<ND, OW, CW>(o, lds, ow, cw, lane);
         if (cw != 0) return;
     }
+    if (lse == -kInf)  // a row that sees nothing, whatever it holds
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
     if (!valid) return;
     if (it.slot >= 0) {
         const int64_t at = ((int64_t)it.slot * p.heads_kv + hk) * (32 * OW) + own;

@@ -350,6 +350,7 @@ int prepare_call(same_cross_plan *pl, Call &c, const void *q, int64_t q_row, int
     c.p.dim = pl->dim;
     c.p.scale = (float)scale;
     c.p.keep_gain = 256.0f / (256.0f - (float)c.p.drop_below);
+    c.p.keep_part = (256.0f - (float)c.p.drop_below) / 256.0f;
     c.p.seed_lo = (uint32_t)seed;
     c.p.seed_hi = (uint32_t)(seed >> 32);
     c.p.call_id = call_id;
