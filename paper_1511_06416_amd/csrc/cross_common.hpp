@@ -79,6 +79,11 @@ struct BothReader {
     __device__ __forceinline__ void renew() {
         asm volatile("" : "+v"(rows), "+v"(columns));
     }
+    // to another buffer, whole tiles away
+    __device__ __forceinline__ void move(int bytes) {
+        rows += bytes;
+        columns += bytes;
+    }
     // chunk 2 t + lane / 32 of row lane % 32, `at` bytes (whole tiles) on
     __device__ __forceinline__ typename Vec<T>::x8 row(uint32_t at, int t) const {
         return *(lds_x8 *)(uintptr_t)((rows ^ (uint32_t)(t << 5)) + at);
@@ -345,6 +350,7 @@ struct QueryStage {
         for (int n = 0; n < L::kN; ++n) {
             const int r = it.beg + L::row() + n * L::kStep;
             g[n] = r % group;
+            a[n] = b[n] = zero8<T>();
             pq[n] = (const T *)p.q.p + row_at(p.q, it.q0, r, group, hk) + L::slot() * 8;
             pg[n] = (const T *)p.dout.p + row_at(p.dout, it.q0, r, group, hk) + L::slot() * 8;
         }
@@ -357,7 +363,8 @@ struct QueryStage {
     __device__ __forceinline__ void load(const CrossParams &p) {
 #pragma unroll
         for (int n = 0; n < L::kN; ++n) {
-            a[n] = b[n] = zero8<T>();
+            // rows past the end keep what an earlier tile had there (or zeros):
+            // their probabilities are zero
             if (n * L::kStep < left) {
                 a[n] = *(const typename Vec<T>::x8 *)pq[n];
                 b[n] = *(const typename Vec<T>::x8 *)pg[n];

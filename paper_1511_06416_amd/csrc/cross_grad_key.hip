@@ -64,13 +64,13 @@ __global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kerne
     const float c = p.scale * kLog2e;
     const float gain = DROP ? p.keep_gain : 1.0f;
     __syncthreads();
-    BothReader<T, NS> rd(lds, lane);
+    BothReader<T, NS> rd(lds + cw * 32 * Tile::kRowBytes, lane);
     int buf = 0;
     for (int row = it.beg; row < it.end; row += QT) {
         sq.load(p);
         if (ow * 32 < it.n_own) {  // waves without keys only help to load
         const int base = cw * 32;
-        const uint32_t at_q = buf * 2 * kTile + base * Tile::kRowBytes, at_g = at_q + kTile;
+        constexpr uint32_t at_q = 0, at_g = kTile;
         rd.renew();
         f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
@@ -139,8 +139,10 @@ __global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kerne
         }
         if (kBufs == 1)
             __syncthreads();
-        else
+        else {
             buf ^= 1;
+            rd.move(buf ? 2 * kTile : -2 * kTile);
+        }
         sq.template store<Tile>(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, (float *)stat[buf][0],
                                 (float *)stat[buf][1], DROP ? stat_id[buf] : nullptr);
         __syncthreads();

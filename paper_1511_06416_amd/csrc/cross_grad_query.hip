@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
     const float gain = DROP ? p.keep_gain : 1.0f;
 
     __syncthreads();
-    BothReader<T, NS> rk(lds, lane);
+    BothReader<T, NS> rk(lds + cw * 32 * KTile::kRowBytes, lane);
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
         sk.load();
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
         ss.load();
         if (ow * 32 < it.n_own) {  // waves without rows only help to load
         const int base = cw * 32;
-        const uint32_t at_k = buf * kTileK + base * KTile::kRowBytes;
+        constexpr uint32_t at_k = 0;
         const char *tv = lds_v + buf * kTileV;
         rk.renew();
         f32x16 s, dp = 0.0f;
@@ -114,8 +114,10 @@ __global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS 
         }
         if (kBufs == 1)
             __syncthreads();
-        else
+        else {
             buf ^= 1;
+            rk.move(buf ? kTileK : -kTileK);
+        }
         sk.template store<KTile>(lds + buf * kTileK);
         sv.template store<VTile>(lds_v + buf * kTileV);
         ss.store(start[buf], nullptr);
