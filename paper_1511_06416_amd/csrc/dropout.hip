@@ -2,6 +2,10 @@
 // The mask is never stored: element e of the matrix (row * cols + column)
 // takes 16 bits, number e % 8 of the Philox block at counter
 // {e / 8, high word, 4 << 24, call}, so any later pass makes it again.
+// Memory bounds it: 65,536 x 1,024 bf16 with a residual 68 us (5.9 TB/s, 402
+// MB), 20,003 x 1,000 fp32 in rows of 1,024 31 us (5.2 TB/s); a copy of 1 GiB
+// runs at 5.1.  16 bits an element keep the generator below that: with 32 it
+// would need about 1.5 times the time of the loads and stores.
 #include "cross.hpp"
 #include "philox.hpp"
 
@@ -9,10 +13,15 @@ namespace same {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 2;  // groups of eight elements a thread has in flight
+// Outputs larger than the L2s together are stored past them: 62 against 68 us
+// for two passes over the fp32 matrix above.  (Two groups a thread instead of
+// one: 69 and 74 us.)
+constexpr int64_t kPastL2 = 32 << 20;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
-struct alignas(sizeof(T) == 4 ? 32 : 16) Group {
+struct alignas(16) Group {
     T v[8];
 };
 
@@ -25,39 +34,46 @@ __device__ __forceinline__ float dropped(const DropoutParams &p, const dev::Phil
     return h >= p.drop_below ? __builtin_fmaf(x, p.keep_gain, base) : base;
 }
 
-// Groups that lie whole in a row (or in a contiguous matrix), 16-byte
-// accesses; per_row groups a row, the last n % 8 elements of a contiguous
-// matrix by their own thread.
-template <typename T, bool RES, bool DROP>
+template <typename T, bool PAST>
+__device__ __forceinline__ void store(T *dst, const Group<T> &g) {
+    if (!PAST) {
+        *(Group<T> *)dst = g;
+        return;
+    }
+    union {
+        Group<T> g;
+        u32x4 w[sizeof(Group<T>) / 16];
+    } u;
+    u.g = g;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Group<T>) / 16); ++i) __builtin_nontemporal_store(u.w[i], (u32x4 *)dst + i);
+}
+
+// Groups of eight that lie whole in a row (or in a contiguous matrix), one a
+// thread, 16-byte accesses; per_row groups a row, the last n % 8 elements of a
+// contiguous matrix by the first thread.
+template <typename T, bool RES, bool DROP, bool PAST>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p, int64_t n_groups, int64_t per_row,
                                                            int tail) {
-    const int64_t first = (int64_t)blockIdx.x * (kThreads * kPer) + threadIdx.x;
-    Group<T> x[kPer], r[kPer];
-    int64_t row[kPer], off[kPer];
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const int64_t g = first + k * kThreads;
-        if (g >= n_groups) continue;
-        row[k] = per_row == n_groups ? 0 : n_groups <= 0xFFFFFFFFll ? (uint32_t)g / (uint32_t)per_row : g / per_row;
-        off[k] = (g - row[k] * per_row) * 8;
-        x[k] = *(const Group<T> *)((const T *)p.x + row[k] * p.x_row + off[k]);
-        if (RES) r[k] = *(const Group<T> *)((const T *)p.residual + row[k] * p.r_row + off[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const int64_t g = first + k * kThreads;
-        if (g >= n_groups) continue;
+    const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (g < n_groups) {
+        const int64_t row = per_row == n_groups          ? 0
+                            : n_groups <= 0xFFFFFFFFll   ? (uint32_t)g / (uint32_t)per_row
+                                                         : g / per_row;
+        const int64_t off = (g - row * per_row) * 8;
+        const Group<T> x = *(const Group<T> *)((const T *)p.x + row * p.x_row + off);
+        Group<T> r, y;
+        if (RES) r = *(const Group<T> *)((const T *)p.residual + row * p.r_row + off);
         dev::Philox4 w;
         if (DROP) w = group_bits(p, g);
-        Group<T> y;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float base = RES ? (float)r[k].v[e] : 0.0f;
-            y.v[e] = (T)(DROP ? dropped(p, w, e, (float)x[k].v[e], base) : (float)x[k].v[e] + base);
+            const float base = RES ? (float)r.v[e] : 0.0f;
+            y.v[e] = (T)(DROP ? dropped(p, w, e, (float)x.v[e], base) : (float)x.v[e] + base);
         }
-        *(Group<T> *)((T *)p.y + row[k] * p.y_row + off[k]) = y;
+        store<T, PAST>((T *)p.y + row * p.y_row + off, y);
     }
-    if (tail && first == 0) {
+    if (tail && g == 0) {
         dev::Philox4 w;
         if (DROP) w = group_bits(p, n_groups);
         for (int e = 0; e < tail; ++e) {
@@ -97,10 +113,13 @@ hipError_t launch(const DropoutParams &p, hipStream_t s) {
     const uintptr_t mix = (uintptr_t)p.x | (uintptr_t)p.y | (RES ? (uintptr_t)p.residual : 0);
     const int64_t steps = p.x_row | p.y_row | (RES ? p.r_row : 0) | p.cols;
     if (mix % 16 == 0 && (whole || steps % 8 == 0)) {
-        const int64_t groups = n / 8, per_block = kThreads * kPer;
-        const dim3 grid((uint32_t)((groups + per_block - 1) / per_block + (groups == 0)));
-        dropout_kernel<T, RES, DROP><<<grid, kThreads, 0, s>>>(p, groups, whole ? groups : p.cols / 8,
-                                                               whole ? (int)(n % 8) : 0);
+        const int64_t groups = n / 8, per_row = whole ? groups : p.cols / 8;
+        const dim3 grid((uint32_t)((groups + kThreads - 1) / kThreads + (groups == 0)));
+        const int tail = whole ? (int)(n % 8) : 0;
+        if (n * (int64_t)sizeof(T) > kPastL2)
+            dropout_kernel<T, RES, DROP, true><<<grid, kThreads, 0, s>>>(p, groups, per_row, tail);
+        else
+            dropout_kernel<T, RES, DROP, false><<<grid, kThreads, 0, s>>>(p, groups, per_row, tail);
     } else {
         const int64_t groups = (n + 7) / 8;
         dropout_any_kernel<T, RES, DROP><<<dim3((uint32_t)((groups + kThreads - 1) / kThreads)), kThreads, 0, s>>>(p, n);
