@@ -61,47 +61,53 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     f32x16 o[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
-    float top = -kInf, sum = 0.0f;
+    // exponents are taken from `from` (in powers of two); a row that has seen
+    // nothing yet has limit -inf
+    float from = 0.0f, limit = -kInf, sum = 0.0f;
     const float c = p.scale * kLog2e;
 
-    auto scores = [&](const char *tk, int ks, bool partial, const float *from) {
+    auto scores = [&](const char *tk, int ks, bool partial, const float *begin) {
         f32x16 s;
         const int base = (cw * KS + ks) * 32;
         const typename Vec<T>::x8 k0 = read_rows<T, KTile>(tk, base + col, half);
         if (partial)
-            s = mfma(k0, qf[0], start_of(from + base, half));
+            s = mfma(k0, qf[0], start_of(begin + base, half));
         else
             s = mfma(k0, qf[0], f32x16(0.0f));
 #pragma unroll
         for (int t = 1; t < NS; ++t) s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
         return s;
     };
-    // The maximum that the exponentials refer to follows the running one only
-    // when that has grown by more than 2^8: until then the probabilities stay
-    // within 2^8, exact in the sums and in range for either type, and the
-    // accumulators need no rescaling.
-    auto raise = [&](const f32x16 &s) {
+    // Scores to exponents.  What they are taken from follows the running
+    // maximum only when that has grown by more than 2^8: until then the
+    // probabilities stay within 2^8, exact in the sums and in range for either
+    // type, and the accumulators need no rescaling.
+    constexpr float kLimit = 8.0f;
+    auto exponents = [&](f32x16 &s) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], c, -from);
         float mx = s[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
         mx = both_max(mx);
-        if (__any(mx * c > __builtin_fmaf(top, c, 8.0f))) {
-            mx = fmaxf(mx, top);
-            // a row whose keys are all hidden so far keeps -inf; 0 stands in for it
-            const float from = top == -kInf ? 0.0f : top, to = mx == -kInf ? 0.0f : mx;
-            const float f = top == -kInf ? 0.0f : __builtin_amdgcn_exp2f((from - to) * c);
+        if (__any(mx > limit)) {
+            const bool up = mx > limit;
+            const float by = up ? mx : 0.0f;
+            const float f = limit == kLimit ? __builtin_amdgcn_exp2f(-by) : 1.0f;  // before: sums are zero
             sum *= f;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
-            top = mx;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] -= by;
+            from += by;
+            limit = up ? kLimit : limit;
         }
     };
     auto weigh = [&](f32x16 &s, const char *tv, int key, int ks) {
-        const float base2 = (top == -kInf ? 0.0f : top) * c;
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+            s[e] = __builtin_amdgcn_exp2f(s[e]);
             part[e & 3] += s[e];
         }
         sum += (part[0] + part[1]) + (part[2] + part[3]);
@@ -153,7 +159,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 if (!kAhead) s = scores(tk, ks, partial, start[buf]);
-                raise(s);
+                exponents(s);
                 f32x16 next;
                 if (kAhead) next = scores(tk, ks, partial, start[buf]);
                 weigh(s, tv, key, ks);
@@ -169,13 +175,14 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
             __syncthreads();
         }
         if (!any) {  // whatever the queries hold, nothing was seen
-            top = -kInf;
+            limit = -kInf;
             sum = 0.0f;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] = 0.0f;
         }
     }
     sum = both_sum(sum);
+    float top = limit == kLimit ? from : -kInf;
     if (CW > 1) {
         // the waves that share these rows bring their sums to the common maximum
         if (half == 0) {
@@ -190,8 +197,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
         float total = 0.0f;
 #pragma unroll
         for (int w = 0; w < CW; ++w)
-            total += stat[1][(ow * CW + w) * 32 + col] * __builtin_amdgcn_exp2f((stat[0][(ow * CW + w) * 32 + col] - to) * c);
-        const float f = __builtin_amdgcn_exp2f((top - to) * c);
+            total += stat[1][(ow * CW + w) * 32 + col] * __builtin_amdgcn_exp2f(stat[0][(ow * CW + w) * 32 + col] - to);
+        const float f = __builtin_amdgcn_exp2f(top - to);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
         join_waves<ND, OW, CW>(o, lds, ow, cw, lane);
@@ -212,7 +219,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     write_owner<T, ND>((T *)p.out + row * p.dim, o, sum > 0.0f ? (DROP ? p.keep_gain : 1.0f) / sum : (sum == 0.0f ? 0.0f : sum), half,
                        p.dim);
     if (p.lse && half == 0)
-        p.lse[row] = sum == 0.0f ? -kInf : top * p.scale + __builtin_amdgcn_logf(sum) * kLn2;
+        p.lse[row] = sum == 0.0f ? -kInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // Joins the parts of split rows: a block per tile, key head and kJoinOwners
@@ -224,7 +231,6 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
     const CrossJoin j = joins[blockIdx.x];
     const int hk = blockIdx.y, tile = kJoinOwners * gridDim.z, first = kJoinOwners * blockIdx.z;
     const int rows = min(kJoinOwners, j.n_own - first);
-    const float c = p.scale * kLog2e;
     {
         const int own = threadIdx.x / 32, l = threadIdx.x % 32;
         float top[kMaxParts / 32], sum[kMaxParts / 32], mx = -kInf;
@@ -246,7 +252,7 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
         float total = 0.0f;
 #pragma unroll
         for (int k = 0; k < kMaxParts / 32; ++k) {
-            const float f = __builtin_amdgcn_exp2f((top[k] - to) * c);
+            const float f = __builtin_amdgcn_exp2f(top[k] - to);
             if (own < kJoinOwners && l + 32 * k < j.n_parts) weight[own][l + 32 * k] = f;
             total += f * sum[k];
         }
@@ -256,7 +262,7 @@ __global__ __launch_bounds__(256) void cross_join_forward_kernel(CrossParams p, 
             gain[own] = total > 0.0f ? p.keep_gain / total : (total == 0.0f ? 0.0f : total);
             if (p.lse)
                 p.lse[row_id(p, j.q0, j.own0 + first + own, hk)] =
-                    total == 0.0f ? -kInf : mx * p.scale + __builtin_amdgcn_logf(total) * kLn2;
+                    total == 0.0f ? -kInf : (mx + __builtin_amdgcn_logf(total)) * kLn2;
         }
     }
     __syncthreads();

@@ -4,8 +4,8 @@
 // {e / 8, high word, 4 << 24, call}, so any later pass makes it again.
 // Memory bounds it: 65,536 x 1,024 bf16 with a residual 68 us (5.9 TB/s, 402
 // MB), 20,003 x 1,000 fp32 in rows of 1,024 31 us (5.2 TB/s); a copy of 1 GiB
-// runs at 5.1.  16 bits an element keep the generator below that: with 32 it
-// would need about 1.5 times the time of the loads and stores.
+// runs at 5.1.  The generator hides behind that: with two blocks for eight
+// elements instead of one the times are the same.
 #include "cross.hpp"
 #include "philox.hpp"
 

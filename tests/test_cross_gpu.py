@@ -80,6 +80,15 @@ def test_split_axes(ql, kl, d, drop):
     compare(ql, kl, 4, 1, d, BF, drop=drop, seed=d)
 
 
+@pytest.mark.parametrize("ql,kl,d", [([200, 130], [300, 65], 96), ([200, 130], [300, 65], 128), ([257], [31], 64),
+                                     ([96, 161], [160, 97], 40), ([5, 12], [33, 700], 32)])
+@pytest.mark.parametrize("drop", [0.0, 0.25])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_geometries(ql, kl, d, drop, dtype):
+    """Tiles of 32, 64, 128 and 256 rows, with hidden keys."""
+    compare(ql, kl, 2, 1, d, dtype, masked=0.2, drop=drop, seed=d)
+
+
 @pytest.mark.parametrize("masked", [0.1, 0.9, 1.0])
 @pytest.mark.parametrize("drop", [0.0, 0.5])
 @pytest.mark.parametrize("d", [32, 128])
@@ -92,11 +101,13 @@ def test_scales_and_large_scores(scale):
     compare([70, 5], [200, 90], 2, 1, 64, HF, spread=2.0, scale=scale, seed=8)
 
 
-@pytest.mark.parametrize("ql,kl", [([3, 50, 1], [40, 200, 300]), ([1, 2], [600, 5]), ([2, 5], [3, 9])])
-def test_hidden_keys_may_hold_anything(ql, kl):
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl", [([3, 50, 1], [40, 200, 300]), ([1, 2], [600, 5]), ([2, 5], [3, 9]),
+                                   ([3, 300], [5000, 40]), ([9, 2], [33, 65])])
+def test_hidden_keys_may_hold_anything(ql, kl, d):
     q_ptr, k_ptr = ptrs(ql), ptrs(kl)
-    q, k, v, dout = inputs(ql, kl, 4, 2, 64, BF)
-    mask = (torch.rand(sum(kl)) >= 0.4).to(torch.uint8)
+    q, k, v, dout = inputs(ql, kl, 4, 2, d, BF)
+    mask = (torch.rand(sum(kl), generator=torch.Generator().manual_seed(4)) >= 0.4).to(torch.uint8)
     mask[:kl[0]] = 0   # the first segment sees nothing
     hidden = (mask == 0).cuda()
     clean = run(q, k, v, q_ptr, k_ptr, dout, mask.cuda(), drop=0.25)
@@ -108,11 +119,13 @@ def test_hidden_keys_may_hold_anything(ql, kl):
             assert torch.equal(got[n], clean[n]), (n, fill)
     assert not got["out"][:ql[0]].any() and bool((got["lse"][:ql[0]] == float("-inf")).all())
     assert not got["dq"][:ql[0]].any() and not got["dk"][hidden].any() and not got["dv"][hidden].any()
-    # whatever an unanswerable query's gradient holds stays with it
-    bad = dout.clone()
-    bad[:ql[0]] = float("nan")
-    got = run(q, k, v, q_ptr, k_ptr, bad, mask.cuda(), drop=0.25)
-    assert torch.equal(got["dk"], clean["dk"]) and torch.equal(got["dv"], clean["dv"])
+    # whatever an unanswerable query or its gradient holds stays with it
+    for fill in (float("nan"), float("inf")):
+        bad, bad_q = dout.clone(), q.clone()
+        bad[:ql[0]], bad_q[:ql[0]] = fill, fill
+        got = run(bad_q, k, v, q_ptr, k_ptr, bad, mask.cuda(), drop=0.25)
+        for n in got:
+            assert torch.equal(got[n], clean[n]), (n, fill)
 
 
 @pytest.mark.parametrize("d", [32, 96])
