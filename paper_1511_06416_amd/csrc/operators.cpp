@@ -10,6 +10,7 @@
 #include <mutex>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/same.h"
@@ -100,6 +101,80 @@ bool build_small(std::vector<CrossSmallItem> &items, const std::vector<int64_t> 
     return true;
 }
 
+// Waves of a block that own tiles of 32 and waves that share the other axis,
+// and the time of an entry of that axis, that of 4 x 1 being one.
+struct Geometry {
+    int32_t own_waves, cut_waves;
+    double entry;
+};
+
+// Tiles [0, whole) are left whole, the others cut into parts of `part` entries.
+struct Cut {
+    double cost = 0.0;
+    int64_t whole = 0, part = kMaxAxis;
+};
+
+// In entries of a full chip: what a block costs before it begins, and a join
+// with its launch.  Parts are multiples of kPart.
+constexpr double kBlock = 128.0, kJoin = 224.0;
+constexpr int64_t kPart = 128;
+
+// How long the tiles (owners and other axis of every segment, longest axis
+// first) take with a geometry.  Whole rounds of blocks are left whole; the
+// tiles of the last, partly filled round are cut into parts that fill it.
+// With many rounds the last one does not matter.
+// A block has part `alone` of its time on an empty chip.
+Cut plan_cut(const Geometry &g, const std::vector<std::pair<int64_t, int64_t>> &segs, int32_t heads_kv, double room,
+             double alone) {
+    const int64_t tile = 32 * g.own_waves, step = 32 * g.cut_waves;
+    auto time_of = [&](int64_t cut) { return kBlock + g.entry * (double)((cut + step - 1) / step * step); };
+    Cut c;
+    int64_t tiles = 0;
+    double total = 0.0;
+    for (const auto &s : segs) {
+        const int64_t t = (s.first + tile - 1) / tile;
+        tiles += t;
+        total += (double)t * time_of(s.second) * heads_kv;
+    }
+    c.whole = tiles;
+    c.cost = total / room;
+    if ((double)tiles * heads_kv > 16.0 * room) return c;
+    c.whole = (int64_t)(std::floor((double)tiles * heads_kv / room) * room / heads_kv);
+    // the tail, tiles of one length together
+    std::vector<std::pair<int64_t, int64_t>> tail;
+    int64_t at = 0, longest = 0;
+    double before = 0.0;
+    for (const auto &s : segs) {
+        const int64_t t = (s.first + tile - 1) / tile, cut_tiles = std::max<int64_t>(0, std::min(t, at + t - c.whole));
+        before += (double)(t - cut_tiles) * time_of(s.second) * heads_kv;
+        at += t;
+        if (!cut_tiles) continue;
+        if (tail.empty() || tail.back().second != s.second) tail.push_back({0, s.second});
+        tail.back().first += cut_tiles;
+        longest = std::max(longest, s.second);
+    }
+    double best = 0.0;
+    for (int64_t k = 1; k <= same::kMaxParts && !tail.empty(); ++k) {
+        const int64_t p = k == 1 ? longest : ((longest + k - 1) / k + kPart - 1) / kPart * kPart;
+        double blocks = 0.0, work = 0.0;
+        for (const auto &t : tail) {
+            const double parts = p ? (double)std::max<int64_t>(1, (t.second + p - 1) / p) : 1.0;
+            blocks += parts * (double)t.first * heads_kv;
+            work += (parts * kBlock + g.entry * (double)t.second) * (double)t.first * heads_kv;
+        }
+        const double one = time_of(std::min(p, longest));
+        const double cost = (blocks <= room ? one * (alone + (1.0 - alone) * blocks / room) : work / room + 0.5 * one) +
+                            (k > 1 ? kJoin : 0.0);
+        if (k == 1 || cost < best) {
+            best = cost;
+            c.part = k == 1 ? kMaxAxis : p;
+        }
+        if (p <= kPart) break;
+    }
+    c.cost = before / room + best;
+    return c;
+}
+
 // Splits the owners of every segment into tiles and, where the tiles alone
 // leave compute units idle, the other axis into parts.
 int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vector<int64_t> &k_ptr, int32_t group,
@@ -108,76 +183,47 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     const bool own_keys = kind == kGradKey;
     auto own_of = [&](int64_t s) { return own_keys ? k_ptr[s + 1] - k_ptr[s] : (q_ptr[s + 1] - q_ptr[s]) * group; };
     auto cut_of = [&](int64_t s) { return own_keys ? (q_ptr[s + 1] - q_ptr[s]) * group : k_ptr[s + 1] - k_ptr[s]; };
-    int64_t max_own = 0;
-    double by4 = 0.0, by2 = 0.0;
     std::vector<int64_t> order;  // longest first; the tiles of a segment stay together
-    for (int64_t s = 0; s < n; ++s) {
-        const int64_t own = own_of(s), cut = cut_of(s);
-        if (own == 0) continue;
-        order.push_back(s);
-        max_own = std::max(max_own, own);
-        by4 += (double)((own + 127) / 128 * 128) * (double)cut;
-        by2 += (double)((own + 63) / 64 * 64) * (double)cut;
-    }
+    for (int64_t s = 0; s < n; ++s)
+        if (own_of(s) > 0) order.push_back(s);
     if (order.empty()) return SAME_OK;
     std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return cut_of(a) > cut_of(b); });
-    // Tiles of 128 owners.  Gradients up to 64 wide: 64 owners where that leaves
-    // much less of a tile empty (128 columns of 330 nodes, 8 heads of 64, a
-    // training step 150 against 170 us).  Forward above 64 wide: 256 owners, so
-    // that a key read from LDS serves more waves (4,099 x 7,951, 16 heads of
-    // 128, 582 against 628 us; 64 wide it loses, 139 against 132 us for 64
-    // columns of 1000 nodes).  Where no segment has more than 32 owners one
-    // wave has them, and four share the other axis.
-    pp.own_waves = 4;
-    if (kind == kForward && dim > 64 && max_own > 128) pp.own_waves = 8;
-    if (kind != kForward && dim <= 64 && by2 < 0.85 * by4) pp.own_waves = 2;
-    if (max_own <= 32) pp.own_waves = 1;
-    pp.cut_waves = pp.own_waves == 1 ? 4 : 1;
-    const int64_t tile = 32 * pp.own_waves;
-    const double room = 1024.0 * waves_per_simd(kind, dim) / (pp.own_waves * pp.cut_waves);  // blocks the chip holds
-    int64_t tiles = 0;
-    for (int64_t s : order) tiles += (own_of(s) + tile - 1) / tile;
-    if (tiles * heads_kv > kMaxBlocks) return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
-
-    // Whole rounds of blocks are left whole; the tiles of the last, partly
-    // filled round are cut into parts that fill it.  With many rounds the last
-    // one does not matter.  A block costs about as much as kBlock entries of
-    // the axis before it begins, a join about kJoin.
-    constexpr double kBlock = 128.0, kJoin = 384.0;
-    int64_t whole = tiles, part = kMaxAxis;
-    if ((double)tiles * heads_kv <= 16.0 * room) {
-        whole = (int64_t)(std::floor((double)tiles * heads_kv / room) * room / heads_kv);
-        std::vector<int64_t> cuts;
-        int64_t at = 0, longest = 0;
-        double work = 0.0;
-        for (int64_t s : order)
-            for (int64_t o = 0; o < own_of(s); o += tile, ++at)
-                if (at >= whole) {
-                    cuts.push_back(cut_of(s));
-                    longest = std::max(longest, cuts.back());
-                    work += (double)cuts.back() * heads_kv;
-                }
-        double best = 0.0;
-        for (int64_t k = 1; k <= same::kMaxParts; ++k) {
-            const int64_t p = k == 1 ? std::max<int64_t>(longest, 1) : ((longest + k - 1) / k + 127) / 128 * 128;
-            if (k > 1 && p < 256) break;
-            double blocks = 0.0;
-            for (int64_t c : cuts) blocks += (double)std::max<int64_t>(1, (c + p - 1) / p);
-            blocks *= heads_kv;
-            double cost = blocks <= room ? p + kBlock : (work + kBlock * blocks) / room + 0.5 * (p + kBlock);
-            if (k > 1) cost += kJoin;
-            if (k == 1 || cost < best) {
-                best = cost;
-                part = k == 1 ? kMaxAxis : p;
-            }
+    std::vector<std::pair<int64_t, int64_t>> segs;
+    for (int64_t s : order) segs.push_back({own_of(s), cut_of(s)});
+    // The geometries a pass is compiled for.  Forward above 64 wide, 8 x 1: a
+    // key read from LDS serves more waves (4,099 x 7,951, 16 heads of 128, 582
+    // against 628 us; 64 wide it loses, 139 against 132 us for 64 columns of
+    // 1000 nodes).  Gradients up to 64 wide, 2 x 1, for segments that leave
+    // much of a tile of 128 empty (128 columns of 330 nodes, 8 heads of 64, a
+    // training step 150 against 170 us).  1 x 4: few owners.
+    std::vector<Geometry> shapes = {{4, 1, 1.0}, {1, 4, 0.33}};
+    if (kind == kForward && dim > 64) shapes.push_back({8, 1, 0.93});
+    if (kind != kForward && dim <= 64) shapes.push_back({2, 1, 1.1});
+    Cut cut;
+    const Geometry *shape = nullptr;
+    for (const Geometry &g : shapes) {
+        // blocks the chip holds
+        const int waves = waves_per_simd(kind, dim);
+        const double room = 1024.0 * waves / (g.own_waves * g.cut_waves);
+        const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : 0.6);
+        if (!shape || c.cost < cut.cost) {
+            cut = c;
+            shape = &g;
         }
     }
+    pp.own_waves = shape->own_waves;
+    pp.cut_waves = shape->cut_waves;
+    const int64_t tile = 32 * pp.own_waves;
+    int64_t tiles = 0;
+    for (const auto &s : segs) tiles += (s.first + tile - 1) / tile;
+    if (tiles * heads_kv > kMaxBlocks) return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
     int64_t at = 0;
     for (int64_t s : order) {
-        const int64_t own = own_of(s), cut = cut_of(s);
+        const int64_t own = own_of(s), len = cut_of(s);
         for (int64_t o = 0; o < own; o += tile, ++at) {
-            const int64_t parts = at < whole ? 1 : std::max<int64_t>(1, (cut + part - 1) / part);
-            const int64_t step = parts == 1 ? std::max<int64_t>(cut, 1) : ((cut + parts - 1) / parts + 127) / 128 * 128;
+            const int64_t parts = at < cut.whole ? 1 : std::max<int64_t>(1, (len + cut.part - 1) / cut.part);
+            const int64_t step = parts == 1 ? std::max<int64_t>(len, 1)
+                                            : ((len + parts - 1) / parts + kPart - 1) / kPart * kPart;
             CrossItem it;
             it.q0 = q_ptr[s];
             it.k0 = k_ptr[s];
@@ -189,12 +235,12 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
             int64_t b = 0;
             do {
                 it.beg = (int32_t)b;
-                it.end = (int32_t)std::min(cut, b + step);
-                if (step < cut) it.slot = pp.n_slots++;
+                it.end = (int32_t)std::min(len, b + step);
+                if (step < len) it.slot = pp.n_slots++;
                 pp.items.push_back(it);
                 b += step;
-            } while (b < cut);
-            if (step < cut) pp.joins.push_back(CrossJoin{it.q0, it.k0, it.own0, it.n_own, first, pp.n_slots - first});
+            } while (b < len);
+            if (step < len) pp.joins.push_back(CrossJoin{it.q0, it.k0, it.own0, it.n_own, first, pp.n_slots - first});
         }
     }
     return SAME_OK;
