@@ -435,20 +435,30 @@ __device__ __forceinline__ typename Vec<T>::x8 round8(const f32x16 &a, int first
     return r;
 }
 
-// Writes the columns of one owner that a lane holds: o[dt][e] is column
-// 32 dt + acc_row(e).
+// Writes the columns of one owner: a lane holds o[dt][e] = column
+// 32 dt + acc_row(e), four and four; the two lanes of an owner exchange them
+// to eight in a row.  Both lanes of an owner call it.
 template <typename T, int ND>
 __device__ __forceinline__ void write_owner(T *dst, const f32x16 (&o)[ND], float gain, int half, int dim) {
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int d = 32 * dt + 8 * g + 4 * half;
-            if (d >= dim) continue;
-            typename Vec<T>::x4 w;
+        for (int g = 0; g < 2; ++g) {
+            union {
+                typename Vec<T>::x4 v[2];
+                uint32_t w[4];
+            } x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (T)(o[dt][4 * g + i] * gain);
-            *(typename Vec<T>::x4 *)(dst + d) = w;
+            for (int i = 0; i < 8; ++i) x.v[i >> 2][i & 3] = (T)(o[dt][8 * g + i] * gain);
+            u32x4 y;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto r = __builtin_amdgcn_permlane32_swap(x.w[i], x.w[2 + i], false, false);
+                y[i] = r[0];
+                y[2 + i] = r[1];
+            }
+            const int d = 32 * dt + 16 * g + 8 * half;
+            if (d < dim) *(u32x4 *)(dst + d) = y;
         }
 }
 
