@@ -178,6 +178,28 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// A 32 x 32 tile of 16-bit numbers that lanes write by rows and read by
+// columns, each in accumulator order: element e of a lane is column (row)
+// 8 (e / 4) + 4 half + e % 4 of its row (column).  The eight-byte pieces of a
+// row are turned by the row number, so that neither way meets a bank twice.
+struct TurnTile {
+    static constexpr int kBytes = 2048;
+    __device__ static __forceinline__ int at(int row, int piece) {
+        return row * 64 + ((piece ^ ((row >> 2) & 7)) << 3);
+    }
+    // elements 4 g .. 4 g + 3 of a lane's row
+    __device__ static __forceinline__ uint64_t *row_piece(char *tile, int lane, int g) {
+        return (uint64_t *)(tile + at(lane & 31, 2 * g + (lane >> 5)));
+    }
+    // elements 4 g .. 4 g + 3 of a lane's column
+    __device__ static __forceinline__ s16x4 column_piece(const char *tile, int lane, int g) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const int t = lane & 15;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4 *)(tile + at(8 * g + 4 * (lane >> 5) + (t >> 2), 4 * ((lane >> 4) & 1) + (t & 3))));
+    }
+};
+
 // ROWS rows on their way from global memory to LDS, 16 bytes a lane: a thread
 // takes the same chunk of every kStep-th row.
 template <typename T, int NS, int ROWS, int NT>

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kerne
     __shared__ __attribute__((aligned(256))) char lds[kLds];
     __shared__ f32x4 stat[kBufs][2][QT / 4];
     __shared__ int64_t stat_id[kBufs][DROP ? QT : 1];
-    __shared__ __attribute__((aligned(256))) char turn_all[DROP ? OW * CW : 1][2048];
+    __shared__ __attribute__((aligned(256))) char turn_all[DROP ? OW * CW : 1][TurnTile::kBytes];
     char *const turn = turn_all[DROP ? threadIdx.x >> 6 : 0];
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
@@ -84,25 +84,20 @@ __global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kerne
         uint32_t mask[8];
         if (DROP) {
             const dev::Philox4 bits = keep_words(p, stat_id[buf][base + col], (it.own0 + ow * 32) >> 5, half);
-            uint32_t *const mine = (uint32_t *)(turn + col * 64 + half * 8);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 uint32_t m[2];
                 keep_pairs(bits.w[g], p.drop_below, m);
-                mine[4 * g] = m[0];
-                mine[4 * g + 1] = m[1];
+                *TurnTile::row_piece(turn, lane, g) = m[0] | (uint64_t)m[1] << 32;
             }
             wave_sync();
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const int t = lane & 15;
-            const char *from = turn + (4 * half + (t >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (t & 3) * 8;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 union {
                     s16x4 h;
                     uint32_t w[2];
                 } u;
-                u.h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 8 * g * 64));
+                u.h = TurnTile::column_piece(turn, lane, g);
                 mask[2 * g] = u.w[0];
                 mask[2 * g + 1] = u.w[1];
             }

@@ -22,7 +22,7 @@ template <int NS>
 struct SmallLds {
     typedef ColumnTile<NS> Tile;
     static constexpr int kTile = 32 * Tile::kRowBytes;
-    static constexpr int kTurn = 2048;  // 32 x 32 of 16 bits
+    static constexpr int kTurn = TurnTile::kBytes;
 };
 
 struct SmallUnit {
@@ -186,28 +186,27 @@ __device__ __forceinline__ void times_rows(f32x16 (&o)[ND], char *tile, const ty
     }
 }
 
-// A 32 x 32 tile of rounded numbers, from lanes that hold rows to lanes that
-// hold keys (both in accumulator order).
+// A tile of rounded numbers, from lanes that hold rows to lanes that hold
+// keys.
 template <typename T>
-__device__ __forceinline__ void turn(char *lds, const f32x16 &s, typename Vec<T>::x8 (&out)[2], const SmallUnit &u) {
-    char *const mine = lds + u.col * 64 + u.half * 8;
+__device__ __forceinline__ void turn(char *tile, const f32x16 &s, typename Vec<T>::x8 (&out)[2], const SmallUnit &u) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        typename Vec<T>::x4 w;
+        union {
+            typename Vec<T>::x4 v;
+            uint64_t w;
+        } x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (T)s[4 * g + i];
-        *(typename Vec<T>::x4 *)(mine + 16 * g) = w;
+        for (int i = 0; i < 4; ++i) x.v[i] = (T)s[4 * g + i];
+        *TurnTile::row_piece(tile, u.lane, g) = x.w;
     }
     wave_sync();
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int t = u.lane & 15;
-    const char *from = lds + (4 * u.half + (t >> 2)) * 64 + ((u.lane >> 4) & 1) * 32 + (t & 3) * 8;
     union {
         s16x4 h[4];
         typename Vec<T>::x8 v[2];
     } r;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) r.h[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 8 * g * 64));
+    for (int g = 0; g < 4; ++g) r.h[g] = TurnTile::column_piece(tile, u.lane, g);
     out[0] = r.v[0];
     out[1] = r.v[1];
     wave_sync();
