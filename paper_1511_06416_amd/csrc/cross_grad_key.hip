@@ -13,7 +13,7 @@ using namespace cross;
 // those heads stays in its accumulators.  S = Q K^T (rows x keys),
 // dV^T += dO^T (D P), dK^T += Q^T dS.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
+__global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> Tile;
     constexpr int kTile = QT * Tile::kRowBytes;

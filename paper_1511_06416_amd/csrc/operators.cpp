@@ -64,9 +64,6 @@ namespace {
 
 enum PassKind { kForward, kGradQuery, kGradKey };
 
-// Waves of a pass's kernel that a SIMD holds (registers).
-int waves_per_simd(PassKind kind, int32_t dim) { return kind == kForward && dim <= 64 ? 4 : 2; }
-
 constexpr int64_t kSmall = 32;  // query rows and keys that a wave takes
 
 // Neighbouring segments into items of at most kSmall rows and keys; false if a
@@ -107,6 +104,12 @@ struct Geometry {
     int32_t own_waves, cut_waves;
     double entry;
 };
+
+// Waves of a pass's kernel that a SIMD holds (registers, LDS).
+int waves_per_simd(PassKind kind, int32_t dim, const Geometry &g) {
+    if (kind == kForward) return dim <= 64 ? 4 : 2;
+    return dim > 64 && g.cut_waves > 1 ? 1 : 2;
+}
 
 // Tiles [0, whole) are left whole, the others cut into parts of `part` entries.
 struct Cut {
@@ -203,7 +206,7 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     const Geometry *shape = nullptr;
     for (const Geometry &g : shapes) {
         // blocks the chip holds
-        const int waves = waves_per_simd(kind, dim);
+        const int waves = waves_per_simd(kind, dim, g);
         const double room = 1024.0 * waves / (g.own_waves * g.cut_waves);
         const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : 0.6);
         if (!shape || c.cost < cut.cost) {
