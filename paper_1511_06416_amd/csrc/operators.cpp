@@ -117,18 +117,22 @@ struct Cut {
     int64_t whole = 0, part = kMaxAxis;
 };
 
-// In entries of a full chip: what a block costs before it begins, and a join
-// with its launch.  Parts are multiples of kPart.
-constexpr double kBlock = 128.0, kJoin = 224.0;
+// In entries of a full chip (about 0.04 us): what a block costs before it
+// begins, a join with its launch, and an element of a part written and read;
+// set by the times of some 120 drawn sets of segments, whose mean is flat
+// around them.  Parts are multiples of kPart.
+constexpr double kBlock = 160.0, kJoin = 96.0, kElement = 1.0 / 16000;
 constexpr int64_t kPart = 128;
+constexpr double kUnits = 256.0;  // compute units
 
 // How long the tiles (owners and other axis of every segment, longest axis
-// first) take with a geometry.  Whole rounds of blocks are left whole; the
-// tiles of the last, partly filled round are cut into parts that fill it.
-// With many rounds the last one does not matter.
-// A block has part `alone` of its time on an empty chip.
+// first) take with a geometry of which the chip holds `room` blocks.  Whole
+// rounds of blocks are left whole; the tiles of the last, partly filled round
+// are cut into parts that fill it.  With many rounds the last one does not
+// matter.  A block takes `alone` of its time where it has a compute unit to
+// itself; a part holds `elements` of a row.
 Cut plan_cut(const Geometry &g, const std::vector<std::pair<int64_t, int64_t>> &segs, int32_t heads_kv, double room,
-             double alone) {
+             double alone, double elements) {
     const int64_t tile = 32 * g.own_waves, step = 32 * g.cut_waves;
     auto time_of = [&](int64_t cut) { return kBlock + g.entry * (double)((cut + step - 1) / step * step); };
     Cut c;
@@ -143,8 +147,10 @@ Cut plan_cut(const Geometry &g, const std::vector<std::pair<int64_t, int64_t>> &
     c.cost = total / room;
     if ((double)tiles * heads_kv > 16.0 * room) return c;
     c.whole = (int64_t)(std::floor((double)tiles * heads_kv / room) * room / heads_kv);
-    // the tail, tiles of one length together
-    std::vector<std::pair<int64_t, int64_t>> tail;
+    struct Tail {
+        int64_t tiles, owners, axis;
+    };
+    std::vector<Tail> tail;  // tiles of one length together
     int64_t at = 0, longest = 0;
     double before = 0.0;
     for (const auto &s : segs) {
@@ -152,22 +158,25 @@ Cut plan_cut(const Geometry &g, const std::vector<std::pair<int64_t, int64_t>> &
         before += (double)(t - cut_tiles) * time_of(s.second) * heads_kv;
         at += t;
         if (!cut_tiles) continue;
-        if (tail.empty() || tail.back().second != s.second) tail.push_back({0, s.second});
-        tail.back().first += cut_tiles;
+        if (tail.empty() || tail.back().axis != s.second) tail.push_back({0, 0, s.second});
+        tail.back().tiles += cut_tiles;
+        tail.back().owners += s.first - (t - cut_tiles) * tile;
         longest = std::max(longest, s.second);
     }
     double best = 0.0;
     for (int64_t k = 1; k <= same::kMaxParts && !tail.empty(); ++k) {
         const int64_t p = k == 1 ? longest : ((longest + k - 1) / k + kPart - 1) / kPart * kPart;
-        double blocks = 0.0, work = 0.0;
-        for (const auto &t : tail) {
-            const double parts = p ? (double)std::max<int64_t>(1, (t.second + p - 1) / p) : 1.0;
-            blocks += parts * (double)t.first * heads_kv;
-            work += (parts * kBlock + g.entry * (double)t.second) * (double)t.first * heads_kv;
+        double blocks = 0.0, work = 0.0, split = 0.0;
+        for (const Tail &t : tail) {
+            const double parts = p ? (double)std::max<int64_t>(1, (t.axis + p - 1) / p) : 1.0;
+            blocks += parts * (double)t.tiles * heads_kv;
+            work += (parts * kBlock + g.entry * (double)t.axis) * (double)t.tiles * heads_kv;
+            if (parts > 1) split += parts * (double)t.owners * heads_kv;
         }
         const double one = time_of(std::min(p, longest));
-        const double cost = (blocks <= room ? one * (alone + (1.0 - alone) * blocks / room) : work / room + 0.5 * one) +
-                            (k > 1 ? kJoin : 0.0);
+        const double full = std::ceil(blocks / kUnits) * kUnits / room;  // of the fullest compute unit
+        const double cost = (full <= 1.0 ? one * (alone + (1.0 - alone) * full) : work / room + 0.5 * one) +
+                            (split ? kJoin + split * elements * kElement : 0.0);
         if (k == 1 || cost < best) {
             best = cost;
             c.part = k == 1 ? kMaxAxis : p;
@@ -198,8 +207,9 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     // against 628 us; 64 wide it loses, 139 against 132 us for 64 columns of
     // 1000 nodes).  Gradients up to 64 wide, 2 x 1, for segments that leave
     // much of a tile of 128 empty (128 columns of 330 nodes, 8 heads of 64, a
-    // training step 150 against 170 us).  1 x 4: few owners.
-    std::vector<Geometry> shapes = {{4, 1, 1.0}, {1, 4, 0.33}};
+    // training step 150 against 170 us).  1 x 4, few owners or short tiles: one
+    // query over keys, or owners that 4 x 1 would have to split and join.
+    std::vector<Geometry> shapes = {{4, 1, 1.0}, {1, 4, 0.4}};
     if (kind == kForward && dim > 64) shapes.push_back({8, 1, 0.93});
     if (kind != kForward && dim <= 64) shapes.push_back({2, 1, 1.1});
     Cut cut;
@@ -207,8 +217,9 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     for (const Geometry &g : shapes) {
         // blocks the chip holds
         const int waves = waves_per_simd(kind, dim, g);
-        const double room = 1024.0 * waves / (g.own_waves * g.cut_waves);
-        const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : 0.6);
+        const double room = 4 * kUnits * waves / (g.own_waves * g.cut_waves);
+        const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : waves > 1 ? 0.45 : 1.0,
+                               (kind == kGradKey ? 2.0 : 1.0) * dim);
         if (!shape || c.cost < cut.cost) {
             cut = c;
             shape = &g;
