@@ -253,15 +253,14 @@ struct KeyStage {
     int64_t step;      // bytes of a row
     uint32_t lane_at;  // bytes
     int left;          // rows from the tile's first one to the end (uniform)
-    __device__ __forceinline__ KeyStage(const CrossTensor &t, const CrossParams &p, const CrossItem &it, int hk,
-                                        int ahead = 0) {
-        const int64_t tok = it.k0 + it.beg + ahead;
+    __device__ __forceinline__ KeyStage(const CrossTensor &t, const CrossParams &p, const CrossItem &it, int hk) {
+        const int64_t tok = it.k0 + it.beg;
         step = 2 * t.row;
         base = (const char *)t.p + tok * step + 2 * (int64_t)hk * t.head;
         mask = p.key_mask ? p.key_mask + tok : nullptr;
         lane_at = L::slot() * 8 < p.dim && !L::idle() ? (uint32_t)L::row() * (uint32_t)step + (uint32_t)L::slot() * 16
                                                       : kOutside;
-        left = it.end - it.beg - ahead;
+        left = it.end - it.beg;
     }
     __device__ __forceinline__ void load() {
 #pragma unroll
@@ -296,9 +295,9 @@ struct SeenStage {
     const uint8_t *mask;  // of the tile (uniform)
     int left;             // keys from the tile's first one to the end (uniform)
     uint32_t m;
-    __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it, int ahead = 0) {
-        mask = p.key_mask ? p.key_mask + it.k0 + it.beg + ahead : nullptr;
-        left = it.end - it.beg - ahead;
+    __device__ __forceinline__ SeenStage(const CrossParams &p, const CrossItem &it) {
+        mask = p.key_mask ? p.key_mask + it.k0 + it.beg : nullptr;
+        left = it.end - it.beg;
     }
     __device__ __forceinline__ void load() {
         if (mask) {

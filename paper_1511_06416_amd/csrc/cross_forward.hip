@@ -14,27 +14,36 @@ using namespace cross;
 // S^T = K Q^T (keys x rows), so that a lane holds 16 scores of its own row;
 // those, rounded to 16 bits, are already the B operand of O^T += V^T P^T with
 // the keys in accumulator order, and V^T is read transposed from LDS in the
-// same order.
+// same order.  The probabilities lie within 2^8 of 1 when they are rounded, so
+// their relative error is the type's; sums, statistics and O stay in fp32.
+//
+// What bounds it: at 128 wide the matrix units and the exponents beside them
+// (each busy 45 % of the time: a wave's products wait for its softmax, which
+// the second wave of the SIMD hides in part), 4,099 rows on 7,951 keys, 16
+// heads, 541 us, 990 TFLOP/s.  At 64 wide with dropout the vector units (76 %
+// busy), 64 columns of 1000 nodes 118 us; the whole call takes 102 us without
+// dropout, 125 with it and 137 with twice the generator's work, which 16 bits
+// instead of 8 a probability would need.  Columns of 330 nodes (132 rows on 198
+// keys) spend most of their 51 us on the way in and out, 13 % on products.  One
+// query over 32,000 keys reads k and v at 5.4 TB/s in 170 us.
+//
+// One buffer: the next tiles come to registers during the products, and the
+// other waves of the SIMD (four up to 64 wide, two above) fill the wait for
+// them to reach LDS.  Scores formed 32 keys ahead, in two buffers, took 71
+// against 62 us for 256 columns of 330 nodes, and the same time at 128 wide.
+// Above 64 wide a tile has 64 keys: 545 against 557 us with 32, 611 with 128.
 template <typename T, int NS, int OW, int CW, int KS, bool DROP>
 __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross_forward_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, KT = 32 * KS * CW, ND = (NS + 1) / 2;
     typedef RowTile<NS> KTile;
     typedef ColumnTile<NS> VTile;
     constexpr int kTileK = KT * KTile::kRowBytes, kTileV = KT * VTile::kRowBytes;
-    // Wide heads leave room for two waves a SIMD: the scores of the next 32
-    // keys are then formed beside the softmax of the present ones (the tiles of
-    // k begin 32 keys after those of v, in two buffers each).  Up to 64 wide,
-    // four waves a SIMD do the same for each other with one buffer: 71 against
-    // 83 us for 256 columns of 330 nodes, 8 heads of 64; at 128 wide 744 with
-    // the scores ahead against 770 us without (4,099 x 7,951, 16 heads).
-    constexpr bool kAhead = OW > 1 && NS > 4;
-    constexpr int kBufs = kAhead ? 2 : 1;
-    constexpr int kLds = max_of((kTileK + kTileV) * kBufs, CW > 1 ? OW * ND * 4096 : 0);
+    constexpr int kLds = max_of(kTileK + kTileV, CW > 1 ? OW * ND * 4096 : 0);
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    __shared__ __attribute__((aligned(16))) float start[2][KT];
+    __shared__ __attribute__((aligned(16))) float start[KT];
     __shared__ uint32_t any;
     __shared__ float stat[2][OW * CW * 32];
-    char *const lds_v = lds + kBufs * kTileK;
+    char *const lds_v = lds + kTileK;
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
     const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
@@ -43,14 +52,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     const bool valid = own < it.n_own;
     const int r = valid ? it.own0 + own : it.own0;
     const int64_t row = row_id(p, it.q0, r, hk);
-    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk, kAhead ? 32 : 0), sv(p.v, p, it, hk);
-    SeenStage<KT> ss(p, it, kAhead ? 32 : 0);
-    SeenStage<32> first_seen(p, it);
-    KeyStage<T, NS, 32, NT> first(p.k, p, it, hk);
-    if (kAhead) {
-        first.load();
-        first_seen.load();
-    }
+    KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
+    SeenStage<KT> ss(p, it);
     if (threadIdx.x == 0) any = 0;
     sk.load();
     sv.load();
@@ -66,16 +69,16 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     float from = 0.0f, limit = -kInf, sum = 0.0f;
     const float c = p.scale * kLog2e;
 
-    auto scores = [&](const char *tk, int ks, bool partial, const float *begin) {
+    auto scores = [&](int ks, bool partial) {
         f32x16 s;
         const int base = (cw * KS + ks) * 32;
-        const typename Vec<T>::x8 k0 = read_rows<T, KTile>(tk, base + col, half);
+        const typename Vec<T>::x8 k0 = read_rows<T, KTile>(lds, base + col, half);
         if (partial)
-            s = mfma(k0, qf[0], start_of(begin + base, half));
+            s = mfma(k0, qf[0], start_of(start + base, half));
         else
             s = mfma(k0, qf[0], f32x16(0.0f));
 #pragma unroll
-        for (int t = 1; t < NS; ++t) s = mfma(read_rows<T, KTile>(tk, base + col, 2 * t + half), qf[t], s);
+        for (int t = 1; t < NS; ++t) s = mfma(read_rows<T, KTile>(lds, base + col, 2 * t + half), qf[t], s);
         return s;
     };
     // Scores to exponents.  What they are taken from follows the running
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
             limit = up ? kLimit : limit;
         }
     };
-    auto weigh = [&](f32x16 &s, const char *tv, int key, int ks) {
+    auto weigh = [&](f32x16 &s, int key, int ks) {
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -130,48 +133,31 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
                 }
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
-                o[dt] = mfma(read_columns<T, VTile>(tv, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf.v, o[dt]);
+                o[dt] = mfma(read_columns<T, VTile>(lds_v, (cw * KS + ks) * 32 + 16 * t, dt, lane), pf.v, o[dt]);
         }
     };
     if (it.beg < it.end) {
-        f32x16 s;
         __syncthreads();
         sk.template store<KTile>(lds);
         sv.template store<VTile>(lds_v);
-        ss.store(start[0], &any);
-        if (kAhead) {
-            first.template store<KTile>(lds + kTileK);
-            first_seen.store(start[1], &any);
-        }
+        ss.store(start, &any);
         __syncthreads();
-        if (kAhead) {
-            s = scores(lds + kTileK, -cw * KS, p.key_mask || it.beg + 32 > it.end, start[1]);
-            __syncthreads();
-        }
-        int buf = 0;
         for (int key = it.beg; key < it.end; key += KT) {
             sk.load();
             sv.load();
             ss.load();
-            const bool partial = p.key_mask || key + KT + (kAhead ? 32 : 0) > it.end;
-            const char *tk = lds + buf * kTileK, *tv = lds_v + buf * kTileV;
+            const bool partial = p.key_mask || key + KT > it.end;
             if (works)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (!kAhead) s = scores(tk, ks, partial, start[buf]);
-                exponents(s);
-                f32x16 next;
-                if (kAhead) next = scores(tk, ks, partial, start[buf]);
-                weigh(s, tv, key, ks);
-                if (kAhead) s = next;
-            }
-            if (kAhead)
-                buf ^= 1;
-            else
-                __syncthreads();
-            sk.template store<KTile>(lds + buf * kTileK);
-            sv.template store<VTile>(lds_v + buf * kTileV);
-            ss.store(start[buf], &any);
+                for (int ks = 0; ks < KS; ++ks) {
+                    f32x16 s = scores(ks, partial);
+                    exponents(s);
+                    weigh(s, key, ks);
+                }
+            __syncthreads();
+            sk.template store<KTile>(lds);
+            sv.template store<VTile>(lds_v);
+            ss.store(start, &any);
             __syncthreads();
         }
         if (!any) {  // whatever the queries hold, nothing was seen

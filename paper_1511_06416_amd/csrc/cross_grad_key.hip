@@ -11,7 +11,15 @@ using namespace cross;
 // The mirror image: a wave owns 32 keys of a key head (a lane one key) and
 // walks the query rows of every head that shares it, so that the sum over
 // those heads stays in its accumulators.  S = Q K^T (rows x keys),
-// dV^T += dO^T (D P), dK^T += Q^T dS.
+// dV^T += dO^T (D P), dK^T += Q^T dS.  D P and dS are rounded to 16 bits as
+// operands, the sums are fp32 and in a fixed order: no atomics.
+//
+// Two accumulators of the head's width a wave leave room for two waves a SIMD
+// (LDS for one where four waves share 32 wide keys).  4,099 rows on 4,095 keys,
+// 8 heads of 128: 291 us, the matrix units busy 40 % of it, LDS 35, the vector
+// units 31; 128 columns of 330 nodes, 8 heads of 64 with dropout: 48 us, of
+// some 38,000 cycles of a wave 9,000 before its first product, 3,500 after its
+// last and 3,300 to 4,600 for each 32 rows.
 template <typename T, int NS, int OW, int CW, bool DROP>
 __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;

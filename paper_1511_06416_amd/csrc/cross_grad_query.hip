@@ -11,9 +11,20 @@ using namespace cross;
 // A wave owns 32 query rows and walks the keys as the forward does:
 // P = exp(S - lse), dP^T = V dO^T, dS = P (D dP - delta),
 // dQ^T += K^T dS^T; delta = sum over the width of dO * O, kept for dK, dV
-// divided by D's value, which every gradient takes at its end.
+// divided by D's value, which every gradient takes at its end.  S and dP are
+// formed again from the operands rather than kept: 4 products of width a pair
+// against 2 x 4 bytes written and read.  dS is rounded to 16 bits as an
+// operand; everything else is fp32.
+//
+// A row's q, dout and accumulators fill the registers of two waves a SIMD (one
+// for four waves that share 32 wide rows, which would spill at two), so the
+// tiles of k and v have two buffers and the loads of the next ones fly during
+// the products.  4,099 rows on 4,095 keys, 8 heads of 128: 212 us, the matrix
+// units busy 43 % of it, the vector units 34; 128 columns of 330 nodes, 8 heads
+// of 64 with dropout: 38 us, of which most is the way in and out.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, OW == 1 && CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(CrossParams p) {
+__global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(
+    CrossParams p) {
     constexpr int NT = 64 * OW * CW, KT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> KTile;
     typedef RowTile<NS> VTile;
