@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsame.so")
-SOURCES = ["kernels.hip", "cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "cross_small.hip", "dropout.hip", "api.cpp", "graph.cpp", "operators.cpp"]
+SOURCES = ["kernels.hip", "cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "cross_small.hip",
+           "dropout.hip", "api.cpp", "graph.cpp", "operators.cpp"]
 ARCH = os.environ.get("SAME_OFFLOAD_ARCH", "gfx950")
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 instructions.
@@ -23,8 +24,21 @@ HIP_FLAGS = [
 # Pairs that the vectoriser forms from scalar code are taken apart again where
 # packed fp32 is off, and that has dropped the sign of one of a pair of
 # products (negated operand, seen in generated code): the operators are
-# compiled without pairs.
-SCALAR = ["cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "cross_small.hip", "dropout.hip"]
+# compiled without pairs.  Nor may their kernels spill vector registers: a
+# spill at the end of a divergent branch has been placed before the lanes come
+# back, and left theirs out (seen in generated code).
+OPERATORS = ["cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "cross_small.hip", "dropout.hip"]
+
+
+def spilled(remarks: str) -> list:
+    """Kernels with spilled vector registers, from the compiler's resource remarks."""
+    names, name = [], "?"
+    for line in remarks.splitlines():
+        if "Function Name:" in line:
+            name = line.split("Function Name:")[1].split()[0]
+        elif " VGPRs Spill:" in line and int(line.split("VGPRs Spill:")[1].split()[0]):
+            names.append(name)
+    return names
 
 
 def build(verbose: bool = False) -> str:
@@ -35,18 +49,31 @@ def build(verbose: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(objdir, src + ".o")
         cmd = [hipcc] + HIP_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
-        if src in SCALAR:
-            cmd.insert(1, "-fno-slp-vectorize")
+        if src in OPERATORS:
+            cmd[1:1] = ["-fno-slp-vectorize", "-Rpass-analysis=kernel-resource-usage"]
         if src.endswith(".cpp"):
             cmd = [hipcc, "-O3", "-std=c++17", "-fPIC",
                    "-I" + os.path.join(ROOT, "include"), "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
-        jobs.append((cmd, subprocess.Popen(cmd)))
+        log = open(obj + ".log", "w") if src in OPERATORS else None
+        jobs.append((cmd, subprocess.Popen(cmd, stderr=log), log))
         objs.append(obj)
-    failed = [cmd for cmd, job in jobs if job.wait() != 0]
+    failed = [(cmd, log) for cmd, job, log in jobs if job.wait() != 0]
+    remarks = {}
+    for cmd, job, log in jobs:
+        if log:
+            log.close()
+            with open(log.name) as f:
+                remarks[log.name] = f.read()
     if failed:
-        raise subprocess.CalledProcessError(1, failed[0])
+        cmd, log = failed[0]
+        if log:
+            sys.stderr.write(remarks[log.name])
+        raise subprocess.CalledProcessError(1, cmd)
+    for text in remarks.values():
+        if spilled(text):
+            raise RuntimeError("kernels with spilled vector registers: " + ", ".join(spilled(text)))
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [hipcc, "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs
     if verbose:

@@ -262,6 +262,8 @@ struct KeyStage {
                                                       : kOutside;
         left = it.end - it.beg;
     }
+    // MASK: with the mask, which k and v of the same rows share
+    template <bool MASK>
     __device__ __forceinline__ void load() {
 #pragma unroll
         for (int n = 0; n < L::kN; ++n) {
@@ -269,20 +271,20 @@ struct KeyStage {
             if (left < ROWS) at = L::row() + n * L::kStep < left ? lane_at : kOutside;
             a[n] = load8<T>(resource(base + n * L::kStep * step), at);
             // rows past the end read as hidden
-            if (mask)
+            if (MASK && mask)
                 m[n] = __builtin_amdgcn_raw_buffer_load_b8(resource(mask, (uint32_t)max(left, 0)),
                                                            L::row() + n * L::kStep, 0, 0);
         }
         base += ROWS * step;
-        if (mask) mask += ROWS;
+        if (MASK && mask) mask += ROWS;
         left -= ROWS;
     }
     template <typename Tile>
-    __device__ __forceinline__ void store(char *tile) {
-        if (mask)
+    __device__ __forceinline__ void store(char *tile, const KeyStage &masked) {
+        if (masked.mask)
 #pragma unroll
             for (int n = 0; n < L::kN; ++n)
-                if (!m[n]) a[n] = zero8<T>();
+                if (!masked.m[n]) a[n] = zero8<T>();
         L::template store<Tile>(tile, a);
     }
 };

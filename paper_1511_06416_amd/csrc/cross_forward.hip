@@ -46,7 +46,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     char *const lds_v = lds + kTileK;
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -55,8 +56,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
     SeenStage<KT> ss(p, it);
     if (threadIdx.x == 0) any = 0;
-    sk.load();
-    sv.load();
+    sk.template load<true>();
+    sv.template load<false>();
     ss.load();
     typename Vec<T>::x8 qf[NS];
     load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
@@ -138,13 +139,13 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     };
     if (it.beg < it.end) {
         __syncthreads();
-        sk.template store<KTile>(lds);
-        sv.template store<VTile>(lds_v);
+        sk.template store<KTile>(lds, sk);
+        sv.template store<VTile>(lds_v, sk);
         ss.store(start, &any);
         __syncthreads();
         for (int key = it.beg; key < it.end; key += KT) {
-            sk.load();
-            sv.load();
+            sk.template load<true>();
+            sv.template load<false>();
             ss.load();
             const bool partial = p.key_mask || key + KT > it.end;
             if (works)
@@ -155,8 +156,8 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
                     weigh(s, key, ks);
                 }
             __syncthreads();
-            sk.template store<KTile>(lds);
-            sv.template store<VTile>(lds_v);
+            sk.template store<KTile>(lds, sk);
+            sv.template store<VTile>(lds_v, sk);
             ss.store(start, &any);
             __syncthreads();
         }

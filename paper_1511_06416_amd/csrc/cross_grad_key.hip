@@ -6,6 +6,13 @@ namespace {
 
 using namespace cross;
 
+// Waves a SIMD: as many as leave every value a register, for spilled ones cost
+// more than the waves bring.
+constexpr int key_waves(int ns, int cw, bool drop) {
+    if (ns > 4 && cw > 1) return 1;
+    return ns == 2 ? 3 : ns == 8 && drop ? 1 : 2;
+}
+
 // -------------------------------------------------------- gradient: dK and dV
 //
 // The mirror image: a wave owns 32 keys of a key head (a lane one key) and
@@ -21,7 +28,7 @@ using namespace cross;
 // some 38,000 cycles of a wave 9,000 before its first product, 3,500 after its
 // last and 3,300 to 4,600 for each 32 rows.
 template <typename T, int NS, int OW, int CW, bool DROP>
-__global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dkv_kernel(CrossParams p) {
+__global__ __launch_bounds__(64 * OW * CW, key_waves(NS, CW, DROP)) void cross_dkv_kernel(CrossParams p) {
     constexpr int NT = 64 * OW * CW, QT = 32 * CW, ND = (NS + 1) / 2;
     typedef BothTile<NS> Tile;
     constexpr int kTile = QT * Tile::kRowBytes;
@@ -36,10 +43,11 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
     __shared__ f32x4 stat[kBufs][2][QT / 4];
     __shared__ int64_t stat_id[kBufs][DROP ? QT : 1];
     __shared__ __attribute__((aligned(256))) char turn_all[DROP ? OW * CW : 1][TurnTile::kBytes];
-    char *const turn = turn_all[DROP ? threadIdx.x >> 6 : 0];
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    char *const turn = turn_all[DROP ? wave : 0];
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -59,7 +67,7 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
             kf[t] = visible ? kf[t] : zero8<T>();
             vf[t] = visible ? vf[t] : zero8<T>();
         }
-    char *const own_v = lds + 2 * kTile * kBufs + ((int)threadIdx.x >> 6) * 32 * OwnTile::kRowBytes;
+    char *const own_v = lds + 2 * kTile * kBufs + wave * 32 * OwnTile::kRowBytes;
     if (kOwnLds)
 #pragma unroll
         for (int t = 0; t < NS; ++t) *(typename Vec<T>::x8 *)(own_v + OwnTile::at(col, 2 * t + half)) = vf[t];

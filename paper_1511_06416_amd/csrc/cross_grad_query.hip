@@ -36,7 +36,8 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
     char *const lds_v = lds + kBufs * kTileK;
     const int hk = (int)(blockIdx.x % (uint32_t)p.heads_kv);
     const CrossItem it = p.items[blockIdx.x / (uint32_t)p.heads_kv];
-    const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int ow = wave % OW, cw = wave / OW;
     const int own = ow * 32 + col;
     const bool valid = own < it.n_own;
@@ -46,8 +47,8 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
     KeyStage<T, NS, KT, NT> sk(p.k, p, it, hk), sv(p.v, p, it, hk);
     SeenStage<KT> ss(p, it);
     if (it.beg < it.end) {
-        sk.load();
-        sv.load();
+        sk.template load<true>();
+        sv.template load<false>();
         ss.load();
     }
     typename Vec<T>::x8 qf[NS], gf[NS], of[NS];
@@ -56,8 +57,8 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
     load_own<T, NS>(qf, (const T *)p.q.p + row_at(p.q, it.q0, r, p.group, hk), valid, half, p.dim);
     const float lse = valid ? p.lse[row] : -kInf;
     if (it.beg < it.end) {
-        sk.template store<KTile>(lds);
-        sv.template store<VTile>(lds_v);
+        sk.template store<KTile>(lds, sk);
+        sv.template store<VTile>(lds_v, sk);
         ss.store(start[0], nullptr);
     }
     float delta = 0.0f;
@@ -80,8 +81,8 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
     BothReader<T, NS> rk(lds + cw * 32 * KTile::kRowBytes, lane);
     int buf = 0;
     for (int key = it.beg; key < it.end; key += KT) {
-        sk.load();
-        sv.load();
+        sk.template load<true>();
+        sv.template load<false>();
         ss.load();
         if (ow * 32 < it.n_own) {  // waves without rows only help to load
         const int base = cw * 32;
@@ -129,8 +130,8 @@ __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 
             buf ^= 1;
             rk.move(buf ? kTileK : -kTileK);
         }
-        sk.template store<KTile>(lds + buf * kTileK);
-        sv.template store<VTile>(lds_v + buf * kTileV);
+        sk.template store<KTile>(lds + buf * kTileK, sk);
+        sv.template store<VTile>(lds_v + buf * kTileV, sk);
         ss.store(start[buf], nullptr);
         __syncthreads();
     }

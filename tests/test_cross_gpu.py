@@ -58,6 +58,14 @@ def test_widths(dtype, d):
     compare(*RAGGED, 4, 2, d, dtype, seed=d)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("drop", [0.0, 0.25])
+@pytest.mark.parametrize("ql,kl", [([2, 30], [200, 140]), ([140, 9], [20, 150]), ([600, 333], [310, 500])])
+def test_widths_in_every_pass(dtype, d, drop, ql, kl):
+    compare(ql, kl, 4, 2, d, dtype, drop=drop, seed=d + len(ql))
+
+
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (8, 8), (16, 2), (35, 5)])
 @pytest.mark.parametrize("drop", [0.0, 0.25])
 def test_heads(hq, hkv, drop):
