@@ -121,7 +121,7 @@ struct Cut {
 // begins, a join with its launch, and an element of a part written and read;
 // set by the times of some 120 drawn sets of segments, whose mean is flat
 // around them.  Parts are multiples of kPart.
-constexpr double kBlock = 160.0, kJoin = 96.0, kElement = 1.0 / 16000;
+constexpr double kBlock = 160.0, kJoin = 96.0, kElement = 1.0 / 32000;
 constexpr int64_t kPart = 128;
 constexpr double kUnits = 256.0;  // compute units
 
@@ -216,8 +216,9 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
         // blocks the chip holds
         const int waves = waves_per_simd(kind, dim, g);
         const double room = 4 * kUnits * waves / (g.own_waves * g.cut_waves);
-        const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : waves > 1 ? 0.45 : 1.0,
-                               (kind == kGradKey ? 2.0 : 1.0) * dim);
+        // a gradient's entry takes longer than the forward's, its parts' elements less of it
+        const Cut c = plan_cut(g, segs, heads_kv, room, waves > 2 ? 0.35 : waves == 1 ? 1.0 : kind == kForward ? 0.45 : 0.55,
+                               (kind == kForward ? 1.0 : kind == kGradQuery ? 0.4 : 0.8) * dim);
         if (!shape || c.cost < cut.cost) {
             cut = c;
             shape = &g;
