@@ -19,13 +19,14 @@ using namespace cross;
 //
 // What bounds it: at 128 wide the matrix units and the exponents beside them
 // (each busy 45 % of the time: a wave's products wait for its softmax, which
-// the second wave of the SIMD hides in part), 4,099 rows on 7,951 keys, 16
-// heads, 541 us, 990 TFLOP/s.  At 64 wide with dropout the vector units (76 %
-// busy), 64 columns of 1000 nodes 118 us; the whole call takes 102 us without
-// dropout, 125 with it and 137 with twice the generator's work, which 16 bits
-// instead of 8 a probability would need.  Columns of 330 nodes (132 rows on 198
-// keys) spend most of their 51 us on the way in and out, 13 % on products.  One
-// query over 32,000 keys reads k and v at 5.4 TB/s in 170 us.
+// the second wave of the SIMD hides in part), 2 x 4,099 rows on 7,951 keys, 16
+// heads on 4, 529 us, 1010 TFLOP/s.  At 64 wide with dropout the vector units
+// (76 % busy), 64 columns of 1000 nodes 118 us; the whole call takes 102 us
+// without dropout, 125 with it and 137 with twice the generator's work, which
+// 16 bits instead of 8 a probability would need.  Columns of 330 nodes (about
+// 165 rows on 149 visible keys) spend most of their 49 us on the way in and
+// out, 13 % on products.  One query in each of 16 columns of up to 20,011 keys
+// reads k and v at 5.4 TB/s in 168 us.
 //
 // One buffer: the next tiles come to registers during the products, and the
 // other waves of the SIMD (four up to 64 wide, two above) fill the wait for

@@ -8,7 +8,7 @@ namespace cross {
 
 // Sums the parts of dQ (SIDES = 1) or of dK and dV (SIDES = 2), in order.
 // Latency bounds it: 5 us where there is little to add, 16 us for dK and dV of
-// 4,095 keys, 8 heads of 128, in parts of 33 MB.
+// 4,095 keys, 4 key heads of 128, in parts of 33 MB.
 template <typename T, int SIDES>
 __global__ __launch_bounds__(256) void cross_join_grad_kernel(CrossParams p, const CrossJoin *joins) {
     const CrossJoin j = joins[blockIdx.x];

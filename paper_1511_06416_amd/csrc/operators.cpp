@@ -203,10 +203,11 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     std::vector<std::pair<int64_t, int64_t>> segs;
     for (int64_t s : order) segs.push_back({own_of(s), cut_of(s)});
     // The geometries a pass is compiled for.  Forward above 64 wide, 8 x 1: a
-    // key read from LDS serves more waves (4,099 x 7,951, 16 heads of 128, 547
-    // against 584 us).  Gradients up to 64 wide, 2 x 1, for segments that leave
-    // much of a tile of 128 empty.  1 x 4, few owners or short tiles: one query
-    // over keys, or owners that 4 x 1 would have to split and join.
+    // key read from LDS serves more waves (2 x 4,099 rows on 7,951 keys, 16
+    // heads on 4 of 128, 547 against 584 us).  Gradients up to 64 wide, 2 x 1,
+    // for segments that leave much of a tile of 128 empty.  1 x 4, few owners or
+    // short tiles: one query over keys, or owners that 4 x 1 would have to split
+    // and join.
     std::vector<Geometry> shapes = {{4, 1, 1.0}, {1, 4, 0.4}};
     if (kind == kForward && dim > 64) shapes.push_back({8, 1, 0.93});
     if (kind != kForward && dim <= 64) shapes.push_back({2, 1, 1.1});
