@@ -54,3 +54,13 @@ def test_pointers_are_copied():
     p = same.same_cross_create(q_ptr, [0, 7], 1, 1, 8, torch.float16)
     q_ptr[1] = 1 << 40
     assert p.n_q == 5 and p.workspace_bytes(True) < 1 << 20
+
+
+def test_spilled_kernels_are_found():
+    from paper_1511_06416_amd.build import spilled
+
+    remarks = "\n".join("a.hip:1:1: remark: %s [-Rpass-analysis=kernel-resource-usage]" % line for line in [
+        "Function Name: one", "    VGPRs: 256", "    SGPRs Spill: 6", "    VGPRs Spill: 0",
+        "Function Name: two", "    VGPRs: 256", "    SGPRs Spill: 0", "    VGPRs Spill: 12"])
+    assert spilled(remarks) == ["two"]
+    assert spilled("") == []
