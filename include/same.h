@@ -624,8 +624,10 @@ int same_cross_attention(same_cross_plan *plan, const void *q, int64_t q_row, in
  * forward's arguments and its out and lse.  The gradient of a key head is the
  * sum over the query heads that share it; inputs repeated by a zero stride
  * get one gradient per repetition, which the caller sums.  Hidden keys get
- * zeros.  Sums are fp32; P and dS are rounded to dtype before their products
- * (in SAME_F16 dS must stay in its range, as with any loss scaling).
+ * zeros.  Sums are fp32; P and dS are rounded to dtype before their products.
+ * In SAME_F16 P carries 2^14 meanwhile, so that a key's small share keeps its
+ * digits; dS follows dout and does not: dout's scale has to keep it in the
+ * type's range (below 2^-14 it loses digits), as with any loss scaling.
  */
 int same_cross_attention_backward(same_cross_plan *plan, const void *q, int64_t q_row,
                                   int64_t q_head, const void *k, int64_t k_row, int64_t k_head,

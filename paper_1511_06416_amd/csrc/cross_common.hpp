@@ -27,6 +27,18 @@ __device__ __forceinline__ f32x16 mfma(Vec<_Float16>::x8 a, Vec<_Float16>::x8 b,
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// Powers of two that probabilities carry while they are rounded, and their
+// inverse: fp16's normal numbers end at 2^-14, where a key that hardly counts,
+// or each of 2^14 alike, would be rounded to a fixed step instead of its own
+// digits.  A normalised one (at most 1) takes kUp and has normal numbers down
+// to 2^-28.  dS has no bound of its own, takes none, and follows dout.
+template <typename T>
+constexpr int kUpBits = __is_same(T, _Float16) ? 14 : 0;
+template <typename T>
+constexpr float kUp = (float)(1 << kUpBits<T>);
+template <typename T>
+constexpr float kDown = 1.0f / kUp<T>;
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
@@ -420,8 +432,9 @@ struct QueryStage {
         L::template store<Tile>(tq, a);
         L::template store<Tile>(tg, b);
         if ((int)threadIdx.x < ROWS) {
-            stat_lse[(int)threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e;
-            stat_delta[(int)threadIdx.x] = -delta;
+            // of P * kUp and of (dP - delta) * kDown
+            stat_lse[(int)threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e - kUpBits<T>;
+            stat_delta[(int)threadIdx.x] = -delta * kDown<T>;
             if (stat_id) stat_id[(int)threadIdx.x] = loaded_id;
         }
     }

@@ -14,8 +14,10 @@ using namespace cross;
 // S^T = K Q^T (keys x rows), so that a lane holds 16 scores of its own row;
 // those, rounded to 16 bits, are already the B operand of O^T += V^T P^T with
 // the keys in accumulator order, and V^T is read transposed from LDS in the
-// same order.  The probabilities lie within 2^8 of 1 when they are rounded, so
-// their relative error is the type's; sums, statistics and O stay in fp32.
+// same order.  A row's largest probability is rounded as a number from 1 to 2^8
+// (fp16: 2^7 to 2^15, so that keys down to 2^-21 of the largest, and not 2^-14,
+// are normal numbers), each with the type's digits; sums, statistics and O stay
+// in fp32.
 //
 // What bounds it: at 128 wide the matrix units and the exponents beside them
 // (each busy 45 % of the time: a wave's products wait for its softmax, which
@@ -85,9 +87,9 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
     };
     // Scores to exponents.  What they are taken from follows the running
     // maximum only when that has grown by more than 2^8: until then the
-    // probabilities stay within 2^8, exact in the sums and in range for either
+    // probabilities stay within 2^8 of kStart's power, in range for either
     // type, and the accumulators need no rescaling.
-    constexpr float kLimit = 8.0f;
+    constexpr float kStart = kUpBits<T> / 2, kLimit = 8.0f + kStart;
     auto exponents = [&](f32x16 &s) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], c, -from);
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(64 * OW * CW, NS <= 4 && OW > 1 ? 4 : 2) void cross
         mx = both_max(mx);
         if (__any(mx > limit)) {
             const bool up = mx > limit;
-            const float by = up ? mx : 0.0f;
+            const float by = up ? mx - kStart : 0.0f;
             const float f = limit == kLimit ? __builtin_amdgcn_exp2f(-by) : 1.0f;  // before: sums are zero
             sum *= f;
 #pragma unroll

@@ -18,8 +18,9 @@ constexpr int key_waves(int ns, int cw, bool drop) {
 // The mirror image: a wave owns 32 keys of a key head (a lane one key) and
 // walks the query rows of every head that shares it, so that the sum over
 // those heads stays in its accumulators.  S = Q K^T (rows x keys),
-// dV^T += dO^T (D P), dK^T += Q^T dS.  D P and dS are rounded to 16 bits as
-// operands, the sums are fp32 and in a fixed order: no atomics.
+// dV^T += dO^T (D P), dK^T += Q^T dS.  D P (in fp16 times 2^14) and dS are
+// rounded to 16 bits as operands, the sums are fp32 and in a fixed order: no
+// atomics.
 //
 // Two accumulators of the head's width a wave leave room for two waves a SIMD
 // (LDS for one where four waves share 32 wide keys).  4,099 rows on 4,095 keys,
@@ -132,9 +133,9 @@ __global__ __launch_bounds__(64 * OW * CW, key_waves(NS, CW, DROP)) void cross_d
                 if (DROP) {
                     const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)mask[e >> 1], 16 * (e & 1), 16);
                     w[e] = __uint_as_float(__float_as_uint(x) & m);
-                    s[e] = __builtin_fmaf(w[e], dp[e], x * d4[i]);   // dS / gain
+                    s[e] = __builtin_fmaf(w[e], dp[e] * kDown<T>, x * d4[i]);   // dS / gain
                 } else {
-                    s[e] = x * (dp[e] + d4[i]);
+                    s[e] = x * __builtin_fmaf(dp[e], kDown<T>, d4[i]);
                 }
             }
         }
@@ -167,6 +168,8 @@ __global__ __launch_bounds__(64 * OW * CW, key_waves(NS, CW, DROP)) void cross_d
     if (!visible)  // whatever the queries hold, a hidden key's gradients are zero
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) ok[dt] = ov[dt] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) ov[dt] *= kDown<T>;
     if (it.slot >= 0) {
         const int64_t at = ((int64_t)it.slot * p.heads_kv + hk) * (32 * OW) + own;
         write_part<ND>(p.part + 2 * at * p.dim, ok, half, p.dim);

@@ -186,10 +186,11 @@ __device__ __forceinline__ void times_rows(f32x16 (&o)[ND], char *tile, const ty
     }
 }
 
-// A tile of rounded numbers, from lanes that hold rows to lanes that hold
-// keys.
+// A tile of numbers, times `up` and rounded, from lanes that hold rows to
+// lanes that hold keys.
 template <typename T>
-__device__ __forceinline__ void turn(char *tile, const f32x16 &s, typename Vec<T>::x8 (&out)[2], const SmallUnit &u) {
+__device__ __forceinline__ void turn(char *tile, const f32x16 &s, float up, typename Vec<T>::x8 (&out)[2],
+                                     const SmallUnit &u) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         union {
@@ -197,7 +198,7 @@ __device__ __forceinline__ void turn(char *tile, const f32x16 &s, typename Vec<T
             uint64_t w;
         } x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[i] = (T)s[4 * g + i];
+        for (int i = 0; i < 4; ++i) x.v[i] = (T)(s[4 * g + i] * up);
         *TurnTile::row_piece(tile, u.lane, g) = x.w;
     }
     wave_sync();
@@ -233,7 +234,8 @@ __global__ __launch_bounds__(64 * units(NS), NS <= 4 ? 4 : 2) void cross_small_f
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
     top = both_max(top);
-    const float c = p.scale * kLog2e, base2 = (top == -kInf ? 0.0f : top) * c;
+    // exponents are at most kUpBits: the sum carries kUp too
+    const float c = p.scale * kLog2e, base2 = __builtin_fmaf(top == -kInf ? 0.0f : top, c, -(float)kUpBits<T>);
     float sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(64 * units(NS), NS <= 4 ? 4 : 2) void cross_small_f
     if (!u.row_in) return;
     write_owner<T, ND>((T *)p.out + u.row * p.dim, o,
                        sum > 0.0f ? (DROP ? p.keep_gain : 1.0f) / sum : (sum == 0.0f ? 0.0f : sum), u.half, p.dim);
-    if (p.lse && u.half == 0) p.lse[u.row] = sum == 0.0f ? -kInf : top * p.scale + __builtin_amdgcn_logf(sum) * kLn2;
+    if (p.lse && u.half == 0) p.lse[u.row] = sum == 0.0f ? -kInf : top * p.scale + __builtin_amdgcn_logf(sum * kDown<T>) * kLn2;
 }
 
 template <int ND>
@@ -304,12 +306,12 @@ __global__ __launch_bounds__(64 * units(NS), NS < 8 ? 2 : 1) void cross_small_gr
     }
     typename Vec<T>::x8 f[2];
     const int64_t at = (u.key * p.heads_kv + u.hk) * p.dim;
-    turn<T>(lds_turn, w, f, u);
+    turn<T>(lds_turn, w, kUp<T>, f, u);
     times_rows<T, NS, ND, false>(o, lds, gf, f, u);
     // whatever the queries hold, a hidden key's gradients are zero
     zero_unless<ND>(u.key_seen, o);
-    if (u.key_in) write_owner<T, ND>((T *)p.dv + at, o, gain, u.half, p.dim);
-    turn<T>(lds_turn, s, f, u);
+    if (u.key_in) write_owner<T, ND>((T *)p.dv + at, o, gain * kDown<T>, u.half, p.dim);
+    turn<T>(lds_turn, s, 1.0f, f, u);
     times_rows<T, NS, ND, false>(o, lds, qf, f, u);
     zero_unless<ND>(u.key_seen, o);
     if (u.key_in) write_owner<T, ND>((T *)p.dk + at, o, p.scale * gain, u.half, p.dim);
