@@ -66,6 +66,11 @@ struct CrossParams {
 constexpr int kCrossF16 = 1, kCrossBf16 = 2;
 constexpr int kJoinOwners = 8;  // owners that a join's block takes
 constexpr int kMaxParts = 64;   // of one tile
+// Blocks (of up to 512 threads) of one launch: the device takes fewer than
+// 2^32 threads and runs the rest of a larger grid without an error, short.
+// More items go into further launches.
+constexpr int32_t kLaunchBlocks = 1 << 22;
+inline int32_t items_per_launch(int32_t heads_kv) { return kLaunchBlocks / heads_kv; }
 
 hipError_t launch_cross_forward(const CrossParams &p, const CrossPass &w, int dtype, hipStream_t s);
 hipError_t launch_cross_small(const CrossParams &p, bool grad, int dtype, hipStream_t s);

@@ -3,6 +3,8 @@
 // type, width and geometry.
 #pragma once
 
+#include <algorithm>
+
 #include "cross.hpp"
 #include "philox.hpp"
 
@@ -566,18 +568,22 @@ void launch_shape(const CrossParams &p, const CrossPass &w, hipStream_t s) {
 template <typename Pass, typename T>
 hipError_t launch_typed(CrossParams p, const CrossPass &w, hipStream_t s) {
     if (w.n_items == 0) return hipSuccess;
-    p.items = w.items;
-    p.n_items = w.n_items;
-    if (p.dim <= 32)
-        launch_shape<Pass, T, 2>(p, w, s);
-    else if (p.dim <= 64)
-        launch_shape<Pass, T, 4>(p, w, s);
-    else if (p.dim <= 96)
-        launch_shape<Pass, T, 6>(p, w, s);
-    else
-        launch_shape<Pass, T, 8>(p, w, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || w.n_joins == 0) return e;
+    const int32_t per = items_per_launch(p.heads_kv);
+    for (int64_t first = 0; first < w.n_items; first += per) {
+        p.items = w.items + first;
+        p.n_items = (int32_t)std::min<int64_t>(per, w.n_items - first);
+        if (p.dim <= 32)
+            launch_shape<Pass, T, 2>(p, w, s);
+        else if (p.dim <= 64)
+            launch_shape<Pass, T, 4>(p, w, s);
+        else if (p.dim <= 96)
+            launch_shape<Pass, T, 6>(p, w, s);
+        else
+            launch_shape<Pass, T, 8>(p, w, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (w.n_joins == 0) return hipSuccess;
     Pass::template join<T>(p, w, dim3((uint32_t)w.n_joins, p.heads_kv, 32 * w.own_waves / kJoinOwners), s);
     return hipGetLastError();
 }

@@ -343,13 +343,20 @@ void launch_width(const CrossParams &p, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_cross_small(const CrossParams &p, bool grad, int dtype, hipStream_t s) {
-    if (p.n_items == 0) return hipSuccess;
-    if (dtype == kCrossBf16)
-        grad ? launch_width<__bf16, true>(p, s) : launch_width<__bf16, false>(p, s);
-    else
-        grad ? launch_width<_Float16, true>(p, s) : launch_width<_Float16, false>(p, s);
-    return hipGetLastError();
+hipError_t launch_cross_small(const CrossParams &all, bool grad, int dtype, hipStream_t s) {
+    const int32_t per = items_per_launch(all.heads_kv);
+    for (int64_t first = 0; first < all.n_items; first += per) {
+        CrossParams p = all;
+        p.small = all.small + first;
+        p.n_items = (int32_t)std::min<int64_t>(per, all.n_items - first);
+        if (dtype == kCrossBf16)
+            grad ? launch_width<__bf16, true>(p, s) : launch_width<__bf16, false>(p, s);
+        else
+            grad ? launch_width<_Float16, true>(p, s) : launch_width<_Float16, false>(p, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace same

@@ -26,7 +26,7 @@ using same::record_error;
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxAxis = (int64_t)1 << 30;  // rows or keys of one segment
-constexpr int64_t kMaxBlocks = (int64_t)1 << 30;
+constexpr int64_t kMaxBlocks = (int64_t)1 << 30;  // of a pass, before its last tiles are cut
 
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p) % a == 0; }
@@ -228,9 +228,10 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
     pp.own_waves = shape->own_waves;
     pp.cut_waves = shape->cut_waves;
     const int64_t tile = 32 * pp.own_waves;
-    int64_t tiles = 0;
-    for (const auto &s : segs) tiles += (s.first + tile - 1) / tile;
-    if (tiles * heads_kv > kMaxBlocks) return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
+    // tiles, of which only a few are cut (see plan_cut)
+    double tiles = 0.0;
+    for (const auto &s : segs) tiles += (double)((s.first + tile - 1) / tile);
+    if (tiles * heads_kv > (double)kMaxBlocks) return record_error(SAME_ESIZE, "the plan has more than 2^30 blocks");
     int64_t at = 0;
     for (int64_t s : order) {
         const int64_t own = own_of(s), len = cut_of(s);
