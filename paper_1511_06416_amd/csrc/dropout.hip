@@ -6,6 +6,8 @@
 // MB), 20,003 x 1,000 fp32 in rows of 1,024 31 us (5.2 TB/s); a copy of 1 GiB
 // runs at 5.1.  The generator hides behind that: with two blocks for eight
 // elements instead of one the times are the same.
+#include <algorithm>
+
 #include "cross.hpp"
 #include "philox.hpp"
 
@@ -13,6 +15,9 @@ namespace same {
 namespace {
 
 constexpr int kThreads = 256;
+// Groups of one launch: the device takes fewer than 2^32 threads and runs the
+// rest of a larger grid without an error, short.
+constexpr int64_t kLaunchGroups = (int64_t)1 << 31;
 // Outputs larger than the L2s together are stored past them: 62 against 68 us
 // for two passes over the fp32 matrix above.  (Two groups a thread instead of
 // one: 69 and 74 us.)
@@ -51,11 +56,11 @@ __device__ __forceinline__ void store(T *dst, const Group<T> &g) {
 
 // Groups of eight that lie whole in a row (or in a contiguous matrix), one a
 // thread, 16-byte accesses; per_row groups a row, the last n % 8 elements of a
-// contiguous matrix by the first thread.
+// contiguous matrix by the first thread.  The launch begins at group `first`.
 template <typename T, bool RES, bool DROP, bool PAST>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p, int64_t n_groups, int64_t per_row,
-                                                           int tail) {
-    const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p, int64_t first, int64_t n_groups,
+                                                           int64_t per_row, int tail) {
+    const int64_t g = first + (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (g < n_groups) {
         const int64_t row = per_row == n_groups          ? 0
                             : n_groups <= 0xFFFFFFFFll   ? (uint32_t)g / (uint32_t)per_row
@@ -86,8 +91,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p, int6
 
 // Any strides and alignment: a thread takes a group of eight, element by element.
 template <typename T, bool RES, bool DROP>
-__global__ __launch_bounds__(kThreads) void dropout_any_kernel(DropoutParams p, int64_t n) {
-    const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+__global__ __launch_bounds__(kThreads) void dropout_any_kernel(DropoutParams p, int64_t first, int64_t n) {
+    const int64_t g = first + (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (g * 8 >= n) return;
     dev::Philox4 w;
     if (DROP) w = group_bits(p, g);
@@ -112,19 +117,22 @@ hipError_t launch(const DropoutParams &p, hipStream_t s) {
     const bool whole = p.x_row == p.cols && p.y_row == p.cols && (!RES || p.r_row == p.cols);
     const uintptr_t mix = (uintptr_t)p.x | (uintptr_t)p.y | (RES ? (uintptr_t)p.residual : 0);
     const int64_t steps = p.x_row | p.y_row | (RES ? p.r_row : 0) | p.cols;
-    if (mix % 16 == 0 && (whole || steps % 8 == 0)) {
-        const int64_t groups = n / 8, per_row = whole ? groups : p.cols / 8;
-        const dim3 grid((uint32_t)((groups + kThreads - 1) / kThreads + (groups == 0)));
-        const int tail = whole ? (int)(n % 8) : 0;
-        if (n * (int64_t)sizeof(T) > kPastL2)
-            dropout_kernel<T, RES, DROP, true><<<grid, kThreads, 0, s>>>(p, groups, per_row, tail);
+    const bool wide = mix % 16 == 0 && (whole || steps % 8 == 0);
+    const int64_t groups = wide ? n / 8 : (n + 7) / 8, per_row = whole ? groups : p.cols / 8;
+    const int tail = wide && whole ? (int)(n % 8) : 0;
+    for (int64_t first = 0; first < groups || first == 0; first += kLaunchGroups) {
+        const int64_t count = std::max<int64_t>(1, std::min(groups - first, kLaunchGroups));  // 1: a tail alone
+        const dim3 grid((uint32_t)((count + kThreads - 1) / kThreads));
+        if (!wide)
+            dropout_any_kernel<T, RES, DROP><<<grid, kThreads, 0, s>>>(p, first, n);
+        else if (n * (int64_t)sizeof(T) > kPastL2)
+            dropout_kernel<T, RES, DROP, true><<<grid, kThreads, 0, s>>>(p, first, groups, per_row, tail);
         else
-            dropout_kernel<T, RES, DROP, false><<<grid, kThreads, 0, s>>>(p, groups, per_row, tail);
-    } else {
-        const int64_t groups = (n + 7) / 8;
-        dropout_any_kernel<T, RES, DROP><<<dim3((uint32_t)((groups + kThreads - 1) / kThreads)), kThreads, 0, s>>>(p, n);
+            dropout_kernel<T, RES, DROP, false><<<grid, kThreads, 0, s>>>(p, first, groups, per_row, tail);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 template <typename T>

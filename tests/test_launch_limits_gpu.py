@@ -16,6 +16,31 @@ def give_back():
     torch.cuda.empty_cache()
 
 
+def rows_kept(first, cols, drop, seed, call_id):
+    """Keep flags of a row that begins at element `first`."""
+    e = np.arange(first, first + cols, dtype=np.uint64)
+    g = np.unique(e // np.uint64(8))
+    w = ref.philox(g & np.uint64(0xFFFFFFFF), g >> np.uint64(32), np.uint64(4 << 24), np.uint64(call_id), seed)
+    half = np.stack([(w >> np.uint64(s)) & np.uint64(0xFFFF) for s in (0, 16)], axis=-1).reshape(-1)
+    at = int(e[0] - g[0] * np.uint64(8))
+    return torch.from_numpy(half[at:at + cols] >= round(drop * 65536))
+
+
+@pytest.mark.parametrize("cols", [1 << 20, (1 << 20) - 1])
+def test_dropout_of_more_than_2_to_35_elements(cols):
+    """In place; groups of eight whose number passes 32 bits, in whole rows and
+    in rows that are not."""
+    rows = (1 << 15) + 3
+    x = torch.ones(rows, 1 << 20, dtype=HF, device="cuda")[:, :cols]
+    same.same_dropout(x, x, 0.25, 4, 9)
+    torch.cuda.synchronize()
+    for r in (0, 1, 4095, 4096, 8192, 16383, 16384, 24576, 32767, 32768, rows - 1):
+        keep = rows_kept(r * cols, cols, 0.25, 4, 9)
+        got = x[r].cpu()
+        assert torch.equal(got > 0, keep), r
+        assert torch.equal(got[keep], torch.full_like(got[keep], 1 / 0.75)), r
+
+
 def test_attention_of_more_than_2_to_25_blocks():
     """One key a segment: out is its value, dv the query's gradient."""
     heads, segs = 8192, 4200
