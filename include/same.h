@@ -592,7 +592,7 @@ int same_cross_workspace_size(const same_cross_plan *plan, int32_t backward, siz
  * pointers are 16-byte aligned.  key_mask (device, one byte per key token; null: all visible): 0
  * hides the key from every query, and what k and v hold there, NaN included,
  * is not used.  A query without a visible key gets out = 0, lse = -inf.
- * scale is positive.  out is contiguous [tokens][heads_q][head_dim]; lse
+ * scale is positive, and a normal number in 32 bits, also times log2(e).  out is contiguous [tokens][heads_q][head_dim]; lse
  * (null: not wanted) is contiguous [tokens][heads_q] fp32, the logarithm of
  * the softmax's sum; the gradient needs it.
  *

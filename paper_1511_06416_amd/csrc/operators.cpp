@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <limits>
 #include <mutex>
 #include <new>
 #include <string>
@@ -381,8 +382,10 @@ struct Call {
 int prepare_call(same_cross_plan *pl, Call &c, const void *q, int64_t q_row, int64_t q_head, const void *k,
                  int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head, const uint8_t *key_mask,
                  double scale, double drop, uint64_t seed, uint32_t call_id, void *workspace, size_t need) {
-    if (!(scale > 0.0) || !std::isfinite(scale) || !std::isfinite((float)scale))
-        return record_error(SAME_EINVAL, "scale must be positive and finite");
+    // what the kernels multiply scores by, among them the -inf of a hidden key
+    const float per_bit = (float)scale * 1.4426950408889634f;
+    if (!((float)scale >= std::numeric_limits<float>::min()) || !std::isfinite(per_bit))
+        return record_error(SAME_EINVAL, "scale must be positive and finite, and so must scale * log2(e) in 32 bits");
     Extent e;
     int rc = check_input("q", q, pl->n_q, pl->heads_q, pl->dim, q_row, q_head, &e);
     if (rc) return rc;

@@ -350,3 +350,9 @@ def test_refusals():
         same.same_cross_attention_backward(plan, q, k, v, out, lse, dout, torch.empty_like(q), dk, dk, ws)
     torch.cuda.synchronize()
     assert not out.any()   # nothing was launched
+
+
+@pytest.mark.parametrize("ql,kl", [([3, 40], [70, 33]), ([2, 5], [9, 0])])
+def test_least_scale(ql, kl):
+    """The smallest scale weighs every visible key alike."""
+    compare(ql, kl, 2, 1, 32, BF, masked=0.3, scale=1.2e-38)

@@ -64,3 +64,19 @@ def test_spilled_kernels_are_found():
         "Function Name: two", "    VGPRs: 256", "    SGPRs Spill: 0", "    VGPRs Spill: 12"])
     assert spilled(remarks) == ["two"]
     assert spilled("") == []
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.0, 1e-46, 1e-39, 2.5e38, 3e38, 1e39, float("inf"), float("nan")])
+@pytest.mark.parametrize("q_ptr", [[0], [0, 0]])
+def test_refused_scales(scale, q_ptr):
+    """Scales that are no positive normal number in 32 bits, before and after
+    log2(e): a plan without tokens would otherwise have nothing to do."""
+    p = same.same_cross_create(q_ptr, q_ptr, 1, 1, 8, torch.float16)
+    lib = same.load_library()
+    none = (None, 0, 0)
+    args = (*none, *none, *none, None, scale, 0.0, 0, 0)
+    assert lib.same_cross_attention(p.handle, *args, None, None, None, None) == same.SAME_EINVAL
+    assert lib.same_cross_attention_backward(p.handle, *args, None, None, *none, None, None, None, None,
+                                             None) == same.SAME_EINVAL
+    args = (*none, *none, *none, None, 1.2e-38, 0.0, 0, 0)
+    assert lib.same_cross_attention(p.handle, *args, None, None, None, None) == same.SAME_OK
