@@ -569,8 +569,8 @@ enum {
  * uploaded synchronously on the first device call per device, so make one
  * before capturing a graph.  A plan serves any number of calls, one host
  * thread at a time; calls on different streams need workspaces of their own.
- * Errors: SAME_EINVAL, SAME_ESIZE (a segment with 2^30 keys, or 2^30 query
- * rows of one key head; over 2^30 blocks), SAME_ENOMEM.
+ * Errors: SAME_EINVAL, SAME_ESIZE (2^31 segments; a segment with 2^30 keys, or
+ * 2^30 query rows of one key head; over 2^30 blocks), SAME_ENOMEM.
  */
 typedef struct same_cross_plan same_cross_plan;
 

@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <exception>
 #include <limits>
 #include <mutex>
 #include <new>
@@ -27,6 +28,7 @@ using same::record_error;
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxAxis = (int64_t)1 << 30;  // rows or keys of one segment
+constexpr int64_t kMaxSegs = (int64_t)1 << 31;
 constexpr int64_t kMaxBlocks = (int64_t)1 << 30;  // of a pass, before its last tiles are cut
 
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
@@ -455,6 +457,7 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
     if (!out) return record_error(SAME_EINVAL, "out is null");
     *out = nullptr;
     if (n_segs < 0) return record_error(SAME_EINVAL, "n_segs must not be negative");
+    if (n_segs >= kMaxSegs) return record_error(SAME_ESIZE, "n_segs must stay below 2^31");
     if (heads_q < 1 || heads_kv < 1 || heads_q % heads_kv != 0)
         return record_error(SAME_EINVAL, "heads_q must be a positive multiple of heads_kv");
     if (heads_q > 65536) return record_error(SAME_ESIZE, "heads_q must be at most 65536");
@@ -495,6 +498,8 @@ int same_cross_create(int64_t n_segs, const int64_t *q_ptr, const int64_t *k_ptr
         }
     } catch (const std::bad_alloc &) {
         rc = record_error(SAME_ENOMEM, "out of host memory");
+    } catch (const std::exception &e) {  // nothing may leave a C entry
+        rc = record_error(SAME_ESIZE, e.what());
     }
     if (rc) {
         delete pl;
@@ -561,6 +566,8 @@ int same_cross_attention(same_cross_plan *pl, const void *q, int64_t q_row, int6
                          "cross attention launch");
     } catch (const std::bad_alloc &) {
         return record_error(SAME_ENOMEM, "out of host memory");
+    } catch (const std::exception &e) {  // the plan's lock
+        return record_error(SAME_EHIP, e.what());
     }
 }
 
@@ -621,6 +628,8 @@ int same_cross_attention_backward(same_cross_plan *pl, const void *q, int64_t q_
                          "key gradient launch");
     } catch (const std::bad_alloc &) {
         return record_error(SAME_ENOMEM, "out of host memory");
+    } catch (const std::exception &e) {  // the plan's lock
+        return record_error(SAME_EHIP, e.what());
     }
 }
 

@@ -1,9 +1,15 @@
 """Plans of cross attention: host checks, no device."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
 
 import paper_1511_06416_amd as same
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.mark.parametrize("code,args", [
@@ -80,3 +86,18 @@ def test_refused_scales(scale, q_ptr):
                                              None) == same.SAME_EINVAL
     args = (*none, *none, *none, None, 1.2e-38, 0.0, 0, 0)
     assert lib.same_cross_attention(p.handle, *args, None, None, None, None) == same.SAME_OK
+
+
+@pytest.mark.parametrize("n_segs,code", [(-1, "SAME_EINVAL"), (1 << 31, "SAME_ESIZE"), (1 << 60, "SAME_ESIZE"),
+                                         (1 << 61, "SAME_ESIZE"), ((1 << 63) - 1, "SAME_ESIZE")])
+def test_refused_numbers_of_segments(n_segs, code):
+    """Refused before the pointers are read or anything is sized by them; in a
+    process of its own, which an exception through the C entry would end."""
+    run = """
+import ctypes, numpy as np, paper_1511_06416_amd as same
+a, h = np.zeros(4, np.int64), ctypes.c_void_p()
+rc = same.load_library().same_cross_create(%d, a.ctypes.data, a.ctypes.data, 1, 1, 8, same.SAME_F16, ctypes.byref(h))
+assert rc == same.%s and not h.value, rc
+""" % (n_segs, code)
+    done = subprocess.run([sys.executable, "-c", run], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0, (done.returncode, done.stderr)
