@@ -636,8 +636,8 @@ class CrossPlan:
                 raise SameError(SAME_EINVAL, "key_mask must be a contiguous byte per key token")
             key_mask = key_mask.data_ptr()
         if need:
-            if workspace is None or workspace.numel() * workspace.element_size() < need:
-                raise SameError(SAME_EINVAL, "workspace must have at least %d bytes" % need)
+            if workspace is None or workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
+                raise SameError(SAME_EINVAL, "workspace must be contiguous, with at least %d bytes" % need)
             _on_device("workspace", workspace)
         return (*self._strided("q", q, self._q_shape), *self._strided("k", k, self._k_shape),
                 *self._strided("v", v, self._k_shape), key_mask)

@@ -101,3 +101,15 @@ assert rc == same.%s and not h.value, rc
 """ % (n_segs, code)
     done = subprocess.run([sys.executable, "-c", run], cwd=ROOT, capture_output=True, text=True)
     assert done.returncode == 0, (done.returncode, done.stderr)
+
+
+def test_workspaces_are_whole():
+    """An expanded workspace has the numbers of bytes, not the memory."""
+    p = same.same_cross_create([0, 1], [0, 100_000], 4, 1, 64, torch.bfloat16)
+    q, k = torch.zeros(1, 4, 64, dtype=torch.bfloat16), torch.zeros(100_000, 1, 64, dtype=torch.bfloat16)
+    need = p.workspace_bytes(True)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2]):
+        with pytest.raises(same.SameError, match="contiguous"):
+            same.same_cross_attention(p, q, k, k, q, None, ws)
+        with pytest.raises(same.SameError, match="contiguous"):
+            same.same_cross_attention_backward(p, q, k, k, q, None, q, q, k, k, ws)
