@@ -4,7 +4,9 @@ trained with the library's cross attention and dropout.
 
 ``cross_attention`` and ``dropout`` are the library's operators with torch's
 automatic differentiation around them; ``Imputer`` is one block of them.  Every
-pass runs in the library's HIP kernels; the projections are torch's.
+pass runs in the library's HIP kernels; the projections are torch's.  Dropout
+is linear and has derivatives of every order; differentiating the attention's
+gradients raises.
 """
 from __future__ import annotations
 
@@ -30,10 +32,23 @@ class _CrossAttention(torch.autograd.Function):
         plan, workspace, scale, drop, seed, call_id = ctx.rest
         if dout.numel() and dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:2]) or dout.data_ptr() % 16:
             dout = dout.contiguous()
+        return _CrossGradients.apply(q, k, v, dout, plan, workspace, out, lse, key_mask, scale, drop, seed,
+                                     call_id) + (None,) * 7
+
+
+class _CrossGradients(torch.autograd.Function):
+    # A function of its own, so that under create_graph its results hang on
+    # what they were computed from and a second derivative finds this node.
+    @staticmethod
+    def forward(ctx, q, k, v, dout, plan, workspace, out, lse, key_mask, scale, drop, seed, call_id):
         dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
         same_cross_attention_backward(plan, q, k, v, out, lse, dout, dq, dk, dv, workspace, key_mask=key_mask,
                                       scale=scale, drop=drop, seed=seed, call_id=call_id)
-        return (dq, dk, dv) + (None,) * 7
+        return dq, dk, dv
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("cross_attention: second derivatives are not provided")
 
 
 def cross_attention(plan, q, k, v, workspace, key_mask=None, scale=None, drop=0.0, seed=0, call_id=0):
@@ -56,9 +71,7 @@ class _Dropout(torch.autograd.Function):
         drop, seed, call_id, with_residual = ctx.rest
         if dy.stride(-1) != 1:
             dy = dy.contiguous()
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-        same_dropout(dy, dx, drop, seed, call_id)
-        return dx, dy if with_residual else None, None, None, None
+        return _Dropout.apply(dy, None, drop, seed, call_id), dy if with_residual else None, None, None, None
 
 
 def dropout(x, drop, seed, call_id, residual=None):
