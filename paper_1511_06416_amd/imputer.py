@@ -31,7 +31,7 @@ class _CrossAttention(torch.autograd.Function):
         q, k, v, out, lse, key_mask = ctx.saved_tensors
         plan, workspace, scale, drop, seed, call_id = ctx.rest
         if dout.numel() and dout.stride(-1) != 1 or any(s % 8 for s in dout.stride()[:2]) or dout.data_ptr() % 16:
-            dout = dout.contiguous()
+            dout = dout.clone(memory_format=torch.contiguous_format)  # contiguous() keeps a misaligned view
         return _CrossGradients.apply(q, k, v, dout, plan, workspace, out, lse, key_mask, scale, drop, seed,
                                      call_id) + (None,) * 7
 

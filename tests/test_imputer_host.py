@@ -63,3 +63,20 @@ def test_second_derivatives_of_attention_are_refused(stand_ins):
     y = imputer.cross_attention(None, x, kv, kv, None)   # the first one as before
     (y * y).sum().backward()
     assert torch.allclose(x.grad, 4 * x.detach() ** 3)
+
+
+def test_gradients_arrive_aligned(stand_ins):
+    """Whatever view of another gradient reaches the attention: the operator
+    takes 16-byte addresses and strides of multiples of eight."""
+    q, kv = torch.randn(4, 2, 8, requires_grad=True), torch.zeros(3, 2, 8)
+    out = imputer.cross_attention(None, q, kv, kv, None)
+    three = torch.zeros(3, requires_grad=True)
+    w = torch.randn(3 + out.numel())
+    (torch.cat([three, out.flatten()]) * w).sum().backward()   # contiguous, 12 bytes into cat's gradient
+    (imputer.cross_attention(None, q, kv, kv, None).transpose(0, 2) * torch.randn(8, 2, 4)).sum().backward()
+    out = imputer.cross_attention(None, q, kv, kv, None)
+    (torch.cat([torch.zeros(4, 2, 3, requires_grad=True), out], dim=2) * torch.randn(4, 2, 11)).sum().backward()
+    assert len(stand_ins) == 3
+    for dout in stand_ins:
+        assert dout.data_ptr() % 16 == 0 and dout.stride(2) == 1 and not any(s % 8 for s in dout.stride()[:2])
+    assert torch.equal(stand_ins[0].flatten(), w[3:])
