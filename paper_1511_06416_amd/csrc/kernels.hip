@@ -1217,10 +1217,12 @@ __device__ __forceinline__ void sweep_table(const SweepParams &P, const Work &W,
 // groups of a larger record) into LDS; then its lanes take the items
 // (latent column, replica quad) in turn.  The node's mode selects the
 // product path for KP = 2, 4, 6, 8 or the threshold path.
-// At least kSweepWaves waves per SIMD (the debug variant keeps the default
-// bound).
+// At least kSweepWaves waves per SIMD; one fewer for 16-bit states with STAGED,
+// where that many would spill a vector register (120 nodes of up to 130 states
+// x 20,000 columns, 459 us per step either way).  The debug variant keeps the
+// default bound.
 template <typename ST, bool DEBUG, bool STAGED>
-__global__ __launch_bounds__(kSweepBlock, DEBUG ? 1 : kSweepWaves) void sweep_fast_kernel(SweepParams P) {
+__global__ __launch_bounds__(kSweepBlock, DEBUG ? 1 : kSweepWaves - (STAGED && Quad<ST>::kBytes == 8)) void sweep_fast_kernel(SweepParams P) {
     if (P.ids) P.sweep_id = P.ids[0];
     extern __shared__ float4 lds4[];
     __shared__ int32_t wave_n[kSweepPasses * kSweepBlock / 64];
@@ -1877,13 +1879,13 @@ constexpr int kCountQuads = 3;  // replica quads whose rows are loaded together 
 // sweep) when the node has at most 2^16 bins, else with 32-bit indices.
 // Padding slots (replicas >= m) and columns past the slab are not counted.
 //
-// Waves per SIMD: 5 for 4-bit states (96 registers, one spilled; 23 in the
-// copy with narrow accesses), 4 for bytes and 2 for 16-bit states (115 and 130
-// registers).  The bound hardly matters: over 12 networks and sizes 4 waves for
-// 4-bit states take 0.996 of the time (three quads and more 1.004), 5 for
-// bytes 1.006, 1 for 16-bit states 1.001.
+// Waves per SIMD: 4, for 16-bit states 2: as many as spill no vector register
+// (5 for 4-bit states: one spilled, 23 in the copy with narrow accesses).  The
+// bound hardly matters: over 12 networks and sizes 4 waves for 4-bit states
+// take 0.996 of the time of 5 (three quads and more 1.004), 5 for bytes 1.006,
+// 1 for 16-bit states 1.001.
 template <typename ST, bool WIDE>
-__global__ __launch_bounds__(kBlock, Quad<ST>::kBytes == 2 ? 5 : Quad<ST>::kBytes == 4 ? 4 : 2) void count_kernel(const int32_t *__restrict__ cdesc,
+__global__ __launch_bounds__(kBlock, Quad<ST>::kBytes == 8 ? 2 : 4) void count_kernel(const int32_t *__restrict__ cdesc,
                                                       const int32_t *__restrict__ cdesc_off,
                                                       const int32_t *__restrict__ cwork,
                                                       int32_t count, int64_t n_slabs,
@@ -2357,8 +2359,10 @@ __device__ __forceinline__ double gamma_mt(double a, uint32_t e, uint32_t q, uin
 // once -- are listed and drawn from their first attempt on by as many lanes
 // as there are of them.  The rows are summed from LDS: one thread per row
 // that read its entries from memory took 55 us for rows of 130 states.
-// 815,059 entries in 196,000 rows: 27-32 us at 5 waves per SIMD (53 + 9 us as
-// a Gamma and a normalising launch); 26 entries 4.7 us (4.2 + 2.6 and a gap).
+// 815,059 entries in 196,000 rows: 27-32 us (53 + 9 us as a Gamma and a
+// normalising launch); 26 entries 4.7 us (4.2 + 2.6 and a gap).  4 waves per
+// SIMD: 5 spill three vector registers, and moving-sum updates of 100 nodes
+// take 109 us either way.
 constexpr int kResampleBlock = kResampleTile;
 
 // One piece of a resample: the shapes of the entries base .. base + n_e - 1
@@ -2424,7 +2428,7 @@ __device__ __forceinline__ void resample_draws(ResampleShared &S, int64_t base, 
 }
 
 template <typename T, bool MOVING>
-__global__ __launch_bounds__(kResampleBlock, 5) void resample_kernel(
+__global__ __launch_bounds__(kResampleBlock, 4) void resample_kernel(
     const int32_t *__restrict__ tile_row, const int32_t *__restrict__ row_off, const int32_t *__restrict__ row_k,
     const int32_t *__restrict__ newc, int32_t *__restrict__ mb, T *__restrict__ totals, double alpha, uint32_t k0,
     uint32_t k1, uint32_t update_id, const uint32_t *__restrict__ ids, float *__restrict__ cpts) {

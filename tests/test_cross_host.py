@@ -113,3 +113,18 @@ def test_workspaces_are_whole():
             same.same_cross_attention(p, q, k, k, q, None, ws)
         with pytest.raises(same.SameError, match="contiguous"):
             same.same_cross_attention_backward(p, q, k, k, q, None, q, q, k, k, ws)
+
+
+def test_every_kernel_source_is_checked():
+    from paper_1511_06416_amd import build
+
+    sources = sorted(f for f in os.listdir(build.CSRC) if f.endswith(".hip"))
+    assert sources == sorted(f for f in build.SOURCES if f.endswith(".hip")) and "kernels.hip" in sources
+    for src in sources:
+        flags = build.command(src, "x.o")
+        assert "-fno-slp-vectorize" in flags and "-Rpass-analysis=kernel-resource-usage" in flags, src
+    one = "a.hip:1:1: remark: Function Name: one [-R]\na.hip:1:1: remark:     VGPRs Spill: %d [-R]\n"
+    build.check_remarks("a.hip", one % 0)
+    for text in (one % 1, "", "a.hip:1:1: remark:     VGPRs Spill: 0 [-R]\n"):
+        with pytest.raises(RuntimeError, match="a.hip"):
+            build.check_remarks("a.hip", text)
