@@ -6,7 +6,10 @@ hidden) and compares its answers for held-out entries with the sampler's.
 
 Per step a random part of the known entries is hidden (key_mask) and answered
 from the rest; the held-out entries are never a key or a target.  The sampler's
-figure is that of same_predict after as many steps as asked for.
+figure is that of same_predict after as many steps as asked for.  Both stand
+beside the node marginals, which know nothing of the column: on these columns
+neither ranks better than they do, so the run compares times and shows the
+operators in use, not what an imputer can learn.
 """
 import argparse
 import os
@@ -28,6 +31,19 @@ def tokens(entries):
     """Column-major order of a [n][columns] selection: (pointers, nodes, columns)."""
     cols, nodes = np.nonzero(entries.T)
     return np.concatenate([[0], np.cumsum(entries.sum(axis=0))]).astype(np.int64), nodes, cols
+
+
+def marginals(w):
+    """AUC of the held-out entries when every node answers with the share of
+    ones among its known entries, whatever the column."""
+    obs, target = holdout(w, 0, 0.2)
+    cols = w.mb_cols(0)
+    known = obs[:, :cols] == 1
+    states = w.states[0][:, 0, :cols].cpu().numpy()
+    share = ((states == 1) & known).sum(axis=1) + 1.0
+    share /= known.sum(axis=1) + 2.0
+    _, nodes, columns = tokens(target[:, :cols] >= 0)
+    return evaluate.auc(share[nodes], states[nodes, columns] == 1)
 
 
 def train_imputer(w, steps, drop=0.1, hide=0.3, lr=3e-3, seed=5):
@@ -106,6 +122,7 @@ def main():
     a.add_argument("--steps", type=int, default=300)
     args = a.parse_args()
     w = make_workload(4, n_cols=args.columns)
+    print("node marginals: held-out AUC %.4f" % marginals(w))
     auc, per_step, ans = train_imputer(w, args.steps)
     print("imputer: held-out AUC %.4f after %d steps of %.2f ms; the answers in %.2f ms"
           % (auc, args.steps, 1e3 * per_step, 1e3 * ans))
