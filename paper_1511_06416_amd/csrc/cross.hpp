@@ -36,8 +36,8 @@ struct CrossSmallItem {
 struct CrossPass {
     const CrossItem *items;
     const CrossJoin *joins;
-    int32_t n_items, n_joins, n_slots;
-    int32_t own_waves, cut_waves;  // waves that own tiles x waves that share the other axis
+    int32_t n_items, n_joins;
+    int32_t own_waves;  // waves of a block that own tiles; one shares the other axis with three more
 };
 
 struct CrossTensor {

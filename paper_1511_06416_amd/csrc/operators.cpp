@@ -38,7 +38,7 @@ inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p) % a == 0; }
 struct PassPlan {
     std::vector<CrossItem> items;
     std::vector<CrossJoin> joins;
-    int32_t own_waves = 1, cut_waves = 1, n_slots = 0;
+    int32_t own_waves = 1, n_slots = 0;
 };
 
 struct DeviceLists {
@@ -108,7 +108,11 @@ struct Geometry {
     double entry;
 };
 
-// Waves of a pass's kernel that a SIMD holds (registers, LDS).
+// Waves of a pass's kernel that the estimate gives a SIMD.  One number for
+// kernels that differ: by their registers, gradients up to 64 wide reach 2 to 4,
+// the forward pass 3 in 1 x 4 at 64 wide and in 8 x 1 at 96, 5 in 4 x 1 at 32, and
+// dK and dV at 128 wide 1 with dropout, which a plan does not know of.  The
+// constants below were set with these numbers.
 int waves_per_simd(PassKind kind, int32_t dim, const Geometry &g) {
     if (kind == kForward) return dim <= 64 ? 4 : 2;
     return dim > 64 && g.cut_waves > 1 ? 1 : 2;
@@ -229,7 +233,6 @@ int build_pass(PassPlan &pp, const std::vector<int64_t> &q_ptr, const std::vecto
         }
     }
     pp.own_waves = shape->own_waves;
-    pp.cut_waves = shape->cut_waves;
     const int64_t tile = 32 * pp.own_waves;
     // tiles, of which only a few are cut (see plan_cut)
     double tiles = 0.0;
@@ -430,9 +433,7 @@ same::CrossPass pass_of(const same_cross_plan *pl, const DeviceLists &d, PassKin
     w.joins = d.joins[kind];
     w.n_items = (int32_t)pp.items.size();
     w.n_joins = (int32_t)pp.joins.size();
-    w.n_slots = pp.n_slots;
     w.own_waves = pp.own_waves;
-    w.cut_waves = pp.cut_waves;
     return w;
 }
 
