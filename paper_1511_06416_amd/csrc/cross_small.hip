@@ -234,12 +234,13 @@ __global__ __launch_bounds__(64 * units(NS), NS <= 4 ? 4 : 2) void cross_small_f
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
     top = both_max(top);
-    // exponents are at most kUpBits: the sum carries kUp too
-    const float c = p.scale * kLog2e, base2 = __builtin_fmaf(top == -kInf ? 0.0f : top, c, -(float)kUpBits<T>);
+    // exponents are at most kUpBits, and that exactly for the largest score
+    // however large it is: the sum carries kUp too
+    const float c = p.scale * kLog2e, from = top == -kInf ? 0.0f : top;
     float sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -base2));
+        s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e] - from, c, (float)kUpBits<T>));
         sum += s[e];
     }
     sum = both_sum(sum);

@@ -95,3 +95,22 @@ def test_certain_keys_stay_in_range(keys):
         for n in got:
             assert bool(got[n].isfinite().all()), n
             ref.check(n, got[n], *want[n])
+
+
+@pytest.mark.parametrize("d", [8, 64, 128])
+@pytest.mark.parametrize("rows,keys,heads", [(5, 20, 2), (1, 500, 3), (300, 500, 40), (2100, 300, 64)])
+@pytest.mark.parametrize("size", [300.0, 5000.0, 3e4])
+@pytest.mark.parametrize("dtype", [HF, torch.bfloat16])
+def test_forward_of_huge_scores(d, rows, keys, heads, size, dtype):
+    """Scores of 2^17 to 2^34, where fp32 has no digits below 1 left: the key
+    on which they are largest takes all, and out is its value exactly."""
+    q = torch.full((rows, 1, d), size).to(dtype)
+    k = torch.full((keys, 1, d), 0.75 * size).to(dtype)
+    v = torch.randn(keys, 1, d, generator=torch.Generator().manual_seed(d)).to(dtype)
+    for best in (0, keys // 2, keys - 1):
+        kk = k.clone()
+        kk[best] = size
+        got = run(*(x.cuda().expand(-1, heads, -1) for x in (q, kk, v)), [0, rows], [0, keys])
+        assert torch.equal(got["out"].cpu(), v[best].expand(rows, heads, d)), best
+        lse = float((q[0, 0].double() * kk[best, 0].double()).sum()) * d ** -0.5
+        assert float((got["lse"].double() - lse).abs().max()) <= 2.0 ** -21 * lse, best
