@@ -356,3 +356,15 @@ def test_refusals():
 def test_least_scale(ql, kl):
     """The smallest scale weighs every visible key alike."""
     compare(ql, kl, 2, 1, 32, BF, masked=0.3, scale=1.2e-38)
+
+
+@pytest.mark.parametrize("drop", [0.0, 0.1])
+def test_mostly_small_segments(drop):
+    """Columns of about 24 entries, some above 32, queries equal to keys: a few
+    longer segments take all of them off the packed path, which the same columns
+    clipped at 32 take."""
+    n = np.random.default_rng(5).binomial(300, 0.08, 700)
+    n[::100] = 0
+    assert 0 < (n > 32).mean() < 0.1
+    compare(n, n, 4, 4, 32, BF, masked=0.3, drop=drop, seed=2)
+    compare(np.minimum(n, 32), np.minimum(n, 32), 4, 4, 32, BF, masked=0.3, drop=drop, seed=2)
