@@ -434,9 +434,8 @@ struct QueryStage {
         L::template store<Tile>(tq, a);
         L::template store<Tile>(tg, b);
         if ((int)threadIdx.x < ROWS) {
-            // of P * kUp and of (dP - delta) * kDown
-            stat_lse[(int)threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e - kUpBits<T>;
-            stat_delta[(int)threadIdx.x] = -delta * kDown<T>;
+            stat_lse[(int)threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e;
+            stat_delta[(int)threadIdx.x] = -delta;
             if (stat_id) stat_id[(int)threadIdx.x] = loaded_id;
         }
     }
@@ -466,10 +465,10 @@ __device__ __forceinline__ float both_sum(float v) {
 __device__ __forceinline__ int acc_row(int e, int half) { return 8 * (e >> 2) + 4 * half + (e & 3); }
 
 template <typename T>
-__device__ __forceinline__ typename Vec<T>::x8 round8(const f32x16 &a, int first) {
+__device__ __forceinline__ typename Vec<T>::x8 round8(const f32x16 &a, int first, float up = 1.0f) {
     typename Vec<T>::x8 r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (T)a[first + i];
+    for (int i = 0; i < 8; ++i) r[i] = (T)(a[first + i] * up);
     return r;
 }
 

@@ -133,15 +133,15 @@ __global__ __launch_bounds__(64 * OW * CW, key_waves(NS, CW, DROP)) void cross_d
                 if (DROP) {
                     const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)mask[e >> 1], 16 * (e & 1), 16);
                     w[e] = __uint_as_float(__float_as_uint(x) & m);
-                    s[e] = __builtin_fmaf(w[e], dp[e] * kDown<T>, x * d4[i]);   // dS / gain
+                    s[e] = __builtin_fmaf(w[e], dp[e], x * d4[i]);   // dS / gain
                 } else {
-                    s[e] = x * __builtin_fmaf(dp[e], kDown<T>, d4[i]);
+                    s[e] = x * (dp[e] + d4[i]);
                 }
             }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const typename Vec<T>::x8 wf = round8<T>(w, 8 * t), df = round8<T>(s, 8 * t);
+            const typename Vec<T>::x8 wf = round8<T>(w, 8 * t, kUp<T>), df = round8<T>(s, 8 * t);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
                 ov[dt] = mfma(rd.column(at_g, t, dt), wf, ov[dt]);
