@@ -548,10 +548,10 @@ void same_graph_destroy(same_graph *graph);
 /*
  * Operators of an amortised imputer.  same_predict answers a column's missing
  * entries by n frozen-CPT sweeps; a network that attends from the missing
- * entries to the same column's known entries answers them in one pass, and
- * its answers can start the latent states.  Its two operators with state of
- * their own are here: cross attention over ragged columns with gradients, and
- * dropout whose mask is made again wherever it is needed.
+ * entries to the same column's known entries answers them in one pass.  Its
+ * two operators with state of their own are here: cross attention over ragged
+ * columns with gradients, and dropout whose mask is made again wherever it is
+ * needed.
  */
 enum {
     SAME_F32 = 0,
@@ -569,8 +569,9 @@ enum {
  * uploaded synchronously on the first device call per device, so make one
  * before capturing a graph.  A plan serves any number of calls, one host
  * thread at a time; calls on different streams need workspaces of their own.
- * Errors: SAME_EINVAL, SAME_ESIZE (2^31 segments; a segment with 2^30 keys, or
- * 2^30 query rows of one key head; over 2^30 blocks), SAME_ENOMEM.
+ * Errors: SAME_EINVAL, SAME_ESIZE (2^31 segments; over 65536 heads; a segment
+ * with 2^30 keys, or 2^30 query rows of one key head; over 2^30 blocks),
+ * SAME_ENOMEM.
  */
 typedef struct same_cross_plan same_cross_plan;
 
@@ -597,7 +598,9 @@ int same_cross_workspace_size(const same_cross_plan *plan, int32_t backward, siz
  * the softmax's sum; the gradient needs it.
  *
  * Scores, maxima, sums and the weighted sum of values are fp32; probabilities
- * are rounded to dtype before the product with v, out once at the end.
+ * are rounded to dtype before the product with v (in SAME_F16 times a power of
+ * two, so that shares down to 2^-20 of a row's largest keep their digits), out
+ * once at the end.
  *
  * drop in [0, 1) is taken to the nearest of 256 parts t (SAME_EINVAL where a
  * positive drop rounds to 0 or 256): D_ij = 0 where the 8-bit number of
@@ -628,6 +631,8 @@ int same_cross_attention(same_cross_plan *plan, const void *q, int64_t q_row, in
  * In SAME_F16 P carries 2^14 meanwhile, so that a key's small share keeps its
  * digits; dS follows dout and does not: dout's scale has to keep it in the
  * type's range (below 2^-14 it loses digits), as with any loss scaling.
+ * delta = dout . out is taken from the rounded out in segments of more than 32
+ * keys.  Errors as for same_cross_attention.
  */
 int same_cross_attention_backward(same_cross_plan *plan, const void *q, int64_t q_row,
                                   int64_t q_head, const void *k, int64_t k_row, int64_t k_head,
@@ -648,7 +653,10 @@ int same_cross_attention_backward(same_cross_plan *plan, const void *q, int64_t 
  * {(e / 8) mod 2^32, e / 8 >> 32, 4<<24, call_id}, and else scaled by
  * 65536 / (65536 - t), in fp32, rounded once.  A dropped element does not use
  * x (NaN included).  y may be x or residual itself (same strides) and must
- * not overlap them otherwise.
+ * not overlap them otherwise.  Rows that lie one after another, or whose
+ * width, strides and addresses are multiples of eight elements and 16 bytes,
+ * are read and written 16 bytes at a time, others element by element.
+ * Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE (10^12 elements), SAME_EHIP.
  */
 int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residual,
                  int64_t residual_row, int64_t rows, int64_t cols, double drop, uint64_t seed,

@@ -20,10 +20,10 @@ using namespace cross;
 // in fp32.
 //
 // What bounds it: at 128 wide the matrix units and the exponents beside them
-// (each busy 45 % of the time: a wave's products wait for its softmax, which
+// (busy 45 and 41 % of the time: a wave's products wait for its softmax, which
 // the second wave of the SIMD hides in part), 2 x 4,099 rows on 7,951 keys, 16
-// heads on 4, 529 us, 1010 TFLOP/s.  At 64 wide with dropout the vector units
-// (76 % busy), 64 columns of 1000 nodes 118 us; the whole call takes 102 us
+// heads on 4, 522 us, 1020 TFLOP/s.  At 64 wide with dropout the vector units
+// (77 % busy), 64 columns of 1000 nodes 118 us; the whole call takes 102 us
 // without dropout, 125 with it and 137 with twice the generator's work, which
 // 16 bits instead of 8 a probability would need.  Columns of 330 nodes (about
 // 165 rows on 149 visible keys) spend most of their 49 us on the way in and

@@ -24,8 +24,9 @@ constexpr int key_waves(int ns, int cw, bool drop) {
 //
 // Two accumulators of the head's width a wave leave room for two waves a SIMD
 // (LDS for one where four waves share 32 wide keys).  4,099 rows on 4,095 keys,
-// 16 heads on 4 of 128: 286 us, the matrix units busy 40 % of it, LDS 35, the vector
-// units 31; 128 columns of 330 nodes, 8 heads of 64 with dropout: 50 us, of
+// 16 heads on 4 of 128: 284 us, the matrix units busy 40 % of it, LDS 35, the vector
+// units 31 (with dropout, one wave a SIMD, some 600 us); 128 columns of 330 nodes, 8 heads
+// of 64 with dropout: 49 us, of
 // some 38,000 cycles of a wave 9,000 before its first product, 3,500 after its
 // last and 3,300 to 4,600 for each 32 rows.
 template <typename T, int NS, int OW, int CW, bool DROP>

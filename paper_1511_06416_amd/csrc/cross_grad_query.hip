@@ -19,8 +19,8 @@ using namespace cross;
 // A row's q, dout and accumulators fill the registers of two waves a SIMD (one
 // for four waves that share 32 wide rows, which would spill at two), so the
 // tiles of k and v have two buffers and the loads of the next ones fly during
-// the products.  4,099 rows on 4,095 keys, 16 heads on 4 of 128: 206 us, the
-// matrix units busy 43 % of it, the vector units 34; 128 columns of 330 nodes, 8 heads
+// the products.  4,099 rows on 4,095 keys, 16 heads on 4 of 128: 204 us, the
+// matrix units busy 44 % of it, the vector units 35; 128 columns of 330 nodes, 8 heads
 // of 64 with dropout: 38 us, of which most is the way in and out.
 template <typename T, int NS, int OW, int CW, bool DROP>
 __global__ __launch_bounds__(64 * OW * CW, CW > 1 && NS > 4 ? 1 : NS == 2 ? 3 : 2) void cross_dq_kernel(
