@@ -77,7 +77,7 @@ enum {
     SAME_EINVAL = -1,  /* bad argument (null pointer, m < 1, n_cols > ld, ...) */
     SAME_EGRAPH = -2,  /* cycle, self-loop, duplicate or out-of-range parent */
     SAME_ECARD = -3,   /* a cardinality outside [2, 32767] */
-    SAME_ESIZE = -4,   /* a size that overflows the library's int32 indexing */
+    SAME_ESIZE = -4,   /* a size that overflows the library's int32 indexing, or a launch of 2^32 threads */
     SAME_ENOMEM = -5,  /* host or device allocation failed */
     SAME_EHIP = -6,    /* a HIP runtime call failed (message has the HIP error) */
     SAME_EALIGN = -7   /* col_offset or ld not a multiple of 4, misaligned pointer */

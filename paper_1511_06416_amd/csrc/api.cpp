@@ -226,6 +226,8 @@ int stream_res_for_current_device(same_ctx *ctx, StreamRes **out) {
 
 int check_hip(hipError_t e, const char *what) {
     if (e == hipSuccess) return SAME_OK;
+    if (e == hipErrorInvalidConfiguration)
+        return set_error(SAME_ESIZE, std::string(what) + ": more threads than one launch takes (2^32); use fewer columns");
     return set_error(SAME_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 

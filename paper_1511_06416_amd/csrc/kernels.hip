@@ -3004,6 +3004,11 @@ __global__ __launch_bounds__(kBlock) void grow_kernel(const char *__restrict__ s
 namespace {
 inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
+// The device takes fewer than 2^32 threads a launch, and runs the rest of a
+// larger grid without an error, short: such a launch is refused.
+inline bool too_large(int64_t blocks, int64_t threads = dev::kBlock) { return blocks * threads > 0xffffffffll; }
+constexpr hipError_t kTooLarge = hipErrorInvalidConfiguration;
+
 // Calls f with a value of the state type of a format: 4-bit (Nib), 8- or
 // 16-bit states.
 template <typename F>
@@ -3175,7 +3180,7 @@ hipError_t launch_sweep(SweepParams P, int32_t begin, int32_t count, int32_t n_l
         if (g == 1) P.block_split = (uint32_t)blocks;
         blocks += (P.geom[g].n_slabs + dev::kXcds - 1) / dev::kXcds * dev::kXcds * P.geom[g].count;
     }
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (too_large(blocks, block_quads)) return kTooLarge;
     const dim3 grid((unsigned)blocks);
     by_format(state_bits, [&](auto tag) { sweep_class<decltype(tag)>(P, klass, lds_bytes, grid, stream); });
     return hipGetLastError();
@@ -3213,6 +3218,7 @@ hipError_t launch_tiny(SweepParams P, const DeviceTables &t, const Compiled &g, 
     O.states = O.list + up16((int64_t)groups * 64 * 2);
     O.wave_bytes = O.states + up16(g.n * mq * 64 * groups * g.quad_bytes);
     const int32_t lds = O.waves + O.wave_bytes * (dev::kBlock / 64);
+    if (too_large(waves + dev::kBlock / 64, 64)) return kTooLarge;
     const dim3 grid((unsigned)((waves + dev::kBlock / 64 - 1) / (dev::kBlock / 64)));
     by_format(g.state_bits, [&](auto tag) {
         using ST = decltype(tag);
@@ -3298,7 +3304,7 @@ hipError_t launch_counts(const DeviceTables &t, const void *states, int32_t stat
     const int64_t n_slabs = col_slabs * rsplit;
     const int64_t rounds = (n_slabs + dev::kXcds - 1) / dev::kXcds;
     const int64_t blocks = rounds * dev::kXcds * n;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (too_large(blocks)) return kTooLarge;
     const dim3 grid((unsigned)blocks);
 #define SAME_LAUNCH_COUNTS(ST, WIDE)                                                                    \
     hipLaunchKernelGGL((dev::count_kernel<ST, WIDE>), grid, dim3(dev::kBlock), 0, stream, t.cdesc, t.cdesc_off, \
@@ -3321,7 +3327,7 @@ hipError_t launch_expand(const int64_t *row_ptr, int32_t n, const int32_t *col_i
     hipError_t e = launch_fill_zero(reinterpret_cast<int32_t *>(obs), (int64_t)n * ld / 4, stream);
     if (e != hipSuccess || nnz <= 0) return e;
     const int64_t blocks = (nnz + dev::kExpandEntries - 1) / dev::kExpandEntries;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (too_large(blocks)) return kTooLarge;
     by_format(state_bits, [&](auto tag) {
         using ST = decltype(tag);
         using E = typename dev::ElemOf<ST>::T;
@@ -3336,7 +3342,7 @@ hipError_t launch_init_latent(const DeviceTables &t, int32_t n, int32_t m, int64
                               void *states, const uint8_t *obs, hipStream_t stream) {
     if (n <= 0 || n_cols <= 0) return hipSuccess;
     const int64_t chunks = (n_cols + 4 * dev::kInitGroups - 1) / (4 * dev::kInitGroups);
-    if (chunks * n > 0x7fffffff) return hipErrorInvalidValue;
+    if (too_large(chunks * n)) return kTooLarge;
     const dim3 grid((unsigned)(chunks * n));
 #define SAME_LAUNCH_INIT(ST, WIDE)                                                                              \
     hipLaunchKernelGGL((dev::init_latent_kernel<ST, WIDE>), grid, dim3(dev::kBlock), 0, stream, t.cdesc, \
@@ -3358,7 +3364,7 @@ hipError_t launch_hits(const void *states, const void *target, int32_t n, int32_
     const int64_t items = (int64_t)n * ((n_cols + 3) / 4);
     if (items <= 0) return hipSuccess;
     const int64_t blocks = (items + dev::kBlock - 1) / dev::kBlock;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (too_large(blocks)) return kTooLarge;
     by_format(state_bits, [&](auto tag) {
         using ST = decltype(tag);
         using E = typename dev::ElemOf<ST>::T;
@@ -3380,6 +3386,7 @@ hipError_t launch_compact_counts(const uint8_t *obs, int64_t obs_ld, int64_t c0,
                                  int32_t *counts, bool prefix, hipStream_t stream) {
     const int32_t chunks = (int32_t)((cols + dev::kCompactChunk - 1) / dev::kCompactChunk);
     if (cols <= 0 || n <= 0) return hipSuccess;
+    if (too_large((int64_t)n * chunks)) return kTooLarge;
     hipLaunchKernelGGL(dev::compact_counts_kernel, dim3((unsigned)((int64_t)n * chunks)), dim3(dev::kBlock), 0,
                        stream, obs, obs_ld, c0, cols, chunks, counts);
     if (prefix)
@@ -3394,6 +3401,7 @@ hipError_t launch_expand_compact(const uint8_t *obs, const void *data, int64_t o
                                  int32_t state_bits, hipStream_t stream) {
     const int32_t chunks = (int32_t)((cols + dev::kCompactChunk - 1) / dev::kCompactChunk);
     if (cols <= 0 || n <= 0) return hipSuccess;
+    if (too_large((int64_t)n * chunks)) return kTooLarge;
     const dim3 grid((unsigned)((int64_t)n * chunks));
     by_format(state_bits, [&](auto tag) {
         using ST = decltype(tag);
@@ -3410,6 +3418,7 @@ hipError_t launch_gather_compact(const uint8_t *obs, int64_t obs_ld, int64_t c0,
                                  int64_t slot_ld, void *lat_states, int32_t state_bits, hipStream_t stream) {
     const int32_t chunks = (int32_t)((cols + dev::kCompactChunk - 1) / dev::kCompactChunk);
     if (cols <= 0 || n <= 0) return hipSuccess;
+    if (too_large((int64_t)n * chunks)) return kTooLarge;
     const dim3 grid((unsigned)((int64_t)n * chunks));
     by_format(state_bits, [&](auto tag) {
         using ST = decltype(tag);
@@ -3428,8 +3437,8 @@ hipError_t launch_grow(const void *src, int32_t m, void *dst, int32_t m2, int32_
     auto run = [&](auto tag, auto nq) {
         constexpr int NQ = decltype(nq)::value;
         const int64_t chunks = (ld + NQ * dev::kBlock - 1) / (NQ * dev::kBlock);
-        if (chunks * n > 0x7fffffff) {
-            e = hipErrorInvalidValue;
+        if (too_large(chunks * n)) {
+            e = kTooLarge;
             return;
         }
         hipLaunchKernelGGL((dev::grow_kernel<decltype(tag), NQ>), dim3((unsigned)(chunks * n)), dim3(dev::kBlock), 0,

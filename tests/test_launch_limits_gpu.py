@@ -5,6 +5,7 @@ import torch
 
 import paper_1511_06416_amd as same
 from tests import cross_reference as ref
+from workloads import make_network
 
 pytestmark = pytest.mark.gpu
 HF = torch.float16
@@ -81,3 +82,24 @@ def test_small_segments_of_more_than_2_to_26_waves():
     for s in range(0, segs, 100):
         n = min(100, segs - s)
         assert torch.equal(out[32 * s:32 * (s + n)].view(n, 32, heads, 8), v[s:s + n, None].expand(n, 32, heads, 8)), s
+
+
+def test_a_launch_that_would_run_short_is_refused():
+    """The sampler's launches: growing five nodes of 860 million columns, whose
+    states begin off the wide accesses' boundaries, takes 16.8 million blocks of
+    256 threads; fewer columns work."""
+    pptr, pidx, card = make_network(1).csr()
+    ctx = same.same_create_ex(pptr, pidx, card, 1.0, state_bits=4)
+    for ld, fits in ((4_000_000, True), (860_000_000, False)):
+        src, dst = (torch.full((ctx.n_nodes * ld + 1,), v, dtype=torch.int16, device="cuda")[1:].view(ctx.n_nodes, 1, ld)
+                    for v in (1, 0))
+        if fits:
+            same.same_grow_replicas(ctx, src, 1, dst, 4, ld)
+            assert bool((dst == 0x1111).all())
+        else:
+            with pytest.raises(same.SameError) as e:
+                same.same_grow_replicas(ctx, src, 1, dst, 4, ld)
+            assert e.value.code == same.SAME_ESIZE
+            assert not bool(dst.any())
+        del src, dst
+    ctx.close()
