@@ -662,6 +662,138 @@ int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residu
                  int64_t residual_row, int64_t rows, int64_t cols, double drop, uint64_t seed,
                  uint32_t call_id, void *y, int64_t y_row, void *stream);
 
+/*
+ * Norms of query and key heads with the rotation by position, in one launch.
+ * Of every head's vector x of head_dim numbers:
+ *     z_i = weight_i x_i / sqrt(mean x^2 + eps)
+ * and of its first rot_dim numbers, h = rot_dim / 2, a_i = position angles_i:
+ *     y_i     = z_i     cos a_i - z_{i+h} sin a_i
+ *     y_{i+h} = z_{i+h} cos a_i + z_i     sin a_i,      i < h,
+ * the others stay z.  Scores of rotated heads depend on positions by their
+ * difference: with the column's number in a segment as position, an entry
+ * tells its own column's entries from the others'.
+ *
+ * q [q_tokens][heads_q][head_dim] and k [k_tokens][heads_kv][head_dim] have
+ * strides and alignment as in same_cross_attention, without the limit on a
+ * token's (0 repeats); either may have no tokens.  head_dim is a multiple of 8
+ * up to 128, rot_dim even (0: no rotation, positions and angles are not used),
+ * angles a host array of rot_dim / 2 radians per position, positions int32 on
+ * the device, of any sign.  The weights are fp32 [head_dim], null: ones.  eps
+ * is a positive normal number in 32 bits.  q_out and k_out are contiguous
+ * [tokens][heads][head_dim] of dtype and may be q or k themselves where those
+ * are contiguous; they overlap nothing else.
+ *
+ * Squares are summed in fp32 (of x 2^-64 where they pass it, eps then counts
+ * nothing), angles reduced to an eighth of a turn in 64 bits from turns held in
+ * two, outputs rounded once.  Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE
+ * (2^40 tokens, over 65536 heads), SAME_EHIP, SAME_ENOMEM.
+ */
+int same_qk_norm(int32_t dtype, int32_t head_dim, const void *q, int64_t q_row, int64_t q_head,
+                 int64_t q_tokens, int32_t heads_q, const float *q_weight,
+                 const int32_t *q_positions, const void *k, int64_t k_row, int64_t k_head,
+                 int64_t k_tokens, int32_t heads_kv, const float *k_weight,
+                 const int32_t *k_positions, double eps, int32_t rot_dim, const double *angles,
+                 void *q_out, void *k_out, void *stream);
+
+/*
+ * Gradients of same_qk_norm with respect to q, k and the weights, from dq_out
+ * and dk_out (strides as q's), with the forward's arguments.  dq and dk are
+ * contiguous; dq may be dq_out itself and dk dk_out, where those are
+ * contiguous.  dq_weight and dk_weight, fp32 [head_dim], are sums over all
+ * tokens and heads in an order that depends on the sizes alone (no atomics);
+ * null: not wanted.  The workspace (same_qk_norm_workspace_size, 256-byte
+ * aligned) is used only for them.  Errors as for same_qk_norm.
+ */
+int same_qk_norm_backward(int32_t dtype, int32_t head_dim, const void *q, int64_t q_row,
+                          int64_t q_head, int64_t q_tokens, int32_t heads_q, const float *q_weight,
+                          const int32_t *q_positions, const void *k, int64_t k_row, int64_t k_head,
+                          int64_t k_tokens, int32_t heads_kv, const float *k_weight,
+                          const int32_t *k_positions, double eps, int32_t rot_dim,
+                          const double *angles, const void *dq_out, int64_t dq_out_row,
+                          int64_t dq_out_head, const void *dk_out, int64_t dk_out_row,
+                          int64_t dk_out_head, void *dq, void *dk, float *dq_weight,
+                          float *dk_weight, void *workspace, void *stream);
+int same_qk_norm_workspace_size(int32_t head_dim, int64_t q_tokens, int32_t heads_q,
+                                int64_t k_tokens, int32_t heads_kv, size_t *bytes);
+
+/*
+ * Log probabilities of given states, with the entropy and the most likely
+ * alternatives.  Row r of logits ([rows][cols] of dtype, unit stride in a row,
+ * rows row_stride apart, 0 repeats one) has counts[r] states (null: cols; taken
+ * to [0, cols]), the logits behind them are not used.  With m the largest of
+ * its logits x and s = sum e^(x_j - m):
+ *     log_probs = x_t - m - log s, t = targets[r]
+ *     sums      = {m, log s}          (the gradient needs them)
+ *     entropy   = log s - sum (x_j - m) e^(x_j - m) / s
+ *     top_ids, top_log_probs [rows][n_top]: the n_top <= 64 most likely states
+ *                 in falling order, ties by the lowest index; where a row has
+ *                 fewer states, -1 and -inf.
+ * log_probs and targets, sums and entropy may be null: not wanted.  A negative
+ * target is not asked for: log_probs = 0.  A target at or behind the count is
+ * impossible: -inf.  Logits of -inf are impossible states.  A row without a
+ * possible state has log_probs = -inf, sums = {-inf, 0}, entropy 0 and
+ * top_log_probs -inf.  A NaN or +inf among its logits makes a row's values NaN;
+ * NaN ranks with -inf among the alternatives.  Sums are fp32, with exponents
+ * relative to m; outputs do not depend on the device's scheduling.
+ *
+ * workspace (same_log_probs_workspace_size; 0: may be null, 256-byte aligned)
+ * holds the parts of long rows.  Outputs must not overlap each other or an
+ * input.  Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE (over 2^21 columns, 2^40
+ * rows), SAME_EHIP, SAME_ENOMEM.
+ */
+int same_log_probs(int32_t dtype, const void *logits, int64_t row_stride, int64_t rows,
+                   int64_t cols, const int32_t *counts, const int32_t *targets, float *log_probs,
+                   float *sums, float *entropy, int32_t n_top, int32_t *top_ids,
+                   float *top_log_probs, void *workspace, void *stream);
+int same_log_probs_workspace_size(int64_t rows, int64_t cols, int32_t n_top, size_t *bytes);
+
+/*
+ * The gradient of same_log_probs with respect to the logits, from those of
+ * log_probs and entropy (either may be null: zeros), with the forward's sums
+ * and entropy (needed with dentropy):
+ *     dlogits_j = dlog_probs (1[j = t] - p_j) - dentropy p_j (l_j + entropy)
+ * where l_j = x_j - m - log s and p_j = e^(l_j).  It is 0 from the row's count
+ * on, and in a row without a possible state.  A negative target has no part
+ * in it.  dlogits ([rows][cols] of dtype, rows dlogits_row >= cols apart) may
+ * be logits itself, with the same stride, and overlaps nothing else.  Errors as
+ * for same_log_probs.
+ */
+int same_log_probs_backward(int32_t dtype, const void *logits, int64_t row_stride, int64_t rows,
+                            int64_t cols, const int32_t *counts, const int32_t *targets,
+                            const float *sums, const float *entropy, const float *dlog_probs,
+                            const float *dentropy, void *dlogits, int64_t dlogits_row,
+                            void *stream);
+
+/*
+ * The orthogonalised update of n_mats matrices of one size by Newton-Schulz
+ * products: X = G / (|G| + eps), |G| the root of G's sum of squares, then
+ * `steps` times with the step's (a, b, c) of coefs (host array [steps][3])
+ *     A = X X^T,  X <- a X + (b A + c A^2) X
+ * and out = scale X: every singular value s of G / (|G| + eps) becomes
+ * scale p(s), p the chain of x (a + b x^2 + c x^4).  With rows > cols the same
+ * is done to the transpose.  A matrix of zeros gives zeros, one with NaN or an
+ * infinity NaN.
+ *
+ * g and out ([n_mats][rows][cols] of dtype, unit stride in a row, rows and
+ * matrices the given strides apart, 0 repeats g's) may be the same with the
+ * same strides and overlap nothing else.  1 <= steps <= 32; coefs must keep
+ * singular values of 1 or less within 16 (SAME_EINVAL; the bound is followed
+ * step by step); eps is a positive normal number in 32 bits.
+ *
+ * Sums of squares are 64-bit, products' sums fp32, of operands held as two
+ * fp16 each (22 bits); in SAME_BF16 the products take the first of them, while
+ * a X and b A are whole, which is off by about as much as rounding the result
+ * to bf16.  workspace (same_orthogonalise_workspace_size, 256-byte aligned)
+ * serves one call at a time.  Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE (a
+ * matrix of over 2^15 by 2^24 or 1.1 10^9 elements), SAME_EHIP, SAME_ENOMEM.
+ */
+int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_row, int64_t n_mats,
+                       int64_t rows, int64_t cols, const double *coefs, int32_t steps, double eps,
+                       double scale, void *out, int64_t out_mat, int64_t out_row, void *workspace,
+                       void *stream);
+int same_orthogonalise_workspace_size(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols,
+                                      size_t *bytes);
+
 /* Message for the calling thread's last failed call ("" if none). */
 const char *same_last_error(void);
 

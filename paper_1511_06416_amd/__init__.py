@@ -24,7 +24,9 @@ __all__ = [
     "same_grow_replicas", "same_debug_thresholds", "same_counts_noalloc", "same_stream_compact_layout",
     "same_stream_pass_compact", "same_step_graph", "same_graph_launch", "same_graph_destroy", "StepGraph",
     "CrossPlan", "same_cross_create", "same_cross_destroy", "same_cross_workspace_size", "same_cross_attention",
-    "same_cross_attention_backward", "same_dropout",
+    "same_cross_attention_backward", "same_dropout", "same_qk_norm", "same_qk_norm_backward",
+    "same_qk_norm_workspace_size", "same_log_probs", "same_log_probs_backward", "same_log_probs_workspace_size",
+    "same_orthogonalise", "same_orthogonalise_workspace_size", "NEWTON_SCHULZ",
     "pack_states", "unpack_states", "state_shape",
     "library_path", "load_library",
 ]
@@ -120,6 +122,16 @@ def load_library():
         L.same_cross_attention.argtypes = [P] + kv + [P, P, P, P]
         L.same_cross_attention_backward.argtypes = [P] + kv + [P, P, P, I64, I64, P, P, P, P, P]
         L.same_dropout.argtypes = [I32, P, I64, P, I64, I64, I64, D, U64, U32, P, I64, P]
+        heads = [P, I64, I64, I64, I32, P, P]
+        norm = [I32, I32] + heads + heads + [D, I32, P]
+        L.same_qk_norm.argtypes = norm + [P, P, P]
+        L.same_qk_norm_backward.argtypes = norm + [P, I64, I64] * 2 + [P] * 6
+        L.same_qk_norm_workspace_size.argtypes = [I32, I64, I32, I64, I32, C.POINTER(C.c_size_t)]
+        L.same_log_probs.argtypes = [I32, P, I64, I64, I64, P, P, P, P, P, I32, P, P, P, P]
+        L.same_log_probs_backward.argtypes = [I32, P, I64, I64, I64] + [P] * 7 + [I64, P]
+        L.same_log_probs_workspace_size.argtypes = [I64, I64, I32, C.POINTER(C.c_size_t)]
+        L.same_orthogonalise.argtypes = [I32, P, I64, I64, I64, I64, I64, P, I32, D, D, P, I64, I64, P, P]
+        L.same_orthogonalise_workspace_size.argtypes = [I32, I64, I64, I64, C.POINTER(C.c_size_t)]
         L.same_last_error.argtypes = []
         L.same_last_error.restype = C.c_char_p
         for f in ("same_create", "same_create_ex", "same_layout", "same_workspace_size", "same_sweep",
@@ -130,7 +142,10 @@ def load_library():
                   "same_stream_pass_ema", "same_grow_replicas", "same_debug_thresholds",
                   "same_counts_noalloc", "same_stream_compact_layout", "same_stream_pass_compact",
                   "same_step_graph", "same_graph_launch", "same_cross_create", "same_cross_workspace_size",
-                  "same_cross_attention", "same_cross_attention_backward", "same_dropout"):
+                  "same_cross_attention", "same_cross_attention_backward", "same_dropout", "same_qk_norm",
+                  "same_qk_norm_backward", "same_qk_norm_workspace_size", "same_log_probs",
+                  "same_log_probs_backward", "same_log_probs_workspace_size", "same_orthogonalise",
+                  "same_orthogonalise_workspace_size"):
             getattr(L, f).restype = C.c_int
         _lib = L
         return L
@@ -701,3 +716,193 @@ def same_dropout(x, y, drop, seed, call_id, residual=None, stream=None):
     _check((_lib or load_library()).same_dropout(dtype, px, x_row, pr, r_row, rows, cols, float(drop), int(seed),
                                                  int(call_id), py, y_row,
                                                  _stream(stream)))
+
+
+# Operators of a training step.  Their calls run on the current device and, by
+# default, its current stream; tensors of another device are refused.
+
+def _here(name, t):
+    """Address of a tensor on the current device."""
+    at = t.get_device()
+    if at < 0:
+        raise SameError(SAME_EINVAL, "%s must be a device tensor" % name)
+    import torch
+    if at != torch.cuda.current_device():
+        raise SameError(SAME_EINVAL, "%s is on device %d, not on the current one" % (name, at))
+    return t.data_ptr()
+
+
+def _flat(name, t, shape, dtype):
+    """Address of a contiguous tensor of one shape and type, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or str(t.dtype) != dtype or not t.is_contiguous():
+        raise SameError(SAME_EINVAL, "%s must be contiguous %s of shape %s, got %s of %s"
+                        % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    return _here(name, t)
+
+
+def _bytes(t, need):
+    """Address of a workspace of at least that many bytes, or None where none is needed."""
+    if not need:
+        return None
+    if t is None or t.numel() * t.element_size() < need or not t.is_contiguous():
+        raise SameError(SAME_EINVAL, "workspace must be contiguous, with at least %d bytes" % need)
+    return _here("workspace", t)
+
+
+def _heads(name, t, dtype, shape=None):
+    """Address and element strides of a token and a head of [tokens][heads][head_dim]."""
+    if t.dim() != 3 or t.dtype != dtype or (shape is not None and t.shape != shape):
+        raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
+                        % (name, dtype, "[tokens][heads][head_dim]" if shape is None else tuple(shape), t.dtype,
+                           tuple(t.shape)))
+    row, head, unit = t.stride()
+    if unit != 1 and t.numel():
+        raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+    n, heads, _ = t.shape
+    return _here(name, t), row if n > 1 else 0, head if heads > 1 else 0
+
+
+def _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps):
+    dtype, dim = _dtype(q.dtype), q.shape[-1]
+    if k.shape[-1] != dim:
+        raise SameError(SAME_EINVAL, "q and k must have heads of one width")
+    if angles is None:
+        rot, turns = 0, None
+    else:
+        angles = np.ascontiguousarray(angles, dtype=np.float64)
+        if angles.ndim != 1:
+            raise SameError(SAME_EINVAL, "angles must be one-dimensional")
+        rot, turns = 2 * len(angles), angles.ctypes.data
+    args = [dtype, dim]
+    for name, t, weight, positions in (("q", q, q_weight, q_positions), ("k", k, k_weight, k_positions)):
+        args += _heads(name, t, q.dtype)
+        args += [t.shape[0], t.shape[1], _flat(name + "_weight", weight, (dim,), "torch.float32"),
+                 _flat(name + "_positions", positions, t.shape[:1], "torch.int32") if rot else None]
+    # angles: kept alive by the caller until the call returns
+    return args + [float(eps), rot, turns], angles
+
+
+def same_qk_norm(q, k, q_out, k_out, q_weight=None, k_weight=None, q_positions=None, k_positions=None, angles=None,
+                 eps=1e-6, stream=None):
+    """angles: float64 numpy array of rot_dim / 2 radians a position (None or empty: no rotation)."""
+    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
+    name = str(q.dtype)
+    _check((_lib or load_library()).same_qk_norm(*args, _flat("q_out", q_out, q.shape, name),
+                                                 _flat("k_out", k_out, k.shape, name), _stream(stream)))
+
+
+def same_qk_norm_backward(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_weight=None, k_weight=None,
+                          q_positions=None, k_positions=None, angles=None, eps=1e-6, stream=None):
+    """dq_weight and dk_weight may be None."""
+    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
+    name, width = str(q.dtype), q.shape[-1:]
+    need = 0
+    if dq_weight is not None or dk_weight is not None:
+        need = same_qk_norm_workspace_size(q.shape[2], q.shape[0], q.shape[1], k.shape[0], k.shape[1])
+    _check((_lib or load_library()).same_qk_norm_backward(
+        *args, *_heads("dq_out", dq_out, q.dtype, q.shape), *_heads("dk_out", dk_out, q.dtype, k.shape),
+        _flat("dq", dq, q.shape, name), _flat("dk", dk, k.shape, name),
+        _flat("dq_weight", dq_weight, width, "torch.float32"), _flat("dk_weight", dk_weight, width, "torch.float32"),
+        _bytes(workspace, need), _stream(stream)))
+
+
+def same_qk_norm_workspace_size(head_dim, q_tokens, heads_q, k_tokens, heads_kv) -> int:
+    out = C.c_size_t()
+    _check((_lib or load_library()).same_qk_norm_workspace_size(int(head_dim), int(q_tokens), int(heads_q),
+                                                                int(k_tokens), int(heads_kv), C.byref(out)))
+    return out.value
+
+
+def _logits(name, t, like):
+    """Address and row stride of a matrix of logits."""
+    if t.dim() != 2 or t.shape != like.shape or t.dtype != like.dtype:
+        raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like logits" % name)
+    row, unit = t.stride()
+    if unit != 1 and t.shape[1] > 1 and t.numel():
+        raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+    return _here(name, t), row
+
+
+def same_log_probs(logits, targets, log_probs, workspace, counts=None, sums=None, entropy=None, top_ids=None,
+                   top_log_probs=None, stream=None):
+    """targets and counts: int32.  targets with log_probs, sums ([rows][2]), entropy, and top_ids (int32) with
+    top_log_probs may be None; the number of alternatives is top_ids' second size."""
+    dtype = _dtype(logits.dtype)
+    at, row = _logits("logits", logits, logits)
+    rows, cols = logits.shape
+    one, n_top = (rows,), 0
+    if (top_ids is None) != (top_log_probs is None):
+        raise SameError(SAME_EINVAL, "top_ids and top_log_probs come together")
+    if top_ids is not None:
+        if top_ids.dim() != 2:
+            raise SameError(SAME_EINVAL, "top_ids must be of shape [rows][n_top]")
+        n_top = top_ids.shape[1]
+    lib = _lib or load_library()
+    need = same_log_probs_workspace_size(rows, cols, n_top) if cols > 64 else 0
+    _check(lib.same_log_probs(
+        dtype, at, row, rows, cols, _flat("counts", counts, one, "torch.int32"),
+        _flat("targets", targets, one, "torch.int32"), _flat("log_probs", log_probs, one, "torch.float32"),
+        _flat("sums", sums, (rows, 2), "torch.float32"), _flat("entropy", entropy, one, "torch.float32"), n_top,
+        _flat("top_ids", top_ids, (rows, n_top), "torch.int32"),
+        _flat("top_log_probs", top_log_probs, (rows, n_top), "torch.float32"), _bytes(workspace, need),
+        _stream(stream)))
+
+
+def same_log_probs_backward(logits, targets, sums, dlogits, counts=None, entropy=None, dlog_probs=None, dentropy=None,
+                            stream=None):
+    """sums and entropy: the forward's.  dlog_probs and dentropy may be None."""
+    dtype = _dtype(logits.dtype)
+    at, row = _logits("logits", logits, logits)
+    rows, cols = logits.shape
+    one = (rows,)
+    _check((_lib or load_library()).same_log_probs_backward(
+        dtype, at, row, rows, cols, _flat("counts", counts, one, "torch.int32"),
+        _flat("targets", targets, one, "torch.int32"), _flat("sums", sums, (rows, 2), "torch.float32"),
+        _flat("entropy", entropy, one, "torch.float32"), _flat("dlog_probs", dlog_probs, one, "torch.float32"),
+        _flat("dentropy", dentropy, one, "torch.float32"), *_logits("dlogits", dlogits, logits), _stream(stream)))
+
+
+def same_log_probs_workspace_size(rows, cols, n_top) -> int:
+    out = C.c_size_t()
+    _check((_lib or load_library()).same_log_probs_workspace_size(int(rows), int(cols), int(n_top), C.byref(out)))
+    return out.value
+
+
+# Five steps that take every singular value from some 0.003 up to about 1
+# (0.7 to 1.2): steep at zero instead of exact at one.
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def _matrices(name, t, like):
+    """Address and strides of [n][rows][cols] or [rows][cols]."""
+    if t.dim() not in (2, 3) or t.shape != like.shape or t.dtype != like.dtype:
+        raise SameError(SAME_EINVAL, "%s must be matrices shaped and typed like g" % name)
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
+        raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
+    return _here(name, t), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)
+
+
+def same_orthogonalise(g, out, workspace, coefs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, stream=None):
+    """g, out: a matrix or [n] matrices.  coefs: (a, b, c) of every step."""
+    dtype = _dtype(g.dtype)
+    at, g_mat, g_row = _matrices("g", g, g)
+    steps = np.ascontiguousarray(coefs, dtype=np.float64)
+    if steps.ndim != 2 or steps.shape[1] != 3:
+        raise SameError(SAME_EINVAL, "coefs must be (a, b, c) of every step")
+    n = g.shape[0] if g.dim() == 3 else 1
+    rows, cols = g.shape[-2:]
+    lib = _lib or load_library()
+    to, out_mat, out_row = _matrices("out", out, g)
+    need = same_orthogonalise_workspace_size(n, rows, cols, g.dtype)
+    _check(lib.same_orthogonalise(dtype, at, g_mat, g_row, n, rows, cols, steps.ctypes.data, len(steps), float(eps),
+                                  float(scale), to, out_mat, out_row, _bytes(workspace, need), _stream(stream)))
+
+
+def same_orthogonalise_workspace_size(n_mats, rows, cols, dtype) -> int:
+    """Bytes for n_mats matrices of rows x cols (dtype: torch's)."""
+    out = C.c_size_t()
+    _check((_lib or load_library()).same_orthogonalise_workspace_size(_dtype(dtype), int(n_mats), int(rows), int(cols),
+                                                                      C.byref(out)))
+    return out.value

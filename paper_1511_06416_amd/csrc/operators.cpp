@@ -16,23 +16,28 @@
 #include <vector>
 
 #include "../../include/same.h"
+#include "checks.hpp"
 #include "cross.hpp"
-#include "errors.hpp"
 
 namespace {
 
+using same::align_up;
+using same::aligned;
+using same::check_apart;
+using same::check_hip;
 using same::CrossItem;
 using same::CrossJoin;
 using same::CrossSmallItem;
+using same::extent;
+using same::Extent;
+using same::kAlign;
+using same::overlap;
 using same::record_error;
 
-constexpr size_t kAlign = 256;
 constexpr int64_t kMaxAxis = (int64_t)1 << 30;  // rows or keys of one segment
 constexpr int64_t kMaxSegs = (int64_t)1 << 31;
 constexpr int64_t kMaxBlocks = (int64_t)1 << 30;  // of a pass, before its last tiles are cut
 
-inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p) % a == 0; }
 
 // The work list of one pass on the host.
 struct PassPlan {
@@ -315,15 +320,6 @@ int lists_for_current_device(same_cross_plan *pl, DeviceLists *out) {
     return SAME_OK;
 }
 
-struct Extent {
-    uintptr_t lo = 0, hi = 0;
-};
-
-inline Extent extent(const void *p, int64_t bytes) { return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}; }
-inline bool overlap(const Extent &a, const Extent &b) {
-    return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
-}
-
 // A strided input [tokens][heads][dim] of 16-bit elements.
 int check_input(const char *name, const void *p, int64_t tokens, int64_t heads, int64_t dim, int64_t row, int64_t head,
                 Extent *ext) {
@@ -349,17 +345,6 @@ int check_output(const char *name, const void *p, int64_t elements, int64_t size
     return SAME_OK;
 }
 
-// Writable buffers must not overlap each other or what is read.
-int check_apart(const std::vector<Extent> &writes, const std::vector<Extent> &reads) {
-    for (size_t i = 0; i < writes.size(); ++i) {
-        for (size_t j = i + 1; j < writes.size(); ++j)
-            if (overlap(writes[i], writes[j])) return record_error(SAME_EINVAL, "two outputs overlap");
-        for (const Extent &r : reads)
-            if (overlap(writes[i], r)) return record_error(SAME_EINVAL, "an output overlaps an input");
-    }
-    return SAME_OK;
-}
-
 // drop as a number of `steps`: what lies below it is dropped.
 int drop_threshold(double drop, uint32_t steps, uint32_t *below) {
     *below = 0;
@@ -370,11 +355,6 @@ int drop_threshold(double drop, uint32_t steps, uint32_t *below) {
         return record_error(SAME_EINVAL, "drop must be 0 or round to 1 .. " + std::to_string(steps - 1) +
                                              " parts of " + std::to_string(steps));
     return SAME_OK;
-}
-
-int check_hip(hipError_t e, const char *what) {
-    if (e == hipSuccess) return SAME_OK;
-    return record_error(SAME_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
 // What both passes share: plan, inputs, scale, dropout, workspace.

@@ -1,0 +1,290 @@
+// Norms of query and key heads with the rotation by position, for gfx950:
+//   r = (mean x^2 + eps)^-1/2, z = w x r, and for the pairs (i, i + h), i < h:
+//   y_i = z_i cos a_i - z_{i+h} sin a_i, y_{i+h} = z_{i+h} cos a_i + z_i sin a_i
+// with a_i = position x angle_i.  Gradient, with dz the inverse rotation of dy
+// and xhat = x r: dx = r (w dz - xhat mean(w dz xhat)), dw = sum dz xhat.
+//
+// Bytes bound it.  A lane takes W elements at one place and the W that turn
+// with them, so that a rotation stays in the lane; a row (a head's vector) is a
+// group of lanes, whose sums are exchanges within the wave.  A wave takes a
+// token, whose sines it makes once, a pair a lane, for all of its heads.
+#include <algorithm>
+
+#include "step.hpp"
+#include "wave.hpp"
+
+namespace same {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxBlocks = 1 << 16;  // of a side: a wave goes on to further tokens
+
+template <typename T, int N>
+struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Chunk {
+    T v[N];
+};
+
+__device__ __forceinline__ float group_sum(float v, int lanes) { return wave::reduce(v, lanes, wave::Add()); }
+
+// cos and sin of 2 pi t for |t| <= 1/8: Taylor's series, whose next terms are
+// below 2^-31.
+__device__ __forceinline__ float2 turn_eighth(float t) {
+    const float x = t * 6.283185307179586f, x2 = x * x;
+    float s = __builtin_fmaf(x2, 2.7557319224e-6f, -1.9841269841e-4f);
+    s = __builtin_fmaf(x2, s, 8.3333333333e-3f);
+    s = __builtin_fmaf(x2, s, -1.6666666667e-1f);
+    s = __builtin_fmaf(x * x2, s, x);
+    float c = __builtin_fmaf(x2, -2.7557319224e-7f, 2.4801587302e-5f);
+    c = __builtin_fmaf(x2, c, -1.3888888889e-3f);
+    c = __builtin_fmaf(x2, c, 4.1666666667e-2f);
+    c = __builtin_fmaf(x2, c, -0.5f);
+    c = __builtin_fmaf(x2, c, 1.0f);
+    return make_float2(c, s);
+}
+
+// cos and sin of a position's angle: the turns in two 64-bit parts, less the
+// whole ones, then the eighth around the nearest quarter in 32 bits.
+__device__ __forceinline__ float2 turn_of(const NormParams &p, int32_t position, int pair) {
+    const double at = (double)position, hi = p.turn[pair];
+    const double whole = at * hi;
+    double t = whole - __builtin_rint(whole);
+    t += __builtin_fma(at, hi, -whole) + at * p.turn_low[pair];
+    const double quarter = __builtin_rint(4.0 * t);
+    const float2 e = turn_eighth((float)__builtin_fma(quarter, -0.25, t));
+    const int q = (int)quarter & 3;
+    const float c = (q & 1) ? -e.y : e.x, s = (q & 1) ? e.x : e.y;
+    return make_float2((q & 2) ? -c : c, (q & 2) ? -s : s);
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void load(const T *row, int a, int b, float (&v)[2 * W]) {
+    const Chunk<T, W> lo = *(const Chunk<T, W> *)(row + a), hi = *(const Chunk<T, W> *)(row + b);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        v[i] = (float)lo.v[i];
+        v[W + i] = (float)hi.v[i];
+    }
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void store(T *row, int a, int b, const float (&v)[2 * W]) {
+    Chunk<T, W> lo, hi;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        lo.v[i] = (T)v[i];
+        hi.v[i] = (T)v[W + i];
+    }
+    *(Chunk<T, W> *)(row + a) = lo;
+    *(Chunk<T, W> *)(row + b) = hi;
+}
+
+// (mean x^2 + eps)^-1/2 of a row.  Where the squares pass 32 bits they are
+// formed again of x 2^-64.
+template <int W>
+__device__ __forceinline__ float inverse_norm(const NormParams &p, const float (&x)[2 * W], int lanes) {
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
+    ss = group_sum(ss, lanes);
+    float up = 1.0f, mean = __builtin_fmaf(ss, p.inv_dim, p.eps);
+    if (__builtin_isinf(mean)) {
+        ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i) {
+            const float small = x[i] * 0x1p-64f;
+            ss = __builtin_fmaf(small, small, ss);
+        }
+        mean = group_sum(ss, lanes) * p.inv_dim;
+        up = 0x1p-64f;
+    }
+    // the hardware's root is off by an ulp: one step of Newton's method
+    float r = __builtin_amdgcn_rsqf(mean);
+    const float e = __builtin_fmaf(-mean * r, r, 1.0f);
+    if (__builtin_fabsf(e) < 0.5f) r = __builtin_fmaf(0.5f * r, e, r);
+    return r * up;
+}
+
+template <typename T, int W, bool GRAD>
+__global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lanes, int split) {
+    __shared__ float2 turns[kWaves][kMaxHeadDim / 2];
+    __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
+    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6;
+    const bool keys = (int)blockIdx.x >= p.side[1].first_block;
+    const NormSide &s = p.side[keys];
+    const int groups = 64 / lanes, group = lane / lanes, unit = lane & (lanes - 1);
+    const int turning = p.half / W;
+    const bool used = unit < p.dim / (2 * W);
+    const bool turned = used && unit < turning;
+    const int a = turned ? unit * W : 2 * p.half + (unit - turning) * 2 * W;
+    const int b = turned ? a + p.half : a + W;
+    float w[2 * W], dw[2 * W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        w[i] = used && s.weight ? s.weight[a + i] : 1.0f;
+        w[W + i] = used && s.weight ? s.weight[b + i] : 1.0f;
+    }
+    if (GRAD) {
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i) dw[i] = 0.0f;
+    }
+    // items: a token, or one of the `split` parts of its heads
+    const int64_t items = s.tokens * split, step = (int64_t)s.blocks * kWaves;
+    const int part = (s.heads + split - 1) / split;
+    for (int64_t item = (int64_t)((int)blockIdx.x - s.first_block) * kWaves + own; item < items; item += step) {
+        const int64_t token = split == 1 ? item : item / split;
+        const int first = split == 1 ? 0 : (int)(item - token * split) * part, last = min(first + part, s.heads);
+        if (p.half) {
+            wave::sync();
+            if (lane < p.half) turns[own][lane] = turn_of(p, s.positions[token], lane);
+            wave::sync();
+        }
+        float c[W], sn[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float2 t = turned ? turns[own][a + i] : make_float2(1.0f, 0.0f);
+            c[i] = t.x;
+            sn[i] = t.y;
+        }
+        for (int h0 = first; h0 < last; h0 += groups) {
+            const int h = h0 + group;
+            const bool here = used && h < last;
+            float x[2 * W], y[2 * W];
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i) x[i] = y[i] = 0.0f;
+            if (here) {
+                load<T, W>((const T *)s.x + token * s.x_row + h * s.x_head, a, b, x);
+                if (GRAD) load<T, W>((const T *)s.dout + token * s.dout_row + h * s.dout_head, a, b, y);
+            }
+            const float r = inverse_norm<W>(p, x, lanes);
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i) x[i] *= r;  // xhat
+            if (!GRAD) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float lo = x[i] * w[i], hi = x[W + i] * w[W + i];
+                    y[i] = turned ? lo * c[i] - hi * sn[i] : lo;
+                    y[W + i] = turned ? hi * c[i] + lo * sn[i] : hi;
+                }
+            } else {
+                float t = 0.0f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float lo = y[i], hi = y[W + i];
+                    const float dlo = turned ? lo * c[i] + hi * sn[i] : lo;
+                    const float dhi = turned ? hi * c[i] - lo * sn[i] : hi;
+                    dw[i] = __builtin_fmaf(dlo, x[i], dw[i]);
+                    dw[W + i] = __builtin_fmaf(dhi, x[W + i], dw[W + i]);
+                    y[i] = dlo * w[i];
+                    y[W + i] = dhi * w[W + i];
+                    t = __builtin_fmaf(y[i], x[i], t);
+                    t = __builtin_fmaf(y[W + i], x[W + i], t);
+                }
+                t = group_sum(t, lanes) * p.inv_dim;
+#pragma unroll
+                for (int i = 0; i < 2 * W; ++i) y[i] = r * __builtin_fmaf(-x[i], t, y[i]);
+            }
+            if (here) store<T, W>((T *)s.out + (token * s.heads + h) * p.dim, a, b, y);
+        }
+    }
+    if (GRAD && s.dweight) {
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i)
+            for (int o = lanes; o < 64; o <<= 1) dw[i] += __shfl_xor(dw[i], o);
+        if (used && group == 0) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sums[own][a + i] = dw[i];
+                sums[own][b + i] = dw[W + i];
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < p.dim; e += kThreads) {
+            float t = 0.0f;
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) t += sums[v][e];
+            p.part[(int64_t)blockIdx.x * p.dim + e] = t;
+        }
+    }
+}
+
+// The weights' gradients of the blocks' parts, summed in a fixed order: a
+// block takes 32 elements of a side.
+__global__ __launch_bounds__(1024) void qk_norm_join_kernel(NormParams p) {
+    __shared__ float sums[32][33];
+    const NormSide &s = p.side[blockIdx.y];
+    if (!s.dweight) return;
+    const int e = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+    float t = 0.0f;
+    if (e < p.dim)
+        for (int b = row; b < s.blocks; b += 32) t += p.part[(int64_t)(s.first_block + b) * p.dim + e];
+    sums[row][threadIdx.x & 31] = t;
+    __syncthreads();
+    if (row == 0 && e < p.dim) {
+        t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += sums[i][threadIdx.x & 31];
+        s.dweight[e] = t;
+    }
+}
+
+template <typename T, int W>
+hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
+    int lanes = 1;
+    while (lanes * 2 * W < p.dim) lanes *= 2;
+    // few tokens: their heads over several waves
+    int split = 1;
+    if (!grad) {
+        const int64_t tokens = std::max<int64_t>(1, p.side[0].tokens + p.side[1].tokens);
+        const int rounds = (std::max(p.side[0].heads, p.side[1].heads) * lanes + 63) / 64;
+        split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, 4096 / tokens));
+    }
+    if (!grad) {
+        int first = 0;
+        for (NormSide &d : p.side) {
+            d.first_block = first;
+            d.blocks = (int)std::min<int64_t>(kMaxBlocks, (d.tokens * split + kWaves - 1) / kWaves);
+            first += d.blocks;
+        }
+    }
+    const int blocks = p.side[1].first_block + p.side[1].blocks;
+    if (grad)
+        qk_norm_kernel<T, W, true><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
+    else
+        qk_norm_kernel<T, W, false><<<blocks, kThreads, 0, s>>>(p, lanes, split);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && grad && (p.side[0].dweight || p.side[1].dweight)) {
+        qk_norm_join_kernel<<<dim3((p.dim + 31) / 32, 2), 1024, 0, s>>>(p);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename T>
+hipError_t launch_typed(NormParams &p, bool grad, hipStream_t s) {
+    const int rest = p.dim - 2 * p.half;
+    if (sizeof(T) == 2 && p.half % 8 == 0 && rest % 16 == 0) return launch<T, sizeof(T) == 2 ? 8 : 4>(p, grad, s);
+    if (p.half % 4 == 0) return launch<T, 4>(p, grad, s);
+    if (p.half % 2 == 0) return launch<T, 2>(p, grad, s);
+    return launch<T, 1>(p, grad, s);
+}
+
+}  // namespace
+
+// A gradient's blocks, of both sides and of the queries: as many as its rows'
+// bytes keep busy, at most kNormBlocks, shared by their rows.
+int qk_norm_grad_blocks(int64_t rows_q, int64_t rows_k, int32_t dim, int32_t *blocks_q) {
+    const double rows = (double)rows_q + (double)rows_k;
+    const double want = std::min((double)kNormBlocks, std::max(2.0, rows * dim / 4096.0));
+    int q = rows_q ? std::max(1, (int)(want * ((double)rows_q / rows))) : 0;
+    int k = rows_k ? std::max(1, (int)(want * ((double)rows_k / rows))) : 0;
+    *blocks_q = q;
+    return q + k;
+}
+
+hipError_t launch_qk_norm(NormParams &p, int dtype, bool grad, hipStream_t s) {
+    if (dtype == 2) return launch_typed<__bf16>(p, grad, s);
+    if (dtype == 1) return launch_typed<_Float16>(p, grad, s);
+    return launch_typed<float>(p, grad, s);
+}
+
+}  // namespace same

@@ -1,0 +1,113 @@
+// Internal interface between the entry points of a training step's operators
+// (step.cpp) and their gfx950 kernels (qk_norm.hip, log_probs*.hip,
+// orthogonalise*.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace same {
+
+// ---- norms of queries and keys with the position rotation
+
+constexpr int kMaxHeadDim = 128;
+constexpr int kNormBlocks = 1024;  // of a gradient: each leaves a part of the weights' gradient
+
+// Queries or keys.
+struct NormSide {
+    const void *x, *dout;
+    int64_t x_row, x_head, dout_row, dout_head;  // strides in elements
+    const float *weight;                         // null: ones
+    const int32_t *positions;
+    void *out;                                   // contiguous: the result, or dx
+    float *dweight;                              // null: not wanted
+    int64_t tokens;
+    int32_t heads;
+    int32_t first_block, blocks;                 // of the launch
+};
+
+struct NormParams {
+    NormSide side[2];
+    float *part;          // [blocks][head_dim]
+    int32_t dim, half;    // half: pairs that turn
+    float eps, inv_dim;
+    // turns a position of every pair, in two parts: far positions need more than 53 bits
+    double turn[kMaxHeadDim / 2], turn_low[kMaxHeadDim / 2];
+};
+
+hipError_t launch_qk_norm(NormParams &p, int dtype, bool grad, hipStream_t s);
+int qk_norm_grad_blocks(int64_t rows_q, int64_t rows_k, int32_t dim, int32_t *blocks_q);
+
+// ---- log probabilities of given states, with entropy and alternatives
+
+constexpr int kMaxTop = 64;
+constexpr int kMaxRowParts = 64;
+
+// A part of a row: its largest logit, and the sums of e^(x - max) and
+// (x - max) e^(x - max).
+struct RowStats {
+    float max, sum, weighted, pad;
+};
+
+struct LogProbsParams {
+    const void *x;
+    int64_t x_row, rows;
+    int32_t cols;
+    const int32_t *counts, *targets;   // null: cols; none asked for
+    float *log_probs;
+    float2 *sums;                      // largest logit, logarithm of the sum relative to it
+    float *entropy;
+    int32_t n_top;
+    int32_t *top_ids;
+    float *top_log_probs;
+    int32_t parts, part_cols;          // of a long row
+    RowStats *part_stats;              // [rows][parts]
+    uint64_t *part_keys;               // [rows][parts][n_top]
+};
+
+struct LogProbsGradParams {
+    const void *x;
+    void *dx;
+    int64_t x_row, dx_row, rows;
+    int32_t cols;
+    const int32_t *counts, *targets;
+    const float2 *sums;
+    const float *entropy, *dlog_probs, *dentropy;  // either gradient may be null
+};
+
+// Parts of a row, and the columns of each.
+void log_probs_parts(int64_t rows, int64_t cols, int32_t *parts, int32_t *part_cols);
+hipError_t launch_log_probs(const LogProbsParams &p, int dtype, hipStream_t s);
+hipError_t launch_log_probs_grad(const LogProbsGradParams &p, int dtype, hipStream_t s);
+
+// ---- orthogonalising an update by Newton-Schulz products
+
+constexpr int kMaxSteps = 32;
+
+// A plane pair holds numbers as the sum of two fp16, times a power of two.
+struct Planes {
+    _Float16 *hi, *lo;
+};
+
+struct OrthoParams {
+    const void *g;
+    void *out;
+    int64_t g_mat, g_row, out_mat, out_row, n_mats;
+    int32_t rows, cols;       // of g
+    int32_t n, m;             // the smaller and the larger of them
+    int32_t np, mp;           // padded
+    bool tall;                // rows > cols: X is g's transpose
+    float eps, out_scale;
+    float sx, sa, sb;         // the planes' powers of two
+    double *squares;          // [n_mats][kNormParts]
+    Planes x, xt[2], a, b;    // [n_mats] of [np][mp], [mp][np], [np][np], [np][np]
+    int32_t steps;
+    float coef[kMaxSteps][3];
+};
+
+constexpr int kNormParts = 64;
+
+int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp);
+hipError_t launch_orthogonalise(const OrthoParams &p, int dtype, hipStream_t s);
+
+}  // namespace same

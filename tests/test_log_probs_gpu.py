@@ -1,0 +1,375 @@
+"""Log probabilities of given states, entropy, alternatives and their gradient
+against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1511_06416_amd as same
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+U = 2.0 ** -24
+INF = float("inf")
+HALF = {t: torch.finfo(t).eps / 2 for t in TYPES}
+TINY = {torch.float32: 0.0, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}
+
+
+def matrix(rows, cols, dtype, seed=0, stride=None, scale=2.5):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(rows, stride or cols, generator=g) * scale).to(dtype).cuda()[:, :cols]
+
+
+class Reference:
+    """Values on the CPU in 64 bits with bounds on a 32-bit form's error.
+
+    d = x - m is off by U |d|, its exponent by 2 U |d| + 2^-22 (the product
+    with log2 e, the hardware's function), sums run over chains of at most 64,
+    exchanges and parts, 128 U in all.  With W and V the mean of |d| and d^2:
+    log s is off by U (2 W + 132) + 2^-22 (1 + log s)."""
+
+    def __init__(self, x, counts, targets):
+        x = x.cpu().double()
+        rows, cols = x.shape
+        n = torch.full((rows,), cols) if counts is None else counts.cpu().long().clamp(0, cols)
+        self.inside = torch.arange(cols)[None] < n[:, None]
+        x = x.masked_fill(~self.inside, -INF)
+        self.x, self.n = x, n
+        m = x.amax(1, keepdim=True) if cols else torch.full((rows, 1), -INF, dtype=torch.float64)
+        none = (m == -INF) & ~x.isnan().any(1, keepdim=True)
+        d = x - torch.where(none, 0.0, m)
+        e = d.exp()
+        s = e.sum(1, keepdim=True)
+        self.none, self.m, self.ls = none[:, 0], m, torch.where(none, 0.0, s.log())
+        far = torch.where(e > 0, d, 0.0) if cols else d
+        mean, square = (far.abs() * e).sum(1, keepdim=True) / s, (far * far * e).sum(1, keepdim=True) / s
+        mean, square = torch.where(none, 0.0, mean), torch.where(none, 0.0, square)
+        self.e_ls = U * (2 * mean + 132) + 2.0 ** -22 * (1 + self.ls.abs())
+        self.l = d - self.ls
+        self.p = torch.where(none, 0.0, self.l.exp())
+        self.h = torch.where(none, 0.0, self.ls + mean)[:, 0]
+        self.e_h = (self.e_ls + U * (2 * square + 136 * mean + 2 * mean * mean) + 2 * U * (self.ls + mean))[:, 0]
+        self.e_l = self.e_ls + 2 * U * (d.abs() + self.ls)
+        self.t = targets
+        if targets is not None:
+            t = targets.cpu().long()
+            hit = (t >= 0) & (t < n)
+            at = torch.where(hit, t, 0)[:, None]
+            lp, el = (self.l.gather(1, at)[:, 0], self.e_l.gather(1, at)[:, 0]) if cols else (self.h, self.h)
+            self.lp = torch.where(t < 0, 0.0, torch.where(hit & ~self.none, lp, -INF))
+            self.e_lp = torch.where(hit & (lp > -INF), el, 0.0)
+            self.one = (torch.arange(cols)[None] == t[:, None]) & hit[:, None]
+            self.asked = t >= 0
+
+    def top(self, k):
+        x = torch.where(self.x.isnan(), -INF, self.x)
+        order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+        # states first, in order; behind the count nothing
+        ids = torch.full((x.shape[0], k), -1, dtype=torch.int64)
+        lp = torch.full((x.shape[0], k), -INF, dtype=torch.float64)
+        err = torch.zeros_like(lp)
+        for r in range(x.shape[0]):
+            o = order[r][self.inside[r][order[r]]] if k <= int(self.n[r]) else torch.sort(
+                x[r, :int(self.n[r])], descending=True, stable=True).indices
+            ids[r, :len(o)] = o
+            lp[r, :len(o)] = -INF if self.none[r] else self.l[r, o]
+            err[r, :len(o)] = self.e_l[r, o]
+        return ids, lp, err
+
+    def grad(self, dl, dh):
+        l = torch.where(self.p > 0, self.l, 0.0)
+        dl = torch.zeros(len(self.n)) if dl is None else dl
+        dh = torch.zeros(len(self.n)) if dh is None else dh
+        dl, dh = torch.where(self.asked, dl.cpu().double(), 0.0)[:, None], dh.cpu().double()[:, None]
+        h, eh = self.h[:, None], self.e_h[:, None]
+        term = dl + dh * (l + h)
+        v = -self.p * term + self.one * dl * ~self.none[:, None]
+        el = torch.where(self.p > 0, self.e_l, 0.0)
+        # what lies below the normal numbers, 2^-126, is flushed to 0 by the hardware's exponential: off by that at most
+        ep = self.p * (el + 2 * U * l.abs() + 2.0 ** -21) + 2.0 ** -126
+        bound = ep * term.abs() + self.p * (dh.abs() * (el + eh + 2 * U * (l.abs() + h)) + 4 * U * (
+            dl.abs() + (dh * l).abs() + (dh * h).abs())) + 2 * U * (v.abs() + self.one * dl.abs())
+        return torch.where(self.inside, v, 0.0), torch.where(self.inside, bound, 0.0) + 1e-37
+
+
+def check(name, got, want, bound):
+    t = got.dtype
+    got = got.cpu().double()
+    if t != torch.float32:
+        bound = bound + HALF[t] * (want.abs() + bound) + TINY[t]
+    same_inf = (want.isinf() & (got == want)) | (want.isnan() & got.isnan())
+    bad = ~(same_inf | ((got - want).abs() <= bound))
+    assert not bad.any(), "%s: %d of %d off, first %s: %s for %s" % (
+        name, int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist(), got[bad][0], want[bad][0])
+
+
+def forward(x, targets, counts=None, top=0, wanted=True):
+    rows, cols = x.shape
+    nan = float("nan")
+    out = dict(log_probs=None if targets is None else torch.full((rows,), nan, device="cuda"),
+               sums=torch.full((rows, 2), nan, device="cuda"), entropy=torch.full((rows,), nan, device="cuda"))
+    if top:
+        out["top_ids"] = torch.full((rows, top), -7, dtype=torch.int32, device="cuda")
+        out["top_log_probs"] = torch.full((rows, top), nan, device="cuda")
+    ws = torch.full((max(1, same.same_log_probs_workspace_size(rows, cols, top)),), 255, dtype=torch.uint8, device="cuda")
+    lp = out.pop("log_probs")
+    same.same_log_probs(x, targets, lp, ws, counts=counts, **out)
+    return dict(out, log_probs=lp)
+
+
+def verify(x, targets, counts=None, top=0, dl=None, dh=None):
+    ref = Reference(x, counts, targets)
+    got = forward(x, targets, counts, top)
+    if targets is not None:
+        check("log_probs", got["log_probs"], ref.lp, ref.e_lp)
+    check("entropy", got["entropy"], ref.h, ref.e_h)
+    check("sums", got["sums"], torch.cat([ref.m, ref.ls], 1), torch.cat([0 * ref.e_ls, ref.e_ls], 1))
+    if top:
+        ids, lp, err = ref.top(top)
+        assert torch.equal(got["top_ids"].cpu().long(), ids)
+        check("top_log_probs", got["top_log_probs"], lp, err)
+    if targets is not None:
+        dx = torch.full_like(x, float("nan"))
+        same.same_log_probs_backward(x, targets, got["sums"], dx, counts=counts, entropy=got["entropy"], dlog_probs=dl,
+                                     dentropy=dh)
+        check("dlogits", dx, *ref.grad(dl, dh))
+    return got
+
+
+def random_rows(rows, cols, seed, ragged):
+    g = torch.Generator().manual_seed(seed)
+    counts = torch.randint(0, cols + 1, (rows,), generator=g, dtype=torch.int32).cuda() if ragged else None
+    targets = torch.randint(-1, cols, (rows,), generator=g, dtype=torch.int32).cuda()
+    return counts, targets, torch.randn(rows, generator=g).cuda(), torch.randn(rows, generator=g).cuda()
+
+
+SHAPES = [(1, 1, 1), (5, 2, 2), (300, 2, 1), (33, 3, 3), (257, 8, 2), (70, 13, 20), (9, 64, 64), (5, 65, 64), (130, 100, 5),
+          (4, 300, 40), (3, 511, 20), (6, 513, 0), (7, 2047, 20), (3, 2049, 64), (2, 8191, 1), (2, 9000, 20), (1, 32767, 20),
+          (2, 32768, 64), (2, 32769, 20), (3, 70_001, 64), (1, 300_003, 20)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("rows,cols,top", SHAPES)
+def test_values(rows, cols, top, ragged, dtype):
+    counts, targets, dl, dh = random_rows(rows, cols, rows + cols, ragged)
+    verify(matrix(rows, cols, dtype, cols, cols + rows % 3), targets, counts, top, dl, dh)
+
+
+@pytest.mark.parametrize("cols", [4, 40, 700, 40_000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ties_masks_and_empty_rows(cols, dtype):
+    """Equal logits, -inf among and throughout, the type's lowest, huge ones,
+    both zeros, steps in rising and falling order; targets on -inf and behind
+    the count; counts of 0, 1, all, more and less than there are."""
+    low = torch.finfo(dtype).min
+    x = matrix(16, cols, dtype, 1).cpu()
+    x[0] = 0.5
+    x[1] = -INF
+    x[2, 1:] = -INF
+    x[3] = low
+    x[4, ::2] = low
+    x[5, ::2] = -INF
+    x[6] = torch.tensor([0.0, -0.0]).repeat(cols)[:cols]
+    x[7] = (torch.arange(cols) % 7).to(dtype)
+    x[8] = -(torch.arange(cols).float() / 8).to(dtype)
+    x[9] = (torch.arange(cols).float() / 8).to(dtype)
+    x[10] = 30_000.0
+    x[10, cols // 2] = 30_016.0 if dtype != torch.bfloat16 else 30_080.0
+    x[11, :] = -30_000.0
+    counts = torch.full((16,), cols, dtype=torch.int32)
+    counts[12], counts[13], counts[14], counts[15] = 0, 1, cols + 5, -3
+    targets = torch.arange(16, dtype=torch.int32) % cols
+    targets[1] = targets[2] = 1
+    targets[13] = 3
+    targets[8] = cols + 2
+    top = min(cols, 20)
+    dl, dh = torch.linspace(-1, 1, 16).cuda(), torch.linspace(2, -1, 16).cuda()
+    got = verify(x.cuda(), targets.cuda(), counts.cuda(), top, dl, dh)
+    assert got["top_ids"][0].tolist() == list(range(top)) and got["top_ids"][6].tolist() == list(range(top))
+    assert got["log_probs"][1] == -INF and got["log_probs"][13] == -INF and got["entropy"][12] == 0
+
+
+@pytest.mark.parametrize("cols", [5, 300, 5000, 40_000])
+def test_missing_and_infinite_logits(cols):
+    x = matrix(4, cols, torch.float32, 3)
+    x[0, 2] = float("nan")
+    x[1, 3] = INF
+    x[2, :] = float("nan")
+    targets = torch.tensor([0, 3, 1, 4], dtype=torch.int32, device="cuda")
+    got = forward(x, targets, None, 3)
+    assert bool(got["log_probs"][:3].isnan().all()) and bool(got["entropy"][:3].isnan().all())
+    ref = Reference(x[3:], None, targets[3:])
+    check("row 3", got["log_probs"][3:], ref.lp, ref.e_lp)
+    order = torch.sort(x[0].cpu().nan_to_num(nan=-INF), descending=True, stable=True).indices[:3]
+    assert got["top_ids"][0].tolist() == order.tolist()
+    assert got["top_ids"][1, 0] == 3 and got["top_ids"][2].tolist() == [0, 1, 2]
+    dx = torch.zeros_like(x)
+    one = torch.ones(4, device="cuda")
+    same.same_log_probs_backward(x, targets, got["sums"], dx, entropy=got["entropy"], dlog_probs=one, dentropy=one)
+    assert bool(dx[0].isnan().all()) and bool(dx[2].isnan().all()) and bool(dx[3].isfinite().all())
+
+
+def test_gradient_against_differences():
+    x = matrix(3, 7, torch.float32, 5)
+    counts = torch.tensor([7, 4, 2], dtype=torch.int32, device="cuda")
+    targets = torch.tensor([6, 0, -1], dtype=torch.int32, device="cuda")
+    dl, dh = torch.tensor([1.5, -0.5, 2.0]).cuda(), torch.tensor([0.3, -2.0, 1.0]).cuda()
+    got = forward(x, targets, counts)
+    dx = torch.empty_like(x)
+    same.same_log_probs_backward(x, targets, got["sums"], dx, counts=counts, entropy=got["entropy"], dlog_probs=dl, dentropy=dh)
+
+    def loss(x):
+        r = Reference(x, counts, targets)
+        return float((r.lp * dl.cpu().double() + r.h * dh.cpu().double()).sum())
+
+    h = 1e-5
+    for r in range(3):
+        for c in range(7):
+            e = torch.zeros(3, 7, dtype=torch.float64)
+            e[r, c] = h
+            slope = (loss(x.cpu().double() + e) - loss(x.cpu().double() - e)) / (2 * h)
+            assert abs(slope - float(dx[r, c])) < 1e-6 * 10
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols,stride,offset", [(13, 13, 1), (100, 107, 3), (5000, 5001, 1), (8, 16, 0), (40_000, 40_003, 5)])
+def test_strides_and_what_lies_between(cols, stride, offset, dtype):
+    rows = 7
+    buf = matrix(1, rows * stride + offset, dtype, 2)[0]
+    x = buf[offset:].view(rows, stride)[:, :cols]
+    _, targets, dl, dh = random_rows(rows, cols, 1, False)
+    want, got = forward(x.contiguous(), targets, None, 5), forward(x, targets, None, 5)
+    assert all(torch.equal(want[k], got[k]) for k in want)
+    grads = torch.full((rows * stride + offset,), 3.0, dtype=dtype, device="cuda")
+    dx = grads[offset:].view(rows, stride)[:, :cols]
+    flat = torch.empty(rows, cols, dtype=dtype, device="cuda")
+    kw = dict(entropy=got["entropy"], dlog_probs=dl, dentropy=dh)
+    same.same_log_probs_backward(x, targets, got["sums"], dx, **kw)
+    same.same_log_probs_backward(x.contiguous(), targets, got["sums"], flat, **kw)
+    assert torch.equal(dx, flat)
+    assert bool((grads[offset:].view(rows, stride)[:, cols:] == 3).all()) and bool((grads[:offset] == 3).all())
+    # in place, and one row repeated
+    y = x.contiguous()
+    same.same_log_probs_backward(y, targets, got["sums"], y, **kw)
+    assert torch.equal(y, flat)
+    one = x[:1].expand(rows, cols)
+    a, b = forward(one, targets, None, 2), forward(one.contiguous(), targets, None, 2)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+@pytest.mark.parametrize("rows,cols", [(50, 8), (20, 3000), (3, 50_000)])
+def test_parts_of_the_outputs(rows, cols):
+    """Each output alone, and each gradient alone."""
+    x = matrix(rows, cols, torch.bfloat16, 2)
+    counts, targets, dl, dh = random_rows(rows, cols, 2, True)
+    full = forward(x, targets, counts, 4)
+    ws = torch.empty(max(1, same.same_log_probs_workspace_size(rows, cols, 4)), dtype=torch.uint8, device="cuda")
+    lp = torch.empty(rows, device="cuda")
+    same.same_log_probs(x, targets, lp, ws, counts=counts)
+    assert torch.equal(lp, full["log_probs"])
+    ent, ids, tl = torch.empty(rows, device="cuda"), torch.empty_like(full["top_ids"]), torch.empty_like(full["top_log_probs"])
+    same.same_log_probs(x, None, None, ws, counts=counts, entropy=ent, top_ids=ids, top_log_probs=tl)
+    assert torch.equal(ent, full["entropy"]) and torch.equal(ids, full["top_ids"]) and torch.equal(tl, full["top_log_probs"])
+    verify(x, targets, counts, 0, dl, None)
+    verify(x, targets, counts, 0, None, dh)
+
+
+def test_many_rows_and_far_offsets():
+    """Rows past 2^31 elements."""
+    rows, cols = 36, 1 << 26
+    x = torch.zeros(rows, cols, dtype=torch.float16, device="cuda")[:, :1000]
+    x.copy_(matrix(rows, 1000, torch.float16, 3))
+    _, targets, dl, dh = random_rows(rows, 1000, 3, False)
+    a, b = forward(x, targets, None, 3), forward(x.contiguous(), targets, None, 3)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+    kw = dict(entropy=a["entropy"], dlog_probs=dl, dentropy=dh)
+    flat = torch.empty(rows, 1000, dtype=torch.float16, device="cuda")
+    same.same_log_probs_backward(x.contiguous(), targets, a["sums"], flat, **kw)
+    same.same_log_probs_backward(x, targets, a["sums"], x, **kw)
+    assert torch.equal(x, flat)
+
+
+def test_more_rows_than_a_launch_takes():
+    rows = (1 << 21) * 256 + 300
+    x = torch.zeros(rows, 1, dtype=torch.float16, device="cuda")
+    x[-1] = 3
+    targets = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    lp, sums = torch.full((rows,), 5.0, device="cuda"), torch.full((rows, 2), 5.0, device="cuda")
+    same.same_log_probs(x, targets, lp, None, sums=sums)
+    assert not lp.any() and sums[-1].tolist() == [3.0, 0.0] and sums[-302].tolist() == [0.0, 0.0]
+    dx = torch.full_like(x, 7)
+    same.same_log_probs_backward(x, targets, sums, dx, dlog_probs=torch.ones(rows, device="cuda"))
+    assert not dx.any()
+
+
+def test_streams_graphs_and_repeats():
+    x = matrix(40, 40_000, torch.bfloat16, 1)
+    _, targets, dl, dh = random_rows(40, 40_000, 1, False)
+    out = forward(x, targets, None, 20)
+    dx = torch.empty_like(x)
+    ws = torch.empty(same.same_log_probs_workspace_size(40, 40_000, 20), dtype=torch.uint8, device="cuda")
+    lp = out.pop("log_probs")
+
+    def both():
+        same.same_log_probs(x, targets, lp, ws, **out)
+        same.same_log_probs_backward(x, targets, out["sums"], dx, entropy=out["entropy"], dlog_probs=dl, dentropy=dh)
+
+    both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for seed in (5, 6, 5):
+        x.copy_(matrix(40, 40_000, torch.bfloat16, seed))
+        for o in (lp, dx, *out.values()):
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in (lp, dx, *out.values())]
+        both()
+        assert all(torch.equal(a, b) for a, b in zip(got, (lp, dx, *out.values())))
+
+
+def test_refusals():
+    x = matrix(4, 100, torch.float16)
+    t, f = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    ids, tl = torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda")
+    ok = dict(logits=x, targets=t, log_probs=f, workspace=None, top_ids=ids, top_log_probs=tl)
+
+    def refuse(code=same.SAME_EINVAL, **kw):
+        with pytest.raises(same.SameError) as e:
+            same.same_log_probs(**dict(ok, **kw))
+        assert e.value.code == code and str(e.value)
+
+    refuse(logits=x.cpu())
+    refuse(logits=x.double())
+    refuse(logits=x[0])
+    refuse(logits=x.T.contiguous().T)
+    refuse(targets=t.long())
+    refuse(targets=t[:3])
+    refuse(targets=None)
+    refuse(counts=t.long())
+    refuse(log_probs=f.half())
+    refuse(log_probs=torch.zeros(8, device="cuda")[::2])
+    refuse(sums=f)
+    refuse(top_ids=None)
+    refuse(top_ids=torch.zeros(4, 65, dtype=torch.int32, device="cuda"), top_log_probs=torch.zeros(4, 65, device="cuda"))
+    refuse(top_log_probs=tl[:, :2])
+    refuse(entropy=f)
+    refuse(logits=matrix(4, 40_000, torch.float16))
+    refuse(same.SAME_ESIZE, logits=torch.zeros(1, (1 << 21) + 1, dtype=torch.float16, device="cuda").expand(4, -1))
+    same.same_log_probs(**ok)
+    s = torch.zeros(4, 2, device="cuda")
+
+    def refuse_grad(**kw):
+        with pytest.raises(same.SameError) as e:
+            same.same_log_probs_backward(**dict(dict(logits=x, targets=t, sums=s, dlogits=torch.zeros_like(x), dlog_probs=f), **kw))
+        assert e.value.code == same.SAME_EINVAL and str(e.value)
+
+    refuse_grad(sums=None)
+    refuse_grad(targets=None)
+    refuse_grad(dentropy=f)
+    refuse_grad(dlogits=x[:3])
+    refuse_grad(dlogits=x[:1].expand(4, 100))
+    refuse_grad(dlogits=x.float())
+    buf = matrix(5, 100, torch.float16)
+    refuse_grad(logits=buf[:4], dlogits=buf[1:])
