@@ -277,19 +277,20 @@ hipError_t run_typed(const OrthoParams &p, hipStream_t s) {
 
 }  // namespace
 
-// Matrices that share the workspace's planes: some 2^28 elements.
+// Some 2^28 elements of a plane.
 int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp) {
     return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(n_mats, 16384), ((int64_t)1 << 28) / (np * mp)));
 }
 
-hipError_t launch_orthogonalise(const OrthoParams &all, int dtype, hipStream_t s) {
-    const int64_t batch = orthogonalise_batch(all.n_mats, all.np, all.mp), size = dtype == 0 ? 4 : 2;
+hipError_t launch_orthogonalise(const OrthoParams &all, int64_t batch, int dtype, hipStream_t s) {
+    const int64_t size = dtype == 0 ? 4 : 2;
     for (int64_t first = 0; first < all.n_mats; first += batch) {
         OrthoParams p = all;
         p.n_mats = std::min(batch, all.n_mats - first);
         p.g = (const char *)all.g + first * all.g_mat * size;
         p.out = (char *)all.out + first * all.out_mat * size;
-        const hipError_t e = dtype == 2   ? run_typed<__bf16, 1>(p, s)
+        const hipError_t e = p.n <= kSmallSide ? launch_ortho_small(p, dtype, s)
+                             : dtype == 2 ? run_typed<__bf16, 1>(p, s)
                              : dtype == 1 ? run_typed<_Float16, 3>(p, s)
                                           : run_typed<float, 3>(p, s);
         if (e != hipSuccess) return e;

@@ -179,6 +179,8 @@ void log_probs_layout(int64_t rows, int64_t cols, int32_t n_top, int32_t *parts,
 struct OrthoLayout {
     int64_t n, m, np, mp, batch;
     size_t squares, wide, square, total;  // bytes of the sums and of one plane of each shape
+    int32_t parts, part_cols;             // small updates: tiles of their parts, and of their factors
+    size_t small_parts, small_factors;
 };
 
 int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, OrthoLayout &l) {
@@ -193,6 +195,15 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
         return record_error(SAME_ESIZE, "a matrix has at most 2^15 by 2^24 and 1.1 10^9 elements");
     if (n_mats >= (int64_t)1 << 40 || (double)n_mats * (double)rows * (double)cols >= 1e15)
         return record_error(SAME_ESIZE, "the matrices pass 10^15 elements");
+    if (l.n <= same::kSmallSide) {
+        size_t tiles = 0;
+        same::ortho_small_parts(l.n, l.m, &l.parts, &l.part_cols, &tiles);
+        l.batch = l.n ? std::min<int64_t>(n_mats, ((int64_t)1 << (l.parts > 1 ? 17 : 22)) / l.parts) : 0;
+        l.small_parts = l.parts > 1 ? align_up((size_t)l.batch * l.parts * tiles) : 0;
+        l.small_factors = l.parts > 1 ? align_up((size_t)l.batch * tiles) : 0;
+        l.total = l.small_parts + l.small_factors;
+        return SAME_OK;
+    }
     const int64_t pad = l.n <= 64 ? 64 : 128;
     l.np = (l.n + pad - 1) / pad * pad;
     l.mp = (l.m + pad - 1) / pad * pad;
@@ -422,7 +433,7 @@ int same_log_probs_backward(int32_t dtype, const void *logits, int64_t row_strid
 
 int same_orthogonalise_workspace_size(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, size_t *bytes) {
     if (!bytes) return record_error(SAME_EINVAL, "bytes is null");
-    OrthoLayout l;
+    OrthoLayout l{};
     const int rc = ortho_layout(dtype, n_mats, rows, cols, l);
     if (rc) return rc;
     *bytes = l.batch ? l.total : 0;
@@ -433,7 +444,7 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
                        int64_t cols, const double *coefs, int32_t steps, double eps, double scale, void *out,
                        int64_t out_mat, int64_t out_row, void *workspace, void *stream) {
     return guarded([&]() -> int {
-        OrthoLayout l;
+        OrthoLayout l{};
         int rc = ortho_layout(dtype, n_mats, rows, cols, l);
         if (rc) return rc;
         if (!coefs) return record_error(SAME_EINVAL, "coefs is null");
@@ -472,7 +483,7 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
         const double far = (double)(n_mats - 1) * (double)std::max(g_mat, out_mat) +
                            (double)(rows - 1) * (double)std::max(g_row, out_row);
         if (far >= 1e18) return record_error(SAME_ESIZE, "strides pass 10^18 elements");
-        if (!workspace) return record_error(SAME_EINVAL, "workspace is null");
+        if (l.total && !workspace) return record_error(SAME_EINVAL, "workspace is null");
         if (!aligned(workspace, kAlign)) return record_error(SAME_EALIGN, "workspace must be 256-byte aligned");
         const Extent eg = extent(g, size * ((n_mats - 1) * g_mat + (rows - 1) * g_row + cols));
         const Extent eo = extent(out, size * ((n_mats - 1) * out_mat + (rows - 1) * out_row + cols));
@@ -503,6 +514,10 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
         p.sa = plane_scale(most * most, 13);
         p.sb = plane_scale(product, 10);
         p.steps = steps;
+        p.parts = l.parts;
+        p.part_cols = l.part_cols;
+        p.small_parts = workspace;
+        p.small_factors = (char *)workspace + l.small_parts;
         char *at = (char *)workspace;
         const auto take = [&](size_t bytes) {
             char *here = at;
@@ -518,7 +533,7 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
             w->hi = (_Float16 *)take(l.square);
             w->lo = (_Float16 *)take(l.square);
         }
-        return check_hip(same::launch_orthogonalise(p, dtype, (hipStream_t)stream), "orthogonalise launch");
+        return check_hip(same::launch_orthogonalise(p, l.batch, dtype, (hipStream_t)stream), "orthogonalise launch");
     });
 }
 

@@ -101,13 +101,21 @@ struct OrthoParams {
     float sx, sa, sb;         // the planes' powers of two
     double *squares;          // [n_mats][kNormParts]
     Planes x, xt[2], a, b;    // [n_mats] of [np][mp], [mp][np], [np][np], [np][np]
+    int32_t parts, part_cols; // of a small update's columns
+    void *small_parts, *small_factors;  // [n_mats][parts] and [n_mats] sets of tiles
     int32_t steps;
     float coef[kMaxSteps][3];
 };
 
 constexpr int kNormParts = 64;
 
+constexpr int kSmallSide = 32;  // of updates that take the small kernels
+
+void ortho_small_parts(int64_t n, int64_t m, int32_t *parts, int32_t *part_cols, size_t *tile_bytes);
+hipError_t launch_ortho_small(const OrthoParams &p, int dtype, hipStream_t s);
+
+// Matrices that share the planes (or tiles) of the workspace, in turn.
 int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp);
-hipError_t launch_orthogonalise(const OrthoParams &p, int dtype, hipStream_t s);
+hipError_t launch_orthogonalise(const OrthoParams &p, int64_t batch, int dtype, hipStream_t s);
 
 }  // namespace same

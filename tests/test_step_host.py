@@ -100,8 +100,8 @@ def test_nothing_to_do(lib):
 
 def ortho_rc(lib, **kw):
     coefs = np.ascontiguousarray(kw.pop("coefs", same.NEWTON_SCHULZ), dtype=np.float64)
-    a = dict(dict(dtype=same.SAME_F32, g=A, g_mat=96, g_row=12, n_mats=2, rows=8, cols=12, coefs=coefs.ctypes.data,
-                  steps=len(coefs), eps=1e-7, scale=1.0, out=A << 1, out_mat=96, out_row=12, workspace=A << 2), **kw)
+    a = dict(dict(dtype=same.SAME_F32, g=A, g_mat=2000, g_row=50, n_mats=2, rows=40, cols=50, coefs=coefs.ctypes.data,
+                  steps=len(coefs), eps=1e-7, scale=1.0, out=A << 1, out_mat=2000, out_row=50, workspace=A << 2), **kw)
     return lib.same_orthogonalise(*a.values(), None)
 
 
@@ -113,7 +113,7 @@ def ortho_rc(lib, **kw):
     (same.SAME_EINVAL, dict(coefs=[(3.0, 0.0, 0.0)] * 3)), (same.SAME_EINVAL, dict(steps=0)), (same.SAME_EINVAL, dict(steps=33)),
     (same.SAME_EINVAL, dict(eps=0.0)), (same.SAME_EINVAL, dict(eps=np.inf)), (same.SAME_EINVAL, dict(scale=1e39)),
     (same.SAME_EINVAL, dict(g=None)), (same.SAME_EINVAL, dict(out=None)), (same.SAME_EALIGN, dict(g=A + 2)),
-    (same.SAME_EINVAL, dict(g_row=-1)), (same.SAME_EINVAL, dict(out_row=11)), (same.SAME_EINVAL, dict(out_mat=95)),
+    (same.SAME_EINVAL, dict(g_row=-1)), (same.SAME_EINVAL, dict(out_row=49)), (same.SAME_EINVAL, dict(out_mat=1999)),
     (same.SAME_ESIZE, dict(g_mat=1 << 61)), (same.SAME_EINVAL, dict(workspace=None)), (same.SAME_EALIGN, dict(workspace=A + 64)),
     (same.SAME_EINVAL, dict(out=A + 4)), (same.SAME_EINVAL, dict(workspace=A)), (same.SAME_EINVAL, dict(out=A << 2)),
     (same.SAME_EINVAL, dict(out=A, workspace=A)),
