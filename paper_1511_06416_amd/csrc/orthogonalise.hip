@@ -20,87 +20,161 @@
 namespace same {
 namespace {
 
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
 constexpr int kStage = 32;  // columns of a stage
+constexpr int kTurn = 36;   // floats of a row of a tile that is turned
 
 __device__ __forceinline__ void split(float v, _Float16 &hi, _Float16 &lo) {
     hi = (_Float16)v;
     lo = (_Float16)(v - (float)hi);
 }
 
-template <typename T>
-__device__ __forceinline__ float read(const OrthoParams &p, int64_t mat, int i, int j) {  // X's element
-    return (float)((const T *)p.g)[mat * p.g_mat + (p.tall ? j * p.g_row + i : i * p.g_row + j)];
-}
-
-// Parts of the sums of squares, in 64 bits: no update is too large or small.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void ortho_squares_kernel(OrthoParams p) {
+// Sums over a block, in every thread.
+__device__ __forceinline__ double block_sum(double t) {
     __shared__ double sums[kThreads / 64];
-    const int64_t mat = blockIdx.y, n = (int64_t)p.rows * p.cols;
-    double t = 0.0;
-    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n; e += (int64_t)gridDim.x * kThreads) {
-        const int64_t i = e / p.cols, j = e - i * p.cols;
-        const double v = (double)(float)((const T *)p.g)[mat * p.g_mat + i * p.g_row + j];
-        t = __builtin_fma(v, v, t);
-    }
     for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = t;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        t = 0.0;
-        for (int w = 0; w < kThreads / 64; ++w) t += sums[w];
-        p.squares[mat * kNormParts + blockIdx.x] = t;
+    t = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) t += sums[w];
+    return t;
+}
+
+// Parts of the sums of squares, in 64 bits: no update is too large or small.
+// A block takes stretches of rows, eight elements a thread.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void ortho_squares_kernel(OrthoParams p, int parts, int across) {
+    const int64_t mat = blockIdx.x / parts;
+    const int part = (int)(blockIdx.x - mat * parts), items = p.rows * across;
+    double t = 0.0;
+    for (int item = part; item < items; item += parts) {
+        const int i = item / across, j = ((item - i * across) * kThreads + threadIdx.x) * 8;
+        const T *src = (const T *)p.g + mat * p.g_mat + i * p.g_row + j;
+        if (j + 8 <= p.cols) {
+            const wave::Loose<T, 8> v = *(const wave::Loose<T, 8> *)src;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t = __builtin_fma((double)(float)v.v[e], (double)(float)v.v[e], t);
+        } else {
+            for (int e = 0; j + e < p.cols; ++e) t = __builtin_fma((double)(float)src[e], (double)(float)src[e], t);
+        }
     }
+    t = block_sum(t);
+    if (threadIdx.x == 0) p.squares[mat * kNormParts + part] = t;
 }
 
 // X in planes, both ways, zeros around it: a block takes 64 x 64.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, int parts) {
+template <typename T, bool LOW>
+__global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, int parts, int tiles_i, int tiles_j) {
     __shared__ float tile[64][65];
-    const int64_t mat = blockIdx.z;
+    const int tiles = tiles_i * tiles_j;
+    const int64_t mat = blockIdx.x / tiles;
+    const int at = (int)(blockIdx.x - mat * tiles);
     double total = 0.0;
-    for (int i = 0; i < parts; ++i) total += p.squares[mat * kNormParts + i];
+    for (int i = threadIdx.x; i < parts; i += kThreads) total += p.squares[mat * kNormParts + i];
+    total = block_sum(total);
     const float factor = (float)((double)p.sx / (__builtin_sqrt(total) + (double)p.eps));
-    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    const int c = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < 64; r += kThreads / 64) {
+    const int i0 = at % tiles_i * 64, j0 = at / tiles_i * 64;
+    const T *g = (const T *)p.g + mat * p.g_mat;
+    const int c = 8 * (threadIdx.x & 7);
+#pragma unroll
+    for (int r = threadIdx.x >> 3; r < 64; r += kThreads / 8) {
         // along g's rows
-        const int i = p.tall ? i0 + c : i0 + r, j = p.tall ? j0 + r : j0 + c;
-        const float v = i < p.n && j < p.m ? read<T>(p, mat, i, j) * factor : 0.0f;
-        tile[p.tall ? c : r][p.tall ? r : c] = v;
+        const int i = p.tall ? j0 + r : i0 + r, j = (p.tall ? i0 : j0) + c;
+        const T *src = g + i * p.g_row + j;
+        float v[8];
+        if (i < p.rows && j + 8 <= p.cols) {
+            const wave::Loose<T, 8> l = *(const wave::Loose<T, 8> *)src;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)l.v[e] * factor;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = i < p.rows && j + e < p.cols ? (float)src[e] * factor : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (p.tall)
+                tile[c + e][r] = v[e];
+            else
+                tile[r][c + e] = v[e];
+        }
     }
     __syncthreads();
     const int64_t x0 = mat * p.np * p.mp;
-    for (int r = threadIdx.x >> 6; r < 64; r += kThreads / 64) {
-        _Float16 hi, lo;
-        split(tile[r][c], hi, lo);
-        const int64_t at = x0 + (int64_t)(i0 + r) * p.mp + j0 + c;
-        p.x.hi[at] = hi;
-        p.x.lo[at] = lo;
-        split(tile[c][r], hi, lo);
-        const int64_t back = x0 + (int64_t)(j0 + r) * p.np + i0 + c;
-        p.xt[0].hi[back] = hi;
-        p.xt[0].lo[back] = lo;
+#pragma unroll
+    for (int r = threadIdx.x >> 3; r < 64; r += kThreads / 8) {
+        f16x8 hi, lo;
+        auto halves = [&](int e, float v) {
+            _Float16 h, l;
+            split(v, h, l);
+            hi[e] = h;
+            lo[e] = l;
+        };
+        if (i0 + r < p.np && j0 + c < p.mp) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) halves(e, tile[r][c + e]);
+            const int64_t to = x0 + (int64_t)(i0 + r) * p.mp + j0 + c;
+            *(f16x8 *)(p.x.hi + to) = hi;
+            if (LOW) *(f16x8 *)(p.x.lo + to) = lo;
+        }
+        if (j0 + r < p.mp && i0 + c < p.np) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) halves(e, tile[c + e][r]);
+            const int64_t to = x0 + (int64_t)(j0 + r) * p.np + i0 + c;
+            *(f16x8 *)(p.xt[0].hi + to) = hi;
+            *(f16x8 *)(p.xt[0].lo + to) = lo;
+        }
+    }
+}
+
+// Eight numbers of a row of out.
+template <typename T>
+__device__ __forceinline__ void write_out(const OrthoParams &p, int64_t mat, int row, int rows, int col, int cols,
+                                          const f32x4 (&v)[2]) {
+    if (row >= rows) return;
+    T *dst = (T *)p.out + mat * p.out_mat + row * p.out_row + col;
+    const float scale = p.out_scale / p.sx;
+    wave::Loose<T, 8> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = (T)(v[e >> 2][e & 3] * scale);
+    if (col + 8 <= cols) {
+        *(wave::Loose<T, 8> *)dst = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (col + e < cols) dst[e] = o.v[e];
     }
 }
 
 enum Kind { kGram, kSquare, kUpdate, kLast };
 
-// C[i][j] = sum_k P[i][k] Q[j][k] over a square tile, WM x WN waves, operands
-// staged in LDS: rows of 64 bytes, whose 16-byte chunks are turned by the row
-// so that a read of 32 rows meets no bank twice.
-template <typename T, int TILE, int WM, int WN, int PROD, int KIND>
+// Waits until at most N of the wave's loads are under way, then for the other
+// waves.  A barrier alone does not wait for loads into LDS.
+template <int N>
+__device__ __forceinline__ void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// C[i][j] = sum_k P[i][k] Q[j][k] over a TM x TN tile by WM x WN waves.
+// Operands come straight into LDS, STAGES stages of 32 columns in turn, all but
+// one under way; rows of 64 bytes, whose 16-byte chunks are turned by the row
+// so that a read of 32 rows meets no bank twice.  Rows past the matrix repeat
+// its last one and are not written.
+template <typename T, int TM, int TN, int WM, int WN, int STAGES, int PROD, int KIND>
 __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams p, int step, int tiles_i, int tiles_j) {
-    constexpr int MT = TILE / WM / 32, NT = TILE / WN / 32, PL = PROD == 1 ? 1 : 2;
-    constexpr int kPlane = TILE * kStage;                 // elements of a staged plane
-    constexpr int kLoads = TILE * 4 / (WM * WN * 64);     // 16-byte loads a lane, per plane
-    static_assert(kLoads >= 1 && kLoads * WM * WN * 64 == TILE * 4, "every lane stages the same");
-    __shared__ _Float16 stage[2][2 * PL][kPlane];
+    constexpr int THREADS = WM * WN * 64, MT = TM / WM / 32, NT = TN / WN / 32, PL = PROD == 1 ? 1 : 2;
+    constexpr int kLoadsP = TM * 4 / THREADS, kLoadsQ = TN * 4 / THREADS;   // 16-byte loads a lane, per plane
+    constexpr int kLoads = PL * (kLoadsP + kLoadsQ), kRows = PL * (TM + TN);
+    static_assert(kLoadsP * THREADS == TM * 4 && kLoadsQ * THREADS == TN * 4, "every lane stages the same");
+    static_assert(MT * WM * 32 == TM && NT * WN * 32 == TN, "whole tiles a wave");
+    static_assert(WM * WN * 32 * kTurn * 4 <= STAGES * kRows * kStage * 2, "tiles are turned where operands were");
+    __shared__ _Float16 stage[STAGES][kRows * kStage];
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6;
     int ti, tj;
     if (KIND == kGram || KIND == kSquare) {
@@ -116,29 +190,39 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     const int64_t mat = blockIdx.y;
     const int64_t x0 = mat * p.np * p.mp, a0 = mat * p.np * p.np;
     const int ld = KIND == kGram ? p.mp : p.np, depth = ld;
+    const int rows_j = KIND == kGram || KIND == kSquare ? p.np : p.mp;
     const Planes from = p.xt[step & 1], to = p.xt[(step & 1) ^ 1];
     const Planes left = KIND == kGram ? p.x : KIND == kSquare ? p.a : p.b;
     const Planes right = KIND == kGram ? p.x : KIND == kSquare ? p.a : from;
-    const int64_t l0 = (KIND == kGram ? x0 : a0) + (int64_t)ti * TILE * ld;
-    const int64_t r0 = (KIND == kSquare ? a0 : x0) + (int64_t)tj * TILE * ld;
-    const _Float16 *src[2 * PL];
-    src[0] = left.hi + l0;
-    src[PL] = right.hi + r0;
-    if (PL == 2) {
-        src[1] = left.lo + l0;
-        src[PL + 1] = right.lo + r0;
+    const int64_t l0 = KIND == kGram ? x0 : a0, r0 = KIND == kSquare ? a0 : x0;
+    // what this lane stages: offsets of its chunks
+    int off_p[kLoadsP], off_q[kLoadsQ];
+#pragma unroll
+    for (int l = 0; l < kLoadsP; ++l) {
+        const int slot = (own * kLoadsP + l) * 64 + lane, row = slot >> 2;
+        off_p[l] = min(ti * TM + row, p.np - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8;
     }
+#pragma unroll
+    for (int l = 0; l < kLoadsQ; ++l) {
+        const int slot = (own * kLoadsQ + l) * 64 + lane, row = slot >> 2;
+        off_q[l] = min(tj * TN + row, rows_j - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8;
+    }
+    auto load = [&](const _Float16 *src, _Float16 *dst) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                         (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+    };
     auto fetch = [&](int buffer, int k) {
+        _Float16 *to_p = &stage[buffer][own * kLoadsP * 512], *to_q = &stage[buffer][PL * TM * kStage + own * kLoadsQ * 512];
 #pragma unroll
-        for (int s = 0; s < 2 * PL; ++s)
+        for (int l = 0; l < kLoadsP; ++l) {
+            load(left.hi + l0 + k + off_p[l], to_p + l * 512);
+            if (PL == 2) load(left.lo + l0 + k + off_p[l], to_p + TM * kStage + l * 512);
+        }
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                const int slot = (own * kLoads + l) * 64 + lane, row = slot >> 2;
-                const int chunk = (slot & 3) ^ ((row >> 1) & 3);
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)(src[s] + (int64_t)row * ld + k + chunk * 8),
-                    (__attribute__((address_space(3))) void *)&stage[buffer][s][(own * kLoads + l) * 512], 16, 0, 0);
-            }
+        for (int l = 0; l < kLoadsQ; ++l) {
+            load(right.hi + r0 + k + off_q[l], to_q + l * 512);
+            if (PL == 2) load(right.lo + r0 + k + off_q[l], to_q + TN * kStage + l * 512);
+        }
     };
     f32x16 acc[MT][NT];
 #pragma unroll
@@ -147,28 +231,32 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const int wi = (own % WM) * (TILE / WM), wj = (own / WM) * (TILE / WN);
-    auto operand = [&](int buffer, int s, int row, int t) {
-        return *(const f16x8 *)&stage[buffer][s][row * kStage + (((2 * t + (lane >> 5)) ^ ((row >> 1) & 3)) << 3)];
+    const int wi = (own % WM) * (TM / WM), wj = (own / WM) * (TN / WN);
+    auto operand = [&](const _Float16 *plane, int row, int t) {
+        return *(const f16x8 *)&plane[row * kStage + (((2 * t + (lane >> 5)) ^ ((row >> 2) & 3)) << 3)];
     };
-    // a barrier alone does not wait for loads into LDS
-    auto arrive = [&]() {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    fetch(0, 0);
-    arrive();
-    for (int k = 0, buffer = 0; k < depth; k += kStage, buffer ^= 1) {
-        if (k + kStage < depth) fetch(buffer ^ 1, k + kStage);
+    const int stages = depth / kStage;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        if (s < stages) fetch(s, s * kStage);
+    int buffer = 0, next = STAGES - 1;
+    for (int s = 0; s < stages; ++s) {
+        // this stage is there, and everyone has left the one that is fetched into
+        if (s + STAGES - 2 < stages)
+            arrive<kLoads * (STAGES - 2)>();
+        else
+            arrive<0>();
+        if (s + STAGES - 1 < stages) fetch(next, (s + STAGES - 1) * kStage);
+        const _Float16 *at_p = stage[buffer], *at_q = stage[buffer] + PL * TM * kStage;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f16x8 l[PL][MT], r[PL][NT];
 #pragma unroll
-            for (int s = 0; s < PL; ++s) {
+            for (int h = 0; h < PL; ++h) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) l[s][i] = operand(buffer, s, wi + 32 * i + (lane & 31), t);
+                for (int i = 0; i < MT; ++i) l[h][i] = operand(at_p + h * TM * kStage, wi + 32 * i + (lane & 31), t);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) r[s][j] = operand(buffer, PL + s, wj + 32 * j + (lane & 31), t);
+                for (int j = 0; j < NT; ++j) r[h][j] = operand(at_q + h * TN * kStage, wj + 32 * j + (lane & 31), t);
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -181,82 +269,157 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[0][i], r[0][j], acc[i][j], 0, 0, 0);
                 }
         }
-        arrive();
+        buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+        next = next + 1 == STAGES ? 0 : next + 1;
     }
-    // a lane holds column j and, in fours, rows i
-    const float ca = p.coef[step][0], cb = p.coef[step][1], cc = p.coef[step][2];
+    // The way out: a wave turns a tile of 32 x 32 at a time in LDS, so that both
+    // places are read and written 16 bytes a lane, 64 bytes of a row.
+    arrive<0>();
+    float(*turn)[kTurn] = (float(*)[kTurn])((float *)&stage[0][0] + own * 32 * kTurn);
+    const float keep = KIND == kGram ? 0.0f : KIND == kSquare ? p.coef[step][1] * (p.sb / p.sa) : p.coef[step][0];
+    const float take = KIND == kGram     ? p.sa / (p.sx * p.sx)
+                       : KIND == kSquare ? p.coef[step][2] * (p.sb / (p.sa * p.sa))
+                                         : 1.0f / p.sb;
+    const bool symmetric = KIND == kGram || KIND == kSquare;
+    // Second halves are read by three products, or as what stays of the old: by
+    // the next square at A[j][i], by the next update at X^T.
+    constexpr bool kLowT = PL == 2 || KIND != kSquare, kLowD = PL == 2;
+    const Planes to_t = KIND == kGram ? p.a : KIND == kSquare ? p.b : to;
+    const Planes to_d = KIND == kGram ? p.a : KIND == kSquare ? p.b : p.x;
+    const int64_t t0 = symmetric ? a0 : x0;
+    const int ld_d = symmetric ? p.np : p.mp;
 #pragma unroll
     for (int it = 0; it < MT; ++it)
 #pragma unroll
         for (int jt = 0; jt < NT; ++jt) {
-            const int j = tj * TILE + wj + 32 * jt + (lane & 31);
+            const int i0 = ti * TM + wi + 32 * it, j0 = tj * TN + wj + 32 * jt;
+            if (i0 >= p.np || j0 >= rows_j) continue;  // whole tiles: both are multiples of 32
+            // Of a symmetric matrix, what lies on and above the diagonal is taken and
+            // written to both places: the other half is summed in another order.
+            if (symmetric && i0 > j0) continue;
+            const bool diagonal = symmetric && i0 == j0;
+            // a lane holds column j and, in fours, rows i
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int i = ti * TILE + wi + 32 * it + 8 * q + 4 * (lane >> 5);
-                float v[4];
-                if (KIND == kGram) {
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)&turn[lane & 31][8 * q + 4 * (lane >> 5)] =
+                    f32x4{acc[it][jt][4 * q], acc[it][jt][4 * q + 1], acc[it][jt][4 * q + 2], acc[it][jt][4 * q + 3]};
+            wave::sync();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = acc[it][jt][4 * q + e] * (p.sa / (p.sx * p.sx));
-                } else {
-                    // what stays of the old: A[j][i..] (symmetric), or X^T
-                    const int64_t at = (KIND == kSquare ? a0 : x0) + (int64_t)j * p.np + i;
+            for (int r = 0; r < 2; ++r) {
+                const int j = 16 * r + (lane >> 2), i = 8 * (lane & 3);
+                const int64_t at = t0 + (int64_t)(j0 + j) * p.np + i0 + i;
+                f32x4 *const here = (f32x4 *)&turn[j][i];
+                f32x4 v[2] = {here[0], here[1]};
+                if (diagonal) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (i + e > j) v[e >> 2][e & 3] = turn[i + e][j];
+                }
+                f16x8 hi, lo;
+                if (KIND != kGram) {
                     const Planes old = KIND == kSquare ? p.a : from;
-                    const f16x4 hi = *(const f16x4 *)(old.hi + at), lo = *(const f16x4 *)(old.lo + at);
-                    const float keep = KIND == kSquare ? cb * (p.sb / p.sa) : ca;
-                    const float take = KIND == kSquare ? cc * (p.sb / (p.sa * p.sa)) : 1.0f / p.sb;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] = __builtin_fmaf(take, acc[it][jt][4 * q + e], keep * ((float)hi[e] + (float)lo[e]));
+                    hi = *(const f16x8 *)(old.hi + at);
+                    lo = *(const f16x8 *)(old.lo + at);
                 }
-                if (KIND == kLast) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (i + e < p.n && j < p.m)
-                            ((T *)p.out)[mat * p.out_mat + (p.tall ? j * p.out_row + i + e : (i + e) * p.out_row + j)] =
-                                (T)(v[e] * (p.out_scale / p.sx));
-                    continue;
-                }
-                f16x4 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 8; ++e) {
+                    float x = take * v[e >> 2][e & 3];
+                    if (KIND != kGram) x = __builtin_fmaf(keep, (float)hi[e] + (float)lo[e], x);
+                    v[e >> 2][e & 3] = x;
                     _Float16 h, l;
-                    split(v[e], h, l);
+                    split(x, h, l);
                     hi[e] = h;
                     lo[e] = l;
                 }
-                const Planes d = KIND == kGram ? p.a : p.b;
-                if (KIND == kUpdate) {
-                    const int64_t at = x0 + (int64_t)j * p.np + i;
-                    *(f16x4 *)(to.hi + at) = hi;
-                    *(f16x4 *)(to.lo + at) = lo;
-                } else if (ti != tj) {  // a tile on the diagonal holds both, rounded apart: one of them is taken
-                    const int64_t at = a0 + (int64_t)j * p.np + i;
-                    *(f16x4 *)(d.hi + at) = hi;
-                    *(f16x4 *)(d.lo + at) = lo;
+                if (!diagonal) {
+                    here[0] = v[0];
+                    here[1] = v[1];
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t at = KIND == kUpdate ? x0 + (int64_t)(i + e) * p.mp + j : a0 + (int64_t)(i + e) * p.np + j;
-                    const Planes w = KIND == kUpdate ? p.x : d;
-                    w.hi[at] = hi[e];
-                    w.lo[at] = lo[e];
+                if (KIND == kLast) {
+                    if (p.tall) write_out<T>(p, mat, j0 + j, p.m, i0 + i, p.n, v);
+                } else {
+                    *(f16x8 *)(to_t.hi + at) = hi;
+                    if (kLowT) *(f16x8 *)(to_t.lo + at) = lo;
                 }
             }
+            wave::sync();
+            if (KIND == kLast ? !p.tall : !diagonal) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int i = 16 * r + (lane & 15), j = 8 * (lane >> 4);
+                    f32x4 v[2];
+                    f16x8 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = turn[j + e][i];
+                        v[e >> 2][e & 3] = x;
+                        _Float16 h, l;
+                        split(x, h, l);
+                        hi[e] = h;
+                        lo[e] = l;
+                    }
+                    if (KIND == kLast) {
+                        write_out<T>(p, mat, i0 + i, p.n, j0 + j, p.m, v);
+                    } else {
+                        const int64_t at = t0 + (int64_t)(i0 + i) * ld_d + j0 + j;
+                        *(f16x8 *)(to_d.hi + at) = hi;
+                        if (kLowD) *(f16x8 *)(to_d.lo + at) = lo;
+                    }
+                }
+            }
+            wave::sync();
         }
 }
 
-template <typename T, int TILE, int WM, int WN, int PROD>
+template <typename T, int TILE, int WM, int WN, int STAGES, int PROD, int KIND>
+void run_product(const OrthoParams &p, int step, hipStream_t s) {
+    const int ti = (p.np + TILE - 1) / TILE, tj = ((KIND == kGram || KIND == kSquare ? p.np : p.mp) + TILE - 1) / TILE;
+    const int tiles = KIND == kGram || KIND == kSquare ? ti * (ti + 1) / 2 : ti * tj;
+    ortho_product_kernel<T, TILE, TILE, WM, WN, STAGES, PROD, KIND>
+        <<<dim3(tiles, (uint32_t)p.n_mats), WM * WN * 64, 0, s>>>(p, step, ti, tj);
+}
+
+// The tile of a pass: the one that is done first, by the tiles that a compute
+// unit gets, the time of a stage and that of the way in and out, in us, as
+// measured on 4,096 x 4,096 and 128 x 128 (one product; three).
+template <int PROD>
+int pick_tile(const OrthoParams &p, bool symmetric, int depth) {
+    constexpr int kTiles[4] = {64, 128, 192, 256};
+    constexpr double kStageUs[2][4] = {{0.17, 0.37, 0.77, 1.16}, {0.33, 0.78, 1.63, 2.8}};
+    constexpr double kWayUs[4] = {3.0, 5.0, 7.0, 9.0};
+    int best = 0;
+    double least = 0.0;
+    for (int t = 0; t < 4; ++t) {
+        const int64_t ti = (p.np + kTiles[t] - 1) / kTiles[t], tj = (p.mp + kTiles[t] - 1) / kTiles[t];
+        const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * p.n_mats;
+        const double cost = (double)((tiles + 255) / 256) * (depth / kStage * kStageUs[PROD != 1][t] + kWayUs[t]);
+        if (t == 0 || cost < least) {
+            least = cost;
+            best = t;
+        }
+    }
+    return best;
+}
+
+template <typename T, int PROD, int KIND>
+void run_pass(const OrthoParams &p, int step, hipStream_t s) {
+    switch (pick_tile<PROD>(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np)) {
+    case 0: return run_product<T, 64, 2, 2, 3, PROD, KIND>(p, step, s);
+    case 1: return run_product<T, 128, 2, 2, PROD == 1 ? 4 : 2, PROD, KIND>(p, step, s);
+    case 2: return run_product<T, 192, 2, 3, PROD == 1 ? 4 : 3, PROD, KIND>(p, step, s);
+    default: return run_product<T, 256, 4, 2, PROD == 1 ? 4 : 2, PROD, KIND>(p, step, s);
+    }
+}
+
+template <typename T, int PROD>
 hipError_t run_products(const OrthoParams &p, hipStream_t s) {
-    const int ti = p.np / TILE, tj = p.mp / TILE, tri = ti * (ti + 1) / 2;
-    constexpr int threads = WM * WN * 64;
-    const dim3 small(tri, (uint32_t)p.n_mats), whole(ti * tj, (uint32_t)p.n_mats);
     for (int k = 0; k < p.steps; ++k) {
-        ortho_product_kernel<float, TILE, WM, WN, PROD, kGram><<<small, threads, 0, s>>>(p, k, ti, tj);
-        ortho_product_kernel<float, TILE, WM, WN, PROD, kSquare><<<small, threads, 0, s>>>(p, k, ti, tj);
+        run_pass<float, PROD, kGram>(p, k, s);
+        run_pass<float, PROD, kSquare>(p, k, s);
         if (k + 1 < p.steps)
-            ortho_product_kernel<float, TILE, WM, WN, PROD, kUpdate><<<whole, threads, 0, s>>>(p, k, ti, tj);
+            run_pass<float, PROD, kUpdate>(p, k, s);
         else
-            ortho_product_kernel<T, TILE, WM, WN, PROD, kLast><<<whole, threads, 0, s>>>(p, k, ti, tj);
+            run_pass<T, PROD, kLast>(p, k, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -265,14 +428,15 @@ hipError_t run_products(const OrthoParams &p, hipStream_t s) {
 
 template <typename T, int PROD>
 hipError_t run_typed(const OrthoParams &p, hipStream_t s) {
-    const int64_t n = (int64_t)p.rows * p.cols;
-    const int parts = (int)std::min<int64_t>(kNormParts, (n + 4 * kThreads - 1) / (4 * kThreads));
-    ortho_squares_kernel<T><<<dim3(parts, (uint32_t)p.n_mats), kThreads, 0, s>>>(p);
-    ortho_split_kernel<T><<<dim3(p.mp / 64, p.np / 64, (uint32_t)p.n_mats), kThreads, 0, s>>>(p, parts);
+    const int across = (p.cols + 8 * kThreads - 1) / (8 * kThreads);
+    const int parts = (int)std::min<int64_t>(kNormParts, ((int64_t)p.rows * across + 1) / 2);
+    const uint32_t mats = (uint32_t)p.n_mats;
+    ortho_squares_kernel<T><<<mats * parts, kThreads, 0, s>>>(p, parts, across);
+    const int ti = (p.np + 63) / 64, tj = (p.mp + 63) / 64;
+    ortho_split_kernel<T, PROD != 1><<<mats * ti * tj, kThreads, 0, s>>>(p, parts, ti, tj);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.np % 128 == 0 && p.mp % 128 == 0) return run_products<T, 128, 2, 2, PROD>(p, s);
-    return run_products<T, 64, 2, 2, PROD>(p, s);
+    return run_products<T, PROD>(p, s);
 }
 
 }  // namespace

@@ -204,7 +204,7 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
         l.total = l.small_parts + l.small_factors;
         return SAME_OK;
     }
-    const int64_t pad = l.n <= 64 ? 64 : 128;
+    const int64_t pad = 32;  // a stage of the products
     l.np = (l.n + pad - 1) / pad * pad;
     l.mp = (l.m + pad - 1) / pad * pad;
     l.batch = l.n && n_mats ? same::orthogonalise_batch(n_mats, l.np, l.mp) : 0;

@@ -107,7 +107,7 @@ struct OrthoParams {
     float coef[kMaxSteps][3];
 };
 
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 1024;  // of a sum of squares
 
 constexpr int kSmallSide = 32;  // of updates that take the small kernels
 
