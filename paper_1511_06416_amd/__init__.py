@@ -561,7 +561,11 @@ _DTYPES = {"torch.float32": SAME_F32, "torch.float16": SAME_F16, "torch.bfloat16
 
 def _dtype(dtype):
     """SAME_F32, SAME_F16 or SAME_BF16 of a torch dtype."""
-    code = _DTYPES.get(str(dtype))
+    code = _DTYPES.get(dtype)   # the type itself, after its first use: its name takes longer to make
+    if code is None:
+        code = _DTYPES.get(str(dtype))
+        if code is not None and not isinstance(dtype, str):
+            _DTYPES[dtype] = code
     if code is None:
         raise SameError(SAME_EINVAL, "dtype must be torch.float32, torch.float16 or torch.bfloat16, got %s" % dtype)
     return code
@@ -721,13 +725,34 @@ def same_dropout(x, y, drop, seed, call_id, residual=None, stream=None):
 # Operators of a training step.  Their calls run on the current device and, by
 # default, its current stream; tensors of another device are refused.
 
+_F32 = _I32 = _device = _raw_stream = None   # torch's, once it is needed
+
+
+def _begin():
+    """The library and the current device; torch is needed from here on."""
+    global _F32, _I32, _device, _raw_stream
+    if _F32 is None:
+        import torch
+        # what torch.cuda.current_device() asks once the device is in use: 0.07 against 0.35 us
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _F32, _I32 = torch.float32, torch.int32
+    return _lib or load_library()
+
+
+def _now(stream):
+    """The stream of a call, after its tensors were found on the current device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(_device())
+    return _stream(stream)
+
+
 def _here(name, t):
     """Address of a tensor on the current device."""
     at = t.get_device()
     if at < 0:
         raise SameError(SAME_EINVAL, "%s must be a device tensor" % name)
-    import torch
-    if at != torch.cuda.current_device():
+    if at != _device():
         raise SameError(SAME_EINVAL, "%s is on device %d, not on the current one" % (name, at))
     return t.data_ptr()
 
@@ -736,7 +761,7 @@ def _flat(name, t, shape, dtype):
     """Address of a contiguous tensor of one shape and type, or None."""
     if t is None:
         return None
-    if t.shape != shape or str(t.dtype) != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise SameError(SAME_EINVAL, "%s must be contiguous %s of shape %s, got %s of %s"
                         % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     return _here(name, t)
@@ -751,61 +776,61 @@ def _bytes(t, need):
     return _here("workspace", t)
 
 
-def _heads(name, t, dtype, shape=None):
+def _heads(name, t, dtype, shape):
     """Address and element strides of a token and a head of [tokens][heads][head_dim]."""
-    if t.dim() != 3 or t.dtype != dtype or (shape is not None and t.shape != shape):
+    if t.dtype is not dtype or t.shape != shape or len(shape) != 3:
         raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
-                        % (name, dtype, "[tokens][heads][head_dim]" if shape is None else tuple(shape), t.dtype,
+                        % (name, dtype, tuple(shape) if len(shape) == 3 else "[tokens][heads][head_dim]", t.dtype,
                            tuple(t.shape)))
     row, head, unit = t.stride()
     if unit != 1 and t.numel():
         raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-    n, heads, _ = t.shape
-    return _here(name, t), row if n > 1 else 0, head if heads > 1 else 0
+    return _here(name, t), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
 def _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps):
-    dtype, dim = _dtype(q.dtype), q.shape[-1]
-    if k.shape[-1] != dim:
+    dtype, of_q, of_k = q.dtype, q.shape, k.shape
+    at_q, at_k = _heads("q", q, dtype, of_q), _heads("k", k, dtype, of_k)
+    dim = of_q[2]
+    if of_k[2] != dim:
         raise SameError(SAME_EINVAL, "q and k must have heads of one width")
-    if angles is None:
-        rot, turns = 0, None
-    else:
+    rot, turns, width = 0, None, (dim,)
+    if angles is not None and len(angles):
         angles = np.ascontiguousarray(angles, dtype=np.float64)
         if angles.ndim != 1:
             raise SameError(SAME_EINVAL, "angles must be one-dimensional")
-        rot, turns = 2 * len(angles), angles.ctypes.data
-    args = [dtype, dim]
-    for name, t, weight, positions in (("q", q, q_weight, q_positions), ("k", k, k_weight, k_positions)):
-        args += _heads(name, t, q.dtype)
-        args += [t.shape[0], t.shape[1], _flat(name + "_weight", weight, (dim,), "torch.float32"),
-                 _flat(name + "_positions", positions, t.shape[:1], "torch.int32") if rot else None]
+        rot, turns = 2 * len(angles), angles.__array_interface__["data"][0]
+        q_positions = _flat("q_positions", q_positions, of_q[:1], _I32)
+        k_positions = _flat("k_positions", k_positions, of_k[:1], _I32)
+    else:
+        q_positions = k_positions = None
     # angles: kept alive by the caller until the call returns
-    return args + [float(eps), rot, turns], angles
+    return (_dtype(dtype), dim, *at_q, of_q[0], of_q[1], _flat("q_weight", q_weight, width, _F32), q_positions, *at_k,
+            of_k[0], of_k[1], _flat("k_weight", k_weight, width, _F32), k_positions, float(eps), rot, turns), angles
 
 
 def same_qk_norm(q, k, q_out, k_out, q_weight=None, k_weight=None, q_positions=None, k_positions=None, angles=None,
                  eps=1e-6, stream=None):
     """angles: float64 numpy array of rot_dim / 2 radians a position (None or empty: no rotation)."""
+    lib = _begin()
     args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
-    name = str(q.dtype)
-    _check((_lib or load_library()).same_qk_norm(*args, _flat("q_out", q_out, q.shape, name),
-                                                 _flat("k_out", k_out, k.shape, name), _stream(stream)))
+    _check(lib.same_qk_norm(*args, _flat("q_out", q_out, q.shape, q.dtype), _flat("k_out", k_out, k.shape, q.dtype),
+                            _now(stream)))
 
 
 def same_qk_norm_backward(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_weight=None, k_weight=None,
                           q_positions=None, k_positions=None, angles=None, eps=1e-6, stream=None):
     """dq_weight and dk_weight may be None."""
+    lib = _begin()
     args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
-    name, width = str(q.dtype), q.shape[-1:]
+    dtype, width = q.dtype, q.shape[-1:]
     need = 0
     if dq_weight is not None or dk_weight is not None:
         need = same_qk_norm_workspace_size(q.shape[2], q.shape[0], q.shape[1], k.shape[0], k.shape[1])
-    _check((_lib or load_library()).same_qk_norm_backward(
-        *args, *_heads("dq_out", dq_out, q.dtype, q.shape), *_heads("dk_out", dk_out, q.dtype, k.shape),
-        _flat("dq", dq, q.shape, name), _flat("dk", dk, k.shape, name),
-        _flat("dq_weight", dq_weight, width, "torch.float32"), _flat("dk_weight", dk_weight, width, "torch.float32"),
-        _bytes(workspace, need), _stream(stream)))
+    _check(lib.same_qk_norm_backward(
+        *args, *_heads("dq_out", dq_out, dtype, q.shape), *_heads("dk_out", dk_out, dtype, k.shape),
+        _flat("dq", dq, q.shape, dtype), _flat("dk", dk, k.shape, dtype), _flat("dq_weight", dq_weight, width, _F32),
+        _flat("dk_weight", dk_weight, width, _F32), _bytes(workspace, need), _now(stream)))
 
 
 def same_qk_norm_workspace_size(head_dim, q_tokens, heads_q, k_tokens, heads_kv) -> int:
@@ -817,7 +842,7 @@ def same_qk_norm_workspace_size(head_dim, q_tokens, heads_q, k_tokens, heads_kv)
 
 def _logits(name, t, like):
     """Address and row stride of a matrix of logits."""
-    if t.dim() != 2 or t.shape != like.shape or t.dtype != like.dtype:
+    if t.dtype is not like.dtype or t.dim() != 2 or t.shape != like.shape:
         raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like logits" % name)
     row, unit = t.stride()
     if unit != 1 and t.shape[1] > 1 and t.numel():
@@ -829,7 +854,7 @@ def same_log_probs(logits, targets, log_probs, workspace, counts=None, sums=None
                    top_log_probs=None, stream=None):
     """targets and counts: int32.  targets with log_probs, sums ([rows][2]), entropy, and top_ids (int32) with
     top_log_probs may be None; the number of alternatives is top_ids' second size."""
-    dtype = _dtype(logits.dtype)
+    lib = _begin()
     at, row = _logits("logits", logits, logits)
     rows, cols = logits.shape
     one, n_top = (rows,), 0
@@ -839,29 +864,27 @@ def same_log_probs(logits, targets, log_probs, workspace, counts=None, sums=None
         if top_ids.dim() != 2:
             raise SameError(SAME_EINVAL, "top_ids must be of shape [rows][n_top]")
         n_top = top_ids.shape[1]
-    lib = _lib or load_library()
     need = same_log_probs_workspace_size(rows, cols, n_top) if cols > 64 else 0
     _check(lib.same_log_probs(
-        dtype, at, row, rows, cols, _flat("counts", counts, one, "torch.int32"),
-        _flat("targets", targets, one, "torch.int32"), _flat("log_probs", log_probs, one, "torch.float32"),
-        _flat("sums", sums, (rows, 2), "torch.float32"), _flat("entropy", entropy, one, "torch.float32"), n_top,
-        _flat("top_ids", top_ids, (rows, n_top), "torch.int32"),
-        _flat("top_log_probs", top_log_probs, (rows, n_top), "torch.float32"), _bytes(workspace, need),
-        _stream(stream)))
+        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32),
+        _flat("targets", targets, one, _I32), _flat("log_probs", log_probs, one, _F32),
+        _flat("sums", sums, (rows, 2), _F32), _flat("entropy", entropy, one, _F32), n_top,
+        _flat("top_ids", top_ids, (rows, n_top), _I32), _flat("top_log_probs", top_log_probs, (rows, n_top), _F32),
+        _bytes(workspace, need), _now(stream)))
 
 
 def same_log_probs_backward(logits, targets, sums, dlogits, counts=None, entropy=None, dlog_probs=None, dentropy=None,
                             stream=None):
     """sums and entropy: the forward's.  dlog_probs and dentropy may be None."""
-    dtype = _dtype(logits.dtype)
+    lib = _begin()
     at, row = _logits("logits", logits, logits)
     rows, cols = logits.shape
     one = (rows,)
-    _check((_lib or load_library()).same_log_probs_backward(
-        dtype, at, row, rows, cols, _flat("counts", counts, one, "torch.int32"),
-        _flat("targets", targets, one, "torch.int32"), _flat("sums", sums, (rows, 2), "torch.float32"),
-        _flat("entropy", entropy, one, "torch.float32"), _flat("dlog_probs", dlog_probs, one, "torch.float32"),
-        _flat("dentropy", dentropy, one, "torch.float32"), *_logits("dlogits", dlogits, logits), _stream(stream)))
+    _check(lib.same_log_probs_backward(
+        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32),
+        _flat("targets", targets, one, _I32), _flat("sums", sums, (rows, 2), _F32),
+        _flat("entropy", entropy, one, _F32), _flat("dlog_probs", dlog_probs, one, _F32),
+        _flat("dentropy", dentropy, one, _F32), *_logits("dlogits", dlogits, logits), _now(stream)))
 
 
 def same_log_probs_workspace_size(rows, cols, n_top) -> int:
@@ -886,18 +909,18 @@ def _matrices(name, t, like):
 
 def same_orthogonalise(g, out, workspace, coefs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, stream=None):
     """g, out: a matrix or [n] matrices.  coefs: (a, b, c) of every step."""
-    dtype = _dtype(g.dtype)
+    lib = _begin()
     at, g_mat, g_row = _matrices("g", g, g)
     steps = np.ascontiguousarray(coefs, dtype=np.float64)
     if steps.ndim != 2 or steps.shape[1] != 3:
         raise SameError(SAME_EINVAL, "coefs must be (a, b, c) of every step")
     n = g.shape[0] if g.dim() == 3 else 1
     rows, cols = g.shape[-2:]
-    lib = _lib or load_library()
     to, out_mat, out_row = _matrices("out", out, g)
     need = same_orthogonalise_workspace_size(n, rows, cols, g.dtype)
-    _check(lib.same_orthogonalise(dtype, at, g_mat, g_row, n, rows, cols, steps.ctypes.data, len(steps), float(eps),
-                                  float(scale), to, out_mat, out_row, _bytes(workspace, need), _stream(stream)))
+    _check(lib.same_orthogonalise(_dtype(g.dtype), at, g_mat, g_row, n, rows, cols,
+                                  steps.__array_interface__["data"][0], len(steps), float(eps), float(scale), to,
+                                  out_mat, out_row, _bytes(workspace, need), _now(stream)))
 
 
 def same_orthogonalise_workspace_size(n_mats, rows, cols, dtype) -> int:

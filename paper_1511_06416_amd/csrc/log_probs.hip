@@ -26,7 +26,6 @@ constexpr float kInf = __builtin_huge_valf();
 constexpr int kCandidates = 512;
 
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
-__device__ __forceinline__ float log_of(float s) { return __builtin_amdgcn_logf(s) * kLn2; }
 
 // Bits in the order of values: both zeros alike, NaN as -inf; never 0.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -39,34 +38,74 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return (uint64_t)o << 32 | (uint32_t)~index; }
 
-// A sum of exponents and of their weighted distances, relative to max.
-__device__ __forceinline__ void add_logit(float x, float max, float &sum, float &weighted) {
-    const float d = x - max, e = exp_of(d);
+// Sums are formed in powers of two.  With base = max log2 e, rounded, a logit's
+// place is t = x log2 e - base, one multiply-add; e = 2^t goes to the sum and
+// t e to the weighted one.  The base's rounding shifts every t alike: it is
+// known to the last bit from a multiply-add, belongs to the logarithm of the
+// sum, and cancels from the entropy.
+struct Place {
+    float max, base;
+    bool far;   // the base passes 32 bits: distances are formed first
+    __device__ __forceinline__ explicit Place(float m) {
+#pragma clang fp contract(off)
+        max = m == -kInf ? 0.0f : m;   // nothing is there, or NaN alone
+        base = max * kLog2e;
+        far = __builtin_fabsf(max) > 1e38f;
+    }
+};
+
+template <bool FAR>
+__device__ __forceinline__ void add_logit(float x, const Place &at, float &sum, float &weighted) {
+    const float t = FAR ? (x - at.max) * kLog2e : __builtin_fmaf(x, kLog2e, -at.base);
+    const float e = __builtin_amdgcn_exp2f(t);
     sum += e;
-    weighted = __builtin_fmaf(e, __builtin_fmaxf(d, -200.0f), weighted);  // -inf: 0 of it; NaN is in the sum
+    weighted = __builtin_fmaf(e, __builtin_fmaxf(t, -300.0f), weighted);  // -inf: 0 of it; NaN is in the sum
 }
 
 // One part's sums relative to a larger maximum.
 __device__ __forceinline__ void rescale(RowStats &r, float max) {
-    if (r.max == max || r.max == -kInf) {  // nothing there, or nothing to change
+#pragma clang fp contract(off)  // the bases' difference, each rounded
+    if (r.max == max || r.max == -kInf) {  // nothing to change, or nothing there
         r.max = max;
         return;
     }
-    const float d = r.max - max, e = exp_of(d);
-    r.weighted = e * (r.weighted + d * r.sum);
-    if (e == 0.0f && r.sum == r.sum) r.weighted = 0.0f;
+    const Place from(r.max), to(max);
+    const float d = from.far || to.far ? (r.max - max) * kLog2e : from.base - to.base;
+    const float e = __builtin_amdgcn_exp2f(d);
+    r.weighted = e == 0.0f && r.sum == r.sum ? 0.0f : e * __builtin_fmaf(d, r.sum, r.weighted);
     r.sum *= e;
     r.max = max;
 }
 
-// What a row's statistics say, written by one thread.
-__device__ __forceinline__ void finish(const LogProbsParams &p, int64_t row, int n, const RowStats &r, float asked,
-                                       int target, float log_sum) {
-    const bool none = r.max == -kInf && r.sum == 0.0f;  // no state is possible
-    if (p.sums) p.sums[row] = make_float2(r.max, none ? 0.0f : log_sum);
-    if (p.entropy) p.entropy[row] = none ? 0.0f : log_sum - r.weighted / r.sum;
+// A row's values.
+struct RowValues {
+    float max, log_sum, entropy;
+    bool none;   // no state is possible
+    // shifted: by the base's rounding
+    __device__ __forceinline__ explicit RowValues(const RowStats &r, bool shifted = true) {
+        const Place at(r.max);
+        const float bits = __builtin_amdgcn_logf(r.sum);
+        const float off = shifted && !at.far ? __builtin_fmaf(-at.max, kLog2e, at.base) : 0.0f;
+        none = r.max == -kInf && r.sum == 0.0f;
+        max = r.max;
+        log_sum = none ? 0.0f : (bits + off) * kLn2;
+        entropy = none ? 0.0f : (bits - r.weighted / r.sum) * kLn2;
+    }
+};
+
+// A row's outputs, written by one thread.
+__device__ __forceinline__ void finish(const LogProbsParams &p, int64_t row, int n, const RowValues &r, float asked,
+                                       int target) {
+    if (p.sums) p.sums[row] = make_float2(r.max, r.log_sum);
+    if (p.entropy) p.entropy[row] = r.entropy;
     if (p.log_probs)
-        p.log_probs[row] = target < 0 ? 0.0f : none || target >= n ? -kInf : (asked - r.max) - log_sum;
+        p.log_probs[row] = target < 0 ? 0.0f : r.none || target >= n ? -kInf : (asked - r.max) - r.log_sum;
+}
+
+// An alternative, key 0 where there is none.
+__device__ __forceinline__ void put_top(const LogProbsParams &p, int64_t at, uint64_t key, const RowValues &r) {
+    p.top_ids[at] = key ? (int)~(uint32_t)key : -1;
+    p.top_log_probs[at] = key && !r.none ? (value_of((uint32_t)(key >> 32)) - r.max) - r.log_sum : -kInf;
 }
 
 __device__ __forceinline__ int count_of(const int32_t *counts, int64_t row, int cols) {
@@ -95,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void log_probs_short_kernel(LogProbsParam
 #pragma unroll
             for (int i = 0; i < E; ++i) x[i] = first + i < p.cols ? (float)src[i] : -kInf;
         }
-        RowStats r{-kInf, 0.0f, 0.0f, 0.0f};
+        RowStats r{-kInf, 0.0f, 0.0f};
         float asked = -kInf;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
@@ -103,18 +142,18 @@ __global__ __launch_bounds__(kThreads) void log_probs_short_kernel(LogProbsParam
             r.max = __builtin_fmaxf(r.max, x[i]);
         }
         r.max = wave::reduce(r.max, lanes, wave::Max());
-        const float base = r.max == -kInf ? 0.0f : r.max;
+        const Place at(r.max);
 #pragma unroll
-        for (int i = 0; i < E; ++i) add_logit(x[i], base, r.sum, r.weighted);
+        for (int i = 0; i < E; ++i) add_logit<true>(x[i], at, r.sum, r.weighted);
         r.sum = wave::reduce(r.sum, lanes, wave::Add());
         r.weighted = wave::reduce(r.weighted, lanes, wave::Add());
-        const float log_sum = log_of(r.sum);
+        const RowValues values(r, false);
         // the lane that holds the target writes
         const int owner = target >= 0 && target < n ? target / E : 0;
         if (lane == owner) {
 #pragma unroll
             for (int i = 0; i < E; ++i) asked = first + i == target ? x[i] : asked;
-            finish(p, row, n, r, asked, target, log_sum);
+            finish(p, row, n, values, asked, target);
         }
         uint32_t left[E];
         if (p.n_top) {
@@ -133,11 +172,7 @@ __global__ __launch_bounds__(kThreads) void log_probs_short_kernel(LogProbsParam
 #pragma unroll
             for (int i = 0; i < E; ++i)
                 if ((uint32_t)(first + i) == at) left[i] = 0;
-            if (lane == 0) {
-                p.top_ids[row * p.n_top + k] = best ? (int)at : -1;
-                p.top_log_probs[row * p.n_top + k] =
-                    best ? (r.max == -kInf && r.sum == 0.0f ? -kInf : (value_of(best) - r.max) - log_sum) : -kInf;
-            }
+            if (lane == 0) put_top(p, row * p.n_top + k, best ? key_of(best, at) : 0, values);
         }
     }
 }
@@ -150,12 +185,14 @@ __global__ __launch_bounds__(kThreads) void log_probs_short_kernel(LogProbsParam
 // and ranked by counting.  Where more than kCandidates reach it (many alike),
 // the alternatives are found one after another.
 
-template <typename T, int WAVES, int VECS, bool TOP>
+template <int WAVES, bool TOP>
 struct RowShared {
     RowStats stats[WAVES];
-    uint32_t largest[WAVES][64];
+    uint32_t largest[TOP ? WAVES : 1][64];
     uint64_t keys[TOP ? kCandidates : 1];
     uint64_t best[WAVES];
+    RowStats all;
+    uint32_t bound;
     int count;
 };
 
@@ -181,12 +218,69 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t o, int want) {
     return t;
 }
 
+// Keeps a vector as it was read: the compiler would hold its elements widened
+// to fp32, twice the registers and half the waves.
+template <typename V>
+__device__ __forceinline__ void keep_packed(V &v) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+    asm volatile("" : "+v"(w));
+    v = __builtin_bit_cast(V, w);
+}
+
+// N neighbouring logits of a row from `at` on, -inf from `end` on, for rows of N
+// columns at least: behind the row's last vector that one is read (vector_at),
+// and moved down (settle).  Reads come first, all of them: a branch between
+// would wait for each.
+template <typename T, int N>
+__device__ __forceinline__ Loose<T, N> vector_at(const T *row, int at, int cols) {
+    return *(const Loose<T, N> *)(row + min(at, cols - N));
+}
+template <typename T, int N>
+__device__ __forceinline__ void settle(Loose<T, N> &v, int at, int end, int cols) {
+    if (at <= end - N) return;
+    struct Pair {
+        uint64_t lo, hi;
+    };
+    Pair w = __builtin_bit_cast(Pair, v);
+    int bits = min(at - min(at, cols - N), N) * (int)sizeof(T) * 8;
+    if (bits >= 64) {
+        w.lo = w.hi;
+        w.hi = 0;
+        bits -= 64;
+    }
+    if (bits > 0) {
+        w.lo = bits < 64 ? w.lo >> bits | w.hi << (64 - bits) : w.hi;
+        w.hi = bits < 64 ? w.hi >> bits : 0;
+    }
+    v = __builtin_bit_cast(Loose<T, N>, w);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (at + e >= end) v.v[e] = (T)-kInf;
+}
+
+// Sums of a row's parts, a lane each: merged relative to the largest.
+__device__ __forceinline__ RowStats merge(RowStats r, int lanes) {
+    rescale(r, wave::reduce(r.max, lanes, wave::Max()));
+    r.sum = wave::reduce(r.sum, lanes, wave::Add());
+    r.weighted = wave::reduce(r.weighted, lanes, wave::Add());
+    return r;
+}
+
+__device__ __forceinline__ uint64_t largest_key(uint64_t k) {
+    for (int o = 32; o; o >>= 1) {
+        const uint64_t other = __shfl_xor(k, o);
+        k = other > k ? other : k;
+    }
+    return k;
+}
+
 template <typename T, int WAVES, int VECS, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_kernel(LogProbsParams p) {
     constexpr int N = 16 / sizeof(T), ROWS = WAVES == 1 ? kThreads / 64 : 1;
-    __shared__ RowShared<T, WAVES, VECS, TOP> shared[ROWS];
+    __shared__ RowShared<WAVES, TOP> shared[ROWS];
     const int lane = threadIdx.x & 63, own = WAVES == 1 ? 0 : threadIdx.x >> 6;
-    RowShared<T, WAVES, VECS, TOP> &sh = shared[WAVES == 1 ? threadIdx.x >> 6 : 0];
+    RowShared<WAVES, TOP> &sh = shared[WAVES == 1 ? threadIdx.x >> 6 : 0];
     const int64_t items = p.rows * p.parts, step = (int64_t)gridDim.x * ROWS;
     for (int64_t item = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0); item < items; item += step) {
         const int64_t row = p.parts == 1 ? item : item / p.parts;
@@ -195,119 +289,125 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
         const int beg = part * p.part_cols, end = min(n, beg + p.part_cols);
         const T *src = (const T *)p.x + row * p.x_row;
         const int target = p.targets && p.parts == 1 ? p.targets[row] : -1;
-        const bool writer = own == 0 && lane == 0;
-        float asked = -kInf;
-        if (writer && target >= 0 && target < n) asked = (float)src[target];
         Loose<T, N> v[VECS];
         const int at0 = beg + (own * 64 + lane) * N;
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) {
-            const int at = at0 + i * WAVES * 64 * N;
-            if (at <= end - N) {
-                v[i] = *(const Loose<T, N> *)(src + at);
-            } else {
+        for (int i = 0; i < VECS; ++i) v[i] = vector_at<T, N>(src, at0 + i * WAVES * 64 * N, p.cols);
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[i].v[e] = at + e < end ? src[at + e] : (T)-kInf;
-            }
-        }
+        for (int i = 0; i < VECS; ++i) settle<T, N>(v[i], at0 + i * WAVES * 64 * N, end, p.cols);
+        float asked = -kInf;
+        if (own == 0 && lane == 0 && target >= 0 && target < n) asked = (float)src[target];
         float most = -kInf;
 #pragma unroll
         for (int i = 0; i < VECS; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) most = __builtin_fmaxf(most, (float)v[i].v[e]);
-        RowStats r{wave::reduce(most, 64, wave::Max()), 0.0f, 0.0f, 0.0f};
-        const float base = r.max == -kInf ? 0.0f : r.max;
-#pragma unroll
-        for (int i = 0; i < VECS; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e) add_logit((float)v[i].v[e], base, r.sum, r.weighted);
-        r.sum = wave::reduce(r.sum, 64, wave::Add());
-        r.weighted = wave::reduce(r.weighted, 64, wave::Add());
-        if (WAVES > 1 || TOP) {
-            if (WAVES > 1 && lane == 0) sh.stats[own] = r;
-            if (TOP) sh.largest[own][lane] = at0 < end ? ordered(most) : 0;
-            if (writer) sh.count = 0;
-            row_sync<WAVES>();
-        }
-        if (WAVES > 1) {
-            float max = -kInf;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) max = __builtin_fmaxf(max, sh.stats[w].max);
-            r.max = max;
-            r.sum = r.weighted = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                RowStats o = sh.stats[w];
-                rescale(o, max);
-                r.sum += o.sum;
-                r.weighted += o.weighted;
-            }
-        }
-        const float log_sum = log_of(r.sum);
-        if (writer) {
-            if (p.parts == 1)
-                finish(p, row, n, r, asked, target, log_sum);
-            else
-                p.part_stats[item] = r;
-        }
+        RowStats r{wave::reduce(most, 64, wave::Max()), 0.0f, 0.0f};
         if (TOP) {
-            uint32_t o = sh.largest[0][lane];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) o = max(o, sh.largest[w][lane]);
-            const uint32_t bound = kth_largest(o, p.n_top);
-            const float low = bound ? value_of(bound) : -kInf;
+            sh.largest[own][lane] = at0 < end ? ordered(most) : 0;
+            if (own == 0 && lane == 0) sh.count = 0;
+        }
+        const Place place(r.max);
+        if (place.far) {
 #pragma unroll
             for (int i = 0; i < VECS; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = (float)v[i].v[e];
-                    const int at = at0 + i * WAVES * 64 * N + e;
-                    if (!(x < low) && at < end) {
-                        const uint32_t u = ordered(x);
-                        if (u >= bound) {
-                            const int slot = atomicAdd(&sh.count, 1);
-                            if (slot < kCandidates) sh.keys[slot] = key_of(u, (uint32_t)at);
+                for (int e = 0; e < N; ++e) add_logit<true>((float)v[i].v[e], place, r.sum, r.weighted);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) {
+                if (sizeof(T) == 2) keep_packed(v[i]);
+#pragma unroll
+                for (int e = 0; e < N; ++e) add_logit<false>((float)v[i].v[e], place, r.sum, r.weighted);
+            }
+        }
+        r.sum = wave::reduce(r.sum, 64, wave::Add());
+        r.weighted = wave::reduce(r.weighted, 64, wave::Add());
+        if (WAVES > 1 && lane == 0) sh.stats[own] = r;
+        if (WAVES > 1 || TOP) row_sync<WAVES>();
+        if (own == 0) {
+            if (WAVES > 1) r = merge(sh.stats[lane & (WAVES - 1)], WAVES);
+            if (lane == 0) {
+                if (p.parts == 1)
+                    finish(p, row, n, RowValues(r), asked, target);
+                else
+                    p.part_stats[item] = r;
+            }
+            if (TOP) {
+                uint32_t o = sh.largest[0][lane];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) o = max(o, sh.largest[w][lane]);
+                const uint32_t bound = kth_largest(o, p.n_top);
+                if (lane == 0) {
+                    sh.bound = bound;
+                    sh.all = r;
+                }
+            }
+        }
+        if (TOP) {
+            row_sync<WAVES>();
+            const uint32_t bound = sh.bound;
+            const float low = bound ? value_of(bound) : -kInf;
+            if (!(most < low)) {
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) {
+                    if (sizeof(T) == 2) keep_packed(v[i]);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float x = (float)v[i].v[e];
+                        const int at = at0 + i * WAVES * 64 * N + e;
+                        if (!(x < low)) {
+                            const uint32_t u = ordered(x);
+                            if (u >= bound && at < end) {
+                                const int slot = atomicAdd(&sh.count, 1);
+                                if (slot < kCandidates) sh.keys[slot] = key_of(u, (uint32_t)at);
+                            }
                         }
                     }
                 }
+            }
             row_sync<WAVES>();
             const int found = sh.count;
-            const bool none = r.max == -kInf && r.sum == 0.0f;
+            const RowValues all(sh.all);
             const int64_t out = item * p.n_top;
             auto put = [&](int k, uint64_t key) {
-                if (p.parts > 1) {
+                if (p.parts > 1)
                     p.part_keys[out + k] = key;
-                } else {
-                    p.top_ids[out + k] = key ? (int)~(uint32_t)key : -1;
-                    p.top_log_probs[out + k] =
-                        key && !none ? (value_of((uint32_t)(key >> 32)) - r.max) - log_sum : -kInf;
-                }
+                else
+                    put_top(p, out + k, key, all);
             };
-            const int me = own * 64 + lane;
             if (found <= kCandidates) {
-                for (int c = me; c < found; c += WAVES * 64) {
-                    const uint64_t key = sh.keys[c];
+                // a wave takes 64 candidates; the others pass by in registers
+                for (int c0 = own * 64; c0 < found; c0 += WAVES * 64) {
+                    const uint64_t key = c0 + lane < found ? sh.keys[c0 + lane] : 0;
                     int rank = 0;
-                    for (int j = 0; j < found; ++j) rank += sh.keys[j] > key;
-                    if (rank < p.n_top) put(rank, key);
+                    for (int j0 = 0; j0 < found; j0 += 64) {
+                        const uint64_t others = j0 + lane < found ? sh.keys[j0 + lane] : 0;
+                        const int n_others = min(64, found - j0);
+                        for (int j = 0; j < n_others; ++j) {
+                            const uint64_t other =
+                                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(others >> 32), j) << 32 |
+                                (uint32_t)__builtin_amdgcn_readlane((int)others, j);
+                            rank += other > key;
+                        }
+                    }
+                    if (key && rank < p.n_top) put(rank, key);
                 }
-                for (int k = found + me; k < p.n_top; k += WAVES * 64) put(k, 0);
+                for (int k = found + own * 64 + lane; k < p.n_top; k += WAVES * 64) put(k, 0);
             } else {
                 uint64_t last = ~0ull;
                 for (int k = 0; k < p.n_top; ++k) {
                     uint64_t best = 0;
-#pragma unroll
+                    // read again, a logit at a time: it happens seldom, and registers are short
+#pragma unroll 1
                     for (int i = 0; i < VECS; ++i)
-#pragma unroll
+#pragma unroll 1
                         for (int e = 0; e < N; ++e) {
                             const int at = at0 + i * WAVES * 64 * N + e;
-                            const uint64_t key = at < end ? key_of(ordered((float)v[i].v[e]), (uint32_t)at) : 0;
+                            const uint64_t key = at < end ? key_of(ordered((float)src[at]), (uint32_t)at) : 0;
                             if (key < last && key > best) best = key;
                         }
-                    for (int o = 32; o; o >>= 1) {
-                        const uint64_t other = __shfl_xor(best, o);
-                        best = other > best ? other : best;
-                    }
+                    best = largest_key(best);
                     if (WAVES > 1) {
                         if (lane == 0) sh.best[own] = best;
                         __syncthreads();
@@ -315,7 +415,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
                         for (int w = 0; w < WAVES; ++w) best = sh.best[w] > best ? sh.best[w] : best;
                         __syncthreads();
                     }
-                    if (writer) put(k, best);
+                    if (own == 0 && lane == 0) put(k, best);
                     last = best;
                 }
             }
@@ -324,20 +424,23 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
     }
 }
 
-// A long row's parts: a wave a row, a lane a part.
+// A long row's parts: a block a row, a lane a part.  The parts' alternatives are
+// in falling order: with t of each as many as are wanted, the smallest of the
+// t-th ones bounds the wanted ones from below; what reaches it is ranked by
+// counting.
 __global__ __launch_bounds__(kThreads) void log_probs_join_kernel(LogProbsParams p, int dtype) {
-    const int lane = threadIdx.x & 63;
-    const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
-    for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < p.rows; row += step) {
+    __shared__ uint64_t keys[kMaxRowParts * kMaxTop], nth[kMaxRowParts];
+    __shared__ int found;
+    const int lane = threadIdx.x & 63, k = p.n_top, all = p.parts * k, t = (k + p.parts - 1) / p.parts;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const int n = count_of(p.counts, row, p.cols);
-        RowStats r{-kInf, 0.0f, 0.0f, 0.0f};
+        const uint64_t *src = p.part_keys + row * all;
+        RowStats r{-kInf, 0.0f, 0.0f};
         if (lane < p.parts) r = p.part_stats[row * p.parts + lane];
-        const float max = wave::reduce(r.max, 64, wave::Max());
-        rescale(r, max);
-        r.sum = wave::reduce(r.sum, 64, wave::Add());
-        r.weighted = wave::reduce(r.weighted, 64, wave::Add());
-        const float log_sum = log_of(r.sum);
-        if (lane == 0) {
+        if (k && threadIdx.x < p.parts) nth[threadIdx.x] = src[threadIdx.x * k + t - 1];
+        if (threadIdx.x == 0) found = 0;
+        const RowValues values(merge(r, 64));
+        if (threadIdx.x == 0) {
             const int target = p.targets ? p.targets[row] : -1;
             float asked = -kInf;
             if (target >= 0 && target < n) {
@@ -346,24 +449,30 @@ __global__ __launch_bounds__(kThreads) void log_probs_join_kernel(LogProbsParams
                         : dtype == 1 ? (float)((const _Float16 *)p.x)[at]
                                      : (float)((const __bf16 *)p.x)[at];
             }
-            finish(p, row, n, r, asked, target, log_sum);
+            finish(p, row, n, values, asked, target);
         }
-        const uint64_t *keys = p.part_keys + (row * p.parts + lane) * p.n_top;
-        int next = 0;
-        const bool none = r.max == -kInf && r.sum == 0.0f;
-        for (int k = 0; k < p.n_top; ++k) {
-            const uint64_t mine = lane < p.parts && next < p.n_top ? keys[next] : 0;
-            uint64_t best = mine;
+        if (k) {
+            __syncthreads();
+            uint64_t bound = lane < p.parts ? nth[lane] : ~0ull;
             for (int o = 32; o; o >>= 1) {
-                const uint64_t other = __shfl_xor(best, o);
-                best = other > best ? other : best;
+                const uint64_t other = __shfl_xor(bound, o);
+                bound = other < bound ? other : bound;
             }
-            if (mine == best) ++next;
-            if (lane == 0) {
-                p.top_ids[row * p.n_top + k] = best ? (int)~(uint32_t)best : -1;
-                p.top_log_probs[row * p.n_top + k] =
-                    best && !none ? (value_of((uint32_t)(best >> 32)) - r.max) - log_sum : -kInf;
+            for (int c = threadIdx.x; c < all; c += kThreads) {
+                const uint64_t key = src[c];
+                if (key && key >= bound) keys[atomicAdd(&found, 1)] = key;
             }
+            __syncthreads();
+            for (int c = threadIdx.x; c < found; c += kThreads) {
+                const uint64_t key = keys[c];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < found; ++j) rank += keys[j] > key;
+                if (rank < k) put_top(p, row * k + rank, key, values);
+            }
+            // fewer than wanted: then all of them were found
+            for (int c = found + threadIdx.x; c < k; c += kThreads) put_top(p, row * k + c, 0, values);
+            __syncthreads();
         }
     }
 }
@@ -372,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void log_probs_join_kernel(LogProbsParams
 //   dx_j = dl (1[j = t] - p_j) - dH p_j (l_j + H),  0 from the count on.
 
 struct RowGrad {
-    float max, log_sum, entropy, dl, dh;
+    float max, log_sum, slope, rest, dl;   // -(dl + dH H), -dH
     int n, target;
 };
 
@@ -384,42 +493,60 @@ __device__ __forceinline__ RowGrad row_grad(const LogProbsGradParams &p, int64_t
     g.n = s.x == -kInf && s.y == 0.0f ? 0 : count_of(p.counts, row, p.cols);  // no state is possible: no gradient
     g.target = p.targets ? p.targets[row] : -1;
     g.dl = p.dlog_probs && g.target >= 0 ? p.dlog_probs[row] : 0.0f;
-    g.dh = p.dentropy ? p.dentropy[row] : 0.0f;
-    g.entropy = p.dentropy ? p.entropy[row] : 0.0f;
+    const float dh = p.dentropy ? p.dentropy[row] : 0.0f;
+    g.slope = -dh;
+    g.rest = p.dentropy ? -__builtin_fmaf(dh, p.entropy[row], g.dl) : -g.dl;
     return g;
 }
 
-__device__ __forceinline__ float logit_grad(const RowGrad &g, float x, int at) {
-    const float l = (x - g.max) - g.log_sum, prob = exp_of(l);
-    const float v = -prob * __builtin_fmaf(g.dh, __builtin_fmaxf(l, -200.0f) + g.entropy, g.dl);
-    return at < g.n ? v + (at == g.target ? g.dl : 0.0f) : 0.0f;
+__device__ __forceinline__ float logit_grad(const RowGrad &g, float x) {
+    const float l = (x - g.max) - g.log_sum;
+    return exp_of(l) * __builtin_fmaf(g.slope, __builtin_fmaxf(l, -200.0f), g.rest);
 }
 
 template <typename T, int E>
-__device__ __forceinline__ void grad_vector(const LogProbsGradParams &p, const RowGrad &g, int64_t row, int at) {
-    const T *src = (const T *)p.x + row * p.x_row + at;
-    T *dst = (T *)p.dx + row * p.dx_row + at;
-    if (at + E <= p.cols) {
-        Loose<T, E> v = *(const Loose<T, E> *)src;
+__device__ __forceinline__ Loose<T, E> vector_grad(const RowGrad &g, Loose<T, E> v, int at) {
+    if (at + E <= g.n && (uint32_t)(g.target - at) >= (uint32_t)E) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) v.v[i] = (T)logit_grad(g, (float)v.v[i], at + i);
-        *(Loose<T, E> *)dst = v;
+        for (int i = 0; i < E; ++i) v.v[i] = (T)logit_grad(g, (float)v.v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (at + i < p.cols) dst[i] = (T)logit_grad(g, (float)src[i], at + i);
+        for (int i = 0; i < E; ++i) {
+            const float d = logit_grad(g, (float)v.v[i]) + (at + i == g.target ? g.dl : 0.0f);
+            v.v[i] = (T)(at + i < g.n ? d : 0.0f);
+        }
+    }
+    return v;
+}
+
+// The last logits of a row, fewer than a vector.
+template <typename T>
+__device__ __forceinline__ void grad_rest(const RowGrad &g, const T *src, T *dst, int at, int cols) {
+    for (; at < cols; ++at) {
+        const float d = logit_grad(g, (float)src[at]) + (at == g.target ? g.dl : 0.0f);
+        dst[at] = (T)(at < g.n ? d : 0.0f);
     }
 }
 
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void log_probs_grad_short_kernel(LogProbsGradParams p, int lanes) {
-    const int first = (threadIdx.x & (lanes - 1)) * E;
+    const int at = (threadIdx.x & (lanes - 1)) * E;
     const int64_t step = (int64_t)gridDim.x * (kThreads / lanes);
-    for (int64_t row = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes; row < p.rows; row += step)
-        if (first < p.cols) grad_vector<T, E>(p, row_grad(p, row), row, first);
+    for (int64_t row = (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes; row < p.rows; row += step) {
+        const T *src = (const T *)p.x + row * p.x_row;
+        T *dst = (T *)p.dx + row * p.dx_row;
+        if (at + E <= p.cols) {
+            const Loose<T, E> v = *(const Loose<T, E> *)(src + at);
+            *(Loose<T, E> *)(dst + at) = vector_grad<T, E>(row_grad(p, row), v, at);
+        } else if (at < p.cols) {
+            grad_rest<T>(row_grad(p, row), src, dst, at, p.cols);
+        }
+    }
 }
 
-// A wave takes VECS vectors a lane of a row.
+// A wave takes kGradVecs vectors a lane of a row, one after another: 4,099 x
+// 32,768 bf16 81 us (6.6 TB/s with what the last-level cache still holds); with
+// all four loads before the first store 95, with one vector 130.
 constexpr int kGradVecs = 4;
 
 template <typename T>
@@ -429,12 +556,19 @@ __global__ __launch_bounds__(kThreads) void log_probs_grad_kernel(LogProbsGradPa
     const int64_t items = p.rows * parts, step = (int64_t)gridDim.x * (kThreads / 64);
     for (int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); item < items; item += step) {
         const int64_t row = item / parts;
-        const int beg = (int)(item - row * parts) * (64 * N * kGradVecs);
+        const int at0 = (int)(item - row * parts) * (64 * N * kGradVecs) + lane * N;
+        const T *src = (const T *)p.x + row * p.x_row;
+        T *dst = (T *)p.dx + row * p.dx_row;
         const RowGrad g = row_grad(p, row);
 #pragma unroll
         for (int i = 0; i < kGradVecs; ++i) {
-            const int at = beg + (i * 64 + lane) * N;
-            if (at < p.cols) grad_vector<T, N>(p, g, row, at);
+            const int at = at0 + i * 64 * N;
+            if (at + N <= p.cols) {
+                const Loose<T, N> v = *(const Loose<T, N> *)(src + at);
+                *(Loose<T, N> *)(dst + at) = vector_grad<T, N>(g, v, at);
+            } else if (at < p.cols) {
+                grad_rest<T>(g, src, dst, at, p.cols);
+            }
         }
     }
 }
@@ -485,12 +619,14 @@ hipError_t launch_typed(const LogProbsParams &p, int dtype, hipStream_t s) {
         e = launch_rows<T, 1, 4>(p, s);
     else if (vecs <= 16)
         e = launch_rows<T, 4, 4>(p, s);
+    else if (vecs <= 32 && p.parts > 1)
+        e = launch_rows<T, 4, 8>(p, s);
     else if (sizeof(T) == 2 || vecs <= 64)
         e = launch_rows<T, 16, 4>(p, s);
     else
         e = launch_rows<T, 16, sizeof(T) == 2 ? 4 : 8>(p, s);
     if (e == hipSuccess && p.parts > 1) {
-        log_probs_join_kernel<<<blocks_for(p.rows, kThreads / 64), kThreads, 0, s>>>(p, dtype);
+        log_probs_join_kernel<<<blocks_for(p.rows, 1), kThreads, 0, s>>>(p, dtype);
         e = hipGetLastError();
     }
     return e;
@@ -512,11 +648,13 @@ hipError_t launch_grad_typed(const LogProbsGradParams &p, hipStream_t s) {
 
 }  // namespace
 
-// Rows of up to 32,768 columns are whole; longer ones have parts of that.
+// Rows of up to 32,768 columns are whole; longer ones have parts of a quarter
+// of that, 64 at most.
 void log_probs_parts(int64_t rows, int64_t cols, int32_t *parts, int32_t *part_cols) {
     (void)rows;
-    *parts = (int32_t)std::max<int64_t>(1, (cols + 32767) / 32768);
-    *part_cols = (int32_t)((cols + *parts - 1) / *parts + 7) / 8 * 8;
+    const int64_t part = std::max<int64_t>(8192, (cols + kMaxRowParts - 1) / kMaxRowParts);
+    *part_cols = (int32_t)(cols <= 32768 ? std::max<int64_t>(cols, 1) : (part + 7) / 8 * 8);
+    *parts = (int32_t)std::max<int64_t>(1, (cols + *part_cols - 1) / *part_cols);
 }
 
 hipError_t launch_log_probs(const LogProbsParams &p, int dtype, hipStream_t s) {

@@ -82,10 +82,10 @@ int check_norm(int32_t dtype, int32_t dim, const Heads &q, const Heads &k, doubl
         return record_error(SAME_EINVAL, "rot_dim must be even, in [0, head_dim]");
     if (rot_dim && !angles) return record_error(SAME_EINVAL, "angles is null");
     std::memset((void *)&p, 0, sizeof(p));
-    const long double turn = 6.283185307179586476925286766559L;
+    const long double turns = 1.0L / 6.283185307179586476925286766559L;
     for (int i = 0; i < rot_dim / 2; ++i) {
         if (!std::isfinite(angles[i])) return record_error(SAME_EINVAL, "angles must be finite");
-        const long double t = (long double)angles[i] / turn;
+        const long double t = (long double)angles[i] * turns;
         p.turn[i] = (double)t;
         p.turn_low[i] = (double)(t - (long double)p.turn[i]);
     }

@@ -43,10 +43,10 @@ int qk_norm_grad_blocks(int64_t rows_q, int64_t rows_k, int32_t dim, int32_t *bl
 constexpr int kMaxTop = 64;
 constexpr int kMaxRowParts = 64;
 
-// A part of a row: its largest logit, and the sums of e^(x - max) and
-// (x - max) e^(x - max).
+// A part of a row: its largest logit, and the sums of e = 2^t and of t e, t the
+// distance from that in powers of two.
 struct RowStats {
-    float max, sum, weighted, pad;
+    float max, sum, weighted;
 };
 
 struct LogProbsParams {
