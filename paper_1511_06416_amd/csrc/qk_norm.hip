@@ -17,7 +17,6 @@ namespace same {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kMaxBlocks = 1 << 16;  // of a side: a wave goes on to further tokens
 
 template <typename T, int N>
 struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Chunk {
@@ -56,15 +55,22 @@ __device__ __forceinline__ float2 turn_of(const NormParams &p, int32_t position,
     return make_float2((q & 2) ? -c : c, (q & 2) ? -s : s);
 }
 
+// What a lane reads of a row, as it is: W elements at either place.
 template <typename T, int W>
-__device__ __forceinline__ void load(const T *row, int a, int b, float (&v)[2 * W]) {
-    const Chunk<T, W> lo = *(const Chunk<T, W> *)(row + a), hi = *(const Chunk<T, W> *)(row + b);
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        v[i] = (float)lo.v[i];
-        v[W + i] = (float)hi.v[i];
+struct Raw {
+    Chunk<T, W> lo, hi;
+    __device__ __forceinline__ void load(const T *row, int a, int b) {
+        lo = *(const Chunk<T, W> *)(row + a);
+        hi = *(const Chunk<T, W> *)(row + b);
     }
-}
+    __device__ __forceinline__ void widen(float (&v)[2 * W]) const {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            v[i] = (float)lo.v[i];
+            v[W + i] = (float)hi.v[i];
+        }
+    }
+};
 
 template <typename T, int W>
 __device__ __forceinline__ void store(T *row, int a, int b, const float (&v)[2 * W]) {
@@ -104,24 +110,27 @@ __device__ __forceinline__ float inverse_norm(const NormParams &p, const float (
     return r * up;
 }
 
+// A row's loads are under way while the one before it is worked on.
 template <typename T, int W, bool GRAD>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lanes, int split) {
     __shared__ float2 turns[kWaves][kMaxHeadDim / 2];
     __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
-    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool keys = (int)blockIdx.x >= p.side[1].first_block;
     const NormSide &s = p.side[keys];
     const int groups = 64 / lanes, group = lane / lanes, unit = lane & (lanes - 1);
     const int turning = p.half / W;
     const bool used = unit < p.dim / (2 * W);
-    const bool turned = used && unit < turning;
-    const int a = turned ? unit * W : 2 * p.half + (unit - turning) * 2 * W;
+    // a lane without a place of its own reads and computes another's, and writes nothing
+    const int place = used ? unit : 0;
+    const bool turned = place < turning;
+    const int a = turned ? place * W : 2 * p.half + (place - turning) * 2 * W;
     const int b = turned ? a + p.half : a + W;
     float w[2 * W], dw[2 * W];
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        w[i] = used && s.weight ? s.weight[a + i] : 1.0f;
-        w[W + i] = used && s.weight ? s.weight[b + i] : 1.0f;
+        w[i] = s.weight ? s.weight[a + i] : 1.0f;
+        w[W + i] = s.weight ? s.weight[b + i] : 1.0f;
     }
     if (GRAD) {
 #pragma unroll
@@ -130,61 +139,95 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lan
     // items: a token, or one of the `split` parts of its heads
     const int64_t items = s.tokens * split, step = (int64_t)s.blocks * kWaves;
     const int part = (s.heads + split - 1) / split;
-    for (int64_t item = (int64_t)((int)blockIdx.x - s.first_block) * kWaves + own; item < items; item += step) {
-        const int64_t token = split == 1 ? item : item / split;
-        const int first = split == 1 ? 0 : (int)(item - token * split) * part, last = min(first + part, s.heads);
-        if (p.half) {
+    struct Spot {   // where a wave is: its groups' rows are first, first + 1, ...
+        int64_t item, token;
+        int first, last;
+    } at, next;
+    auto enter = [&](Spot &o, int64_t item) {
+        o.item = item;
+        o.token = split == 1 ? item : item / split;
+        o.first = split == 1 ? 0 : (int)(item - o.token * split) * part;
+        o.last = min(o.first + part, s.heads);
+    };
+    Raw<T, W> x, y, next_x, next_y;
+    auto load = [&](const Spot &o, Raw<T, W> &rx, Raw<T, W> &ry) {
+        const int64_t h = min(o.first + group, s.heads - 1);  // rows that are not there repeat the last
+        rx.load((const T *)s.x + o.token * s.x_row + h * s.x_head, a, b);
+        if (GRAD) ry.load((const T *)s.dout + o.token * s.dout_row + h * s.dout_head, a, b);
+    };
+    float c[W], sn[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        c[i] = 1.0f;
+        sn[i] = 0.0f;
+    }
+    enter(at, (int64_t)((int)blockIdx.x - s.first_block) * kWaves + own);
+    bool entered = true;
+    if (at.item < items) load(at, x, y);
+    while (at.item < items) {
+        next = at;
+        next.first += groups;
+        const bool leaves = next.first >= next.last;
+        if (leaves) enter(next, at.item + step);
+        if (next.item < items) load(next, next_x, next_y);
+        if (entered && p.half) {
             wave::sync();
-            if (lane < p.half) turns[own][lane] = turn_of(p, s.positions[token], lane);
+            if (lane < p.half) turns[own][lane] = turn_of(p, s.positions[at.token], lane);
             wave::sync();
-        }
-        float c[W], sn[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float2 t = turned ? turns[own][a + i] : make_float2(1.0f, 0.0f);
-            c[i] = t.x;
-            sn[i] = t.y;
-        }
-        for (int h0 = first; h0 < last; h0 += groups) {
-            const int h = h0 + group;
-            const bool here = used && h < last;
-            float x[2 * W], y[2 * W];
-#pragma unroll
-            for (int i = 0; i < 2 * W; ++i) x[i] = y[i] = 0.0f;
-            if (here) {
-                load<T, W>((const T *)s.x + token * s.x_row + h * s.x_head, a, b, x);
-                if (GRAD) load<T, W>((const T *)s.dout + token * s.dout_row + h * s.dout_head, a, b, y);
-            }
-            const float r = inverse_norm<W>(p, x, lanes);
-#pragma unroll
-            for (int i = 0; i < 2 * W; ++i) x[i] *= r;  // xhat
-            if (!GRAD) {
+            if (turned) {
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    const float lo = x[i] * w[i], hi = x[W + i] * w[W + i];
-                    y[i] = turned ? lo * c[i] - hi * sn[i] : lo;
-                    y[W + i] = turned ? hi * c[i] + lo * sn[i] : hi;
+                    const float2 t = turns[own][a + i];
+                    c[i] = t.x;
+                    sn[i] = t.y;
                 }
-            } else {
-                float t = 0.0f;
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const float lo = y[i], hi = y[W + i];
-                    const float dlo = turned ? lo * c[i] + hi * sn[i] : lo;
-                    const float dhi = turned ? hi * c[i] - lo * sn[i] : hi;
-                    dw[i] = __builtin_fmaf(dlo, x[i], dw[i]);
-                    dw[W + i] = __builtin_fmaf(dhi, x[W + i], dw[W + i]);
-                    y[i] = dlo * w[i];
-                    y[W + i] = dhi * w[W + i];
-                    t = __builtin_fmaf(y[i], x[i], t);
-                    t = __builtin_fmaf(y[W + i], x[W + i], t);
-                }
-                t = group_sum(t, lanes) * p.inv_dim;
-#pragma unroll
-                for (int i = 0; i < 2 * W; ++i) y[i] = r * __builtin_fmaf(-x[i], t, y[i]);
             }
-            if (here) store<T, W>((T *)s.out + (token * s.heads + h) * p.dim, a, b, y);
         }
+        const int h = at.first + group;
+        const bool here = used && h < at.last;
+        float v[2 * W], u[2 * W];
+        x.widen(v);
+        if (!used) {   // nothing to the sums
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i) v[i] = 0.0f;
+        }
+        const float norm = inverse_norm<W>(p, v, lanes);
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i) v[i] *= norm;  // xhat
+        if (!GRAD) {
+            // where nothing turns, cos is 1 and sin 0
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float lo = v[i] * w[i], hi = v[W + i] * w[W + i];
+                u[i] = lo * c[i] - hi * sn[i];
+                u[W + i] = hi * c[i] + lo * sn[i];
+            }
+        } else {
+            y.widen(u);
+            if (!here) {
+#pragma unroll
+                for (int i = 0; i < 2 * W; ++i) u[i] = 0.0f;
+            }
+            float t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float lo = u[i] * c[i] + u[W + i] * sn[i], hi = u[W + i] * c[i] - u[i] * sn[i];
+                dw[i] = __builtin_fmaf(lo, v[i], dw[i]);
+                dw[W + i] = __builtin_fmaf(hi, v[W + i], dw[W + i]);
+                u[i] = lo * w[i];
+                u[W + i] = hi * w[W + i];
+                t = __builtin_fmaf(u[i], v[i], t);
+                t = __builtin_fmaf(u[W + i], v[W + i], t);
+            }
+            t = group_sum(t, lanes) * p.inv_dim;
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i) u[i] = norm * __builtin_fmaf(-v[i], t, u[i]);
+        }
+        if (here) store<T, W>((T *)s.out + (at.token * s.heads + h) * p.dim, a, b, u);
+        entered = leaves;
+        at = next;
+        x = next_x;
+        if (GRAD) y = next_y;
     }
     if (GRAD && s.dweight) {
 #pragma unroll
@@ -210,20 +253,21 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lan
 // The weights' gradients of the blocks' parts, summed in a fixed order: a
 // block takes 32 elements of a side.
 __global__ __launch_bounds__(1024) void qk_norm_join_kernel(NormParams p) {
-    __shared__ float sums[32][33];
+    __shared__ double sums[32][33];
     const NormSide &s = p.side[blockIdx.y];
     if (!s.dweight) return;
     const int e = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
-    float t = 0.0f;
+    double t = 0.0;
     if (e < p.dim)
-        for (int b = row; b < s.blocks; b += 32) t += p.part[(int64_t)(s.first_block + b) * p.dim + e];
+#pragma unroll 8
+        for (int b = row; b < s.blocks; b += 32) t += (double)p.part[(int64_t)(s.first_block + b) * p.dim + e];
     sums[row][threadIdx.x & 31] = t;
     __syncthreads();
     if (row == 0 && e < p.dim) {
-        t = 0.0f;
+        t = 0.0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) t += sums[i][threadIdx.x & 31];
-        s.dweight[e] = t;
+        s.dweight[e] = (float)t;
     }
 }
 
@@ -237,13 +281,18 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
         const int64_t tokens = std::max<int64_t>(1, p.side[0].tokens + p.side[1].tokens);
         const int rounds = (std::max(p.side[0].heads, p.side[1].heads) * lanes + 63) / 64;
         split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, 4096 / tokens));
-    }
-    if (!grad) {
-        int first = 0;
-        for (NormSide &d : p.side) {
-            d.first_block = first;
-            d.blocks = (int)std::min<int64_t>(kMaxBlocks, (d.tokens * split + kWaves - 1) / kWaves);
-            first += d.blocks;
+        int64_t all[2], first = 0;
+        for (int i = 0; i < 2; ++i) all[i] = (p.side[i].tokens * split + kWaves - 1) / kWaves;
+        // blocks go on to further tokens: about three each, of 4,096 to 8,192
+        // (65,536 tokens of 16 + 4 heads 126 us with 8,192, 135 with half of
+        // them, 143 with one token a wave; 21,120 of 8 + 8 heads of 64, 29, 25.5
+        // and 31)
+        const int64_t total = all[0] + all[1];
+        const int64_t want = std::min<int64_t>(total, std::min<int64_t>(8192, std::max<int64_t>(4096, total / 3)));
+        for (int i = 0; i < 2; ++i) {
+            p.side[i].first_block = (int)first;
+            p.side[i].blocks = (int)std::min<int64_t>(all[i], (want * all[i] + total - 1) / std::max<int64_t>(1, total));
+            first += p.side[i].blocks;
         }
     }
     const int blocks = p.side[1].first_block + p.side[1].blocks;
@@ -261,8 +310,6 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_typed(NormParams &p, bool grad, hipStream_t s) {
-    const int rest = p.dim - 2 * p.half;
-    if (sizeof(T) == 2 && p.half % 8 == 0 && rest % 16 == 0) return launch<T, sizeof(T) == 2 ? 8 : 4>(p, grad, s);
     if (p.half % 4 == 0) return launch<T, 4>(p, grad, s);
     if (p.half % 2 == 0) return launch<T, 2>(p, grad, s);
     return launch<T, 1>(p, grad, s);
