@@ -1,0 +1,182 @@
+"""A training step's operators together, as the imputer uses them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1511_06416_amd as same
+from examples.imputer import train_imputer
+from paper_1511_06416_amd.imputer import Imputer, Orthogonal, cross_attention, log_probs, qk_norm
+from tests import test_orthogonalise_gpu as ortho
+from workloads import make_workload
+
+pytestmark = pytest.mark.gpu
+
+
+def plain(q, k, v, wq, wk, pq, pk, angles, q_ptr, k_ptr, answer, counts, targets):
+    """norm, rotation, attention and loss from elementary operations, in the inputs' type."""
+    def norm(x, w, pos):
+        z = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w
+        h = len(angles)
+        t = pos[:, None, None] * torch.from_numpy(angles)
+        a, b = z[..., :h], z[..., h:2 * h]
+        return torch.cat([a * t.cos() - b * t.sin(), b * t.cos() + a * t.sin(), z[..., 2 * h:]], -1)
+    q, k = norm(q, wq, pq), norm(k, wk, pk)
+    seen = torch.zeros_like(q)
+    for s in range(len(q_ptr) - 1):
+        i, j = slice(q_ptr[s], q_ptr[s + 1]), slice(k_ptr[s], k_ptr[s + 1])
+        p = torch.softmax(torch.einsum("ihd,jhd->hij", q[i], k[j]) * q.shape[2] ** -0.5, -1)
+        seen = torch.cat([seen[:i.start], torch.einsum("hij,jhd->ihd", p, v[j]), seen[i.stop:]])
+    logits = seen.flatten(1) @ answer
+    inside = torch.arange(logits.shape[1])[None] < counts[:, None]
+    lp = torch.log_softmax(logits.masked_fill(~inside, -torch.inf), 1)
+    there = torch.where(inside, lp, 0.0)
+    entropy = -(torch.where(inside, there.exp(), 0.0) * there).sum(1)
+    return lp.gather(1, targets.long()[:, None])[:, 0], entropy
+
+
+def test_gradients_of_a_step():
+    """norm + rotation -> attention -> log probabilities and entropy, fp16 heads,
+    against 64 bits.  Each head's number is rounded to fp16 four times on the way
+    out (norm, P, out) and back (dout, P, dS, d): with 2^-11 each, sums of terms
+    of either sign, the gradients' size stays within 16 x 2^-11 of the largest."""
+    q_ptr, k_ptr = [0, 5, 40], [0, 9, 77]
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(n, 2, 32, generator=g).half() for n in (40, 77, 77))
+    wq, wk = (1 + 0.2 * torch.randn(32, generator=g) for _ in range(2))
+    pq, pk = (torch.randint(0, 9, (n,), generator=g, dtype=torch.int32) for n in (40, 77))
+    angles = 100.0 ** (-np.arange(8) / 8.0)
+    answer = torch.randn(64, 6, generator=g) * 0.3
+    counts = torch.randint(2, 7, (40,), generator=g, dtype=torch.int32)
+    targets = (torch.rand(40, generator=g) * counts).to(torch.int32)
+
+    ref = [x.double().requires_grad_() for x in (q, k, v, wq, wk, answer)]
+    lp, h = plain(*ref[:5], pq, pk, angles, q_ptr, k_ptr, ref[5], counts, targets)
+    (-lp.sum() - 0.1 * h.sum()).backward()
+
+    own = [x.cuda().requires_grad_() for x in (q, k, v, wq, wk, answer)]
+    plan = same.same_cross_create(q_ptr, k_ptr, 2, 2, 32, torch.float16)
+    a, b = qk_norm(*own[:2], *own[3:5], pq.cuda(), pk.cuda(), angles)
+    seen = cross_attention(plan, a, b, own[2], plan.new_workspace(backward=True))
+    got_lp, got_h, ids, top = log_probs(seen.flatten(1).float() @ own[5], targets.cuda(), counts.cuda(), 2)
+    (-got_lp.sum() - 0.1 * got_h.sum()).backward()
+    for got, want in ((got_lp, lp), (got_h, h)):
+        assert float((got.cpu() - want).detach().abs().max()) < 16 * 2.0 ** -11 * (1 + float(want.detach().abs().max()))
+    for x, r in zip(own, ref):
+        off = (x.grad.cpu().double() - r.grad).abs().max()
+        assert float(off) < 16 * 2.0 ** -11 * float(r.grad.abs().max())
+    assert bool((top[:, 0] >= got_lp - 1e-6).all()) and bool((ids < counts.cuda()[:, None]).all())
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_orthogonal_steps(nesterov):
+    """Three steps of a matrix, a batch and one held row by row, against the
+    formula with the operator's own tolerance."""
+    g = torch.Generator().manual_seed(1)
+    shapes, kept = [(20, 12), (3, 6, 9), (5, 24)], [(1, 20, 12), (3, 6, 9), (10, 3, 4)]
+    start = [torch.randn(s, generator=g) for s in shapes]
+    params = [torch.nn.Parameter(x.clone().cuda()) for x in start]
+    opt = Orthogonal([dict(params=params[:2]), dict(params=params[2:], shape=(3, 4))], lr=0.1, nesterov=nesterov,
+                     weight_decay=0.5)
+    want, momentum = [x.double() for x in start], [torch.zeros(s, dtype=torch.float64) for s in shapes]
+    for _ in range(3):
+        for i, p in enumerate(params):
+            grad = torch.randn(shapes[i], generator=g)
+            p.grad = grad.cuda()
+            momentum[i] = 0.95 * momentum[i] + grad.double()
+            u = grad.double() + 0.95 * momentum[i] if nesterov else momentum[i]
+            u = u.view(kept[i])
+            o = torch.stack([ortho.exact(x, same.NEWTON_SCHULZ, 1e-7) for x in u])
+            scale = max(1.0, kept[i][1] / kept[i][2]) ** 0.5
+            want[i] = 0.95 * want[i] - 0.1 * scale * o.view(shapes[i])
+        opt.step()
+    for p, w in zip(params, want):
+        # a step's share is at most 0.1 x 1.3 x 1.3; fp32 updates are off by less than 1e-5 of it, momentum and
+        # weights by a few 2^-24 of themselves
+        assert float((p.detach().cpu().double() - w).abs().max()) < 3 * (1e-5 + 8 * 2.0 ** -24 * 4)
+
+
+def test_training_with_positions_runs():
+    """Several columns in one segment, an entry's column as its position: every
+    parameter gets a finite gradient and a step, and answers change with the
+    positions."""
+    columns, segs = 4, 50
+    torch.manual_seed(3)
+    net = Imputer(2, 2, heads=4, head_dim=32, norm=True, rot_dim=32).cuda()
+    opts = net.optimisers()
+    ptr = np.arange(segs + 1) * columns
+    plan = same.same_cross_create(ptr, ptr, 4, 4, 32, net.dtype)
+    ws = plan.new_workspace(backward=True)
+    n = segs * columns
+    nodes = torch.zeros(n, dtype=torch.int64, device="cuda")
+    pos = torch.arange(columns, dtype=torch.int32, device="cuda").repeat(segs)
+    before = [p.detach().clone() for p in net.parameters()]
+
+    def answers(states, positions):
+        logits = net(plan, ws, nodes + 1, nodes, states, query_positions=positions, key_positions=pos)
+        return log_probs(logits, states.to(torch.int32))[0]
+
+    for _ in range(3):
+        states = torch.randint(0, 2, (n,), device="cuda")
+        for o in opts:
+            o.zero_grad(set_to_none=True)
+        (-answers(states, pos).mean()).backward()
+        assert all(p.grad is not None and bool(p.grad.isfinite().all()) for p in net.parameters())
+        for o in opts:
+            o.step()
+    assert all(bool(p.isfinite().all()) and not torch.equal(p, b) for p, b in zip(net.parameters(), before))
+    with torch.no_grad():
+        assert not torch.equal(answers(states, pos), answers(states, pos.flip(0)))
+
+
+def test_a_captured_step():
+    """Norm, attention, log probabilities, their gradients and the update in one
+    graph, replayed with new inputs between eager work."""
+    q_ptr = [0, 30, 64]
+    plan = same.same_cross_create(q_ptr, q_ptr, 2, 2, 32, torch.bfloat16)
+    ws = plan.new_workspace(backward=True)
+    x = torch.randn(64, 2, 32, device="cuda").bfloat16()
+    w = torch.randn(64, 40, device="cuda")
+    targets = torch.randint(0, 40, (64,), device="cuda", dtype=torch.int32)
+    pos = torch.arange(64, dtype=torch.int32, device="cuda")
+    angles = 10.0 ** -np.arange(16.0)
+    out = {}
+
+    def step():
+        q, a = x.detach().requires_grad_(), w.detach().requires_grad_()
+        qn, kn = qk_norm(q, q, None, None, pos, pos, angles)
+        lp, h, ids, top = log_probs(cross_attention(plan, qn, kn, q, ws).flatten(1).float() @ a, targets, None, 3)
+        dq, da = torch.autograd.grad(-lp.sum() - h.sum(), (q, a))
+        update = torch.empty_like(da)
+        room = torch.empty(same.same_orthogonalise_workspace_size(1, 64, 40, da.dtype), dtype=torch.uint8, device="cuda")
+        same.same_orthogonalise(da, update, room)
+        for name, t in (("lp", lp), ("h", h), ("ids", ids), ("top", top), ("dq", dq), ("da", da), ("update", update)):
+            if name in out:
+                out[name].copy_(t.detach())
+            else:
+                out[name] = t.detach().clone()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (1, 2, 1):
+        torch.manual_seed(seed)
+        x.copy_(torch.randn(64, 2, 32, device="cuda"))
+        w.copy_(torch.randn(64, 40, device="cuda"))
+        for t in out.values():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: t.clone() for n, t in out.items()}
+        step()
+        for n in ("lp", "h", "ids", "top", "dq", "da", "update"):
+            assert torch.equal(got[n], out[n]), n
+
+
+def test_example_runs():
+    auc, per_step, seconds = train_imputer(make_workload(4, n_cols=400), 5, orthogonal=True)
+    assert 0.0 <= auc <= 1.0 and per_step > 0 and seconds > 0
