@@ -23,7 +23,6 @@ constexpr int64_t kMaxBlocks = 1 << 21;  // of up to 1024 threads: 2^32 and more
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
-constexpr int kCandidates = 512;
 
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
@@ -182,18 +181,19 @@ __global__ __launch_bounds__(kThreads) void log_probs_short_kernel(LogProbsParam
 // lane.  Candidates for the alternatives: the n_top-th largest of the 64 lanes'
 // maxima (over the row's waves) bounds the n_top-th largest logit from below,
 // and about as many logits reach it as are wanted; they are collected in LDS
-// and ranked by counting.  Where more than kCandidates reach it (many alike),
+// and ranked by counting.  Where more than kept reach it (many alike),
 // the alternatives are found one after another.
 
 template <int WAVES, bool TOP>
 struct RowShared {
+    static constexpr int kKept = WAVES == 1 ? 512 : WAVES == 4 ? 256 : 128;   // candidates of a wave
     RowStats stats[WAVES];
     uint32_t largest[TOP ? WAVES : 1][64];
-    uint64_t keys[TOP ? kCandidates : 1];
+    uint64_t keys[TOP ? WAVES : 1][TOP ? kKept : 1];
+    int count[WAVES];
     uint64_t best[WAVES];
     RowStats all;
     uint32_t bound;
-    int count;
 };
 
 template <int WAVES>
@@ -279,10 +279,11 @@ template <typename T, int WAVES, int VECS, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_kernel(LogProbsParams p) {
     constexpr int N = 16 / sizeof(T), ROWS = WAVES == 1 ? kThreads / 64 : 1;
     __shared__ RowShared<WAVES, TOP> shared[ROWS];
-    const int lane = threadIdx.x & 63, own = WAVES == 1 ? 0 : threadIdx.x >> 6;
-    RowShared<WAVES, TOP> &sh = shared[WAVES == 1 ? threadIdx.x >> 6 : 0];
+    const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int own = WAVES == 1 ? 0 : wave_id, which = WAVES == 1 ? wave_id : 0;
+    RowShared<WAVES, TOP> &sh = shared[which];
     const int64_t items = p.rows * p.parts, step = (int64_t)gridDim.x * ROWS;
-    for (int64_t item = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0); item < items; item += step) {
+    for (int64_t item = (int64_t)blockIdx.x * ROWS + which; item < items; item += step) {
         const int64_t row = p.parts == 1 ? item : item / p.parts;
         const int part = p.parts == 1 ? 0 : (int)(item - row * p.parts);
         const int n = count_of(p.counts, row, p.cols);
@@ -303,10 +304,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
 #pragma unroll
             for (int e = 0; e < N; ++e) most = __builtin_fmaxf(most, (float)v[i].v[e]);
         RowStats r{wave::reduce(most, 64, wave::Max()), 0.0f, 0.0f};
-        if (TOP) {
-            sh.largest[own][lane] = at0 < end ? ordered(most) : 0;
-            if (own == 0 && lane == 0) sh.count = 0;
-        }
+        if (TOP) sh.largest[own][lane] = at0 < end ? ordered(most) : 0;
         const Place place(r.max);
         if (place.far) {
 #pragma unroll
@@ -348,26 +346,36 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
             row_sync<WAVES>();
             const uint32_t bound = sh.bound;
             const float low = bound ? value_of(bound) : -kInf;
-            if (!(most < low)) {
+            int mine = 0;
+            if (__ballot(!(most < low))) {
 #pragma unroll
                 for (int i = 0; i < VECS; ++i) {
                     if (sizeof(T) == 2) keep_packed(v[i]);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         const float x = (float)v[i].v[e];
-                        const int at = at0 + i * WAVES * 64 * N + e;
-                        if (!(x < low)) {
+                        if (__ballot(!(x < low))) {
+                            const int at = at0 + i * WAVES * 64 * N + e;
                             const uint32_t u = ordered(x);
-                            if (u >= bound && at < end) {
-                                const int slot = atomicAdd(&sh.count, 1);
-                                if (slot < kCandidates) sh.keys[slot] = key_of(u, (uint32_t)at);
-                            }
+                            const bool in = u >= bound && at < end;
+                            const uint64_t who = __ballot(in);
+                            const int slot = mine + __builtin_amdgcn_mbcnt_hi(
+                                                        (uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                            if (in && slot < sh.kKept) sh.keys[own][slot] = key_of(u, (uint32_t)at);
+                            mine += __builtin_popcountll(who);
                         }
                     }
                 }
             }
+            if (lane == 0) sh.count[own] = mine;
             row_sync<WAVES>();
-            const int found = sh.count;
+            int found = 0;
+            bool kept = true;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                found += sh.count[w];
+                kept = kept && sh.count[w] <= sh.kKept;
+            }
             const RowValues all(sh.all);
             const int64_t out = item * p.n_top;
             auto put = [&](int k, uint64_t key) {
@@ -376,13 +384,24 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
                 else
                     put_top(p, out + k, key, all);
             };
-            if (found <= kCandidates) {
+            // candidate c of the waves' lists, one after another
+            auto candidate = [&](int c) {
+                uint64_t key = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const int n_w = sh.count[w];
+                    if (c >= 0 && c < n_w) key = sh.keys[w][c];
+                    c -= n_w;
+                }
+                return key;
+            };
+            if (kept) {
                 // a wave takes 64 candidates; the others pass by in registers
                 for (int c0 = own * 64; c0 < found; c0 += WAVES * 64) {
-                    const uint64_t key = c0 + lane < found ? sh.keys[c0 + lane] : 0;
+                    const uint64_t key = candidate(c0 + lane);
                     int rank = 0;
                     for (int j0 = 0; j0 < found; j0 += 64) {
-                        const uint64_t others = j0 + lane < found ? sh.keys[j0 + lane] : 0;
+                        const uint64_t others = j0 == c0 ? key : candidate(j0 + lane);
                         const int n_others = min(64, found - j0);
                         for (int j = 0; j < n_others; ++j) {
                             const uint64_t other =
@@ -605,6 +624,9 @@ hipError_t launch_typed(const LogProbsParams &p, int dtype, hipStream_t s) {
     if (p.cols <= kShort) {
         if (p.cols <= 2) {
             log_probs_short_kernel<T, 2><<<blocks_for(p.rows, kThreads), kThreads, 0, s>>>(p, 1);
+        } else if (p.cols % 8 == 0) {
+            const int lanes = lanes_for(p.cols, 8);
+            log_probs_short_kernel<T, 8><<<blocks_for(p.rows, kThreads / lanes), kThreads, 0, s>>>(p, lanes);
         } else {
             const int lanes = lanes_for(p.cols, 4);
             log_probs_short_kernel<T, 4><<<blocks_for(p.rows, kThreads / lanes), kThreads, 0, s>>>(p, lanes);
@@ -636,6 +658,9 @@ template <typename T>
 hipError_t launch_grad_typed(const LogProbsGradParams &p, hipStream_t s) {
     if (p.cols <= 2) {
         log_probs_grad_short_kernel<T, 2><<<blocks_for(p.rows, kThreads), kThreads, 0, s>>>(p, 1);
+    } else if (p.cols <= kShort && p.cols % 8 == 0) {
+        const int lanes = lanes_for(p.cols, 8);
+        log_probs_grad_short_kernel<T, 8><<<blocks_for(p.rows, kThreads / lanes), kThreads, 0, s>>>(p, lanes);
     } else if (p.cols <= kShort) {
         const int lanes = lanes_for(p.cols, 4);
         log_probs_grad_short_kernel<T, 4><<<blocks_for(p.rows, kThreads / lanes), kThreads, 0, s>>>(p, lanes);

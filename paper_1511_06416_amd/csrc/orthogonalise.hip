@@ -14,24 +14,16 @@
 // to both places.
 #include <algorithm>
 
+#include "halves.hpp"
 #include "step.hpp"
 #include "wave.hpp"
 
 namespace same {
 namespace {
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 constexpr int kThreads = 256;
 constexpr int kStage = 32;  // columns of a stage
 constexpr int kTurn = 36;   // floats of a row of a tile that is turned
-
-__device__ __forceinline__ void split(float v, _Float16 &hi, _Float16 &lo) {
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
-}
 
 // Sums over a block, in every thread.
 __device__ __forceinline__ double block_sum(double t) {
@@ -108,22 +100,14 @@ __global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, in
 #pragma unroll
     for (int r = threadIdx.x >> 3; r < 64; r += kThreads / 8) {
         f16x8 hi, lo;
-        auto halves = [&](int e, float v) {
-            _Float16 h, l;
-            split(v, h, l);
-            hi[e] = h;
-            lo[e] = l;
-        };
         if (i0 + r < p.np && j0 + c < p.mp) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) halves(e, tile[r][c + e]);
+            split_all<8>([&](int e) { return tile[r][c + e]; }, hi, lo);
             const int64_t to = x0 + (int64_t)(i0 + r) * p.mp + j0 + c;
             *(f16x8 *)(p.x.hi + to) = hi;
             if (LOW) *(f16x8 *)(p.x.lo + to) = lo;
         }
         if (j0 + r < p.mp && i0 + c < p.np) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) halves(e, tile[c + e][r]);
+            split_all<8>([&](int e) { return tile[c + e][r]; }, hi, lo);
             const int64_t to = x0 + (int64_t)(j0 + r) * p.np + i0 + c;
             *(f16x8 *)(p.xt[0].hi + to) = hi;
             *(f16x8 *)(p.xt[0].lo + to) = lo;
@@ -176,16 +160,22 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     static_assert(WM * WN * 32 * kTurn * 4 <= STAGES * kRows * kStage * 2, "tiles are turned where operands were");
     __shared__ _Float16 stage[STAGES][kRows * kStage];
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6;
+    // Neighbouring blocks go to different XCDs: each gets a stretch of tiles, which
+    // share operands in its L2.
+    const int tiles = gridDim.x, each = tiles / 8, rest = tiles % 8, xcd = blockIdx.x % 8;
+    const int tile = xcd * each + min(xcd, rest) + blockIdx.x / 8;
     int ti, tj;
     if (KIND == kGram || KIND == kSquare) {
         // on and above the diagonal, by columns
-        tj = (int)((__builtin_sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-        while ((tj + 1) * (tj + 2) / 2 <= (int)blockIdx.x) ++tj;
-        while (tj * (tj + 1) / 2 > (int)blockIdx.x) --tj;
-        ti = blockIdx.x - tj * (tj + 1) / 2;
+        tj = (int)((__builtin_sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
+        while ((tj + 1) * (tj + 2) / 2 <= tile) ++tj;
+        while (tj * (tj + 1) / 2 > tile) --tj;
+        ti = tile - tj * (tj + 1) / 2;
     } else {
-        ti = blockIdx.x % tiles_i;
-        tj = blockIdx.x / tiles_i;
+        // bands of four rows, by columns
+        const int band = tile / (4 * tiles_j), height = min(4, tiles_i - 4 * band), at = tile - band * 4 * tiles_j;
+        ti = 4 * band + at % height;
+        tj = at / height;
     }
     const int64_t mat = blockIdx.y;
     const int64_t x0 = mat * p.np * p.mp, a0 = mat * p.np * p.np;
@@ -232,45 +222,65 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int wi = (own % WM) * (TM / WM), wj = (own / WM) * (TN / WN);
-    auto operand = [&](const _Float16 *plane, int row, int t) {
-        return *(const f16x8 *)&plane[row * kStage + (((2 * t + (lane >> 5)) ^ ((row >> 2) & 3)) << 3)];
+    struct Operands {
+        f16x8 l[PL][MT], r[PL][NT];
+    };
+    // where this lane's chunks of a stage's first 16 columns are; the others' are one bit apart
+    const int turned = ((lane >> 5) ^ ((lane >> 2) & 3)) << 3;
+    const int off_l = (wi + (lane & 31)) * kStage + turned, off_r = PL * TM * kStage + (wj + (lane & 31)) * kStage + turned;
+    auto fill = [&](int buffer, int t, Operands &o) {
+        const _Float16 *at_l = &stage[buffer][off_l ^ (t << 4)], *at_r = &stage[buffer][off_r ^ (t << 4)];
+#pragma unroll
+        for (int h = 0; h < PL; ++h) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) o.l[h][i] = *(const f16x8 *)(at_l + (h * TM + 32 * i) * kStage);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) o.r[h][j] = *(const f16x8 *)(at_r + (h * TN + 32 * j) * kStage);
+        }
+    };
+    auto multiply = [&](const Operands &o) {
+        __builtin_amdgcn_sched_barrier(0);   // reads under way stay before the products
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if (PL == 2) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[PL - 1][i], o.r[0][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[0][i], o.r[PL - 1][j], acc[i][j], 0, 0, 0);
+                }
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[0][i], o.r[0][j], acc[i][j], 0, 0, 0);
+            }
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
     };
     const int stages = depth / kStage;
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
         if (s < stages) fetch(s, s * kStage);
-    int buffer = 0, next = STAGES - 1;
-    for (int s = 0; s < stages; ++s) {
-        // this stage is there, and everyone has left the one that is fetched into
+    // A wave reads half a stage ahead of its products.  When it arrives at a
+    // stage, that is there, and everyone has left the one before it, whose place
+    // the next fetch takes.
+    auto reach = [&](int s) {
         if (s + STAGES - 2 < stages)
             arrive<kLoads * (STAGES - 2)>();
         else
             arrive<0>();
+    };
+    Operands now, then;
+    reach(0);
+    fill(0, 0, now);
+    for (int s = 0, buffer = 0, next = STAGES - 1; s < stages; ++s) {
         if (s + STAGES - 1 < stages) fetch(next, (s + STAGES - 1) * kStage);
-        const _Float16 *at_p = stage[buffer], *at_q = stage[buffer] + PL * TM * kStage;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f16x8 l[PL][MT], r[PL][NT];
-#pragma unroll
-            for (int h = 0; h < PL; ++h) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) l[h][i] = operand(at_p + h * TM * kStage, wi + 32 * i + (lane & 31), t);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) r[h][j] = operand(at_q + h * TN * kStage, wj + 32 * j + (lane & 31), t);
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (PL == 2) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[PL - 1][i], r[0][j], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[0][i], r[PL - 1][j], acc[i][j], 0, 0, 0);
-                    }
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[0][i], r[0][j], acc[i][j], 0, 0, 0);
-                }
-        }
+        fill(buffer, 1, then);
+        multiply(now);
         buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
         next = next + 1 == STAGES ? 0 : next + 1;
+        if (s + 1 < stages) {
+            reach(s + 1);
+            fill(buffer, 0, now);
+        }
+        multiply(then);
     }
     // The way out: a wave turns a tile of 32 x 32 at a time in LDS, so that both
     // places are read and written 16 bytes a lane, 64 bytes of a row.
@@ -326,11 +336,8 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
                     float x = take * v[e >> 2][e & 3];
                     if (KIND != kGram) x = __builtin_fmaf(keep, (float)hi[e] + (float)lo[e], x);
                     v[e >> 2][e & 3] = x;
-                    _Float16 h, l;
-                    split(x, h, l);
-                    hi[e] = h;
-                    lo[e] = l;
                 }
+                split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
                 if (!diagonal) {
                     here[0] = v[0];
                     here[1] = v[1];
@@ -350,14 +357,8 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
                     f32x4 v[2];
                     f16x8 hi, lo;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = turn[j + e][i];
-                        v[e >> 2][e & 3] = x;
-                        _Float16 h, l;
-                        split(x, h, l);
-                        hi[e] = h;
-                        lo[e] = l;
-                    }
+                    for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = turn[j + e][i];
+                    split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
                     if (KIND == kLast) {
                         write_out<T>(p, mat, i0 + i, p.n, j0 + j, p.m, v);
                     } else {
@@ -385,7 +386,7 @@ void run_product(const OrthoParams &p, int step, hipStream_t s) {
 template <int PROD>
 int pick_tile(const OrthoParams &p, bool symmetric, int depth) {
     constexpr int kTiles[4] = {64, 128, 192, 256};
-    constexpr double kStageUs[2][4] = {{0.17, 0.37, 0.77, 1.16}, {0.33, 0.78, 1.63, 2.8}};
+    constexpr double kStageUs[2][4] = {{0.17, 0.34, 0.65, 1.05}, {0.33, 0.76, 1.45, 2.7}};
     constexpr double kWayUs[4] = {3.0, 5.0, 7.0, 9.0};
     int best = 0;
     double least = 0.0;
@@ -405,9 +406,9 @@ template <typename T, int PROD, int KIND>
 void run_pass(const OrthoParams &p, int step, hipStream_t s) {
     switch (pick_tile<PROD>(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np)) {
     case 0: return run_product<T, 64, 2, 2, 3, PROD, KIND>(p, step, s);
-    case 1: return run_product<T, 128, 2, 2, PROD == 1 ? 4 : 2, PROD, KIND>(p, step, s);
-    case 2: return run_product<T, 192, 2, 3, PROD == 1 ? 4 : 3, PROD, KIND>(p, step, s);
-    default: return run_product<T, 256, 4, 2, PROD == 1 ? 4 : 2, PROD, KIND>(p, step, s);
+    case 1: return run_product<T, 128, 2, 2, PROD == 1 ? 3 : 2, PROD, KIND>(p, step, s);
+    case 2: return run_product<T, 192, 2, PROD == 1 ? 3 : 2, PROD == 1 ? 4 : 3, PROD, KIND>(p, step, s);
+    default: return run_product<T, 256, 2, 4, PROD == 1 ? 3 : 2, PROD, KIND>(p, step, s);
     }
 }
 
@@ -453,7 +454,8 @@ hipError_t launch_orthogonalise(const OrthoParams &all, int64_t batch, int dtype
         p.n_mats = std::min(batch, all.n_mats - first);
         p.g = (const char *)all.g + first * all.g_mat * size;
         p.out = (char *)all.out + first * all.out_mat * size;
-        const hipError_t e = p.n <= kSmallSide ? launch_ortho_small(p, dtype, s)
+        const hipError_t e = p.n <= kSmallSide                          ? launch_ortho_small(p, dtype, s)
+                             : ortho_whole(p.n, p.m)                    ? launch_ortho_whole(p, dtype, s)
                              : dtype == 2 ? run_typed<__bf16, 1>(p, s)
                              : dtype == 1 ? run_typed<_Float16, 3>(p, s)
                                           : run_typed<float, 3>(p, s);

@@ -204,6 +204,11 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
         l.total = l.small_parts + l.small_factors;
         return SAME_OK;
     }
+    if (same::ortho_whole(l.n, l.m)) {  // nothing is kept outside the block
+        l.batch = std::min<int64_t>(n_mats, (int64_t)1 << 21);
+        l.total = 0;
+        return SAME_OK;
+    }
     const int64_t pad = 32;  // a stage of the products
     l.np = (l.n + pad - 1) / pad * pad;
     l.mp = (l.m + pad - 1) / pad * pad;

@@ -114,6 +114,12 @@ constexpr int kSmallSide = 32;  // of updates that take the small kernels
 void ortho_small_parts(int64_t n, int64_t m, int32_t *parts, int32_t *part_cols, size_t *tile_bytes);
 hipError_t launch_ortho_small(const OrthoParams &p, int dtype, hipStream_t s);
 
+// Updates that one block holds.
+inline bool ortho_whole(int64_t n, int64_t m) {
+    return n <= 96 ? m <= 256 : n <= 128 && m <= 128;
+}
+hipError_t launch_ortho_whole(const OrthoParams &p, int dtype, hipStream_t s);
+
 // Matrices that share the planes (or tiles) of the workspace, in turn.
 int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp);
 hipError_t launch_orthogonalise(const OrthoParams &p, int64_t batch, int dtype, hipStream_t s);

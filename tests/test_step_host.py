@@ -100,8 +100,8 @@ def test_nothing_to_do(lib):
 
 def ortho_rc(lib, **kw):
     coefs = np.ascontiguousarray(kw.pop("coefs", same.NEWTON_SCHULZ), dtype=np.float64)
-    a = dict(dict(dtype=same.SAME_F32, g=A, g_mat=2000, g_row=50, n_mats=2, rows=40, cols=50, coefs=coefs.ctypes.data,
-                  steps=len(coefs), eps=1e-7, scale=1.0, out=A << 1, out_mat=2000, out_row=50, workspace=A << 2), **kw)
+    a = dict(dict(dtype=same.SAME_F32, g=A, g_mat=21000, g_row=150, n_mats=2, rows=140, cols=150, coefs=coefs.ctypes.data,
+                  steps=len(coefs), eps=1e-7, scale=1.0, out=A << 1, out_mat=21000, out_row=150, workspace=A << 2), **kw)
     return lib.same_orthogonalise(*a.values(), None)
 
 
@@ -113,7 +113,7 @@ def ortho_rc(lib, **kw):
     (same.SAME_EINVAL, dict(coefs=[(3.0, 0.0, 0.0)] * 3)), (same.SAME_EINVAL, dict(steps=0)), (same.SAME_EINVAL, dict(steps=33)),
     (same.SAME_EINVAL, dict(eps=0.0)), (same.SAME_EINVAL, dict(eps=np.inf)), (same.SAME_EINVAL, dict(scale=1e39)),
     (same.SAME_EINVAL, dict(g=None)), (same.SAME_EINVAL, dict(out=None)), (same.SAME_EALIGN, dict(g=A + 2)),
-    (same.SAME_EINVAL, dict(g_row=-1)), (same.SAME_EINVAL, dict(out_row=49)), (same.SAME_EINVAL, dict(out_mat=1999)),
+    (same.SAME_EINVAL, dict(g_row=-1)), (same.SAME_EINVAL, dict(out_row=149)), (same.SAME_EINVAL, dict(out_mat=20999)),
     (same.SAME_ESIZE, dict(g_mat=1 << 61)), (same.SAME_EINVAL, dict(workspace=None)), (same.SAME_EALIGN, dict(workspace=A + 64)),
     (same.SAME_EINVAL, dict(out=A + 4)), (same.SAME_EINVAL, dict(workspace=A)), (same.SAME_EINVAL, dict(out=A << 2)),
     (same.SAME_EINVAL, dict(out=A, workspace=A)),
@@ -129,13 +129,15 @@ def test_orthogonalise_nothing_to_do(lib):
 
 def test_workspace_sizes():
     assert same.same_log_probs_workspace_size(1000, 64, 20) == 0
-    assert same.same_log_probs_workspace_size(3, 1 << 21, 20) >= 3 * 64 * (16 + 20 * 8)
+    assert same.same_log_probs_workspace_size(3, 1 << 21, 20) >= 3 * 64 * (12 + 20 * 8)
     assert same.same_qk_norm_workspace_size(64, 0, 1, 0, 1) == 0
     assert 4 * 64 <= same.same_qk_norm_workspace_size(64, 1 << 30, 8, 1, 1) <= 1 << 21
     assert same.same_orthogonalise_workspace_size(0, 5, 5, torch.float32) == 0
-    # many matrices share their planes
-    few, many = (same.same_orthogonalise_workspace_size(n, 3, 5, torch.float32) for n in (1 << 14, 1 << 20))
-    assert few == many
+    # many matrices share their planes; those that a block holds need none
+    few, many = (same.same_orthogonalise_workspace_size(n, 200, 300, torch.float32) for n in (1 << 14, 1 << 20))
+    assert 0 < few == many
+    for rows, cols in ((32, 2048), (256, 64), (96, 256), (128, 128)):
+        assert same.same_orthogonalise_workspace_size(1 << 20, rows, cols, torch.float32) == 0
     for call, args in ((same.same_log_probs_workspace_size, (-1, 5, 0)), (same.same_log_probs_workspace_size, (1, 5, 65)),
                        (same.same_qk_norm_workspace_size, (12, 1, 1, 1, 1)),
                        (same.same_orthogonalise_workspace_size, (1, -1, 1, torch.float32))):
