@@ -136,6 +136,89 @@ __device__ __forceinline__ void write_out(const OrthoParams &p, int64_t mat, int
 
 enum Kind { kGram, kSquare, kUpdate, kLast };
 
+// What a product becomes, from a tile of 32 x 32 that a wave holds in LDS, column
+// by column: both of its places are read and written 16 bytes a lane, 64 bytes of
+// a row.
+template <typename T, int KIND, int PL>
+__device__ __forceinline__ void leave(const OrthoParams &p, int64_t mat, int step, int i0, int j0,
+                                      float (*turn)[kTurn]) {
+    constexpr bool symmetric = KIND == kGram || KIND == kSquare;
+    // Second halves are read by three products, or as what stays of the old: by
+    // the next square at A[j][i], by the next update at X^T.
+    constexpr bool kLowT = PL == 2 || KIND != kSquare, kLowD = PL == 2;
+    const int lane = threadIdx.x & 63;
+    const float keep = KIND == kGram ? 0.0f : KIND == kSquare ? p.coef[step][1] * (p.sb / p.sa) : p.coef[step][0];
+    const float take = KIND == kGram     ? p.sa / (p.sx * p.sx)
+                       : KIND == kSquare ? p.coef[step][2] * (p.sb / (p.sa * p.sa))
+                                         : 1.0f / p.sb;
+    const Planes old = KIND == kSquare ? p.a : p.xt[step & 1];
+    const Planes to_t = KIND == kGram ? p.a : KIND == kSquare ? p.b : p.xt[(step & 1) ^ 1];
+    const Planes to_d = KIND == kGram ? p.a : KIND == kSquare ? p.b : p.x;
+    const int64_t t0 = mat * p.np * (symmetric ? p.np : p.mp);
+    const int ld_d = symmetric ? p.np : p.mp;
+    const bool diagonal = symmetric && i0 == j0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int j = 16 * r + (lane >> 2), i = 8 * (lane & 3);
+        const int64_t at = t0 + (int64_t)(j0 + j) * p.np + i0 + i;
+        f32x4 *const here = (f32x4 *)&turn[j][i];
+        f32x4 v[2] = {here[0], here[1]};
+        if (diagonal) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i + e > j) v[e >> 2][e & 3] = turn[i + e][j];
+        }
+        f16x8 hi, lo;
+        if (KIND != kGram) {
+            hi = *(const f16x8 *)(old.hi + at);
+            lo = *(const f16x8 *)(old.lo + at);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = take * v[e >> 2][e & 3];
+            if (KIND != kGram) x = __builtin_fmaf(keep, (float)hi[e] + (float)lo[e], x);
+            v[e >> 2][e & 3] = x;
+        }
+        split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
+        if (!diagonal) {
+            here[0] = v[0];
+            here[1] = v[1];
+        }
+        if (KIND == kLast) {
+            if (p.tall) write_out<T>(p, mat, j0 + j, p.m, i0 + i, p.n, v);
+        } else {
+            *(f16x8 *)(to_t.hi + at) = hi;
+            if (kLowT) *(f16x8 *)(to_t.lo + at) = lo;
+        }
+    }
+    wave::sync();
+    if (KIND == kLast ? p.tall : diagonal) return;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int i = 16 * r + (lane & 15), j = 8 * (lane >> 4);
+        f32x4 v[2];
+        f16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = turn[j + e][i];
+        if (KIND == kLast) {
+            write_out<T>(p, mat, i0 + i, p.n, j0 + j, p.m, v);
+        } else {
+            split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
+            const int64_t at = t0 + (int64_t)(i0 + i) * ld_d + j0 + j;
+            *(f16x8 *)(to_d.hi + at) = hi;
+            if (kLowD) *(f16x8 *)(to_d.lo + at) = lo;
+        }
+    }
+}
+
+// Tile `tile` on and above the diagonal, by columns.
+__device__ __forceinline__ void triangle(int tile, int &ti, int &tj) {
+    tj = (int)((__builtin_sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
+    while ((tj + 1) * (tj + 2) / 2 <= tile) ++tj;
+    while (tj * (tj + 1) / 2 > tile) --tj;
+    ti = tile - tj * (tj + 1) / 2;
+}
+
 // Waits until at most N of the wave's loads are under way, then for the other
 // waves.  A barrier alone does not wait for loads into LDS.
 template <int N>
@@ -166,11 +249,7 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     const int tile = xcd * each + min(xcd, rest) + blockIdx.x / 8;
     int ti, tj;
     if (KIND == kGram || KIND == kSquare) {
-        // on and above the diagonal, by columns
-        tj = (int)((__builtin_sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
-        while ((tj + 1) * (tj + 2) / 2 <= tile) ++tj;
-        while (tj * (tj + 1) / 2 > tile) --tj;
-        ti = tile - tj * (tj + 1) / 2;
+        triangle(tile, ti, tj);
     } else {
         // bands of four rows, by columns
         const int band = tile / (4 * tiles_j), height = min(4, tiles_i - 4 * band), at = tile - band * 4 * tiles_j;
@@ -179,12 +258,14 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     }
     const int64_t mat = blockIdx.y;
     const int64_t x0 = mat * p.np * p.mp, a0 = mat * p.np * p.np;
-    const int ld = KIND == kGram ? p.mp : p.np, depth = ld;
+    const int ld = KIND == kGram ? p.mp : p.np;
     const int rows_j = KIND == kGram || KIND == kSquare ? p.np : p.mp;
-    const Planes from = p.xt[step & 1], to = p.xt[(step & 1) ^ 1];
     const Planes left = KIND == kGram ? p.x : KIND == kSquare ? p.a : p.b;
-    const Planes right = KIND == kGram ? p.x : KIND == kSquare ? p.a : from;
-    const int64_t l0 = KIND == kGram ? x0 : a0, r0 = KIND == kSquare ? a0 : x0;
+    const Planes right = KIND == kGram ? p.x : KIND == kSquare ? p.a : p.xt[step & 1];
+    // a part of a long sum, in stages
+    const int all = ld / kStage, share = KIND == kGram ? (all + p.splits - 1) / p.splits : all;
+    const int first = KIND == kGram ? min((int)blockIdx.z * share, all) : 0, stages = min(share, all - first);
+    const int64_t l0 = (KIND == kGram ? x0 : a0) + first * kStage, r0 = (KIND == kSquare ? a0 : x0) + first * kStage;
     // what this lane stages: offsets of its chunks
     int off_p[kLoadsP], off_q[kLoadsQ];
 #pragma unroll
@@ -254,7 +335,6 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    const int stages = depth / kStage;
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
         if (s < stages) fetch(s, s * kStage);
@@ -282,22 +362,9 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
         }
         multiply(then);
     }
-    // The way out: a wave turns a tile of 32 x 32 at a time in LDS, so that both
-    // places are read and written 16 bytes a lane, 64 bytes of a row.
+    // The way out, a tile of 32 x 32 at a time
     arrive<0>();
     float(*turn)[kTurn] = (float(*)[kTurn])((float *)&stage[0][0] + own * 32 * kTurn);
-    const float keep = KIND == kGram ? 0.0f : KIND == kSquare ? p.coef[step][1] * (p.sb / p.sa) : p.coef[step][0];
-    const float take = KIND == kGram     ? p.sa / (p.sx * p.sx)
-                       : KIND == kSquare ? p.coef[step][2] * (p.sb / (p.sa * p.sa))
-                                         : 1.0f / p.sb;
-    const bool symmetric = KIND == kGram || KIND == kSquare;
-    // Second halves are read by three products, or as what stays of the old: by
-    // the next square at A[j][i], by the next update at X^T.
-    constexpr bool kLowT = PL == 2 || KIND != kSquare, kLowD = PL == 2;
-    const Planes to_t = KIND == kGram ? p.a : KIND == kSquare ? p.b : to;
-    const Planes to_d = KIND == kGram ? p.a : KIND == kSquare ? p.b : p.x;
-    const int64_t t0 = symmetric ? a0 : x0;
-    const int ld_d = symmetric ? p.np : p.mp;
 #pragma unroll
     for (int it = 0; it < MT; ++it)
 #pragma unroll
@@ -306,70 +373,55 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
             if (i0 >= p.np || j0 >= rows_j) continue;  // whole tiles: both are multiples of 32
             // Of a symmetric matrix, what lies on and above the diagonal is taken and
             // written to both places: the other half is summed in another order.
-            if (symmetric && i0 > j0) continue;
-            const bool diagonal = symmetric && i0 == j0;
+            if ((KIND == kGram || KIND == kSquare) && i0 > j0) continue;
             // a lane holds column j and, in fours, rows i
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 *(f32x4 *)&turn[lane & 31][8 * q + 4 * (lane >> 5)] =
                     f32x4{acc[it][jt][4 * q], acc[it][jt][4 * q + 1], acc[it][jt][4 * q + 2], acc[it][jt][4 * q + 3]};
             wave::sync();
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int j = 16 * r + (lane >> 2), i = 8 * (lane & 3);
-                const int64_t at = t0 + (int64_t)(j0 + j) * p.np + i0 + i;
-                f32x4 *const here = (f32x4 *)&turn[j][i];
-                f32x4 v[2] = {here[0], here[1]};
-                if (diagonal) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (i + e > j) v[e >> 2][e & 3] = turn[i + e][j];
-                }
-                f16x8 hi, lo;
-                if (KIND != kGram) {
-                    const Planes old = KIND == kSquare ? p.a : from;
-                    hi = *(const f16x8 *)(old.hi + at);
-                    lo = *(const f16x8 *)(old.lo + at);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = take * v[e >> 2][e & 3];
-                    if (KIND != kGram) x = __builtin_fmaf(keep, (float)hi[e] + (float)lo[e], x);
-                    v[e >> 2][e & 3] = x;
-                }
-                split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
-                if (!diagonal) {
-                    here[0] = v[0];
-                    here[1] = v[1];
-                }
-                if (KIND == kLast) {
-                    if (p.tall) write_out<T>(p, mat, j0 + j, p.m, i0 + i, p.n, v);
-                } else {
-                    *(f16x8 *)(to_t.hi + at) = hi;
-                    if (kLowT) *(f16x8 *)(to_t.lo + at) = lo;
-                }
-            }
-            wave::sync();
-            if (KIND == kLast ? !p.tall : !diagonal) {
+            if (KIND == kGram && p.splits > 1) {
+                float *part = p.gram_parts + (mat * p.splits + blockIdx.z) * p.np * p.np;
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int i = 16 * r + (lane & 15), j = 8 * (lane >> 4);
-                    f32x4 v[2];
-                    f16x8 hi, lo;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = turn[j + e][i];
-                    split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
-                    if (KIND == kLast) {
-                        write_out<T>(p, mat, i0 + i, p.n, j0 + j, p.m, v);
-                    } else {
-                        const int64_t at = t0 + (int64_t)(i0 + i) * ld_d + j0 + j;
-                        *(f16x8 *)(to_d.hi + at) = hi;
-                        if (kLowD) *(f16x8 *)(to_d.lo + at) = lo;
-                    }
+                    const int j = 16 * r + (lane >> 2), i = 8 * (lane & 3);
+                    f32x4 *to = (f32x4 *)(part + (int64_t)(j0 + j) * p.np + i0 + i);
+                    to[0] = *(const f32x4 *)&turn[j][i];
+                    to[1] = *(const f32x4 *)&turn[j][i + 4];
                 }
+            } else {
+                leave<T, KIND, PL>(p, mat, step, i0, j0, turn);
             }
             wave::sync();
         }
+}
+
+// A, from the parts of its sums: a wave takes 32 x 32 on or above the diagonal.
+template <int PL>
+__global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoParams p, int tiles) {
+    __shared__ float turns[kThreads / 64][32][kTurn];
+    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = blockIdx.x * (kThreads / 64) + own;
+    if (tile >= tiles) return;
+    int ti, tj;
+    triangle(tile, ti, tj);
+    const int64_t mat = blockIdx.y;
+    const float *part = p.gram_parts + mat * p.splits * p.np * p.np;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int j = 16 * r + (lane >> 2), i = 8 * (lane & 3);
+        f32x4 v[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) {
+            const f32x4 *from = (const f32x4 *)(part + ((int64_t)s * p.np + 32 * tj + j) * p.np + 32 * ti + i);
+            v[0] += from[0];
+            v[1] += from[1];
+        }
+        *(f32x4 *)&turns[own][j][i] = v[0];
+        *(f32x4 *)&turns[own][j][i + 4] = v[1];
+    }
+    wave::sync();
+    leave<float, kGram, PL>(p, mat, 0, 32 * ti, 32 * tj, turns[own]);
 }
 
 template <typename T, int TILE, int WM, int WN, int STAGES, int PROD, int KIND>
@@ -377,14 +429,14 @@ void run_product(const OrthoParams &p, int step, hipStream_t s) {
     const int ti = (p.np + TILE - 1) / TILE, tj = ((KIND == kGram || KIND == kSquare ? p.np : p.mp) + TILE - 1) / TILE;
     const int tiles = KIND == kGram || KIND == kSquare ? ti * (ti + 1) / 2 : ti * tj;
     ortho_product_kernel<T, TILE, TILE, WM, WN, STAGES, PROD, KIND>
-        <<<dim3(tiles, (uint32_t)p.n_mats), WM * WN * 64, 0, s>>>(p, step, ti, tj);
+        <<<dim3(tiles, (uint32_t)p.n_mats, KIND == kGram ? p.splits : 1), WM * WN * 64, 0, s>>>(p, step, ti, tj);
 }
 
 // The tile of a pass: the one that is done first, by the tiles that a compute
 // unit gets, the time of a stage and that of the way in and out, in us, as
 // measured on 4,096 x 4,096 and 128 x 128 (one product; three).
 template <int PROD>
-int pick_tile(const OrthoParams &p, bool symmetric, int depth) {
+int pick_tile(const OrthoParams &p, bool symmetric, int depth, int splits) {
     constexpr int kTiles[4] = {64, 128, 192, 256};
     constexpr double kStageUs[2][4] = {{0.17, 0.34, 0.65, 1.05}, {0.33, 0.76, 1.45, 2.7}};
     constexpr double kWayUs[4] = {3.0, 5.0, 7.0, 9.0};
@@ -392,8 +444,8 @@ int pick_tile(const OrthoParams &p, bool symmetric, int depth) {
     double least = 0.0;
     for (int t = 0; t < 4; ++t) {
         const int64_t ti = (p.np + kTiles[t] - 1) / kTiles[t], tj = (p.mp + kTiles[t] - 1) / kTiles[t];
-        const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * p.n_mats;
-        const double cost = (double)((tiles + 255) / 256) * (depth / kStage * kStageUs[PROD != 1][t] + kWayUs[t]);
+        const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * p.n_mats * splits;
+        const double cost = (double)((tiles + 255) / 256) * (depth / kStage / splits * kStageUs[PROD != 1][t] + kWayUs[t]);
         if (t == 0 || cost < least) {
             least = cost;
             best = t;
@@ -404,7 +456,7 @@ int pick_tile(const OrthoParams &p, bool symmetric, int depth) {
 
 template <typename T, int PROD, int KIND>
 void run_pass(const OrthoParams &p, int step, hipStream_t s) {
-    switch (pick_tile<PROD>(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np)) {
+    switch (pick_tile<PROD>(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np, KIND == kGram ? p.splits : 1)) {
     case 0: return run_product<T, 64, 2, 2, 3, PROD, KIND>(p, step, s);
     case 1: return run_product<T, 128, 2, 2, PROD == 1 ? 3 : 2, PROD, KIND>(p, step, s);
     case 2: return run_product<T, 192, 2, PROD == 1 ? 3 : 2, PROD == 1 ? 4 : 3, PROD, KIND>(p, step, s);
@@ -416,6 +468,11 @@ template <typename T, int PROD>
 hipError_t run_products(const OrthoParams &p, hipStream_t s) {
     for (int k = 0; k < p.steps; ++k) {
         run_pass<float, PROD, kGram>(p, k, s);
+        if (p.splits > 1) {
+            const int side = p.np / 32, tiles = side * (side + 1) / 2;
+            ortho_join_kernel<PROD == 1 ? 1 : 2>
+                <<<dim3((tiles + kThreads / 64 - 1) / (kThreads / 64), (uint32_t)p.n_mats), kThreads, 0, s>>>(p, tiles);
+        }
         run_pass<float, PROD, kSquare>(p, k, s);
         if (k + 1 < p.steps)
             run_pass<float, PROD, kUpdate>(p, k, s);
@@ -441,6 +498,16 @@ hipError_t run_typed(const OrthoParams &p, hipStream_t s) {
 }
 
 }  // namespace
+
+// Parts of X X^T where its tiles are few and its sums long: eight stages each at
+// least, 512 tiles of 64 together; under four parts the pass that joins them
+// costs what they save (300 x 500 122 us, 131 in two; 100 x 4,000 284 us, 130 in
+// 15).  By the matrix alone, so that its result does not depend on its batch.
+int orthogonalise_splits(int64_t np, int64_t mp) {
+    const int64_t side = (np + 63) / 64, tiles = side * (side + 1) / 2;
+    const int64_t splits = std::min<int64_t>(std::min<int64_t>(mp / kStage / 8, 512 / tiles), 64);
+    return splits < 4 ? 1 : (int)splits;
+}
 
 // Some 2^28 elements of a plane.
 int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp) {

@@ -181,6 +181,8 @@ struct OrthoLayout {
     size_t squares, wide, square, total;  // bytes of the sums and of one plane of each shape
     int32_t parts, part_cols;             // small updates: tiles of their parts, and of their factors
     size_t small_parts, small_factors;
+    int32_t splits;                       // of the sums of X X^T, and their parts
+    size_t gram_parts;
 };
 
 int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, OrthoLayout &l) {
@@ -216,7 +218,9 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
     l.squares = align_up((size_t)l.batch * same::kNormParts * sizeof(double));
     l.wide = align_up((size_t)l.batch * l.np * l.mp * 2);
     l.square = align_up((size_t)l.batch * l.np * l.np * 2);
-    l.total = l.squares + 6 * l.wide + 4 * l.square;
+    l.splits = same::orthogonalise_splits(l.np, l.mp);
+    l.gram_parts = l.splits > 1 ? align_up((size_t)l.batch * l.splits * l.np * l.np * 4) : 0;
+    l.total = l.squares + 6 * l.wide + 4 * l.square + l.gram_parts;
     return SAME_OK;
 }
 
@@ -529,7 +533,9 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
             at += bytes;
             return here;
         };
+        p.splits = l.splits;
         p.squares = (double *)take(l.squares);
+        p.gram_parts = (float *)take(l.gram_parts);
         for (same::Planes *w : {&p.x, &p.xt[0], &p.xt[1]}) {
             w->hi = (_Float16 *)take(l.wide);
             w->lo = (_Float16 *)take(l.wide);

@@ -101,6 +101,8 @@ struct OrthoParams {
     float sx, sa, sb;         // the planes' powers of two
     double *squares;          // [n_mats][kNormParts]
     Planes x, xt[2], a, b;    // [n_mats] of [np][mp], [mp][np], [np][np], [np][np]
+    int32_t splits;           // of the sums of X X^T
+    float *gram_parts;        // [n_mats][splits][np][np]
     int32_t parts, part_cols; // of a small update's columns
     void *small_parts, *small_factors;  // [n_mats][parts] and [n_mats] sets of tiles
     int32_t steps;
@@ -114,6 +116,7 @@ constexpr int kSmallSide = 32;  // of updates that take the small kernels
 void ortho_small_parts(int64_t n, int64_t m, int32_t *parts, int32_t *part_cols, size_t *tile_bytes);
 hipError_t launch_ortho_small(const OrthoParams &p, int dtype, hipStream_t s);
 
+int orthogonalise_splits(int64_t np, int64_t mp);
 // Updates that one block holds.
 inline bool ortho_whole(int64_t n, int64_t m) {
     return n <= 96 ? m <= 256 : n <= 128 && m <= 128;

@@ -92,8 +92,9 @@ def run(g, **kw):
 
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 7, 1), (2, 2, 3), (5, 8, 128), (3, 128, 8), (2, 16, 16), (1, 17, 300), (2, 31, 33),
           (1, 32, 1000), (2, 33, 65), (1, 64, 64), (1, 100, 64), (2, 65, 130), (1, 128, 128), (1, 129, 127),
-          (1, 200, 333), (1, 300, 90), (1, 40, 2000), (1, 260, 260), (1, 1500, 70), (1, 33, 256), (2, 256, 64), (1, 64, 257), (2, 250, 96), (1, 97, 128), (3, 65, 97), (1, 96, 257),
-                   (2, 4097, 5), (1, 20, 7000), (1, 12, 9001)]
+          (1, 200, 333), (1, 300, 90), (1, 40, 2000), (1, 260, 260), (1, 1500, 70), (1, 33, 256), (2, 256, 64), (1, 64, 257),
+          (2, 250, 96), (1, 97, 128), (3, 65, 97), (1, 96, 257),
+          (2, 4097, 5), (1, 20, 7000), (1, 513, 1025), (2, 1030, 100), (1, 10, 1023), (1, 31, 1024), (1, 12, 9001)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -168,6 +169,11 @@ def test_a_matrix_does_not_depend_on_its_batch():
         out = run(g)
         for i in (0, 17, 299):
             assert torch.equal(run(g[i:i + 1])[0], out[i])
+    for dtype in TYPES:   # sums in parts
+        g = matrices(40, 70, 1100, dtype, 6)
+        out = run(g)
+        for i in (0, 39):
+            assert torch.equal(run(g[i:i + 1])[0], out[i])
 
 
 def test_many_matrices():
@@ -183,7 +189,7 @@ def test_many_matrices():
 
 
 def test_streams_graphs_and_repeats():
-    for shape in ((50, 8, 128), (1, 128, 128), (1, 200, 300), (2, 20, 9000)):
+    for shape in ((50, 8, 128), (1, 128, 128), (1, 200, 300), (2, 20, 9000), (1, 70, 1500)):
         g = matrices(*shape, torch.bfloat16, 1)
         out = torch.empty_like(g)
         ws = torch.empty(same.same_orthogonalise_workspace_size(*shape, g.dtype), dtype=torch.uint8, device="cuda")
