@@ -506,15 +506,18 @@ struct RowGrad {
 
 __device__ __forceinline__ RowGrad row_grad(const LogProbsGradParams &p, int64_t row) {
     RowGrad g;
+    // all loads first: none waits for another
     const float2 s = p.sums[row];
+    const int n = count_of(p.counts, row, p.cols), target = p.targets ? p.targets[row] : -1;
+    const float dl = p.dlog_probs ? p.dlog_probs[row] : 0.0f, dh = p.dentropy ? p.dentropy[row] : 0.0f;
+    const float entropy = p.dentropy ? p.entropy[row] : 0.0f;
     g.max = s.x;
     g.log_sum = s.y;
-    g.n = s.x == -kInf && s.y == 0.0f ? 0 : count_of(p.counts, row, p.cols);  // no state is possible: no gradient
-    g.target = p.targets ? p.targets[row] : -1;
-    g.dl = p.dlog_probs && g.target >= 0 ? p.dlog_probs[row] : 0.0f;
-    const float dh = p.dentropy ? p.dentropy[row] : 0.0f;
+    g.n = s.x == -kInf && s.y == 0.0f ? 0 : n;  // no state is possible: no gradient
+    g.target = target;
+    g.dl = target >= 0 ? dl : 0.0f;
     g.slope = -dh;
-    g.rest = p.dentropy ? -__builtin_fmaf(dh, p.entropy[row], g.dl) : -g.dl;
+    g.rest = p.dentropy ? -__builtin_fmaf(dh, entropy, g.dl) : -g.dl;
     return g;
 }
 

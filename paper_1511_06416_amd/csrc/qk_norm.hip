@@ -296,7 +296,9 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
         }
     }
     const int blocks = p.side[1].first_block + p.side[1].blocks;
-    if (grad)
+    if (blocks == 0) {
+        // no token: the weights' gradients alone are written
+    } else if (grad)
         qk_norm_kernel<T, W, true><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
     else
         qk_norm_kernel<T, W, false><<<blocks, kThreads, 0, s>>>(p, lanes, split);

@@ -200,7 +200,7 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
     if (l.n <= same::kSmallSide) {
         size_t tiles = 0;
         same::ortho_small_parts(l.n, l.m, &l.parts, &l.part_cols, &tiles);
-        l.batch = l.n ? std::min<int64_t>(n_mats, ((int64_t)1 << (l.parts > 1 ? 17 : 22)) / l.parts) : 0;
+        l.batch = l.n ? std::min<int64_t>(n_mats, ((int64_t)1 << (l.parts > 1 ? 15 : 22)) / l.parts) : 0;
         l.small_parts = l.parts > 1 ? align_up((size_t)l.batch * l.parts * tiles) : 0;
         l.small_factors = l.parts > 1 ? align_up((size_t)l.batch * tiles) : 0;
         l.total = l.small_parts + l.small_factors;
@@ -467,7 +467,8 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
         double bound = 1.0, most = 1.0, product = 1.0;
         for (int t = 0; t < steps; ++t) {
             for (int i = 0; i < 3; ++i) {
-                if (!std::isfinite(coefs[3 * t + i])) return record_error(SAME_EINVAL, "coefs must be finite");
+                if (!std::isfinite((float)coefs[3 * t + i]))
+                    return record_error(SAME_EINVAL, "coefs must be finite in 32 bits");
                 p.coef[t][i] = (float)coefs[3 * t + i];
             }
             const double b2 = bound * bound;
@@ -487,11 +488,11 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
         if (n_mats == 1) g_mat = out_mat = 0;
         if (g_row < 0 || g_mat < 0 || out_row < 0 || out_mat < 0)
             return record_error(SAME_EINVAL, "strides must not be negative");
-        if (out_row < cols || (n_mats > 1 && out_mat < (rows - 1) * out_row + cols))
-            return record_error(SAME_EINVAL, "out's rows and matrices must not overlap");
         const double far = (double)(n_mats - 1) * (double)std::max(g_mat, out_mat) +
                            (double)(rows - 1) * (double)std::max(g_row, out_row);
         if (far >= 1e18) return record_error(SAME_ESIZE, "strides pass 10^18 elements");
+        if (out_row < cols || (n_mats > 1 && out_mat < (rows - 1) * out_row + cols))
+            return record_error(SAME_EINVAL, "out's rows and matrices must not overlap");
         if (l.total && !workspace) return record_error(SAME_EINVAL, "workspace is null");
         if (!aligned(workspace, kAlign)) return record_error(SAME_EALIGN, "workspace must be 256-byte aligned");
         const Extent eg = extent(g, size * ((n_mats - 1) * g_mat + (rows - 1) * g_row + cols));

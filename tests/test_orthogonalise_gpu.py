@@ -182,6 +182,10 @@ def test_many_matrices():
     out = run(g)
     for i in (0, 65_535, 65_536, 69_999):
         check(out[i], g[i])
+    g = matrices(16_500, 5, 1030, torch.float16, 2)   # two parts: 2^15 parts are 16,384
+    out = run(g)
+    for i in (0, 16_383, 16_384, 16_499):
+        check(out[i], g[i])
     g = matrices(10_500, 130, 131, torch.float16, 2)   # 2^28 padded elements are 10,485
     out = run(g)
     for i in (0, 10_484, 10_485, 10_499):

@@ -113,6 +113,15 @@ def test_values_and_gradients(nq, nk, hq, hk, d, rot, dtype):
     assert torch.equal(dq, dq2) and torch.equal(dk, dk2)
 
 
+def test_no_tokens():
+    q, k = heads(0, 2, 32, torch.float16, 1), heads(0, 1, 32, torch.float16, 2)
+    w = torch.ones(32, device="cuda")
+    same.same_qk_norm(q, k, q.clone(), k.clone(), q_weight=w)
+    dw = torch.full((2, 32), float("nan"), device="cuda")
+    same.same_qk_norm_backward(q, k, q, k, q.clone(), k.clone(), dw[0], dw[1], None, q_weight=w)
+    assert not dw.any()
+
+
 def test_gradient_against_differences():
     """fp32, one head: central differences of the loss sum(y dy)."""
     q = heads(3, 2, 24, torch.float32, 1).double().float()

@@ -110,6 +110,7 @@ def ortho_rc(lib, **kw):
     (same.SAME_ESIZE, dict(rows=1 << 16, cols=1 << 16)), (same.SAME_ESIZE, dict(rows=1, cols=1 << 25)),
     (same.SAME_ESIZE, dict(n_mats=1 << 40)), (same.SAME_EINVAL, dict(coefs=[(30.0, 0.0, 0.0)])),
     (same.SAME_EINVAL, dict(coefs=[(1.0, 0.0, 20.0)])), (same.SAME_EINVAL, dict(coefs=[(np.nan, 0.0, 0.0)])),
+    (same.SAME_EINVAL, dict(coefs=[(0.0, 0.0, 0.0), (0.5, 1e39, 0.0)])), (same.SAME_ESIZE, dict(out_row=1 << 62)),
     (same.SAME_EINVAL, dict(coefs=[(3.0, 0.0, 0.0)] * 3)), (same.SAME_EINVAL, dict(steps=0)), (same.SAME_EINVAL, dict(steps=33)),
     (same.SAME_EINVAL, dict(eps=0.0)), (same.SAME_EINVAL, dict(eps=np.inf)), (same.SAME_EINVAL, dict(scale=1e39)),
     (same.SAME_EINVAL, dict(g=None)), (same.SAME_EINVAL, dict(out=None)), (same.SAME_EALIGN, dict(g=A + 2)),
@@ -136,7 +137,7 @@ def test_workspace_sizes():
     # many matrices share their planes; those that a block holds need none
     few, many = (same.same_orthogonalise_workspace_size(n, 200, 300, torch.float32) for n in (1 << 14, 1 << 20))
     assert 0 < few == many
-    for rows, cols in ((32, 2048), (256, 64), (96, 256), (128, 128)):
+    for rows, cols in ((32, 1023), (256, 64), (96, 256), (128, 128)):
         assert same.same_orthogonalise_workspace_size(1 << 20, rows, cols, torch.float32) == 0
     for call, args in ((same.same_log_probs_workspace_size, (-1, 5, 0)), (same.same_log_probs_workspace_size, (1, 5, 65)),
                        (same.same_qk_norm_workspace_size, (12, 1, 1, 1, 1)),
