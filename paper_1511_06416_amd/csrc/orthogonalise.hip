@@ -223,6 +223,7 @@ __device__ __forceinline__ void triangle(int tile, int &ti, int &tj) {
 // waves.  A barrier alone does not wait for loads into LDS.
 template <int N>
 __device__ __forceinline__ void arrive() {
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0) as the compiler counts: later waits are for later reads alone
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     static_assert(MT * WM * 32 == TM && NT * WN * 32 == TN, "whole tiles a wave");
     static_assert(WM * WN * 32 * kTurn * 4 <= STAGES * kRows * kStage * 2, "tiles are turned where operands were");
     __shared__ _Float16 stage[STAGES][kRows * kStage];
-    const int lane = threadIdx.x & 63, own = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Neighbouring blocks go to different XCDs: each gets a stretch of tiles, which
     // share operands in its L2.
     const int tiles = gridDim.x, each = tiles / 8, rest = tiles % 8, xcd = blockIdx.x % 8;
@@ -265,34 +266,40 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     // a part of a long sum, in stages
     const int all = ld / kStage, share = KIND == kGram ? (all + p.splits - 1) / p.splits : all;
     const int first = KIND == kGram ? min((int)blockIdx.z * share, all) : 0, stages = min(share, all - first);
-    const int64_t l0 = (KIND == kGram ? x0 : a0) + first * kStage, r0 = (KIND == kSquare ? a0 : x0) + first * kStage;
-    // what this lane stages: offsets of its chunks
-    int off_p[kLoadsP], off_q[kLoadsQ];
+    const int64_t l0 = KIND == kGram ? x0 : a0, r0 = KIND == kSquare ? a0 : x0;
+    // what this lane stages: its chunks, in bytes from the first row
+    uint32_t off_p[kLoadsP], off_q[kLoadsQ];
 #pragma unroll
     for (int l = 0; l < kLoadsP; ++l) {
         const int slot = (own * kLoadsP + l) * 64 + lane, row = slot >> 2;
-        off_p[l] = min(ti * TM + row, p.np - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8;
+        off_p[l] = 2u * (uint32_t)(min(ti * TM + row, p.np - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8);
     }
 #pragma unroll
     for (int l = 0; l < kLoadsQ; ++l) {
         const int slot = (own * kLoadsQ + l) * 64 + lane, row = slot >> 2;
-        off_q[l] = min(tj * TN + row, rows_j - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8;
+        off_q[l] = 2u * (uint32_t)(min(tj * TN + row, rows_j - 1) * ld + ((slot & 3) ^ ((row >> 2) & 3)) * 8);
     }
-    auto load = [&](const _Float16 *src, _Float16 *dst) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                         (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+    // planes of this matrix as buffers of their size
+    const auto plane = [&](const _Float16 *at, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)at, (short)0, (int)(2u * (uint32_t)rows * (uint32_t)ld), 0x00020000);
     };
-    auto fetch = [&](int buffer, int k) {
+    const __amdgpu_buffer_rsrc_t left_hi = plane(left.hi + l0, p.np), left_lo = plane(left.lo + l0, p.np);
+    const __amdgpu_buffer_rsrc_t right_hi = plane(right.hi + r0, rows_j), right_lo = plane(right.lo + r0, rows_j);
+    auto load = [&](__amdgpu_buffer_rsrc_t src, uint32_t off, int k, _Float16 *dst) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void *)dst, 16, off, 2 * k, 0, 0);
+    };
+    auto fetch = [&](int buffer, int s) {
+        const int k = (first + s) * kStage;
         _Float16 *to_p = &stage[buffer][own * kLoadsP * 512], *to_q = &stage[buffer][PL * TM * kStage + own * kLoadsQ * 512];
 #pragma unroll
         for (int l = 0; l < kLoadsP; ++l) {
-            load(left.hi + l0 + k + off_p[l], to_p + l * 512);
-            if (PL == 2) load(left.lo + l0 + k + off_p[l], to_p + TM * kStage + l * 512);
+            load(left_hi, off_p[l], k, to_p + l * 512);
+            if (PL == 2) load(left_lo, off_p[l], k, to_p + TM * kStage + l * 512);
         }
 #pragma unroll
         for (int l = 0; l < kLoadsQ; ++l) {
-            load(right.hi + r0 + k + off_q[l], to_q + l * 512);
-            if (PL == 2) load(right.lo + r0 + k + off_q[l], to_q + TN * kStage + l * 512);
+            load(right_hi, off_q[l], k, to_q + l * 512);
+            if (PL == 2) load(right_lo, off_q[l], k, to_q + TN * kStage + l * 512);
         }
     };
     f32x16 acc[MT][NT];
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
-        if (s < stages) fetch(s, s * kStage);
+        if (s < stages) fetch(s, s);
     // A wave reads half a stage ahead of its products.  When it arrives at a
     // stage, that is there, and everyone has left the one before it, whose place
     // the next fetch takes.
@@ -351,15 +358,13 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
     reach(0);
     fill(0, 0, now);
     for (int s = 0, buffer = 0, next = STAGES - 1; s < stages; ++s) {
-        if (s + STAGES - 1 < stages) fetch(next, (s + STAGES - 1) * kStage);
+        if (s + STAGES - 1 < stages) fetch(next, s + STAGES - 1);
         fill(buffer, 1, then);
         multiply(now);
         buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
         next = next + 1 == STAGES ? 0 : next + 1;
-        if (s + 1 < stages) {
-            reach(s + 1);
-            fill(buffer, 0, now);
-        }
+        reach(s + 1);
+        fill(buffer, 0, now);   // behind the last stage for nothing
         multiply(then);
     }
     // The way out, a tile of 32 x 32 at a time
