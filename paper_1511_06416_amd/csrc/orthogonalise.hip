@@ -230,8 +230,9 @@ __device__ __forceinline__ void arrive() {
 }
 
 // C[i][j] = sum_k P[i][k] Q[j][k] over a TM x TN tile by WM x WN waves.
-// Operands come straight into LDS, STAGES stages of 32 columns in turn, all but
-// one under way; rows of 64 bytes, whose 16-byte chunks are turned by the row
+// Operands come straight into LDS by buffer loads, whose stage is a scalar offset
+// (addresses of 64 bits a lane cost 6 %), STAGES stages of 32 columns in turn, all
+// but one under way; rows of 64 bytes, whose 16-byte chunks are turned by the row
 // so that a read of 32 rows meets no bank twice.  Rows past the matrix repeat
 // its last one and are not written.
 template <typename T, int TM, int TN, int WM, int WN, int STAGES, int PROD, int KIND>
@@ -437,20 +438,37 @@ void run_product(const OrthoParams &p, int step, hipStream_t s) {
         <<<dim3(tiles, (uint32_t)p.n_mats, KIND == kGram ? p.splits : 1), WM * WN * 64, 0, s>>>(p, step, ti, tj);
 }
 
-// The tile of a pass: the one that is done first, by the tiles that a compute
-// unit gets, the time of a stage and that of the way in and out, in us, as
-// measured on 4,096 x 4,096 and 128 x 128 (one product; three).
+// The tile of a pass: the one that is done first, in us.  Either the compute
+// units' rounds of blocks, as many side by side as their LDS takes, each with its
+// stages and its way in and out; or all tiles at the rate of a full device.
+// Fitted to 87 sizes and numbers of matrices: what it picks takes 1.01 times the
+// best tile's time in the mean, 1.4 at most.
+struct TileCost {
+    double start, stage, way;         // of the rounds
+    int together;
+    double full_stage, full_way;      // of the full device, a tile a compute unit
+};
 template <int PROD>
 int pick_tile(const OrthoParams &p, bool symmetric, int depth, int splits) {
     constexpr int kTiles[4] = {64, 128, 192, 256};
-    constexpr double kStageUs[2][4] = {{0.17, 0.34, 0.65, 1.05}, {0.33, 0.76, 1.45, 2.7}};
-    constexpr double kWayUs[4] = {3.0, 5.0, 7.0, 9.0};
+    constexpr TileCost kOne[4] = {{3.19, 0.27, 0.00, 6, 0.15, 1.03},
+                                  {7.20, 0.28, 0.00, 3, 0.38, 4.84},
+                                  {5.05, 0.65, 1.48, 1, 0.71, 9.88},
+                                  {6.62, 0.82, 0.44, 1, 1.32, 12.59}};
+    constexpr TileCost kThree[4] = {{4.35, 0.25, 0.00, 3, 0.28, 1.47},
+                                    {5.91, 0.86, 0.00, 2, 0.88, 8.33},
+                                    {4.43, 1.67, 2.33, 1, 1.41, 20.31},
+                                    {5.93, 2.03, 1.89, 1, 3.11, 11.10}};
+    const int stages = (depth / kStage + splits - 1) / splits;
     int best = 0;
     double least = 0.0;
     for (int t = 0; t < 4; ++t) {
+        const TileCost &c = PROD == 1 ? kOne[t] : kThree[t];
         const int64_t ti = (p.np + kTiles[t] - 1) / kTiles[t], tj = (p.mp + kTiles[t] - 1) / kTiles[t];
         const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * p.n_mats * splits;
-        const double cost = (double)((tiles + 255) / 256) * (depth / kStage / splits * kStageUs[PROD != 1][t] + kWayUs[t]);
+        const int64_t rounds = ((tiles + 255) / 256 + c.together - 1) / c.together;
+        const double cost = c.start + std::max((double)rounds * (stages * c.stage + c.way),
+                                               (double)tiles / 256.0 * (stages * c.full_stage + c.full_way));
         if (t == 0 || cost < least) {
             least = cost;
             best = t;
