@@ -13,10 +13,12 @@
 // 24 without).
 //
 // Measured: 65,536 tokens of 16 + 4 heads of 128 in bf16 124 us, 5.4 TB/s, the
-// copy's rate.  Smaller ones stay in the last-level cache and reach 3.6 (24 us)
-// and 4.6 TB/s (29 us): about half of the vector units' time goes to the
-// conversions, sums and turns.
+// copy's rate.  The 21,120 tokens stay in the last-level cache: 23 us (3.8 TB/s,
+// vector units two thirds busy) and, with the gradient, 29 (4.5 TB/s, loads under
+// way: more blocks make more parts of the weights' gradients, 32 us with 1,536
+// blocks for 1,024).
 #include <algorithm>
+#include <type_traits>
 
 #include "step.hpp"
 #include "wave.hpp"
@@ -118,9 +120,12 @@ __device__ __forceinline__ float inverse_norm(const NormParams &p, const float (
     return r * up;
 }
 
-// A row's loads are under way while the one before it is worked on.
-template <typename T, int W, bool GRAD>
-__global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lanes, int split) {
+// A row's loads are under way while the one before it is worked on.  With LANES
+// a row fills that many lanes, known to the compiler (21,120 tokens of 8 + 8 heads
+// of 64 23 us, 24 without); LANES = 0 takes any width.
+template <typename T, int W, bool GRAD, int LANES>
+__global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any_lanes, int split) {
+    const int lanes = LANES ? LANES : any_lanes;
     __shared__ float2 turns[kWaves][kMaxHeadDim / 2];
     __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
     const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -128,7 +133,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lan
     const NormSide &s = p.side[keys];
     const int groups = 64 / lanes, group = lane / lanes, unit = lane & (lanes - 1);
     const int turning = p.half / W;
-    const bool used = unit < p.dim / (2 * W);
+    const bool used = LANES || unit < p.dim / (2 * W);
+    const int dim = LANES ? LANES * 2 * W : p.dim;
     // a lane without a place of its own reads and computes another's, and writes nothing
     const int place = used ? unit : 0;
     const bool turned = place < turning;
@@ -158,10 +164,16 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lan
         o.last = min(o.first + part, s.heads);
     };
     Raw<T, W> x, y, next_x, next_y;
+    const T *from_x = (const T *)s.x, *from_y = (const T *)s.dout;
+    T *to = (T *)s.out;
+    asm("" : "+s"(from_x), "+s"(from_y), "+s"(to));   // in registers: else they are read again for each row
+    // scalar addresses of the wave's first row; this lane's is ahead of it
+    const int64_t x_ahead = group * s.x_head, y_ahead = group * s.dout_head;
+    const int out_ahead = group * dim;
     auto load = [&](const Spot &o, Raw<T, W> &rx, Raw<T, W> &ry) {
-        const int64_t h = min(o.first + group, s.heads - 1);  // rows that are not there repeat the last
-        rx.load((const T *)s.x + o.token * s.x_row + h * s.x_head, a, b);
-        if (GRAD) ry.load((const T *)s.dout + o.token * s.dout_row + h * s.dout_head, a, b);
+        const bool there = o.first + group < s.heads;   // rows that are not there repeat the first
+        rx.load(from_x + o.token * s.x_row + o.first * s.x_head + (there ? x_ahead : 0), a, b);
+        if (GRAD) ry.load(from_y + o.token * s.dout_row + o.first * s.dout_head + (there ? y_ahead : 0), a, b);
     };
     float c[W], sn[W];
 #pragma unroll
@@ -239,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int lan
 #pragma unroll
             for (int i = 0; i < 2 * W; ++i) u[i] = norm * __builtin_fmaf(-v[i], t, u[i]);
         }
-        if (here) store<T, W>((T *)s.out + (at.token * s.heads + h) * p.dim, a, b, u);
+        if (here) store<T, W>(to + (at.token * s.heads + at.first) * dim, out_ahead + a, out_ahead + b, u);
         entered = leaves;
         at = next;
         x = next_x;
@@ -314,10 +326,22 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
     const int blocks = p.side[1].first_block + p.side[1].blocks;
     if (blocks == 0) {
         // no token: the weights' gradients alone are written
-    } else if (grad)
-        qk_norm_kernel<T, W, true><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
-    else
-        qk_norm_kernel<T, W, false><<<blocks, kThreads, 0, s>>>(p, lanes, split);
+    } else {
+        // rows of a power of two of places
+        const int known = W == 4 && lanes >= 4 && lanes * 2 * W == p.dim ? lanes : 0;
+        const auto run = [&](auto l) {
+            if (grad)
+                qk_norm_kernel<T, W, true, decltype(l)::value><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
+            else
+                qk_norm_kernel<T, W, false, decltype(l)::value><<<blocks, kThreads, 0, s>>>(p, lanes, split);
+        };
+        if constexpr (W == 4) {
+            if (known == 4) run(std::integral_constant<int, 4>());
+            if (known == 8) run(std::integral_constant<int, 8>());
+            if (known == 16) run(std::integral_constant<int, 16>());
+        }
+        if (!known) run(std::integral_constant<int, 0>());
+    }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && grad && (p.side[0].dweight || p.side[1].dweight)) {
         qk_norm_join_kernel<<<dim3((p.dim + 31) / 32, 2), 1024, 0, s>>>(p);
