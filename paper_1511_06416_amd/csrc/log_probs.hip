@@ -567,8 +567,8 @@ __global__ __launch_bounds__(kThreads) void log_probs_grad_short_kernel(LogProbs
 }
 
 // A wave takes kGradVecs vectors a lane of a row, one after another: 4,099 x
-// 32,768 bf16 81 us (6.6 TB/s with what the last-level cache still holds); with
-// all four loads before the first store 95, with one vector 130.
+// 32,768 bf16 77 us; with all four loads before the first store 95, with one vector
+// 130 (81 then).
 constexpr int kGradVecs = 4;
 
 template <typename T>
