@@ -192,6 +192,30 @@ def test_many_matrices():
         check(out[i], g[i])
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(65, 1 << 24, torch.bfloat16), (1 << 24, 65, torch.float16)])
+def test_the_largest_matrix(rows, cols, dtype):
+    """Planes of over 2^31 bytes.  A one in every column, at row j % 65: rows are
+    orthogonal, the singular values are the roots of their numbers of ones over 4,096."""
+    n, m = min(rows, cols), max(rows, cols)
+    one = torch.arange(m, device="cuda") % n
+    g = torch.zeros(rows, cols, dtype=dtype, device="cuda")
+    place = one[None, :] if rows == n else one[:, None]
+    g.scatter_(0 if rows == n else 1, place, 1.0)
+    run_out = torch.empty_like(g)
+    ws = torch.empty(same.same_orthogonalise_workspace_size(1, rows, cols, dtype), dtype=torch.uint8, device="cuda")
+    same.same_orthogonalise(g, run_out, ws, coefs=[(1.5, -0.5, 0.0)] * 4)
+    got = run_out.gather(0 if rows == n else 1, place).flatten().double()
+    counts = torch.bincount(one, minlength=n).double()
+    s = counts.sqrt() / 4096
+    for _ in range(4):
+        s = s * (1.5 - 0.5 * s * s)
+    # bf16's products take 11 bits of their operands, each of three a step in at most
+    # half of x: 4 steps x 3 x 2^-11 of it, and the rounding of out
+    want = (s / counts.sqrt())[one]
+    assert bool(((got - want).abs() <= (12 * 2.0 ** -11 + torch.finfo(dtype).eps) * want).all())
+    assert int((run_out != 0).sum()) == m
+
+
 def test_streams_graphs_and_repeats():
     for shape in ((50, 8, 128), (1, 128, 128), (1, 200, 300), (2, 20, 9000), (1, 70, 1500)):
         g = matrices(*shape, torch.bfloat16, 1)

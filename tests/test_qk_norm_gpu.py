@@ -240,6 +240,31 @@ def test_huge_tiny_and_missing_values(dtype):
         check("row %d" % row, dx[row], want[row], bound[row])
 
 
+def test_far_offsets():
+    """More than 2^31 elements, and a view whose rows lie as far apart: a row's result is its own."""
+    n = 2_100_000
+    q = torch.zeros(n, 8, 128, dtype=torch.bfloat16, device="cuda")
+    q.view(-1)[:1 << 20].normal_()
+    q[-5:] = heads(5, 8, 128, torch.bfloat16, 3)
+    dy, k = q, heads(0, 1, 128, torch.bfloat16, 1)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    kw = dict(k_positions=pos[:0], angles=angles(64))
+    y = torch.empty_like(q)
+    same.same_qk_norm(q, k, y, k.clone(), q_positions=pos, **kw)
+    want = torch.empty_like(q[-5:])
+    same.same_qk_norm(q[-5:], k, want, k.clone(), q_positions=pos[-5:], **kw)
+    assert torch.equal(y[-5:], want)
+    same.same_qk_norm_backward(q, k, dy, k, y, k.clone(), None, None, None, q_positions=pos, **kw)
+    same.same_qk_norm_backward(q[-5:], k, dy[-5:], k, want, k.clone(), None, None, None, q_positions=pos[-5:], **kw)
+    assert torch.equal(y[-5:], want)
+    far = q.view(-1).as_strided((2, 2, 128), (n * 1024 - 2048, 1024, 1))   # the first and the last two tokens' first heads
+    got = torch.empty(2, 2, 128, dtype=q.dtype, device="cuda")
+    same.same_qk_norm(far, k, got, k.clone(), q_positions=pos[:2], **kw)
+    again = torch.empty_like(got)
+    same.same_qk_norm(far.contiguous(), k, again, k.clone(), q_positions=pos[:2], **kw)
+    assert torch.equal(got, again) and bool(got[1].float().abs().sum() > 0)
+
+
 def test_streams_graphs_and_repeats():
     q, k = heads(300, 8, 64, torch.bfloat16, 1), heads(200, 2, 64, torch.bfloat16, 2)
     pos = torch.arange(300, dtype=torch.int32, device="cuda")
