@@ -734,49 +734,52 @@ def _begin():
     if _F32 is None:
         import torch
         # what torch.cuda.current_device() asks once the device is in use: 0.07 against 0.35 us
-        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        # (-2: no device, and no tensor is there)
+        _device = (lambda: -2) if not torch.cuda.is_available() else getattr(
+            torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _F32, _I32 = torch.float32, torch.int32
-    return _lib or load_library()
+    return _lib or load_library(), _device()
 
 
-def _now(stream):
+def _now(stream, here):
     """The stream of a call, after its tensors were found on the current device."""
     if stream is None and _raw_stream is not None:
-        return _raw_stream(_device())
+        return _raw_stream(here)
     return _stream(stream)
 
 
-def _here(name, t):
-    """Address of a tensor on the current device."""
+def _elsewhere(name, t, here):
     at = t.get_device()
     if at < 0:
         raise SameError(SAME_EINVAL, "%s must be a device tensor" % name)
-    if at != _device():
-        raise SameError(SAME_EINVAL, "%s is on device %d, not on the current one" % (name, at))
-    return t.data_ptr()
+    raise SameError(SAME_EINVAL, "%s is on device %d, not on the current one (%d)" % (name, at, here))
 
 
-def _flat(name, t, shape, dtype):
-    """Address of a contiguous tensor of one shape and type, or None."""
+def _flat(name, t, shape, dtype, here):
+    """Address of a contiguous tensor of one shape and type on the current device, or None."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise SameError(SAME_EINVAL, "%s must be contiguous %s of shape %s, got %s of %s"
                         % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-    return _here(name, t)
+    if t.get_device() != here:
+        _elsewhere(name, t, here)
+    return t.data_ptr()
 
 
-def _bytes(t, need):
+def _bytes(t, need, here):
     """Address of a workspace of at least that many bytes, or None where none is needed."""
     if not need:
         return None
     if t is None or t.numel() * t.element_size() < need or not t.is_contiguous():
         raise SameError(SAME_EINVAL, "workspace must be contiguous, with at least %d bytes" % need)
-    return _here("workspace", t)
+    if t.get_device() != here:
+        _elsewhere("workspace", t, here)
+    return t.data_ptr()
 
 
-def _heads(name, t, dtype, shape):
+def _heads(name, t, dtype, shape, here):
     """Address and element strides of a token and a head of [tokens][heads][head_dim]."""
     if t.dtype is not dtype or t.shape != shape or len(shape) != 3:
         raise SameError(SAME_EINVAL, "%s must be %s of shape %s, got %s of %s"
@@ -785,14 +788,17 @@ def _heads(name, t, dtype, shape):
     row, head, unit = t.stride()
     if unit != 1 and t.numel():
         raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-    return _here(name, t), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+    if t.get_device() != here:
+        _elsewhere(name, t, here)
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
-def _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps):
+def _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps, here):
     dtype, of_q, of_k = q.dtype, q.shape, k.shape
-    at_q, at_k = _heads("q", q, dtype, of_q), _heads("k", k, dtype, of_k)
-    dim = of_q[2]
-    if of_k[2] != dim:
+    at_q, at_k = _heads("q", q, dtype, of_q, here), _heads("k", k, dtype, of_k, here)
+    q_tokens, heads_q, dim = of_q
+    k_tokens, heads_kv, k_dim = of_k
+    if k_dim != dim:
         raise SameError(SAME_EINVAL, "q and k must have heads of one width")
     rot, turns, width = 0, None, (dim,)
     if angles is not None and len(angles):
@@ -800,37 +806,39 @@ def _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps):
         if angles.ndim != 1:
             raise SameError(SAME_EINVAL, "angles must be one-dimensional")
         rot, turns = 2 * len(angles), angles.__array_interface__["data"][0]
-        q_positions = _flat("q_positions", q_positions, of_q[:1], _I32)
-        k_positions = _flat("k_positions", k_positions, of_k[:1], _I32)
+        q_positions = _flat("q_positions", q_positions, (q_tokens,), _I32, here)
+        k_positions = _flat("k_positions", k_positions, (k_tokens,), _I32, here)
     else:
         q_positions = k_positions = None
     # angles: kept alive by the caller until the call returns
-    return (_dtype(dtype), dim, *at_q, of_q[0], of_q[1], _flat("q_weight", q_weight, width, _F32), q_positions, *at_k,
-            of_k[0], of_k[1], _flat("k_weight", k_weight, width, _F32), k_positions, float(eps), rot, turns), angles
+    return (_dtype(dtype), dim, *at_q, q_tokens, heads_q, _flat("q_weight", q_weight, width, _F32, here), q_positions,
+            *at_k, k_tokens, heads_kv, _flat("k_weight", k_weight, width, _F32, here), k_positions, float(eps), rot,
+            turns), angles
 
 
 def same_qk_norm(q, k, q_out, k_out, q_weight=None, k_weight=None, q_positions=None, k_positions=None, angles=None,
                  eps=1e-6, stream=None):
     """angles: float64 numpy array of rot_dim / 2 radians a position (None or empty: no rotation)."""
-    lib = _begin()
-    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
-    _check(lib.same_qk_norm(*args, _flat("q_out", q_out, q.shape, q.dtype), _flat("k_out", k_out, k.shape, q.dtype),
-                            _now(stream)))
+    lib, here = _begin()
+    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps, here)
+    _check(lib.same_qk_norm(*args, _flat("q_out", q_out, q.shape, q.dtype, here),
+                            _flat("k_out", k_out, k.shape, q.dtype, here), _now(stream, here)))
 
 
 def same_qk_norm_backward(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, q_weight=None, k_weight=None,
                           q_positions=None, k_positions=None, angles=None, eps=1e-6, stream=None):
     """dq_weight and dk_weight may be None."""
-    lib = _begin()
-    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps)
+    lib, here = _begin()
+    args, kept = _norm_args(q, k, q_weight, k_weight, q_positions, k_positions, angles, eps, here)
     dtype, width = q.dtype, q.shape[-1:]
     need = 0
     if dq_weight is not None or dk_weight is not None:
         need = same_qk_norm_workspace_size(q.shape[2], q.shape[0], q.shape[1], k.shape[0], k.shape[1])
     _check(lib.same_qk_norm_backward(
-        *args, *_heads("dq_out", dq_out, dtype, q.shape), *_heads("dk_out", dk_out, dtype, k.shape),
-        _flat("dq", dq, q.shape, dtype), _flat("dk", dk, k.shape, dtype), _flat("dq_weight", dq_weight, width, _F32),
-        _flat("dk_weight", dk_weight, width, _F32), _bytes(workspace, need), _now(stream)))
+        *args, *_heads("dq_out", dq_out, dtype, q.shape, here), *_heads("dk_out", dk_out, dtype, k.shape, here),
+        _flat("dq", dq, q.shape, dtype, here), _flat("dk", dk, k.shape, dtype, here),
+        _flat("dq_weight", dq_weight, width, _F32, here), _flat("dk_weight", dk_weight, width, _F32, here),
+        _bytes(workspace, need, here), _now(stream, here)))
 
 
 def same_qk_norm_workspace_size(head_dim, q_tokens, heads_q, k_tokens, heads_kv) -> int:
@@ -840,22 +848,24 @@ def same_qk_norm_workspace_size(head_dim, q_tokens, heads_q, k_tokens, heads_kv)
     return out.value
 
 
-def _logits(name, t, like):
+def _logits(name, t, like, here):
     """Address and row stride of a matrix of logits."""
     if t.dtype is not like.dtype or t.dim() != 2 or t.shape != like.shape:
         raise SameError(SAME_EINVAL, "%s must be a matrix shaped and typed like logits" % name)
     row, unit = t.stride()
     if unit != 1 and t.shape[1] > 1 and t.numel():
         raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-    return _here(name, t), row
+    if t.get_device() != here:
+        _elsewhere(name, t, here)
+    return t.data_ptr(), row
 
 
 def same_log_probs(logits, targets, log_probs, workspace, counts=None, sums=None, entropy=None, top_ids=None,
                    top_log_probs=None, stream=None):
     """targets and counts: int32.  targets with log_probs, sums ([rows][2]), entropy, and top_ids (int32) with
     top_log_probs may be None; the number of alternatives is top_ids' second size."""
-    lib = _begin()
-    at, row = _logits("logits", logits, logits)
+    lib, here = _begin()
+    at, row = _logits("logits", logits, logits, here)
     rows, cols = logits.shape
     one, n_top = (rows,), 0
     if (top_ids is None) != (top_log_probs is None):
@@ -866,25 +876,26 @@ def same_log_probs(logits, targets, log_probs, workspace, counts=None, sums=None
         n_top = top_ids.shape[1]
     need = same_log_probs_workspace_size(rows, cols, n_top) if cols > 64 else 0
     _check(lib.same_log_probs(
-        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32),
-        _flat("targets", targets, one, _I32), _flat("log_probs", log_probs, one, _F32),
-        _flat("sums", sums, (rows, 2), _F32), _flat("entropy", entropy, one, _F32), n_top,
-        _flat("top_ids", top_ids, (rows, n_top), _I32), _flat("top_log_probs", top_log_probs, (rows, n_top), _F32),
-        _bytes(workspace, need), _now(stream)))
+        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32, here),
+        _flat("targets", targets, one, _I32, here), _flat("log_probs", log_probs, one, _F32, here),
+        _flat("sums", sums, (rows, 2), _F32, here), _flat("entropy", entropy, one, _F32, here), n_top,
+        _flat("top_ids", top_ids, (rows, n_top), _I32, here),
+        _flat("top_log_probs", top_log_probs, (rows, n_top), _F32, here), _bytes(workspace, need, here),
+        _now(stream, here)))
 
 
 def same_log_probs_backward(logits, targets, sums, dlogits, counts=None, entropy=None, dlog_probs=None, dentropy=None,
                             stream=None):
     """sums and entropy: the forward's.  dlog_probs and dentropy may be None."""
-    lib = _begin()
-    at, row = _logits("logits", logits, logits)
+    lib, here = _begin()
+    at, row = _logits("logits", logits, logits, here)
     rows, cols = logits.shape
     one = (rows,)
     _check(lib.same_log_probs_backward(
-        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32),
-        _flat("targets", targets, one, _I32), _flat("sums", sums, (rows, 2), _F32),
-        _flat("entropy", entropy, one, _F32), _flat("dlog_probs", dlog_probs, one, _F32),
-        _flat("dentropy", dentropy, one, _F32), *_logits("dlogits", dlogits, logits), _now(stream)))
+        _dtype(logits.dtype), at, row, rows, cols, _flat("counts", counts, one, _I32, here),
+        _flat("targets", targets, one, _I32, here), _flat("sums", sums, (rows, 2), _F32, here),
+        _flat("entropy", entropy, one, _F32, here), _flat("dlog_probs", dlog_probs, one, _F32, here),
+        _flat("dentropy", dentropy, one, _F32, here), *_logits("dlogits", dlogits, logits, here), _now(stream, here)))
 
 
 def same_log_probs_workspace_size(rows, cols, n_top) -> int:
@@ -898,29 +909,31 @@ def same_log_probs_workspace_size(rows, cols, n_top) -> int:
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 
-def _matrices(name, t, like):
+def _matrices(name, t, like, here):
     """Address and strides of [n][rows][cols] or [rows][cols]."""
     if t.dim() not in (2, 3) or t.shape != like.shape or t.dtype != like.dtype:
         raise SameError(SAME_EINVAL, "%s must be matrices shaped and typed like g" % name)
     if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
         raise SameError(SAME_EINVAL, "%s must have unit stride in its last axis" % name)
-    return _here(name, t), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)
+    if t.get_device() != here:
+        _elsewhere(name, t, here)
+    return t.data_ptr(), t.stride(0) if t.dim() == 3 else 0, t.stride(-2)
 
 
 def same_orthogonalise(g, out, workspace, coefs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, stream=None):
     """g, out: a matrix or [n] matrices.  coefs: (a, b, c) of every step."""
-    lib = _begin()
-    at, g_mat, g_row = _matrices("g", g, g)
+    lib, here = _begin()
+    at, g_mat, g_row = _matrices("g", g, g, here)
     steps = np.ascontiguousarray(coefs, dtype=np.float64)
     if steps.ndim != 2 or steps.shape[1] != 3:
         raise SameError(SAME_EINVAL, "coefs must be (a, b, c) of every step")
     n = g.shape[0] if g.dim() == 3 else 1
     rows, cols = g.shape[-2:]
-    to, out_mat, out_row = _matrices("out", out, g)
+    to, out_mat, out_row = _matrices("out", out, g, here)
     need = same_orthogonalise_workspace_size(n, rows, cols, g.dtype)
     _check(lib.same_orthogonalise(_dtype(g.dtype), at, g_mat, g_row, n, rows, cols,
                                   steps.__array_interface__["data"][0], len(steps), float(eps), float(scale), to,
-                                  out_mat, out_row, _bytes(workspace, need), _now(stream)))
+                                  out_mat, out_row, _bytes(workspace, need, here), _now(stream, here)))
 
 
 def same_orthogonalise_workspace_size(n_mats, rows, cols, dtype) -> int:
