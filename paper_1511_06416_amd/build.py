@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsame.so")
 SOURCES = ["kernels.hip", "cross_forward.hip", "cross_grad_query.hip", "cross_grad_key.hip", "cross_small.hip",
            "dropout.hip", "qk_norm.hip", "log_probs.hip", "orthogonalise.hip", "ortho_small.hip", "ortho_whole.hip",
+           "ortho_columns.hip",
            "api.cpp", "graph.cpp", "operators.cpp", "step.cpp"]
 ARCH = os.environ.get("SAME_OFFLOAD_ARCH", "gfx950")
 

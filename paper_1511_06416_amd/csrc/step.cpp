@@ -182,7 +182,7 @@ struct OrthoLayout {
     int32_t parts, part_cols;             // small updates: tiles of their parts, and of their factors
     size_t small_parts, small_factors;
     int32_t splits;                       // of the sums of X X^T, and their parts
-    size_t gram_parts;
+    size_t gram_parts, x32;
 };
 
 int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, OrthoLayout &l) {
@@ -209,6 +209,19 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
     if (same::ortho_whole(l.n, l.m)) {  // nothing is kept outside the block
         l.batch = std::min<int64_t>(n_mats, (int64_t)1 << 21);
         l.total = 0;
+        return SAME_OK;
+    }
+    if (same::ortho_columns(l.n, l.m, dtype == SAME_BF16)) {
+        size_t x, part, plane;
+        same::ortho_columns_layout(l.n, l.m, &l.parts, &l.part_cols, &x, &part, &plane);
+        // some 2^30 bytes of X
+        l.batch = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(n_mats, 16384), ((int64_t)1 << 30) / (int64_t)x));
+        if (n_mats == 0) l.batch = 0;
+        l.squares = align_up((size_t)l.batch * same::kNormParts * sizeof(double));
+        l.x32 = align_up((size_t)l.batch * x);
+        l.gram_parts = align_up((size_t)l.batch * part);
+        l.square = align_up((size_t)l.batch * plane);
+        l.total = l.squares + l.x32 + l.gram_parts + 2 * l.square;
         return SAME_OK;
     }
     const int64_t pad = 32;  // a stage of the products
@@ -537,6 +550,7 @@ int same_orthogonalise(int32_t dtype, const void *g, int64_t g_mat, int64_t g_ro
         p.splits = l.splits;
         p.squares = (double *)take(l.squares);
         p.gram_parts = (float *)take(l.gram_parts);
+        p.x32 = (float *)take(l.x32);
         for (same::Planes *w : {&p.x, &p.xt[0], &p.xt[1]}) {
             w->hi = (_Float16 *)take(l.wide);
             w->lo = (_Float16 *)take(l.wide);

@@ -102,7 +102,8 @@ struct OrthoParams {
     double *squares;          // [n_mats][kNormParts]
     Planes x, xt[2], a, b;    // [n_mats] of [np][mp], [mp][np], [np][np], [np][np]
     int32_t splits;           // of the sums of X X^T
-    float *gram_parts;        // [n_mats][splits][np][np]
+    float *gram_parts;        // [n_mats][splits][np][np], or of columns
+    float *x32;               // X between steps, of columns
     int32_t parts, part_cols; // of a small update's columns
     void *small_parts, *small_factors;  // [n_mats][parts] and [n_mats] sets of tiles
     int32_t steps;
@@ -122,6 +123,20 @@ inline bool ortho_whole(int64_t n, int64_t m) {
     return n <= 96 ? m <= 256 : n <= 128 && m <= 128;
 }
 hipError_t launch_ortho_whole(const OrthoParams &p, int dtype, hipStream_t s);
+
+// Updates of which each block holds some columns, at most 16 parts of four strips
+// of 128; one_product: the tiled form would take one (us, here and there: 60 x
+// 1,000 52 and 91, in one product 85; 750 of 905 x 33 613 and 1,012, 736; 128 x
+// 1,000 85 and 102, 94; 30 of 100 x 1,500 191 and 216, 167).
+inline bool ortho_columns(int64_t n, int64_t m, bool one_product) {
+    return n <= 64 ? m <= 8192 : n <= 128 && m <= 4096 && !one_product;
+}
+void ortho_columns_layout(int64_t n, int64_t m, int32_t *parts, int32_t *part_cols, size_t *x_bytes,
+                          size_t *part_bytes, size_t *plane_bytes);
+hipError_t launch_ortho_columns(const OrthoParams &p, int dtype, hipStream_t s);
+
+// Sums of squares of all matrices, in `parts` parts each.
+hipError_t launch_ortho_squares(const OrthoParams &p, int dtype, hipStream_t s, int *parts);
 
 // Matrices that share the planes (or tiles) of the workspace, in turn.
 int64_t orthogonalise_batch(int64_t n_mats, int64_t np, int64_t mp);

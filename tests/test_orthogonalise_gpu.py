@@ -92,9 +92,12 @@ def run(g, **kw):
 
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 7, 1), (2, 2, 3), (5, 8, 128), (3, 128, 8), (2, 16, 16), (1, 17, 300), (2, 31, 33),
           (1, 32, 1000), (2, 33, 65), (1, 64, 64), (1, 100, 64), (2, 65, 130), (1, 128, 128), (1, 129, 127),
-          (1, 200, 333), (1, 300, 90), (1, 40, 2000), (1, 260, 260), (1, 1500, 70), (1, 33, 256), (2, 256, 64), (1, 64, 257),
+          (1, 200, 333), (1, 300, 90), (1, 40, 2000), (1, 260, 260), (1, 1500, 70), (1, 33, 256), (2, 256, 64),
+          (1, 64, 257),
           (2, 250, 96), (1, 97, 128), (3, 65, 97), (1, 96, 257),
-          (2, 4097, 5), (1, 20, 7000), (1, 513, 1025), (2, 1030, 100), (1, 10, 1023), (1, 31, 1024), (1, 12, 9001)]
+          (2, 4097, 5), (1, 20, 7000), (1, 513, 1025), (2, 1030, 100), (1, 10, 1023), (1, 31, 1024), (1, 12, 9001),
+          (2, 34, 300), (3, 700, 64), (1, 64, 2100), (2, 96, 300), (1, 1000, 90), (1, 128, 129), (1, 64, 8192),
+          (1, 64, 8193), (1, 128, 4096)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -114,7 +117,7 @@ def test_other_steps(rows, cols, dtype):
     check(run(g, coefs=wild), g, coefs=wild)
 
 
-@pytest.mark.parametrize("rows,cols", [(6, 9), (20, 5000), (70, 40), (130, 200)])
+@pytest.mark.parametrize("rows,cols", [(6, 9), (20, 5000), (70, 40), (130, 200), (50, 300)])
 def test_sizes_of_values(rows, cols):
     """Updates near the type's limits, zeros, NaN: each matrix by itself."""
     g = matrices(6, rows, cols, torch.float32, 1)
@@ -169,8 +172,8 @@ def test_a_matrix_does_not_depend_on_its_batch():
         out = run(g)
         for i in (0, 17, 299):
             assert torch.equal(run(g[i:i + 1])[0], out[i])
-    for dtype in TYPES:   # sums in parts
-        g = matrices(40, 70, 1100, dtype, 6)
+    for dtype, rows in [(t, r) for t in TYPES for r in (50, 70, 150)]:   # sums in parts, columns of blocks
+        g = matrices(40, rows, 1100, dtype, 6)
         out = run(g)
         for i in (0, 39):
             assert torch.equal(run(g[i:i + 1])[0], out[i])
@@ -185,6 +188,10 @@ def test_many_matrices():
     g = matrices(16_500, 5, 1030, torch.float16, 2)   # two parts: 2^15 parts are 16,384
     out = run(g)
     for i in (0, 16_383, 16_384, 16_499):
+        check(out[i], g[i])
+    g = matrices(11_000, 34, 290, torch.float16, 2)   # 2^30 bytes of kept columns are 10,922 matrices
+    out = run(g)
+    for i in (0, 10_921, 10_922, 10_999):
         check(out[i], g[i])
     g = matrices(10_500, 130, 131, torch.float16, 2)   # 2^28 padded elements are 10,485
     out = run(g)
@@ -217,7 +224,7 @@ def test_the_largest_matrix(rows, cols, dtype):
 
 
 def test_streams_graphs_and_repeats():
-    for shape in ((50, 8, 128), (1, 128, 128), (1, 200, 300), (2, 20, 9000), (1, 70, 1500)):
+    for shape in ((50, 8, 128), (1, 128, 128), (1, 200, 300), (2, 20, 9000), (1, 70, 1500), (2, 40, 700)):
         g = matrices(*shape, torch.bfloat16, 1)
         out = torch.empty_like(g)
         ws = torch.empty(same.same_orthogonalise_workspace_size(*shape, g.dtype), dtype=torch.uint8, device="cuda")
