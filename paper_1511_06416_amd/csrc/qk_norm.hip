@@ -120,13 +120,21 @@ __device__ __forceinline__ float inverse_norm(const NormParams &p, const float (
     return r * up;
 }
 
+// Tokens that a wave's groups of lanes take at once where they have few heads
+// (53,073 + 43,339 tokens of one head of 40 with gradient 31 us, 79 with one).
+int pack_of(const NormSide &s, int lanes) {
+    const int groups = 64 / lanes;
+    return s.heads < groups && s.tokens >= groups ? groups / s.heads : 1;
+}
+
 // A row's loads are under way while the one before it is worked on.  With LANES
 // a row fills that many lanes, known to the compiler (21,120 tokens of 8 + 8 heads
-// of 64 23 us, 24 without); LANES = 0 takes any width.
-template <typename T, int W, bool GRAD, int LANES>
+// of 64 23 us, 24 without); LANES = 0 takes any width.  PACK: a side's tokens are
+// packed (the scalar work for it cost 2 to 8 % where none are).
+template <typename T, int W, bool GRAD, int LANES, bool PACK>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any_lanes, int split) {
     const int lanes = LANES ? LANES : any_lanes;
-    __shared__ float2 turns[kWaves][kMaxHeadDim / 2];
+    __shared__ float2 turns[kWaves][PACK ? 64 * W : 64];
     __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
     const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool keys = (int)blockIdx.x >= p.side[1].first_block;
@@ -150,28 +158,30 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
 #pragma unroll
         for (int i = 0; i < 2 * W; ++i) dw[i] = 0.0f;
     }
-    // items: a token, or one of the `split` parts of its heads
-    const int64_t items = s.tokens * split, step = (int64_t)s.blocks * kWaves;
-    const int part = (s.heads + split - 1) / split;
+    // items: a token, one of the `cut` parts of its heads, or `pack` tokens of few heads
+    const int pack = PACK ? s.pack : 1, cut = pack > 1 ? 1 : split;
+    const int64_t items = (s.tokens + pack - 1) / pack * cut, step = (int64_t)s.blocks * kWaves;
+    const int part = (s.heads + cut - 1) / cut;
     struct Spot {   // where a wave is: its groups' rows are first, first + 1, ...
         int64_t item, token;
         int first, last;
     } at, next;
     auto enter = [&](Spot &o, int64_t item) {
         o.item = item;
-        o.token = split == 1 ? item : item / split;
-        o.first = split == 1 ? 0 : (int)(item - o.token * split) * part;
-        o.last = min(o.first + part, s.heads);
+        o.token = cut == 1 ? item * pack : item / cut;
+        o.first = cut == 1 ? 0 : (int)(item - o.token * cut) * part;
+        o.last = pack == 1 ? min(o.first + part, s.heads) : (int)min((int64_t)pack, s.tokens - o.token) * s.heads;
     };
     Raw<T, W> x, y, next_x, next_y;
     const T *from_x = (const T *)s.x, *from_y = (const T *)s.dout;
     T *to = (T *)s.out;
     asm("" : "+s"(from_x), "+s"(from_y), "+s"(to));   // in registers: else they are read again for each row
     // scalar addresses of the wave's first row; this lane's is ahead of it
-    const int64_t x_ahead = group * s.x_head, y_ahead = group * s.dout_head;
+    const int up = pack == 1 ? 0 : min(group / s.heads, pack - 1), head = group - up * s.heads;
+    const int64_t x_ahead = up * s.x_row + head * s.x_head, y_ahead = up * s.dout_row + head * s.dout_head;
     const int out_ahead = group * dim;
     auto load = [&](const Spot &o, Raw<T, W> &rx, Raw<T, W> &ry) {
-        const bool there = o.first + group < s.heads;   // rows that are not there repeat the first
+        const bool there = o.first + group < o.last;   // rows that are not there repeat the first
         rx.load(from_x + o.token * s.x_row + o.first * s.x_head + (there ? x_ahead : 0), a, b);
         if (GRAD) ry.load(from_y + o.token * s.dout_row + o.first * s.dout_head + (there ? y_ahead : 0), a, b);
     };
@@ -181,8 +191,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
         c[i] = 1.0f;
         sn[i] = 0.0f;
     }
-    // sines of as many of the wave's items as it has lanes, a pair a lane
-    const int half = max(p.half, 1), ahead = 64 / half, turn_item = lane / half, turn_pair = lane - turn_item * half;
+    // sines of an item, or of as many as the wave has lanes; divisions of numbers below 256
+    const int half = max(p.half, 1), pairs = pack * half, ahead = max(1, 64 / pairs);
+    const int by_pairs = (65535 + pairs) / pairs, by_half = (65535 + half) / half;
+    const int turn_item = lane / half, turn_pair = lane - turn_item * half;
     int made = ahead;
     enter(at, (int64_t)((int)blockIdx.x - s.first_block) * kWaves + own);
     bool entered = true;
@@ -197,14 +209,24 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
             if (made == ahead) {
                 made = 0;
                 wave::sync();
-                const int64_t of = min(at.item + turn_item * step, items - 1);
-                if (turn_item < ahead) turns[own][lane] = turn_of(p, s.positions[split == 1 ? of : of / split], turn_pair);
+                if (PACK) {
+                    for (int e = lane; e < ahead * pairs; e += 64) {
+                        const int later = e * by_pairs >> 16, rest = e - later * pairs;
+                        const int over = rest * by_half >> 16, pair = rest - over * half;
+                        const int64_t item = min(at.item + later * step, items - 1);
+                        const int64_t token = cut == 1 ? min(item * pack + over, s.tokens - 1) : item / cut;
+                        turns[own][e] = turn_of(p, s.positions[token], pair);
+                    }
+                } else {
+                    const int64_t item = min(at.item + turn_item * step, items - 1);
+                    if (turn_item < ahead) turns[own][lane] = turn_of(p, s.positions[cut == 1 ? item : item / cut], turn_pair);
+                }
                 wave::sync();
             }
             if (turned) {
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    const float2 t = turns[own][made * p.half + a + i];
+                    const float2 t = turns[own][made * pairs + up * half + a + i];
                     c[i] = t.x;
                     sn[i] = t.y;
                 }
@@ -303,6 +325,8 @@ template <typename T, int W>
 hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
     int lanes = 1;
     while (lanes * 2 * W < p.dim) lanes *= 2;
+    for (NormSide &side : p.side) side.pack = pack_of(side, lanes);
+    const bool packed = p.side[0].pack > 1 || p.side[1].pack > 1;
     // few tokens: their heads over several waves
     int split = 1;
     if (!grad) {
@@ -310,7 +334,11 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
         const int rounds = (std::max(p.side[0].heads, p.side[1].heads) * lanes + 63) / 64;
         split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, 4096 / tokens));
         int64_t all[2], first = 0;
-        for (int i = 0; i < 2; ++i) all[i] = (p.side[i].tokens * split + kWaves - 1) / kWaves;
+        for (int i = 0; i < 2; ++i) {
+            const int pack = p.side[i].pack;
+            const int64_t items = pack > 1 ? (p.side[i].tokens + pack - 1) / pack : p.side[i].tokens * split;
+            all[i] = (items + kWaves - 1) / kWaves;
+        }
         // blocks go on to further tokens: about three each, of 4,096 to 8,192
         // (65,536 tokens of 16 + 4 heads 126 us with 8,192, 135 with half of
         // them, 143 with one token a wave; 21,120 of 8 + 8 heads of 64, 29, 25.5
@@ -329,12 +357,14 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
     } else {
         // rows of a power of two of places
         const int known = W == 4 && lanes >= 4 && lanes * 2 * W == p.dim ? lanes : 0;
-        const auto run = [&](auto l) {
+        const auto run_packed = [&](auto l, auto pack) {
             if (grad)
-                qk_norm_kernel<T, W, true, decltype(l)::value><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
+                qk_norm_kernel<T, W, true, decltype(l)::value, decltype(pack)::value><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
             else
-                qk_norm_kernel<T, W, false, decltype(l)::value><<<blocks, kThreads, 0, s>>>(p, lanes, split);
+                qk_norm_kernel<T, W, false, decltype(l)::value, decltype(pack)::value>
+                    <<<blocks, kThreads, 0, s>>>(p, lanes, split);
         };
+        const auto run = [&](auto l) { packed ? run_packed(l, std::true_type()) : run_packed(l, std::false_type()); };
         if constexpr (W == 4) {
             if (known == 4) run(std::integral_constant<int, 4>());
             if (known == 8) run(std::integral_constant<int, 8>());

@@ -23,6 +23,7 @@ struct NormSide {
     float *dweight;                              // null: not wanted
     int64_t tokens;
     int32_t heads;
+    int32_t pack;                                // tokens that a wave takes at once
     int32_t first_block, blocks;                 // of the launch
 };
 

@@ -79,7 +79,10 @@ def check(name, got, want, bound):
 
 
 SHAPES = [  # q, k, heads of q and k, width, turned
-    (1, 1, 1, 1, 8, 8), (1, 1, 8, 2, 64, 64), (3, 0, 4, 1, 32, 32), (0, 5, 4, 4, 40, 40), (7, 130, 3, 1, 40, 20),
+    (501, 77, 1, 1, 64, 64), (300, 1001, 2, 1, 40, 8), (133, 200, 1, 2, 128, 128), (65, 9, 2, 2, 24, 6),
+    (9, 1030, 16, 1, 32, 32), (70, 70, 3, 3, 16, 0), (77, 501, 3, 5, 64, 48), (50, 1, 7, 1, 8, 8),
+    (1, 1, 1, 1, 8, 8), (1, 1, 8, 2, 64, 64), (3, 0, 4, 1, 32, 32), (0, 5, 4, 4, 40, 40),
+    (7, 130, 3, 1, 40, 20),
     (257, 33, 16, 4, 128, 128), (65, 64, 2, 2, 80, 0), (31, 9, 5, 5, 96, 96), (10, 10, 4, 2, 24, 6), (5, 6, 2, 1, 8, 2),
     (4, 3, 1, 1, 104, 100), (12, 1, 33, 11, 16, 16), (6, 6, 8, 8, 128, 64), (9, 2, 4, 4, 120, 4), (2, 8, 1, 1, 112, 0),
 ]
