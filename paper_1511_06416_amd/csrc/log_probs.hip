@@ -296,11 +296,12 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * 64) void log_probs_
         const T *src = (const T *)p.x + row * p.x_row;
         const int target = p.targets && p.parts == 1 ? p.targets[row] : -1;
         Loose<T, N> v[VECS];
+        const int limit = max(end, N);   // nothing behind the states is read
         const int at0 = beg + (own * 64 + lane) * N;
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) v[i] = vector_at<T, N>(src, at0 + i * WAVES * 64 * N, p.cols);
+        for (int i = 0; i < VECS; ++i) v[i] = vector_at<T, N>(src, at0 + i * WAVES * 64 * N, limit);
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) settle<T, N>(v[i], at0 + i * WAVES * 64 * N, end, p.cols);
+        for (int i = 0; i < VECS; ++i) settle<T, N>(v[i], at0 + i * WAVES * 64 * N, end, limit);
         float asked = -kInf;
         if (own == 0 && lane == 0 && target >= 0 && target < n) asked = (float)src[target];
         float most = -kInf;
@@ -643,16 +644,32 @@ hipError_t launch_typed(const LogProbsParams &p, int dtype, hipStream_t s) {
     }
     const int64_t vecs = (p.part_cols + 64 * N - 1) / (64 * N);
     hipError_t e;
+    // Few waves a row, so that other rows' loads run beside its chain, and vectors
+    // that fit: 4,095 rows of 15,406 fp16 with 20 alternatives 42 us by four waves of
+    // eight, 128 by 16 of four; of 30,000 80 by eight of eight, 128 by 16 of four.
+    // A lone row, or sums alone, take more waves (32,767 columns 7.7 us for 8.1).
     if (vecs <= 1)
         e = launch_rows<T, 1, 1>(p, s);
+    else if (vecs <= 2)
+        e = launch_rows<T, 1, 2>(p, s);
     else if (vecs <= 4)
         e = launch_rows<T, 1, 4>(p, s);
+    else if (vecs <= 8)
+        e = launch_rows<T, 4, 2>(p, s);
+    else if (vecs <= 12)
+        e = launch_rows<T, 4, 3>(p, s);
     else if (vecs <= 16)
         e = launch_rows<T, 4, 4>(p, s);
-    else if (vecs <= 32 && p.parts > 1)
+    else if (vecs <= 24)
+        e = launch_rows<T, 4, 6>(p, s);
+    else if (vecs <= 32)
         e = launch_rows<T, 4, 8>(p, s);
-    else if (sizeof(T) == 2 || vecs <= 64)
+    else if (vecs <= 64 && (p.rows <= 256 || (sizeof(T) == 2 && !p.n_top)))
         e = launch_rows<T, 16, 4>(p, s);
+    else if (vecs <= 48)
+        e = launch_rows<T, 8, 6>(p, s);
+    else if (sizeof(T) == 2 || vecs <= 64)
+        e = launch_rows<T, 8, 8>(p, s);
     else
         e = launch_rows<T, 16, sizeof(T) == 2 ? 4 : 8>(p, s);
     if (e == hipSuccess && p.parts > 1) {

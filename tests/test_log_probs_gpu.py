@@ -144,7 +144,8 @@ def random_rows(rows, cols, seed, ragged):
 
 SHAPES = [(1, 1, 1), (5, 2, 2), (300, 2, 1), (33, 3, 3), (257, 8, 2), (70, 13, 20), (9, 64, 64), (5, 65, 64), (130, 100, 5),
           (4, 300, 40), (3, 511, 20), (6, 513, 0), (7, 2047, 20), (3, 2049, 64), (2, 8191, 1), (2, 9000, 20), (1, 32767, 20),
-          (2, 32768, 64), (2, 32769, 20), (3, 70_001, 64), (1, 300_003, 20)]
+          (2, 32768, 64), (2, 32769, 20), (3, 70_001, 64), (1, 300_003, 20), (5, 600, 7), (3, 3000, 20), (3, 5003, 20),
+          (3, 11_000, 5), (3, 16_001, 64), (260, 20_001, 3), (257, 30_000, 20), (3, 28_000, 0)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
