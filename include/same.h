@@ -734,7 +734,7 @@ int same_qk_norm_workspace_size(int32_t head_dim, int64_t q_tokens, int32_t head
  * possible state has log_probs = -inf, sums = {-inf, 0}, entropy 0 and
  * top_log_probs -inf.  A NaN or +inf among its logits makes a row's values NaN;
  * NaN ranks with -inf among the alternatives.  Sums are fp32, with exponents
- * relative to m; outputs do not depend on the device's scheduling.
+ * relative to m, in an order that depends on rows, cols and n_top alone.
  *
  * workspace (same_log_probs_workspace_size; 0: may be null, 256-byte aligned)
  * holds the parts of long rows.  Outputs must not overlap each other or an
