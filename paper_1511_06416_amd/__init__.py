@@ -12,6 +12,8 @@ from __future__ import annotations
 import ctypes as C
 import os
 import threading
+from array import array
+from itertools import chain
 
 import numpy as np
 
@@ -924,15 +926,18 @@ def same_orthogonalise(g, out, workspace, coefs=NEWTON_SCHULZ, eps=1e-7, scale=1
     """g, out: a matrix or [n] matrices.  coefs: (a, b, c) of every step."""
     lib, here = _begin()
     at, g_mat, g_row = _matrices("g", g, g, here)
-    steps = np.ascontiguousarray(coefs, dtype=np.float64)
-    if steps.ndim != 2 or steps.shape[1] != 3:
+    try:   # half the time that an array of numpy's takes
+        steps, threes = array("d", chain.from_iterable(coefs)), set(map(len, coefs)) == {3}
+    except TypeError:
+        threes = False
+    if not threes:
         raise SameError(SAME_EINVAL, "coefs must be (a, b, c) of every step")
     n = g.shape[0] if g.dim() == 3 else 1
     rows, cols = g.shape[-2:]
     to, out_mat, out_row = _matrices("out", out, g, here)
     need = same_orthogonalise_workspace_size(n, rows, cols, g.dtype)
     _check(lib.same_orthogonalise(_dtype(g.dtype), at, g_mat, g_row, n, rows, cols,
-                                  steps.__array_interface__["data"][0], len(steps), float(eps), float(scale), to,
+                                  steps.buffer_info()[0], len(steps) // 3, float(eps), float(scale), to,
                                   out_mat, out_row, _bytes(workspace, need, here), _now(stream, here)))
 
 

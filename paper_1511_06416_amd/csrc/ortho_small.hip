@@ -12,9 +12,9 @@
 // lane % 16 and the columns 4 t + lane / 16: of a symmetric matrix the same
 // numbers, so the chain needs no exchange within a tile.
 //
-// Measured: 1,000 of 8 x 128 12 us, 1,000 of 30 x 40 34, mostly the steps' chain of
-// dependent 64-bit products (matrix units 33 % busy); one launch where a block holds
-// a matrix's columns.
+// Measured: 1,000 of 8 x 128 8.8 us (12.6 with the factors through LDS and all 16
+// columns contracted), 1,000 of 30 x 40 33, mostly the steps' chain of dependent
+// 64-bit products; one launch where a block holds a matrix's columns.
 #include <algorithm>
 
 #include "step.hpp"
@@ -28,9 +28,11 @@ using wave::Loose;
 
 constexpr int kThreads = 256, kWaves = 4;
 
+// FOURS of the operands' columns, four each; zeros behind them would add nothing.
+template <int FOURS>
 __device__ __forceinline__ f64x4 product(f64x4 p, f64x4 q, f64x4 c) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f64_16x16x4f64(p[t], q[t], c, 0, 0, 0);
+    for (int t = 0; t < FOURS; ++t) c = __builtin_amdgcn_mfma_f64_16x16x4f64(p[t], q[t], c, 0, 0, 0);
     return c;
 }
 __device__ __forceinline__ f64x4 zero4() { return f64x4{0.0, 0.0, 0.0, 0.0}; }
@@ -71,7 +73,7 @@ __device__ __forceinline__ void gram(const OrthoParams &p, int64_t mat, int beg,
 #pragma unroll
         for (int a = 0; a < SIDE; ++a)
 #pragma unroll
-            for (int b = 0; b < SIDE; ++b) acc[a][b] = product(x[a], x[b], acc[a][b]);
+            for (int b = 0; b < SIDE; ++b) acc[a][b] = product<4>(x[a], x[b], acc[a][b]);
     }
 }
 
@@ -93,7 +95,7 @@ __device__ __forceinline__ void gather(f64x4 (&acc)[SIDE][SIDE], Tiles<SIDE> (&p
 }
 
 // From A = G G^T in `a` to T in `t`, by one wave a tile.
-template <int SIDE>
+template <int SIDE, int FOURS>
 __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Tiles<SIDE> &t, Tiles<SIDE> &u) {
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
     // the trace of G G^T is the sum of squares
@@ -104,13 +106,41 @@ __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Ti
         for (int e = 0; e < 4; ++e) trace += 4 * e + g == r ? a.v[s][s][lane][e] : 0.0;
     for (int o = 32; o; o >>= 1) trace += __shfl_xor(trace, o);
     const double f = 1.0 / (__builtin_sqrt(trace) + (double)p.eps);
+    if constexpr (SIDE == 1) {
+        // one wave, whose numbers already are the next operands
+        if (own == 0) {
+            f64x4 x = a.v[0][0][lane] * f * f, one = zero4();   // f^2 may pass 64 bits where A is 0
+#pragma unroll
+            for (int e = 0; e < 4; ++e) one[e] = 4 * e + g == r ? 1.0 : 0.0;
+            f64x4 y = one;
+            // without a branch between products and what reads them: the compiler
+            // has left too few wait states there
+            auto factor = [&](int step) {
+                const double ca = p.coef[step][0], cb = p.coef[step][1], cc = p.coef[step][2];
+                f64x4 s = product<FOURS>(x, x, zero4());
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = cc * s[e] + cb * x[e] + ca * one[e];
+                return s;
+            };
+            for (int step = 0; step + 1 < p.steps; ++step) {
+                const f64x4 s = factor(step);
+                x = product<FOURS>(s, x, zero4());
+                y = product<FOURS>(s, y, zero4());
+                x = product<FOURS>(s, x, zero4());
+            }
+            y = product<FOURS>(factor(p.steps - 1), y, zero4());
+            t.v[0][0][lane] = y * (f * (double)p.out_scale);
+        }
+        __syncthreads();
+        return;
+    }
     const bool mine = own < SIDE * SIDE;
     const int i = own / SIDE % SIDE, j = own % SIDE;   // the output tile of this wave
     // P Q of two matrices that commute: tile (i, j), which is operand (j, i)
     auto times = [&](const Tiles<SIDE> &l, const Tiles<SIDE> &q) {
         f64x4 c = zero4();
 #pragma unroll
-        for (int k = 0; k < SIDE; ++k) c = product(l.v[i][k][lane], q.v[j][k][lane], c);
+        for (int k = 0; k < SIDE; ++k) c = product<FOURS>(l.v[i][k][lane], q.v[j][k][lane], c);
         return c;
     };
     if (mine) {
@@ -155,7 +185,7 @@ __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Ti
 }
 
 // out = T G over the columns [beg, end): a wave takes 16 at a time.
-template <typename T, int SIDE>
+template <typename T, int SIDE, int FOURS>
 __device__ __forceinline__ void apply(const OrthoParams &p, int64_t mat, int beg, int end, const Tiles<SIDE> &t) {
     const int lane = threadIdx.x & 63, own = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     const T *base = (const T *)p.g + mat * p.g_mat;
@@ -170,14 +200,15 @@ __device__ __forceinline__ void apply(const OrthoParams &p, int64_t mat, int beg
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int row = 16 * s + 4 * e + g;
-                const float v = (float)base[min(row, p.n - 1) * down + min(j, p.m - 1) * across];
+                float v = 0.0f;
+                if (e < FOURS) v = (float)base[min(row, p.n - 1) * down + min(j, p.m - 1) * across];
                 x[s][e] = row < p.n && j < end ? (double)v : 0.0;
             }
 #pragma unroll
         for (int a = 0; a < SIDE; ++a) {
             f64x4 y = zero4();
 #pragma unroll
-            for (int k = 0; k < SIDE; ++k) y = product(t.v[a][k][lane], x[k], y);
+            for (int k = 0; k < SIDE; ++k) y = product<FOURS>(t.v[a][k][lane], x[k], y);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int row = 16 * a + 4 * e + g;
@@ -187,7 +218,7 @@ __device__ __forceinline__ void apply(const OrthoParams &p, int64_t mat, int beg
     }
 }
 
-template <typename T, int SIDE>
+template <typename T, int SIDE, int FOURS>
 __global__ __launch_bounds__(kThreads) void ortho_small_kernel(OrthoParams p) {
     __shared__ Tiles<SIDE> part[kWaves], a;
     const int64_t mat = blockIdx.x;
@@ -198,9 +229,9 @@ __global__ __launch_bounds__(kThreads) void ortho_small_kernel(OrthoParams p) {
         for (int j = 0; j < SIDE; ++j) acc[i][j] = zero4();
     gram<T, SIDE>(p, mat, 0, p.m, acc);
     gather<SIDE>(acc, part, a);
-    iterate<SIDE>(p, a, part[0], part[1]);
+    iterate<SIDE, FOURS>(p, a, part[0], part[1]);
     // out may be g: it is written where this block alone has read
-    apply<T, SIDE>(p, mat, 0, p.m, part[0]);
+    apply<T, SIDE, FOURS>(p, mat, 0, p.m, part[0]);
 }
 
 // Long rows: parts of A, the steps, parts of out.
@@ -220,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void ortho_gram_kernel(OrthoParams p) {
     for (int e = threadIdx.x; e < SIDE * SIDE * 64; e += kThreads) to->v[0][0][e] = a.v[0][0][e];
 }
 
-template <int SIDE>
+template <int SIDE, int FOURS>
 __global__ __launch_bounds__(kThreads) void ortho_steps_kernel(OrthoParams p) {
     __shared__ Tiles<SIDE> part[kWaves], a;
     const int64_t mat = blockIdx.x;
@@ -235,12 +266,12 @@ __global__ __launch_bounds__(kThreads) void ortho_steps_kernel(OrthoParams p) {
             for (int k = own; k < p.parts; k += kWaves) acc[i][j] += from[k].v[j][i][lane];
         }
     gather<SIDE>(acc, part, a);
-    iterate<SIDE>(p, a, part[0], part[1]);
+    iterate<SIDE, FOURS>(p, a, part[0], part[1]);
     Tiles<SIDE> *to = (Tiles<SIDE> *)p.small_factors + mat;
     for (int e = threadIdx.x; e < SIDE * SIDE * 64; e += kThreads) to->v[0][0][e] = part[0].v[0][0][e];
 }
 
-template <typename T, int SIDE>
+template <typename T, int SIDE, int FOURS>
 __global__ __launch_bounds__(kThreads) void ortho_apply_kernel(OrthoParams p) {
     __shared__ Tiles<SIDE> t;
     const int64_t mat = blockIdx.x / p.parts;
@@ -248,25 +279,28 @@ __global__ __launch_bounds__(kThreads) void ortho_apply_kernel(OrthoParams p) {
     const Tiles<SIDE> *from = (const Tiles<SIDE> *)p.small_factors + mat;
     for (int e = threadIdx.x; e < SIDE * SIDE * 64; e += kThreads) t.v[0][0][e] = from->v[0][0][e];
     __syncthreads();
-    apply<T, SIDE>(p, mat, beg, min(p.m, beg + p.part_cols), t);
+    apply<T, SIDE, FOURS>(p, mat, beg, min(p.m, beg + p.part_cols), t);
 }
 
-template <typename T, int SIDE>
+template <typename T, int SIDE, int FOURS>
 hipError_t run_side(const OrthoParams &p, hipStream_t s) {
     const uint32_t mats = (uint32_t)p.n_mats, parts = mats * (uint32_t)p.parts;
     if (p.parts == 1) {
-        ortho_small_kernel<T, SIDE><<<mats, kThreads, 0, s>>>(p);
+        ortho_small_kernel<T, SIDE, FOURS><<<mats, kThreads, 0, s>>>(p);
     } else {
         ortho_gram_kernel<T, SIDE><<<parts, kThreads, 0, s>>>(p);
-        ortho_steps_kernel<SIDE><<<mats, kThreads, 0, s>>>(p);
-        ortho_apply_kernel<T, SIDE><<<parts, kThreads, 0, s>>>(p);
+        ortho_steps_kernel<SIDE, FOURS><<<mats, kThreads, 0, s>>>(p);
+        ortho_apply_kernel<T, SIDE, FOURS><<<parts, kThreads, 0, s>>>(p);
     }
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t run_typed(const OrthoParams &p, hipStream_t s) {
-    return p.n <= 16 ? run_side<T, 1>(p, s) : run_side<T, 2>(p, s);
+    // contracted rows, in fours: a count at run time costs more than it saves
+    if (p.n <= 4) return run_side<T, 1, 1>(p, s);
+    if (p.n <= 8) return run_side<T, 1, 2>(p, s);
+    return p.n <= 16 ? run_side<T, 1, 4>(p, s) : run_side<T, 2, 4>(p, s);
 }
 
 }  // namespace

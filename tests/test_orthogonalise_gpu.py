@@ -264,6 +264,8 @@ def test_refusals():
     refuse(workspace=ws[:64])
     refuse(coefs=[])
     refuse(coefs=[(1.0, 2.0)])
+    refuse(coefs=[1.0, 2.0, 3.0])
+    refuse(coefs=[(1.0, 2.0), (1.0, 2.0, 3.0, 4.0)])
     refuse(coefs=[(float("nan"), 0.0, 0.0)])
     refuse(coefs=[(30.0, 0.0, 0.0)])
     refuse(coefs=[(3.0, 0.0, 0.0)] * 3)
