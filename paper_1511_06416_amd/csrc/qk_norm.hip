@@ -132,7 +132,7 @@ int pack_of(const NormSide &s, int lanes) {
 // of 64 23 us, 24 without); LANES = 0 takes any width.  PACK: a side's tokens are
 // packed (the scalar work for it cost 2 to 8 % where none are).
 template <typename T, int W, bool GRAD, int LANES, bool PACK>
-__global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any_lanes, int split) {
+__global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any_lanes) {
     const int lanes = LANES ? LANES : any_lanes;
     __shared__ float2 turns[kWaves][PACK ? 64 * W : 64];
     __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
@@ -158,10 +158,9 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
 #pragma unroll
         for (int i = 0; i < 2 * W; ++i) dw[i] = 0.0f;
     }
-    // items: a token, one of the `cut` parts of its heads, or `pack` tokens of few heads
-    const int pack = PACK ? s.pack : 1, cut = pack > 1 ? 1 : split;
+    // items: a token, one of the shares of its heads, or `pack` tokens of few heads
+    const int pack = PACK ? s.pack : 1, cut = s.shares.cut, part = s.shares.part;
     const int64_t items = (s.tokens + pack - 1) / pack * cut, step = (int64_t)s.blocks * kWaves;
-    const int part = (s.heads + cut - 1) / cut;
     struct Spot {   // where a wave is: its groups' rows are first, first + 1, ...
         int64_t item, token;
         int first, last;
@@ -333,10 +332,13 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
         const int64_t tokens = std::max<int64_t>(1, p.side[0].tokens + p.side[1].tokens);
         const int rounds = (std::max(p.side[0].heads, p.side[1].heads) * lanes + 63) / 64;
         split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, 4096 / tokens));
+    }
+    for (NormSide &side : p.side) side.shares = norm_shares(side.heads, side.pack > 1 ? 1 : split);
+    if (!grad) {
         int64_t all[2], first = 0;
         for (int i = 0; i < 2; ++i) {
             const int pack = p.side[i].pack;
-            const int64_t items = pack > 1 ? (p.side[i].tokens + pack - 1) / pack : p.side[i].tokens * split;
+            const int64_t items = (p.side[i].tokens + pack - 1) / pack * p.side[i].shares.cut;
             all[i] = (items + kWaves - 1) / kWaves;
         }
         // blocks go on to further tokens: about three each, of 4,096 to 8,192
@@ -359,10 +361,9 @@ hipError_t launch(NormParams &p, bool grad, hipStream_t s) {
         const int known = W == 4 && lanes >= 4 && lanes * 2 * W == p.dim ? lanes : 0;
         const auto run_packed = [&](auto l, auto pack) {
             if (grad)
-                qk_norm_kernel<T, W, true, decltype(l)::value, decltype(pack)::value><<<blocks, kThreads, 0, s>>>(p, lanes, 1);
+                qk_norm_kernel<T, W, true, decltype(l)::value, decltype(pack)::value><<<blocks, kThreads, 0, s>>>(p, lanes);
             else
-                qk_norm_kernel<T, W, false, decltype(l)::value, decltype(pack)::value>
-                    <<<blocks, kThreads, 0, s>>>(p, lanes, split);
+                qk_norm_kernel<T, W, false, decltype(l)::value, decltype(pack)::value><<<blocks, kThreads, 0, s>>>(p, lanes);
         };
         const auto run = [&](auto l) { packed ? run_packed(l, std::true_type()) : run_packed(l, std::false_type()); };
         if constexpr (W == 4) {

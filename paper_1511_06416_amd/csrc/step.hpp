@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
+#include "norm_shares.hpp"
+
 namespace same {
 
 // ---- norms of queries and keys with the position rotation
@@ -24,6 +26,7 @@ struct NormSide {
     int64_t tokens;
     int32_t heads;
     int32_t pack;                                // tokens that a wave takes at once
+    NormShares shares;                           // of a token's heads
     int32_t first_block, blocks;                 // of the launch
 };
 

@@ -116,6 +116,20 @@ def test_values_and_gradients(nq, nk, hq, hk, d, rot, dtype):
     assert torch.equal(dq, dq2) and torch.equal(dk, dk2)
 
 
+@pytest.mark.parametrize("nq,nk,hq,hk,d,rot", [
+    (350, 350, 32, 8, 128, 128), (1, 1, 64, 8, 128, 128), (1, 1, 2, 64, 64, 64), (5, 3, 5, 7, 128, 126),
+    (2, 900, 24, 5, 104, 100), (3, 2, 65, 17, 40, 40)])
+def test_few_tokens_of_unlike_heads(nq, nk, hq, hk, d, rot):
+    """A token's heads go over several waves, as many as the side with more heads has: the other
+    side's heads are fewer than its waves, and nothing behind them is read."""
+    q, k = heads(nq, hq, d, torch.bfloat16, 1), heads(nk, hk, d, torch.bfloat16, 2)
+    pq, pk = (torch.arange(n, dtype=torch.int32, device="cuda") for n in (nq, nk))
+    oq, ok = torch.full_like(q, float("nan")), torch.full_like(k, float("nan"))
+    same.same_qk_norm(q, k, oq, ok, q_positions=pq, k_positions=pk, angles=angles(rot))
+    check("q", oq, *reference(q, None, pq, angles(rot), 1e-6))
+    check("k", ok, *reference(k, None, pk, angles(rot), 1e-6))
+
+
 def test_no_tokens():
     q, k = heads(0, 2, 32, torch.float16, 1), heads(0, 1, 32, torch.float16, 2)
     w = torch.ones(32, device="cuda")

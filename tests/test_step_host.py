@@ -1,12 +1,14 @@
 """Refusals of a training step's operators at the C entries: found before
 anything is enqueued, so no device is needed."""
 import ctypes as C
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 import paper_1511_06416_amd as same
+from paper_1511_06416_amd import build
 
 A = 1 << 20   # an address that is never read
 OK = same.SAME_OK
@@ -154,3 +156,19 @@ def test_host_tensors_are_refused():
         same.same_log_probs(x[0], None, None, None)
     with pytest.raises(same.SameError, match="device"):
         same.same_orthogonalise(x, x, None)
+
+
+def test_shares_of_heads(tmp_path):
+    """Every head of a token is in one share, and none is empty: a wave reads its share's first head."""
+    source, lib = tmp_path / "shares.cpp", tmp_path / "shares.so"
+    source.write_text('''#include "norm_shares.hpp"
+extern "C" int wrong(int heads, int split) {
+    const same::NormShares s = same::norm_shares(heads, split);
+    return s.cut < 1 || s.cut > split || (s.cut - 1) * s.part >= heads || s.cut * s.part < heads;
+}
+''')
+    subprocess.check_call(["g++", "-std=c++17", "-shared", "-fPIC", "-I", build.CSRC, "-o", str(lib), str(source)])
+    wrong = C.CDLL(str(lib)).wrong
+    for heads in list(range(1, 140)) + [4096, 65535, 65536]:
+        for split in list(range(1, 140)) + [4096]:
+            assert not wrong(heads, split), (heads, split)
