@@ -134,6 +134,7 @@ __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Ti
         __syncthreads();
         return;
     }
+    __syncthreads();   // every wave has the trace: the tiles that it comes from are scaled in place
     const bool mine = own < SIDE * SIDE;
     const int i = own / SIDE % SIDE, j = own % SIDE;   // the output tile of this wave
     // P Q of two matrices that commute: tile (i, j), which is operand (j, i)

@@ -179,6 +179,17 @@ def test_a_matrix_does_not_depend_on_its_batch():
             assert torch.equal(run(g[i:i + 1])[0], out[i])
 
 
+@pytest.mark.parametrize("rows,cols,n", [(30, 40, 3000), (17, 18, 3000), (32, 32, 3000), (25, 2000, 300)])
+def test_many_blocks_agree(rows, cols, n):
+    """Smaller sides of 17 to 32, where four waves share the tiles of A: with compute units full
+    of blocks, whose waves run apart, equal matrices have equal results, pass after pass."""
+    g = matrices(1, rows, cols, torch.float32, 8)
+    want = run(g)
+    check(want, g)
+    for _ in range(20):
+        assert bool((run(g.expand(n, rows, cols)) == want).all())
+
+
 def test_many_matrices():
     """More matrices than a grid's axis takes, and than the workspace holds at a time."""
     g = matrices(70_000, 3, 5, torch.float32, 2)
