@@ -46,16 +46,22 @@ __device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return 
 // place is t = x log2 e - base, one multiply-add; e = 2^t goes to the sum and
 // t e to the weighted one.  The base's rounding shifts every t alike: it is
 // known to the last bit from a multiply-add, belongs to the logarithm of the
-// sum, and cancels from the entropy.
+// sum, and cancels from the entropy.  It is half of the base's last place: 2^-8
+// up to kFar, all of fp16; beyond, it would reach whole powers of two, and from
+// 2^31 on leave the exponents' range, so that distances are formed first.
+constexpr float kFar = 65536.0f;
+
 struct Place {
     float max, base;
-    bool far;   // the base passes 32 bits: distances are formed first
+    bool far;   // distances are formed first: t has no shift
     __device__ __forceinline__ explicit Place(float m) {
 #pragma clang fp contract(off)
         max = m == -kInf ? 0.0f : m;   // nothing is there, or NaN alone
         base = max * kLog2e;
-        far = __builtin_fabsf(max) > 1e38f;
+        far = __builtin_fabsf(max) > kFar;
     }
+    // What t's of this place lack, the base's rounding.
+    __device__ __forceinline__ float shift() const { return far ? 0.0f : __builtin_fmaf(-max, kLog2e, base); }
 };
 
 template <bool FAR>
@@ -74,7 +80,8 @@ __device__ __forceinline__ void rescale(RowStats &r, float max) {
         return;
     }
     const Place from(r.max), to(max);
-    const float d = from.far || to.far ? (r.max - max) * kLog2e : from.base - to.base;
+    const float d =
+        from.far || to.far ? (r.max - max) * kLog2e + (from.shift() - to.shift()) : from.base - to.base;
     const float e = __builtin_amdgcn_exp2f(d);
     r.weighted = e == 0.0f && r.sum == r.sum ? 0.0f : e * __builtin_fmaf(d, r.sum, r.weighted);
     r.sum *= e;
@@ -89,7 +96,7 @@ struct RowValues {
     __device__ __forceinline__ explicit RowValues(const RowStats &r, bool shifted = true) {
         const Place at(r.max);
         const float bits = __builtin_amdgcn_logf(r.sum);
-        const float off = shifted && !at.far ? __builtin_fmaf(-at.max, kLog2e, at.base) : 0.0f;
+        const float off = shifted ? at.shift() : 0.0f;
         none = r.max == -kInf && r.sum == 0.0f;
         max = r.max;
         log_sum = none ? 0.0f : (bits + off) * kLn2;

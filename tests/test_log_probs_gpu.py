@@ -190,6 +190,33 @@ def test_ties_masks_and_empty_rows(cols, dtype):
     assert got["log_probs"][1] == -INF and got["log_probs"][13] == -INF and got["entropy"][12] == 0
 
 
+@pytest.mark.parametrize("cols", [60, 65, 700, 5000, 20_000, 40_000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sizes_of_the_largest_logit(cols, dtype):
+    """Rows whose logits lie around one value: all alike (masked throughout), spread over what
+    the type can tell apart, and with maxima on either side of it in neighbouring stretches,
+    which waves and parts sum apart."""
+    middles = [30_000.0, 60_000.0, -60_000.0]
+    if dtype != torch.float16:
+        middles += [s * v for v in (65_536.0, 1e5, 1e6, 6e6, 1.6e7, 1e9, 3e9, 5e9, 1e10, 1e20, 1e30, 1e37, 2e38)
+                    for s in (1, -1)]
+    g = torch.Generator().manual_seed(cols)
+    rows = []
+    for v in middles:
+        alike = torch.full((cols,), v, dtype=torch.float64)
+        steps = torch.arange(cols) // 64 % 5 - 2.0
+        rows += [alike, alike + 2.5 * torch.randn(cols, generator=g), alike + 1.5 * steps + 0.3 * torch.randn(cols, generator=g),
+                 alike * (1 + 1e-3 * steps)]
+    x = torch.stack(rows).to(dtype).cuda()
+    counts, targets, dl, dh = random_rows(len(rows), cols, cols, True)
+    for c in (None, counts):
+        got = verify(x, targets, c, min(cols, 20), dl, dh)
+    got = forward(x[::4], None)
+    log_n = float(np.log(cols))   # of the rows of equal logits; log s and the entropy round to 2^-22 (1 + log n)
+    for a in (got["entropy"], got["sums"][:, 1]):
+        assert float((a.cpu().double() - log_n).abs().max()) < 2.0 ** -20 * (1 + log_n)
+
+
 @pytest.mark.parametrize("cols", [5, 300, 5000, 40_000])
 def test_missing_and_infinite_logits(cols):
     x = matrix(4, cols, torch.float32, 3)
