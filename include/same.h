@@ -683,8 +683,8 @@ int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residu
  * [tokens][heads][head_dim] of dtype and may be q or k themselves where those
  * are contiguous; they overlap nothing else.
  *
- * Squares are summed in fp32 (of x 2^-64 where they pass it, eps then counts
- * nothing), angles reduced to an eighth of a turn in 64 bits from turns held in
+ * Squares are summed in fp32 (of x 2^-72 where they pass it: no finite head is
+ * too large), angles reduced to an eighth of a turn in 64 bits from turns held in
  * two, outputs rounded once.  Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE
  * (2^40 tokens, over 65536 heads), SAME_EHIP, SAME_ENOMEM.
  */

@@ -94,30 +94,32 @@ __device__ __forceinline__ void store(T *row, int a, int b, const float (&v)[2 *
     *(Chunk<T, W> *)(row + b) = hi;
 }
 
-// (mean x^2 + eps)^-1/2 of a row.  Where the squares pass 32 bits they are
-// formed again of x 2^-64.
+// (mean x^2 + eps)^-1/2 of a row.  Where the squares pass 32 bits, the row becomes
+// x 2^-72 and the result is that row's: 128 squares of the type's largest number
+// stay below 2^119.  `up` is what x was scaled by.
 template <int W>
-__device__ __forceinline__ float inverse_norm(const NormParams &p, const float (&x)[2 * W], int lanes) {
+__device__ __forceinline__ float inverse_norm(const NormParams &p, float (&x)[2 * W], int lanes, float &up) {
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2 * W; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
     ss = group_sum(ss, lanes);
-    float up = 1.0f, mean = __builtin_fmaf(ss, p.inv_dim, p.eps);
+    float mean = __builtin_fmaf(ss, p.inv_dim, p.eps);
+    up = 1.0f;
     if (__builtin_isinf(mean)) {
+        up = 0x1p-72f;
         ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < 2 * W; ++i) {
-            const float small = x[i] * 0x1p-64f;
-            ss = __builtin_fmaf(small, small, ss);
+            x[i] *= up;
+            ss = __builtin_fmaf(x[i], x[i], ss);
         }
-        mean = group_sum(ss, lanes) * p.inv_dim;
-        up = 0x1p-64f;
+        mean = __builtin_fmaf(group_sum(ss, lanes), p.inv_dim, p.eps * up * up);
     }
     // the hardware's root is off by an ulp: one step of Newton's method
     float r = __builtin_amdgcn_rsqf(mean);
     const float e = __builtin_fmaf(-mean * r, r, 1.0f);
     if (__builtin_fabsf(e) < 0.5f) r = __builtin_fmaf(0.5f * r, e, r);
-    return r * up;
+    return r;
 }
 
 // Tokens that a wave's groups of lanes take at once where they have few heads
@@ -240,7 +242,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
 #pragma unroll
             for (int i = 0; i < 2 * W; ++i) v[i] = 0.0f;
         }
-        const float norm = inverse_norm<W>(p, v, lanes);
+        float scaled;
+        const float norm = inverse_norm<W>(p, v, lanes, scaled);
 #pragma unroll
         for (int i = 0; i < 2 * W; ++i) v[i] *= norm;  // xhat
         if (!GRAD) {
@@ -269,8 +272,9 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
                 t = __builtin_fmaf(u[W + i], v[W + i], t);
             }
             t = group_sum(t, lanes) * p.inv_dim;
+            const float of_x = norm * scaled;
 #pragma unroll
-            for (int i = 0; i < 2 * W; ++i) u[i] = norm * __builtin_fmaf(-v[i], t, u[i]);
+            for (int i = 0; i < 2 * W; ++i) u[i] = of_x * __builtin_fmaf(-v[i], t, u[i]);
         }
         if (here) store<T, W>(to + (at.token * s.heads + at.first) * dim, out_ahead + a, out_ahead + b, u);
         entered = leaves;

@@ -257,6 +257,40 @@ def test_huge_tiny_and_missing_values(dtype):
         check("row %d" % row, dx[row], want[row], bound[row])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,rot", [(128, 128), (64, 0), (40, 20), (8, 2)])
+def test_the_largest_values(d, rot, dtype):
+    """Heads up to the type's largest number in every element, and an eps that passes 32 bits
+    together with the squares.  The gradient's own factor, 1 / |x|, is below the normal numbers
+    there and held to 2^-22 of itself, within the bound's room of 24 U for 18."""
+    big = torch.finfo(dtype).max
+    q = heads(9, 2, d, dtype, 1).float()
+    q[0] = torch.where(q[0] < 0, -big, big)
+    q[1] = 0
+    q[1, :, :2] = big
+    q[2] = min(3.1e37, big)
+    q[3] *= big / 8
+    q[4] = min(1e19, big)
+    q[5] *= min(1e19, big / 8)
+    q[6] = 0
+    q[6, :, 1] = -big
+    q[7] *= min(3e18, big / 8)
+    q = q.clamp(-big, big).to(dtype)
+    w = (1 + 0.1 * torch.arange(d)).float().cuda()
+    pos, a = torch.arange(9, dtype=torch.int32, device="cuda"), angles(rot)
+    k, dy = q[:0], (1000 * heads(9, 2, d, dtype, 2).float()).clamp(-big, big).to(dtype)
+    ws = torch.empty(same.same_qk_norm_workspace_size(d, 9, 2, 0, 2), dtype=torch.uint8, device="cuda")
+    for eps in (1e-6, 3e38):
+        kw = dict(q_weight=w, q_positions=pos, k_positions=pos[:0], angles=a, eps=eps)
+        y, dx, dw = torch.empty_like(q), torch.empty_like(q), torch.empty_like(w)
+        same.same_qk_norm(q, k, y, k, **kw)
+        same.same_qk_norm_backward(q, k, dy, k, dx, k, dw, None, ws, **kw)
+        check("y", y, *reference(q, w, pos, a, eps))
+        (want, bound), (want_w, bound_w) = reference(q, w, pos, a, eps, dy)
+        check("dx", dx, want, bound)
+        check("dw", dw, want_w, bound_w)
+
+
 def test_far_offsets():
     """More than 2^31 elements, and a view whose rows lie as far apart: a row's result is its own."""
     n = 2_100_000
