@@ -20,6 +20,21 @@ __device__ __forceinline__ void split(float a, float b, f16x2 &hi, f16x2 &lo) {
         f32x2{__builtin_fmaf((float)hi[0], -1.0f, a), __builtin_fmaf((float)hi[1], -1.0f, b)}, f16x2);
 }
 
+// X in planes, sx G / (|G| + eps), of one number of G.  The factor lies between
+// 2^-132 and 2^138 and passes 32 bits at both ends: its power of two comes first,
+// exact where X is not below 2^-126 by then, so that one rounding is left.
+struct PlaneFactor {
+    float part;
+    int power;
+    __device__ __forceinline__ PlaneFactor() : part(0.0f), power(0) {}
+    __device__ __forceinline__ PlaneFactor(float sx, double squares, float eps) {
+        const double f = (double)sx / (__builtin_sqrt(squares) + (double)eps);
+        part = (float)__builtin_amdgcn_frexp_mant(f);   // 0 stays 0, NaN NaN
+        power = __builtin_amdgcn_frexp_exp(f);
+    }
+    __device__ __forceinline__ float operator()(float g) const { return __builtin_amdgcn_ldexpf(g, power) * part; }
+};
+
 // N numbers v(0), v(1), ...
 template <int N, typename V, typename H>
 __device__ __forceinline__ void split_all(V v, H &hi, H &lo) {

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kThreads) void ortho_columns_kernel(OrthoParams p, 
     const int b = own % NT, a0 = own / NT;
     const bool squares = a0 < kGroups && a0 < NT;
     f32x16 acc[kMine];
-    float factor = 0.0f;
+    PlaneFactor of_g;
     if (PASS == kFirst) {
         double total = 0.0;
         for (int i = threadIdx.x; i < square_parts; i += kThreads) total += p.squares[mat * kNormParts + i];
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads) void ortho_columns_kernel(OrthoParams p, 
         total = 0.0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) total += sums[w];
-        factor = (float)((double)p.sx / (__builtin_sqrt(total) + (double)p.eps));
+        of_g = PlaneFactor(p.sx, total, p.eps);
     } else {
         // B = b A + c A A, where A was
         constexpr int kChunks = 4 * NT;   // of 16 bytes a row
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void ortho_columns_kernel(OrthoParams p, 
                 for (int e = 0; e < 4; ++e) {
                     const int i = 16 * t + 4 * quarter + e;
                     const float v = (float)mine[min(i, p.n - 1) * down];
-                    x[t][e] = i < p.n && j < p.m ? v * factor : 0.0f;
+                    x[t][e] = i < p.n && j < p.m ? of_g(v) : 0.0f;
                 }
         } else {
 #pragma unroll

@@ -59,11 +59,11 @@ __global__ __launch_bounds__(MT * 64) void ortho_whole_kernel(OrthoParams p) {
     __syncthreads();
     total = 0.0;
     for (int w = 0; w < waves; ++w) total += sums[w];
-    const float factor = (float)((double)p.sx / (__builtin_sqrt(total) + (double)p.eps));
+    const PlaneFactor of_g(p.sx, total, p.eps);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[t][e] *= factor;
+        for (int e = 0; e < 16; ++e) x[t][e] = of_g(x[t][e]);
 
     // Of the small products a wave takes tiles (a, b) of one column b, every
     // groups-th; both halves of a symmetric matrix are formed, which costs less
@@ -229,9 +229,11 @@ __global__ __launch_bounds__(512) void ortho_strips_kernel(OrthoParams p) {
     total = 0.0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) total += sums[w];
-    const float factor = (float)((double)p.sx / (__builtin_sqrt(total) + (double)p.eps));
+    const PlaneFactor of_g(p.sx, total, p.eps);
 #pragma unroll
-    for (int t = 0; t < 2 * NT; ++t) x[t] *= factor;
+    for (int t = 0; t < 2 * NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][e] = of_g(x[t][e]);
 
     // of the small products a wave takes tiles (a0 + groups i, b)
     const int b = own % NT, a0 = own / NT;

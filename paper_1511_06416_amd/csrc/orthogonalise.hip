@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, in
     double total = 0.0;
     for (int i = threadIdx.x; i < parts; i += kThreads) total += p.squares[mat * kNormParts + i];
     total = block_sum(total);
-    const float factor = (float)((double)p.sx / (__builtin_sqrt(total) + (double)p.eps));
+    const PlaneFactor of_g(p.sx, total, p.eps);
     const int i0 = at % tiles_i * 64, j0 = at / tiles_i * 64;
     const T *g = (const T *)p.g + mat * p.g_mat;
     const int c = 8 * (threadIdx.x & 7);
@@ -91,10 +91,10 @@ __global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, in
         if (i < p.rows && j + 8 <= p.cols) {
             const wave::Loose<T, 8> l = *(const wave::Loose<T, 8> *)src;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)l.v[e] * factor;
+            for (int e = 0; e < 8; ++e) v[e] = of_g((float)l.v[e]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = i < p.rows && j + e < p.cols ? (float)src[e] * factor : 0.0f;
+            for (int e = 0; e < 8; ++e) v[e] = i < p.rows && j + e < p.cols ? of_g((float)src[e]) : 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

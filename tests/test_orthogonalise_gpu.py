@@ -138,6 +138,25 @@ def test_sizes_of_values(rows, cols):
     assert abs(float(got[0, 2, 3]) + want) < 1e-5 and int((got != 0).sum()) == 1
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(6, 9), (20, 5000), (40, 70), (64, 256), (128, 100), (130, 200), (300, 50),
+                                       (90, 1500), (70, 8200)])
+def test_the_smallest_eps(rows, cols, dtype):
+    """eps = 2^-126, in every form: zeros stay zeros, and updates whose norm and eps together
+    stay far below 2^-113, where a factor of 2^12 over them passes 32 bits, come out whole."""
+    eps, least = 2.0 ** -126, torch.finfo(dtype).smallest_normal
+    g = matrices(4, rows, cols, torch.float32, 2)
+    g[0] = 0
+    g[1] *= least / 16    # of fp32: 20 bits and fewer an entry, which are what the update is made of
+    g[2] *= least * 64
+    g = (g * (torch.arange(4, device="cuda") < 3)[:, None, None]).to(dtype)
+    g[3, 1, 2] = torch.finfo(dtype).max
+    out = run(g, eps=eps)
+    assert not out[0].any()
+    for i in (1, 2, 3):
+        check(out[i], g[i], eps=eps)
+
+
 def test_orthogonal():
     """Steps that converge give the polar factor: U U^T = 1."""
     g = matrices(2, 60, 200, torch.float32, 9)
