@@ -95,6 +95,8 @@ def dropout(x, drop, seed, call_id, residual=None):
 class _QkNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, q_positions, k_positions, angles, eps):
+        if angles is not None:   # the backward pass turns by what the forward pass did, whatever becomes of the caller's
+            angles = np.array(angles, dtype=np.float64)
         q_out, k_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
         same_qk_norm(q, k, q_out, k_out, q_weight=q_weight, k_weight=k_weight, q_positions=q_positions,
                      k_positions=k_positions, angles=angles, eps=eps)

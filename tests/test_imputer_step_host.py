@@ -1,5 +1,6 @@
 """The autograd functions around a training step's operators, with plain
 arithmetic in the operators' place: what reaches them and what comes back."""
+import numpy as np
 import pytest
 import torch
 
@@ -70,6 +71,19 @@ def test_norm_gradients(stand_ins):
     for dq_out, dk_out, *_ in stand_ins:
         for g in (dq_out, dk_out):
             assert g.data_ptr() % 16 == 0 and g.stride(2) == 1 and not any(s % 8 for s in g.stride()[:2])
+
+
+def test_angles_are_the_forward_pass_s(stand_ins, monkeypatch):
+    """A caller who changes its angles before the backward pass gets the gradient of what was computed."""
+    seen = []
+    plain = imputer.same_qk_norm_backward
+    monkeypatch.setattr(imputer, "same_qk_norm_backward", lambda *a, **kw: (seen.append(kw["angles"]), plain(*a, **kw)))
+    q, pos = torch.randn(4, 2, 8, requires_grad=True), torch.arange(4, dtype=torch.int32)
+    angles = np.array([1.0, 0.5])
+    a, b = imputer.qk_norm(q, q, None, None, pos, pos, angles)
+    angles[:] = 7.0
+    (a.sum() + b.sum()).backward()
+    assert seen[0].tolist() == [1.0, 0.5]
 
 
 def test_log_probs_gradients(stand_ins):
