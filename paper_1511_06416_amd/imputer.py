@@ -196,6 +196,10 @@ class Orthogonal(torch.optim.Optimizer):
 
         m <- momentum m + g,  u = g + momentum m (nesterov) or m
         w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) orthogonalise(u)
+
+    Momentum is held in 32 bits whatever the parameter's type.  u is orthogonalised
+    in that type; of fp16 parameters in 32 bits, as sums of gradients pass fp16's
+    range.
     """
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, coefs=NEWTON_SCHULZ,
@@ -221,6 +225,19 @@ class Orthogonal(torch.optim.Optimizer):
             raise ValueError("a parameter of shape %s is neither a matrix nor a row of them" % (tuple(p.shape),))
         return (1, *p.shape) if p.dim() == 2 else tuple(p.shape)
 
+    @staticmethod
+    def _wide(p):
+        return torch.promote_types(p.dtype, torch.float32)
+
+    def load_state_dict(self, state_dict):
+        """As torch's, which would give the momentum its parameter's type."""
+        super().load_state_dict(state_dict)
+        saved = [i for group in state_dict["param_groups"] for i in group["params"]]
+        params = [p for group in self.param_groups for p in group["params"]]
+        for i, p in zip(saved, params):
+            if "momentum" in state_dict["state"].get(i, ()):
+                self.state[p]["momentum"] = state_dict["state"][i]["momentum"].to(p.device, self._wide(p), copy=True)
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
@@ -235,10 +252,10 @@ class Orthogonal(torch.optim.Optimizer):
                 shape = self._shape(p, group)
                 state = self.state[p]
                 if "momentum" not in state:
-                    state["momentum"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
+                    state["momentum"] = torch.zeros_like(p, dtype=self._wide(p), memory_format=torch.contiguous_format)
                 m = state["momentum"].mul_(momentum).add_(p.grad)
                 u = p.grad.add(m, alpha=momentum) if group["nesterov"] else m
-                u = u.contiguous().view(shape)
+                u = u.to(torch.float32 if p.dtype is torch.float16 else p.dtype).contiguous().view(shape)
                 out = torch.empty_like(u)
                 workspace = torch.empty(max(same_orthogonalise_workspace_size(*shape, u.dtype), 1), dtype=torch.uint8,
                                         device=u.device)

@@ -95,6 +95,25 @@ def test_orthogonal_steps(nesterov):
         assert float((p.detach().cpu().double() - w).abs().max()) < 3 * (1e-5 + 8 * 2.0 ** -24 * 4)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_orthogonal_steps_of_16_bits(dtype):
+    """The step is the operator on a momentum in 32 bits, bit for bit."""
+    g = torch.Generator().manual_seed(1)
+    p = torch.nn.Parameter(torch.randn(20, 12, generator=g).to(dtype).cuda())
+    opt, m, want = Orthogonal([p], lr=0.1), torch.zeros(20, 12, device="cuda"), p.detach().clone()
+    room = torch.empty(same.same_orthogonalise_workspace_size(1, 20, 12, torch.float32) + 1, dtype=torch.uint8, device="cuda")
+    for _ in range(5):
+        p.grad = (30_000 * torch.rand(20, 12, generator=g)).to(dtype).cuda()
+        m.mul_(0.95).add_(p.grad)
+        u = p.grad.add(m, alpha=0.95)
+        u = u.bfloat16() if dtype is torch.bfloat16 else u
+        out = torch.empty_like(u)
+        same.same_orthogonalise(u, out, room, scale=(20 / 12) ** 0.5)
+        want.add_(out, alpha=-0.1)
+        opt.step()
+        assert torch.equal(p.detach(), want) and bool(p.isfinite().all())
+
+
 def test_training_with_positions_runs():
     """Several columns in one segment, an entry's column as its position: every
     parameter gets a finite gradient and a step, and answers change with the

@@ -114,6 +114,35 @@ def test_second_derivatives_are_refused(stand_ins):
             torch.autograd.grad((g * g).sum() + (y ** 3).sum(), y)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_momentum_is_held_in_32_bits(dtype, monkeypatch):
+    """Against sums in 64 bits, with gradients of which fp16 cannot hold twenty, and through a
+    state_dict.  Each of a step's three roundings is 2^-24 of a momentum of at most 20 gradients."""
+    taken = []
+    monkeypatch.setattr(imputer, "same_orthogonalise_workspace_size", lambda *a: 8)
+    monkeypatch.setattr(imputer, "same_orthogonalise", lambda u, out, *a, **kw: (taken.append(u.clone()), out.zero_()))
+    g = torch.Generator().manual_seed(2)
+    p = torch.nn.Parameter(torch.zeros(6, 8, dtype=dtype))
+    opt = imputer.Orthogonal([p], momentum=0.95)
+    m, most = torch.zeros(6, 8, dtype=torch.float64), 60_000.0
+    for step in range(60):
+        p.grad = (most * (1 - 0.02 * torch.rand(6, 8, generator=g))).to(dtype)
+        m = 0.95 * m + p.grad.double()
+        opt.step()
+        if step == 30:
+            again = imputer.Orthogonal([p], momentum=0.95)
+            again.load_state_dict(opt.state_dict())
+            opt = again
+    off = 60 * 3 * 2.0 ** -24 * 20 * most
+    held = opt.state[p]["momentum"]
+    assert held.dtype is torch.float32 and float((held.double() - m).abs().max()) < off
+    # what is orthogonalised: fp16's in 32 bits, bf16's rounded once
+    want = p.grad.double() + 0.95 * m
+    half = torch.finfo(taken[-1].dtype).eps / 2
+    assert taken[-1].dtype is (torch.bfloat16 if dtype is torch.bfloat16 else torch.float32)
+    assert bool(((taken[-1][0].double() - want).abs() <= off + half * (want + off)).all())
+
+
 def test_orthogonal_refusals():
     p = torch.nn.Parameter(torch.zeros(6, 8))
     for kw in (dict(lr=-1.0), dict(momentum=1.0), dict(weight_decay=-0.1), dict(shape=(5, 4))):
