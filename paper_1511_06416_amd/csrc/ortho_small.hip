@@ -135,7 +135,7 @@ __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Ti
         return;
     }
     __syncthreads();   // every wave has the trace: the tiles that it comes from are scaled in place
-    const bool mine = own < SIDE * SIDE;
+    static_assert(SIDE == 1 || SIDE * SIDE == kWaves, "a wave takes a tile");
     const int i = own / SIDE % SIDE, j = own % SIDE;   // the output tile of this wave
     // P Q of two matrices that commute: tile (i, j), which is operand (j, i)
     auto times = [&](const Tiles<SIDE> &l, const Tiles<SIDE> &q) {
@@ -144,44 +144,39 @@ __device__ __forceinline__ void iterate(const OrthoParams &p, Tiles<SIDE> &a, Ti
         for (int k = 0; k < SIDE; ++k) c = product<FOURS>(l.v[i][k][lane], q.v[j][k][lane], c);
         return c;
     };
-    if (mine) {
-        // one of f's factors at a time: f^2 may pass 64 bits where A is 0
-        a.v[j][i][lane] = a.v[j][i][lane] * f * f;
-        f64x4 one = zero4();
+    // one of f's factors at a time: f^2 may pass 64 bits where A is 0
+    a.v[j][i][lane] = a.v[j][i][lane] * f * f;
+    f64x4 one = zero4();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) one[e] = i == j && 4 * e + g == r ? 1.0 : 0.0;
-        t.v[j][i][lane] = one;
-    }
+    for (int e = 0; e < 4; ++e) one[e] = i == j && 4 * e + g == r ? 1.0 : 0.0;
+    t.v[j][i][lane] = one;
     __syncthreads();
-    for (int step = 0; step < p.steps; ++step) {
+    // straight-line code between products and what reads them, as above
+    auto factor = [&](int step) {
         const double ca = p.coef[step][0], cb = p.coef[step][1], cc = p.coef[step][2];
-        if (mine) {
-            f64x4 s = times(a, a);
-            const f64x4 old = a.v[j][i][lane];
+        f64x4 s = times(a, a);
+        const f64x4 old = a.v[j][i][lane];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                s[e] = cc * s[e] + cb * old[e] + (i == j && 4 * e + g == r ? ca : 0.0);
-            u.v[j][i][lane] = s;
-        }
+        for (int e = 0; e < 4; ++e) s[e] = cc * s[e] + cb * old[e] + (i == j && 4 * e + g == r ? ca : 0.0);
+        u.v[j][i][lane] = s;
         __syncthreads();
-        f64x4 next, q;
-        if (mine) {
-            next = times(u, t);
-            if (step + 1 < p.steps) q = times(u, a);
-        }
+    };
+    for (int step = 0; step + 1 < p.steps; ++step) {
+        factor(step);
+        const f64x4 next = times(u, t), half = times(u, a);
         __syncthreads();
-        if (mine) {
-            t.v[j][i][lane] = next;
-            if (step + 1 < p.steps) a.v[j][i][lane] = q;
-        }
+        t.v[j][i][lane] = next;
+        a.v[j][i][lane] = half;
         __syncthreads();
-        if (step + 1 == p.steps) break;
-        if (mine) q = times(u, a);
+        const f64x4 whole = times(u, a);
         __syncthreads();
-        if (mine) a.v[j][i][lane] = q;
+        a.v[j][i][lane] = whole;
         __syncthreads();
     }
-    if (mine) t.v[j][i][lane] = t.v[j][i][lane] * (f * (double)p.out_scale);
+    factor(p.steps - 1);
+    const f64x4 last = times(u, t);
+    __syncthreads();
+    t.v[j][i][lane] = last * (f * (double)p.out_scale);
     __syncthreads();
 }
 

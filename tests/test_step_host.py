@@ -1,6 +1,7 @@
 """Refusals of a training step's operators at the C entries: found before
 anything is enqueued, so no device is needed."""
 import ctypes as C
+import re
 import subprocess
 
 import numpy as np
@@ -172,3 +173,69 @@ extern "C" int wrong(int heads, int split) {
     for heads in list(range(1, 140)) + [4096, 65535, 65536]:
         for split in list(range(1, 140)) + [4096]:
             assert not wrong(heads, split), (heads, split)
+
+
+def closest_read(listing):
+    """The fewest wait states from a 64-bit matrix product to an instruction that reads its result
+    as no sum, over every path of a listing's kernels."""
+    def registers(operand):
+        m = re.match(r"-?\|?([av])\[(\d+):(\d+)\]|-?\|?([av])(\d+)\b", operand)
+        if not m:
+            return set()
+        if m[1]:
+            return {(m[1], i) for i in range(int(m[2]), int(m[3]) + 1)}
+        return {(m[4], int(m[5]))}
+
+    least, products = 99, 0
+    for body in re.findall(r"^_ZN\S*kernel\S*:.*?\n(.*?)s_endpgm", listing, re.M | re.S):
+        lines = [line.split(";")[0].split() for line in body.split("\n")]
+        lines = [[x.strip(",") for x in line] for line in lines if line and not (line[0].startswith(".") and ":" not in line[0])]
+        labels = {line[0][:-1]: i for i, line in enumerate(lines) if line[0].endswith(":")}
+        for start, line in enumerate(lines):
+            if not line[0].startswith("v_mfma_f64"):
+                continue
+            products += 1
+            result, paths, seen = registers(line[1]), [(start + 1, 0)], {}
+            while paths:
+                at, states = paths.pop()
+                while at < len(lines) and states < least and seen.get(at, 99) > states:
+                    seen[at] = states
+                    op, *args = lines[at]
+                    at += 1
+                    if op.endswith(":"):
+                        continue
+                    if op.startswith("v_mfma"):
+                        if any(registers(a) & result for a in args[1:3]):
+                            least = states
+                        if registers(args[0]) & result:
+                            break   # its own sum goes on: that product is looked at by itself
+                        states += 16 if "f64" in op else 4
+                        continue
+                    reads = args[1:] if op.startswith("v_") else args if op.startswith(("ds_write", "global_store", "buffer_store")) else []
+                    if any(registers(a) & result for a in reads):
+                        least = states
+                    if op == "s_branch":
+                        at, states = labels[args[0]], states + 1
+                        continue
+                    if op.startswith("s_cbranch"):
+                        paths.append((labels[args[0]], states + 1))
+                    states += int(args[0]) + 1 if op == "s_nop" else 1
+    return least, products
+
+
+def test_results_of_64_bit_products_are_waited_for(tmp_path):
+    """A compiler has read such a result behind a branch too few wait states after its product, and
+    a step of a small update was lost without an error: it takes 18 of them to be there."""
+    listing = tmp_path / "small.s"
+    command = build.command("ortho_small.hip", str(listing))
+    at = command.index("-c")
+    subprocess.check_call(command[:at] + ["--cuda-device-only", "-S"] + command[at + 1:], stderr=subprocess.DEVNULL)
+    least, products = closest_read(listing.read_text())
+    assert products >= 34 and least >= 18, (products, least)   # of 34 kernels, each with one at least
+
+
+def test_reads_behind_branches_are_found():
+    kernel = "_ZN4same6kernelE:\n v_mfma_f64_16x16x4_f64 v[0:7], v[8:9], v[10:11], 0\n %s\n s_endpgm\n"
+    assert closest_read(kernel % "s_nop 15\n s_nop 1\n v_add_f64 v[8:9], v[2:3], v[2:3]")[0] == 18
+    assert closest_read(kernel % "s_cbranch_scc1 .LBB0_2\n s_nop 15\n s_nop 3\n.LBB0_2:\n s_nop 4\n ds_write_b64 v20, v[6:7]")[0] == 6
+    assert closest_read(kernel % "v_mfma_f64_16x16x4_f64 v[0:7], v[12:13], v[14:15], v[0:7]\n s_nop 6\n v_mov_b32 v9, v0")[0] == 7
