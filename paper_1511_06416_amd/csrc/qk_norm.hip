@@ -129,6 +129,10 @@ int pack_of(const NormSide &s, int lanes) {
     return s.heads < groups && s.tokens >= groups ? groups / s.heads : 1;
 }
 
+// Rows of which a lane sums the weights' gradients in 32 bits before they go to a
+// sum in 64, so that the error does not grow with the tokens.
+constexpr int kRun = 16;
+
 // A row's loads are under way while the one before it is worked on.  With LANES
 // a row fills that many lanes, known to the compiler (21,120 tokens of 8 + 8 heads
 // of 64 23 us, 24 without); LANES = 0 takes any width.  PACK: a side's tokens are
@@ -137,7 +141,7 @@ template <typename T, int W, bool GRAD, int LANES, bool PACK>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any_lanes) {
     const int lanes = LANES ? LANES : any_lanes;
     __shared__ float2 turns[kWaves][PACK ? 64 * W : 64];
-    __shared__ float sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
+    __shared__ double sums[GRAD ? kWaves : 1][GRAD ? kMaxHeadDim : 1];
     const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool keys = (int)blockIdx.x >= p.side[1].first_block;
     const NormSide &s = p.side[keys];
@@ -156,9 +160,14 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
         w[i] = s.weight ? s.weight[a + i] : 1.0f;
         w[W + i] = s.weight ? s.weight[b + i] : 1.0f;
     }
+    double dws[2 * W];
+    int run = 0;
     if (GRAD) {
 #pragma unroll
-        for (int i = 0; i < 2 * W; ++i) dw[i] = 0.0f;
+        for (int i = 0; i < 2 * W; ++i) {
+            dw[i] = 0.0f;
+            dws[i] = 0.0;
+        }
     }
     // items: a token, one of the shares of its heads, or `pack` tokens of few heads
     const int pack = PACK ? s.pack : 1, cut = s.shares.cut, part = s.shares.part;
@@ -281,24 +290,34 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(NormParams p, int any
         at = next;
         x = next_x;
         if (GRAD) y = next_y;
+        if (GRAD && ++run == kRun) {
+            run = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i) {
+                dws[i] += (double)dw[i];
+                dw[i] = 0.0f;
+            }
+        }
     }
     if (GRAD && s.dweight) {
 #pragma unroll
-        for (int i = 0; i < 2 * W; ++i)
-            for (int o = lanes; o < 64; o <<= 1) dw[i] += __shfl_xor(dw[i], o);
+        for (int i = 0; i < 2 * W; ++i) {
+            dws[i] += (double)dw[i];
+            for (int o = lanes; o < 64; o <<= 1) dws[i] += __shfl_xor(dws[i], o);
+        }
         if (used && group == 0) {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                sums[own][a + i] = dw[i];
-                sums[own][b + i] = dw[W + i];
+                sums[own][a + i] = dws[i];
+                sums[own][b + i] = dws[W + i];
             }
         }
         __syncthreads();
         for (int e = threadIdx.x; e < p.dim; e += kThreads) {
-            float t = 0.0f;
+            double t = 0.0;
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) t += sums[v][e];
-            p.part[(int64_t)blockIdx.x * p.dim + e] = t;
+            p.part[(int64_t)blockIdx.x * p.dim + e] = (float)t;
         }
     }
 }

@@ -130,6 +130,22 @@ def test_few_tokens_of_unlike_heads(nq, nk, hq, hk, d, rot):
     check("k", ok, *reference(k, None, pk, angles(rot), 1e-6))
 
 
+@pytest.mark.parametrize("d,rot", [(72, 2), (128, 0)])
+def test_sums_of_many_tokens(d, rot):
+    """The weights' gradients of 2^24 equal tokens, whose roundings all go one way.  Sums are
+    16 terms in 32 bits, then 64, with one rounding of a part and one of the result: 18 U of
+    the terms beside the terms' own errors, whatever their number."""
+    n = 1 << 24
+    q, dy, k = heads(1, 1, d, torch.bfloat16, 1), heads(1, 1, d, torch.bfloat16, 2), heads(0, 1, d, torch.bfloat16, 3)
+    pos, dw = torch.full((n,), 3, dtype=torch.int32, device="cuda"), torch.empty(d, device="cuda")
+    dq = torch.empty(n, 1, d, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(same.same_qk_norm_workspace_size(d, n, 1, 0, 1), dtype=torch.uint8, device="cuda")
+    same.same_qk_norm_backward(q.expand(n, 1, d), k, dy.expand(n, 1, d), k, dq, k, dw, None, ws, q_positions=pos,
+                               k_positions=pos[:0], angles=angles(rot))
+    _, (want, bound) = reference(q, None, pos[:1], angles(rot), 1e-6, dy)   # of one token: its terms' errors, and U
+    check("dw", dw, n * want, n * (bound + 18 * U * want.abs()))
+
+
 def test_no_tokens():
     q, k = heads(0, 2, 32, torch.float16, 1), heads(0, 1, 32, torch.float16, 2)
     w = torch.ones(32, device="cuda")
