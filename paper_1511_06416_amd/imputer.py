@@ -197,9 +197,10 @@ class Orthogonal(torch.optim.Optimizer):
         m <- momentum m + g,  u = g + momentum m (nesterov) or m
         w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) orthogonalise(u)
 
-    Momentum is held in 32 bits whatever the parameter's type.  u is orthogonalised
-    in that type; of fp16 parameters in 32 bits, as sums of gradients pass fp16's
-    range.
+    Momentum is held in 32 bits whatever the parameter's type; the first step
+    creates it and cannot be captured into a graph, later ones can.  u is
+    orthogonalised in the parameter's type; of fp16 parameters in 32 bits, as sums
+    of gradients pass fp16's range.
     """
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, coefs=NEWTON_SCHULZ,
@@ -252,6 +253,8 @@ class Orthogonal(torch.optim.Optimizer):
                 shape = self._shape(p, group)
                 state = self.state[p]
                 if "momentum" not in state:
+                    if p.is_cuda and torch.cuda.is_current_stream_capturing():   # every replay would clear it
+                        raise RuntimeError("Orthogonal: the first step creates the momentum; take it before the capture")
                     state["momentum"] = torch.zeros_like(p, dtype=self._wide(p), memory_format=torch.contiguous_format)
                 m = state["momentum"].mul_(momentum).add_(p.grad)
                 u = p.grad.add(m, alpha=momentum) if group["nesterov"] else m

@@ -114,6 +114,32 @@ def test_orthogonal_steps_of_16_bits(dtype):
         assert torch.equal(p.detach(), want) and bool(p.isfinite().all())
 
 
+def test_captured_steps_keep_their_momentum():
+    """A captured first step would clear the momentum in each replay: it is refused.  Later ones
+    are replayed as they run."""
+    start = torch.randn(20, 12, generator=torch.Generator().manual_seed(1))
+    grads = [torch.randn(20, 12, generator=torch.Generator().manual_seed(s)) for s in range(4)]
+    params = [torch.nn.Parameter(start.clone().cuda()) for _ in range(2)]
+    for p in params:
+        p.grad = grads[0].cuda()
+    opts = [Orthogonal([p], weight_decay=0.5) for p in params]
+    with pytest.raises(RuntimeError, match="before the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            opts[0].step()
+    for o in opts:
+        o.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opts[0].step()
+    for g in grads[1:]:
+        for p in params:
+            p.grad.copy_(g)
+        graph.replay()
+        opts[1].step()
+        torch.cuda.synchronize()
+        assert torch.equal(params[0], params[1])
+
+
 def test_training_with_positions_runs():
     """Several columns in one segment, an entry's column as its position: every
     parameter gets a finite gradient and a step, and answers change with the
