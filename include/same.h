@@ -677,8 +677,8 @@ int same_dropout(int32_t dtype, const void *x, int64_t x_row, const void *residu
  * strides and alignment as in same_cross_attention, without the limit on a
  * token's (0 repeats); either may have no tokens.  head_dim is a multiple of 8
  * up to 128, rot_dim even (0: no rotation, positions and angles are not used),
- * angles a host array of rot_dim / 2 radians per position, positions int32 on
- * the device, of any sign.  The weights are fp32 [head_dim], null: ones.  eps
+ * angles a host array of rot_dim / 2 radians per position, within 2^40,
+ * positions int32 on the device, of any sign.  The weights are fp32 [head_dim], null: ones.  eps
  * is a positive normal number in 32 bits.  q_out and k_out are contiguous
  * [tokens][heads][head_dim] of dtype and may be q or k themselves where those
  * are contiguous; they overlap nothing else.

@@ -56,6 +56,21 @@ struct Heads {
     const int32_t *positions;
 };
 
+constexpr double kMaxAngle = (double)((int64_t)1 << 40);
+
+// An angle in turns, less the whole ones, which no whole position notices: of what is
+// left a position of 2^31 asks for all 64 bits.  2 pi is taken off in three parts, of
+// which the first two have 23 bits, so that their products with up to 2^38 turns are
+// exact.
+long double turn_of_angle(double angle) {
+    const long double turns = 1.0L / 6.283185307179586476925286766559L;
+    if (std::fabs(angle) <= 3.0) return (long double)angle * turns;   // none whole
+    const long double whole = std::rint((long double)angle * turns);
+    const long double rest =
+        (((long double)angle - whole * 0x6.487EDp0L) - whole * 0x5.110B4p-24L) - whole * 0x6.11A62633145C06E0Ep-48L;
+    return rest * turns;
+}
+
 int check_heads(const std::string &name, const void *p, int64_t row, int64_t head, int64_t tokens, int64_t heads,
                 int64_t dim, int64_t size, std::vector<Extent> &reads) {
     if (tokens == 0) return SAME_OK;
@@ -82,10 +97,9 @@ int check_norm(int32_t dtype, int32_t dim, const Heads &q, const Heads &k, doubl
         return record_error(SAME_EINVAL, "rot_dim must be even, in [0, head_dim]");
     if (rot_dim && !angles) return record_error(SAME_EINVAL, "angles is null");
     std::memset((void *)&p, 0, sizeof(p));
-    const long double turns = 1.0L / 6.283185307179586476925286766559L;
     for (int i = 0; i < rot_dim / 2; ++i) {
-        if (!std::isfinite(angles[i])) return record_error(SAME_EINVAL, "angles must be finite");
-        const long double t = (long double)angles[i] * turns;
+        if (!(std::fabs(angles[i]) <= kMaxAngle)) return record_error(SAME_EINVAL, "angles must lie within 2^40");
+        const long double t = turn_of_angle(angles[i]);
         p.turn[i] = (double)t;
         p.turn_low[i] = (double)(t - (long double)p.turn[i]);
     }

@@ -1,5 +1,7 @@
 """Norms of queries and keys with the position rotation against their
 definition in 64 bits."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -247,6 +249,23 @@ def test_far_positions(far):
                       z[..., 4:] * whole.cos() + z[..., :4] * whole.sin()], dim=-1)
     room = abs(far) * 2 * np.pi * 2.0 ** -53 + 32 * U
     assert bool(((got.cpu().double() - want).abs() <= room * (z[..., :4].abs() + z[..., 4:].abs()).repeat(1, 1, 2)).all())
+
+
+@pytest.mark.parametrize("far", [1, 1000, -(1 << 20), (1 << 31) - 1])
+def test_large_angles(far):
+    """Angles of many turns a position: their place in the turn from 60 digits of pi."""
+    two_pi = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459")
+    turns = np.array([0.7, -3.5, 12345.678, 1e9 + 0.1, -1e12 - 0.3, 2.0 ** 40, 500.25, 1e6 + 0.7])
+    q, k = heads(1, 2, 16, torch.float32, 1), heads(0, 1, 16, torch.float32, 2)
+    pos, got = torch.tensor([far], dtype=torch.int32, device="cuda"), torch.empty_like(q)
+    same.same_qk_norm(q, k, got, k, q_positions=pos, k_positions=pos[:0], angles=turns)
+    place = torch.tensor([float(Fraction(a) * far / two_pi % 1) for a in turns], dtype=torch.float64) * 2 * np.pi
+    x = q.cpu().double()
+    z = x / (x.square().mean(-1, keepdim=True) + float(np.float32(1e-6))).sqrt()
+    want = torch.cat([z[..., :8] * place.cos() - z[..., 8:] * place.sin(),
+                      z[..., 8:] * place.cos() + z[..., :8] * place.sin()], dim=-1)
+    room = 32 * U + abs(far) * 2 * np.pi * 2.0 ** -63   # a turn's 64 bits, of at most half of one, twice rounded
+    assert bool(((got.cpu().double() - want).abs() <= room * (z[..., :8].abs() + z[..., 8:].abs()).repeat(1, 1, 2)).all())
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])

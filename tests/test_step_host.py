@@ -40,6 +40,7 @@ def norm_rc(lib, backward=False, **kw):
     (same.SAME_EINVAL, dict(rot_dim=-2)), (same.SAME_EINVAL, dict(rot_dim=7)), (same.SAME_EINVAL, dict(rot_dim=66)),
     (same.SAME_EINVAL, dict(rot_dim=8)),
     (same.SAME_EINVAL, dict(rot_dim=2, angles=np.array([np.inf]))),
+    (same.SAME_EINVAL, dict(rot_dim=2, angles=np.array([-1.1e12]))),
     (same.SAME_EINVAL, dict(rot_dim=2, angles=np.array([1.0]), q_tokens=1)),
     (same.SAME_EINVAL, dict(q_tokens=-1)), (same.SAME_EINVAL, dict(heads_kv=0)), (same.SAME_ESIZE, dict(heads_q=65537)),
     (same.SAME_ESIZE, dict(q_tokens=1 << 40)), (same.SAME_ESIZE, dict(q_tokens=1 << 39, q_row=1 << 40)),
