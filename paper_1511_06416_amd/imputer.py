@@ -218,6 +218,8 @@ class Orthogonal(torch.optim.Optimizer):
         shape = group["shape"]
         if shape is not None:
             rows, cols = shape
+            if rows < 1 or cols < 1:
+                raise ValueError("shape must be a matrix's, got %s" % (tuple(shape),))
             if p.numel() % (rows * cols):
                 raise ValueError("a parameter of shape %s holds no whole matrices of %d x %d"
                                  % (tuple(p.shape), rows, cols))
@@ -248,7 +250,7 @@ class Orthogonal(torch.optim.Optimizer):
         for group in self.param_groups:
             lr, momentum = group["lr"], group["momentum"]
             for p in group["params"]:
-                if p.grad is None:
+                if p.grad is None or not p.numel():
                     continue
                 shape = self._shape(p, group)
                 state = self.state[p]

@@ -154,3 +154,15 @@ def test_orthogonal_refusals():
     imputer.Orthogonal([p], shape=(4, 4))
     with pytest.raises(ValueError):
         imputer.Imputer(3, 2, rot_dim=8)
+
+
+def test_matrices_without_entries():
+    p = torch.nn.Parameter(torch.zeros(6, 8))
+    for shape in ((0, 4), (4, 0), (-2, 4)):
+        with pytest.raises(ValueError, match="shape"):
+            imputer.Orthogonal([p], shape=shape)
+    empty = [torch.nn.Parameter(torch.zeros(s)) for s in ((3, 0), (0, 3), (2, 4, 0), (0, 4, 4))]
+    opt = imputer.Orthogonal(empty)
+    for e in empty:
+        e.grad = torch.zeros_like(e)
+    opt.step()
