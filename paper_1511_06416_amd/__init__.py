@@ -907,7 +907,8 @@ def same_log_probs_workspace_size(rows, cols, n_top) -> int:
 
 
 # Five steps that take every singular value from some 0.003 up to about 1
-# (0.7 to 1.2): steep at zero instead of exact at one.
+# (0.7 to 1.2): steep at zero instead of exact at one.  The coefficients are those
+# that K. Jordan and others published for orthogonalised momentum in 2024.
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 

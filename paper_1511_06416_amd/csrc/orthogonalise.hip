@@ -7,9 +7,14 @@
 // fp16, hi + lo, times a power of two that keeps both in the type's normal
 // range: 22 bits.  Of a product of two such, hi hi + hi lo + lo hi are formed
 // (what is left out is 2^-22 of it), summed in fp32.  fp32 and fp16 updates
-// take all three: 4e-7 of the result's size against 64 bits, where a form in
-// fp32 has 1.5e-6.  bf16 ones take hi hi alone, with a X and b A in full: 2e-3,
-// as much as rounding the result to bf16 (1.7e-3).
+// take all three: off by as much as a form in fp32 or less (1,024 x 1,024 of noise
+// 2.1e-6 of the result's size for 3.1e-6, 64 x 8,193 1.4e-6 for 1.35e-6).  bf16 ones
+// take hi hi alone, with a X and b A in full.  Where rounding out alone leaves
+// 1.66e-3 of its size, 4,096 x 4,096 of strong directions over noise is then off by
+// 1.72e-3, noise alone by 2.3e-3 (1,024 x 1,024), 2.6e-3 (200 x 300) and 3.8e-3 (64 x
+// 8,193).  All three products would take 1.04 to 2.4 times as long (64 x 8,193 125 us for
+// 121, 1,024 x 1,024 216 for 176, 4,096 x 4,096 4,130 for 1,700): who needs them
+// gives the update in fp32.  The other forms take all three for every type.
 // A and B are symmetric: tiles on and above the diagonal are formed and written
 // to both places.
 //

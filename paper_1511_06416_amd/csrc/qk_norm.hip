@@ -14,7 +14,7 @@
 //
 // Measured: 65,536 tokens of 16 + 4 heads of 128 in bf16 124 us, 5.4 TB/s, the
 // copy's rate.  The 21,120 tokens stay in the last-level cache: 23 us (3.8 TB/s,
-// vector units two thirds busy) and, with the gradient, 29 (4.5 TB/s, loads under
+// vector units two thirds busy) and, with the gradient, 28 (4.6 TB/s, loads under
 // way: more blocks make more parts of the weights' gradients, 32 us with 1,536
 // blocks for 1,024).
 #include <algorithm>
@@ -130,7 +130,8 @@ int pack_of(const NormSide &s, int lanes) {
 }
 
 // Rows of which a lane sums the weights' gradients in 32 bits before they go to a
-// sum in 64, so that the error does not grow with the tokens.
+// sum in 64, so that the error does not grow with the tokens (in 32 bits alone it was
+// 10^-5 of a sum of 2^24 equal terms; the times are the same).
 constexpr int kRun = 16;
 
 // A row's loads are under way while the one before it is worked on.  With LANES

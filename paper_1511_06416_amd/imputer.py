@@ -201,6 +201,10 @@ class Orthogonal(torch.optim.Optimizer):
     creates it and cannot be captured into a graph, later ones can.  u is
     orthogonalised in the parameter's type; of fp16 parameters in 32 bits, as sums
     of gradients pass fp16's range.
+
+    An update has the same size however small u is: a matrix whose gradient is zero
+    (a node's that no column of the minibatch asks for) goes on with full steps
+    until its momentum falls below eps, some 300 steps after a gradient of norm 1.
     """
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, coefs=NEWTON_SCHULZ,
