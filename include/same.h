@@ -781,13 +781,8 @@ int same_log_probs_backward(int32_t dtype, const void *logits, int64_t row_strid
  * step by step); eps is a positive normal number in 32 bits.
  *
  * Sums of squares are 64-bit, products' sums fp32, of operands held as two
- * fp16 each (22 bits); with a smaller side up to 32 all of it is 64-bit.  In
- * SAME_BF16 products take the first of the two alone, while a X and b A are
- * whole, where the smaller side is over 128, or over 96, 64 or 32 with a larger
- * side over 128, 256 or 8,192.  The result is then off by up to 2.3 times what
- * its rounding to bf16 makes of it (measured; noise of 64 x 8,193), elsewhere by
- * that rounding; an update given in SAME_F32 takes both whatever its size.
- * workspace (same_orthogonalise_workspace_size, 256-byte aligned)
+ * fp16 each (22 bits), whatever dtype is; with a smaller side up to 32 all of it
+ * is 64-bit.  workspace (same_orthogonalise_workspace_size, 256-byte aligned)
  * serves one call at a time.  Errors: SAME_EINVAL, SAME_EALIGN, SAME_ESIZE (a
  * matrix of over 2^15 by 2^24 or 1.1 10^9 elements), SAME_EHIP, SAME_ENOMEM.
  */

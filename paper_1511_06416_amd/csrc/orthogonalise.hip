@@ -6,21 +6,18 @@
 // Products run on the fp16 matrix units.  A number is held as the sum of two
 // fp16, hi + lo, times a power of two that keeps both in the type's normal
 // range: 22 bits.  Of a product of two such, hi hi + hi lo + lo hi are formed
-// (what is left out is 2^-22 of it), summed in fp32.  fp32 and fp16 updates
-// take all three: off by as much as a form in fp32 or less (1,024 x 1,024 of noise
-// 2.1e-6 of the result's size for 3.1e-6, 64 x 8,193 1.4e-6 for 1.35e-6).  bf16 ones
-// take hi hi alone, with a X and b A in full.  Where rounding out alone leaves
-// 1.66e-3 of its size, 4,096 x 4,096 of strong directions over noise is then off by
-// 1.72e-3, noise alone by 2.3e-3 (1,024 x 1,024), 2.6e-3 (200 x 300) and 3.8e-3 (64 x
-// 8,193).  All three products would take 1.04 to 2.4 times as long (64 x 8,193 125 us for
-// 121, 1,024 x 1,024 216 for 176, 4,096 x 4,096 4,130 for 1,700): who needs them
-// gives the update in fp32.  The other forms take all three for every type.
+// (what is left out is 2^-22 of it), summed in fp32, for every type: off by as much
+// as a form in fp32 or less (1,024 x 1,024 of noise 2.1e-6 of the result's size for
+// 3.1e-6, 64 x 8,193 1.4e-6 for 1.35e-6).  hi hi alone was tried for bf16: 4,096 x
+// 4,096 took 1,690 us, but noise of 64 x 8,193 was off by 3.8e-3 and of 200 x 300 by
+// 2.6e-3, where rounding out leaves 1.66e-3.
 // A and B are symmetric: tiles on and above the diagonal are formed and written
 // to both places.
 //
-// Measured: 4,096 x 4,096 in bf16, five steps, 1,643 us, 836 TFLOP/s of what has to
-// be computed; a step is 84 us for A, 89 for B, 142 to 158 for X, matrix units 44 to
-// 55 % busy.  In fp32 four of 1,024 x 1,024 take 534 us, where a form in fp32
+// Measured: 4,096 x 4,096 in bf16, five steps, 4,060 us (fp32 4,080): 1,015 TFLOP/s of
+// the three products that have to be computed, where a large library product of fp16
+// reaches 1,117; a step is 215 us for A, 224 for B, 344 to 366 for X, matrix units 50
+// to 67 % busy.  In fp32 four of 1,024 x 1,024 take 540 us, where a form in fp32
 // products takes 1,450.
 #include <algorithm>
 
@@ -74,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void ortho_squares_kernel(OrthoParams p, 
 }
 
 // X in planes, both ways, zeros around it: a block takes 64 x 64.
-template <typename T, bool LOW>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, int parts, int tiles_i, int tiles_j) {
     __shared__ float tile[64][65];
     const int tiles = tiles_i * tiles_j;
@@ -118,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void ortho_split_kernel(OrthoParams p, in
             split_all<8>([&](int e) { return tile[r][c + e]; }, hi, lo);
             const int64_t to = x0 + (int64_t)(i0 + r) * p.mp + j0 + c;
             *(f16x8 *)(p.x.hi + to) = hi;
-            if (LOW) *(f16x8 *)(p.x.lo + to) = lo;
+            *(f16x8 *)(p.x.lo + to) = lo;
         }
         if (j0 + r < p.mp && i0 + c < p.np) {
             split_all<8>([&](int e) { return tile[c + e][r]; }, hi, lo);
@@ -153,13 +150,10 @@ enum Kind { kGram, kSquare, kUpdate, kLast };
 // What a product becomes, from a tile of 32 x 32 that a wave holds in LDS, column
 // by column: both of its places are read and written 16 bytes a lane, 64 bytes of
 // a row.
-template <typename T, int KIND, int PL>
+template <typename T, int KIND>
 __device__ __forceinline__ void leave(const OrthoParams &p, int64_t mat, int step, int i0, int j0,
                                       float (*turn)[kTurn]) {
     constexpr bool symmetric = KIND == kGram || KIND == kSquare;
-    // Second halves are read by three products, or as what stays of the old: by
-    // the next square at A[j][i], by the next update at X^T.
-    constexpr bool kLowT = PL == 2 || KIND != kSquare, kLowD = PL == 2;
     const int lane = threadIdx.x & 63;
     const float keep = KIND == kGram ? 0.0f : KIND == kSquare ? p.coef[step][1] * (p.sb / p.sa) : p.coef[step][0];
     const float take = KIND == kGram     ? p.sa / (p.sx * p.sx)
@@ -202,7 +196,7 @@ __device__ __forceinline__ void leave(const OrthoParams &p, int64_t mat, int ste
             if (p.tall) write_out<T>(p, mat, j0 + j, p.m, i0 + i, p.n, v);
         } else {
             *(f16x8 *)(to_t.hi + at) = hi;
-            if (kLowT) *(f16x8 *)(to_t.lo + at) = lo;
+            *(f16x8 *)(to_t.lo + at) = lo;
         }
     }
     wave::sync();
@@ -220,7 +214,7 @@ __device__ __forceinline__ void leave(const OrthoParams &p, int64_t mat, int ste
             split_all<8>([&](int e) { return v[e >> 2][e & 3]; }, hi, lo);
             const int64_t at = t0 + (int64_t)(i0 + i) * ld_d + j0 + j;
             *(f16x8 *)(to_d.hi + at) = hi;
-            if (kLowD) *(f16x8 *)(to_d.lo + at) = lo;
+            *(f16x8 *)(to_d.lo + at) = lo;
         }
     }
 }
@@ -249,9 +243,9 @@ __device__ __forceinline__ void arrive() {
 // but one under way; rows of 64 bytes, whose 16-byte chunks are turned by the row
 // so that a read of 32 rows meets no bank twice.  Rows past the matrix repeat
 // its last one and are not written.
-template <typename T, int TM, int TN, int WM, int WN, int STAGES, int PROD, int KIND>
+template <typename T, int TM, int TN, int WM, int WN, int STAGES, int KIND>
 __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams p, int step, int tiles_i, int tiles_j) {
-    constexpr int THREADS = WM * WN * 64, MT = TM / WM / 32, NT = TN / WN / 32, PL = PROD == 1 ? 1 : 2;
+    constexpr int THREADS = WM * WN * 64, MT = TM / WM / 32, NT = TN / WN / 32, PL = 2;   // planes
     constexpr int kLoadsP = TM * 4 / THREADS, kLoadsQ = TN * 4 / THREADS;   // 16-byte loads a lane, per plane
     constexpr int kLoads = PL * (kLoadsP + kLoadsQ), kRows = PL * (TM + TN);
     static_assert(kLoadsP * THREADS == TM * 4 && kLoadsQ * THREADS == TN * 4, "every lane stages the same");
@@ -309,12 +303,12 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
 #pragma unroll
         for (int l = 0; l < kLoadsP; ++l) {
             load(left_hi, off_p[l], k, to_p + l * 512);
-            if (PL == 2) load(left_lo, off_p[l], k, to_p + TM * kStage + l * 512);
+            load(left_lo, off_p[l], k, to_p + TM * kStage + l * 512);
         }
 #pragma unroll
         for (int l = 0; l < kLoadsQ; ++l) {
             load(right_hi, off_q[l], k, to_q + l * 512);
-            if (PL == 2) load(right_lo, off_q[l], k, to_q + TN * kStage + l * 512);
+            load(right_lo, off_q[l], k, to_q + TN * kStage + l * 512);
         }
     };
     f32x16 acc[MT][NT];
@@ -348,10 +342,8 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                if (PL == 2) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[PL - 1][i], o.r[0][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[0][i], o.r[PL - 1][j], acc[i][j], 0, 0, 0);
-                }
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[1][i], o.r[0][j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[0][i], o.r[1][j], acc[i][j], 0, 0, 0);
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.l[0][i], o.r[0][j], acc[i][j], 0, 0, 0);
             }
         __builtin_amdgcn_s_setprio(0);
@@ -410,14 +402,13 @@ __global__ __launch_bounds__(WM * WN * 64) void ortho_product_kernel(OrthoParams
                     to[1] = *(const f32x4 *)&turn[j][i + 4];
                 }
             } else {
-                leave<T, KIND, PL>(p, mat, step, i0, j0, turn);
+                leave<T, KIND>(p, mat, step, i0, j0, turn);
             }
             wave::sync();
         }
 }
 
 // A, from the parts of its sums: a wave takes 32 x 32 on or above the diagonal.
-template <int PL>
 __global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoParams p, int tiles) {
     __shared__ float turns[kThreads / 64][32][kTurn];
     const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -441,14 +432,14 @@ __global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoParams p, int
         *(f32x4 *)&turns[own][j][i + 4] = v[1];
     }
     wave::sync();
-    leave<float, kGram, PL>(p, mat, 0, 32 * ti, 32 * tj, turns[own]);
+    leave<float, kGram>(p, mat, 0, 32 * ti, 32 * tj, turns[own]);
 }
 
-template <typename T, int TILE, int WM, int WN, int STAGES, int PROD, int KIND>
+template <typename T, int TILE, int WM, int WN, int STAGES, int KIND>
 void run_product(const OrthoParams &p, int step, hipStream_t s) {
     const int ti = (p.np + TILE - 1) / TILE, tj = ((KIND == kGram || KIND == kSquare ? p.np : p.mp) + TILE - 1) / TILE;
     const int tiles = KIND == kGram || KIND == kSquare ? ti * (ti + 1) / 2 : ti * tj;
-    ortho_product_kernel<T, TILE, TILE, WM, WN, STAGES, PROD, KIND>
+    ortho_product_kernel<T, TILE, TILE, WM, WN, STAGES, KIND>
         <<<dim3(tiles, (uint32_t)p.n_mats, KIND == kGram ? p.splits : 1), WM * WN * 64, 0, s>>>(p, step, ti, tj);
 }
 
@@ -462,14 +453,9 @@ struct TileCost {
     int together;
     double full_stage, full_way;      // of the full device, a tile a compute unit
 };
-template <int PROD>
 int pick_tile(const OrthoParams &p, bool symmetric, int depth, int splits) {
     constexpr int kTiles[4] = {64, 128, 192, 256};
-    constexpr TileCost kOne[4] = {{3.19, 0.27, 0.00, 6, 0.15, 1.03},
-                                  {7.20, 0.28, 0.00, 3, 0.38, 4.84},
-                                  {5.05, 0.65, 1.48, 1, 0.71, 9.88},
-                                  {6.62, 0.82, 0.44, 1, 1.32, 12.59}};
-    constexpr TileCost kThree[4] = {{4.35, 0.25, 0.00, 3, 0.28, 1.47},
+    constexpr TileCost kCosts[4] = {{4.35, 0.25, 0.00, 3, 0.28, 1.47},
                                     {5.91, 0.86, 0.00, 2, 0.88, 8.33},
                                     {4.43, 1.67, 2.33, 1, 1.41, 20.31},
                                     {5.93, 2.03, 1.89, 1, 3.11, 11.10}};
@@ -477,7 +463,7 @@ int pick_tile(const OrthoParams &p, bool symmetric, int depth, int splits) {
     int best = 0;
     double least = 0.0;
     for (int t = 0; t < 4; ++t) {
-        const TileCost &c = PROD == 1 ? kOne[t] : kThree[t];
+        const TileCost &c = kCosts[t];
         const int64_t ti = (p.np + kTiles[t] - 1) / kTiles[t], tj = (p.mp + kTiles[t] - 1) / kTiles[t];
         const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * p.n_mats * splits;
         const int64_t rounds = ((tiles + 255) / 256 + c.together - 1) / c.together;
@@ -491,30 +477,29 @@ int pick_tile(const OrthoParams &p, bool symmetric, int depth, int splits) {
     return best;
 }
 
-template <typename T, int PROD, int KIND>
+template <typename T, int KIND>
 void run_pass(const OrthoParams &p, int step, hipStream_t s) {
-    switch (pick_tile<PROD>(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np, KIND == kGram ? p.splits : 1)) {
-    case 0: return run_product<T, 64, 2, 2, 3, PROD, KIND>(p, step, s);
-    case 1: return run_product<T, 128, 2, 2, PROD == 1 ? 3 : 2, PROD, KIND>(p, step, s);
-    case 2: return run_product<T, 192, 2, PROD == 1 ? 3 : 2, PROD == 1 ? 4 : 3, PROD, KIND>(p, step, s);
-    default: return run_product<T, 256, 2, 4, PROD == 1 ? 3 : 2, PROD, KIND>(p, step, s);
+    switch (pick_tile(p, KIND == kGram || KIND == kSquare, KIND == kGram ? p.mp : p.np, KIND == kGram ? p.splits : 1)) {
+    case 0: return run_product<T, 64, 2, 2, 3, KIND>(p, step, s);
+    case 1: return run_product<T, 128, 2, 2, 2, KIND>(p, step, s);
+    case 2: return run_product<T, 192, 2, 2, 3, KIND>(p, step, s);
+    default: return run_product<T, 256, 2, 4, 2, KIND>(p, step, s);
     }
 }
 
-template <typename T, int PROD>
+template <typename T>
 hipError_t run_products(const OrthoParams &p, hipStream_t s) {
     for (int k = 0; k < p.steps; ++k) {
-        run_pass<float, PROD, kGram>(p, k, s);
+        run_pass<float, kGram>(p, k, s);
         if (p.splits > 1) {
             const int side = p.np / 32, tiles = side * (side + 1) / 2;
-            ortho_join_kernel<PROD == 1 ? 1 : 2>
-                <<<dim3((tiles + kThreads / 64 - 1) / (kThreads / 64), (uint32_t)p.n_mats), kThreads, 0, s>>>(p, tiles);
+            ortho_join_kernel<<<dim3((tiles + kThreads / 64 - 1) / (kThreads / 64), (uint32_t)p.n_mats), kThreads, 0, s>>>(p, tiles);
         }
-        run_pass<float, PROD, kSquare>(p, k, s);
+        run_pass<float, kSquare>(p, k, s);
         if (k + 1 < p.steps)
-            run_pass<float, PROD, kUpdate>(p, k, s);
+            run_pass<float, kUpdate>(p, k, s);
         else
-            run_pass<T, PROD, kLast>(p, k, s);
+            run_pass<T, kLast>(p, k, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -532,15 +517,15 @@ int run_squares(const OrthoParams &p, hipStream_t s) {
     return parts;
 }
 
-template <typename T, int PROD>
+template <typename T>
 hipError_t run_typed(const OrthoParams &p, hipStream_t s) {
     const uint32_t mats = (uint32_t)p.n_mats;
     const int parts = run_squares<T>(p, s);
     const int ti = (p.np + 63) / 64, tj = (p.mp + 63) / 64;
-    ortho_split_kernel<T, PROD != 1><<<mats * ti * tj, kThreads, 0, s>>>(p, parts, ti, tj);
+    ortho_split_kernel<T><<<mats * ti * tj, kThreads, 0, s>>>(p, parts, ti, tj);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return run_products<T, PROD>(p, s);
+    return run_products<T>(p, s);
 }
 
 }  // namespace
@@ -572,12 +557,12 @@ hipError_t launch_orthogonalise(const OrthoParams &all, int64_t batch, int dtype
         p.n_mats = std::min(batch, all.n_mats - first);
         p.g = (const char *)all.g + first * all.g_mat * size;
         p.out = (char *)all.out + first * all.out_mat * size;
-        const hipError_t e = p.n <= kSmallSide                          ? launch_ortho_small(p, dtype, s)
-                             : ortho_whole(p.n, p.m)                    ? launch_ortho_whole(p, dtype, s)
-                             : ortho_columns(p.n, p.m, dtype == 2)      ? launch_ortho_columns(p, dtype, s)
-                             : dtype == 2 ? run_typed<__bf16, 1>(p, s)
-                             : dtype == 1 ? run_typed<_Float16, 3>(p, s)
-                                          : run_typed<float, 3>(p, s);
+        const hipError_t e = p.n <= kSmallSide           ? launch_ortho_small(p, dtype, s)
+                             : ortho_whole(p.n, p.m)     ? launch_ortho_whole(p, dtype, s)
+                             : ortho_columns(p.n, p.m)   ? launch_ortho_columns(p, dtype, s)
+                             : dtype == 2 ? run_typed<__bf16>(p, s)
+                             : dtype == 1 ? run_typed<_Float16>(p, s)
+                                          : run_typed<float>(p, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -225,7 +225,7 @@ int ortho_layout(int32_t dtype, int64_t n_mats, int64_t rows, int64_t cols, Orth
         l.total = 0;
         return SAME_OK;
     }
-    if (same::ortho_columns(l.n, l.m, dtype == SAME_BF16)) {
+    if (same::ortho_columns(l.n, l.m)) {
         size_t x, part, plane;
         same::ortho_columns_layout(l.n, l.m, &l.parts, &l.part_cols, &x, &part, &plane);
         // some 2^30 bytes of X

@@ -129,11 +129,10 @@ inline bool ortho_whole(int64_t n, int64_t m) {
 hipError_t launch_ortho_whole(const OrthoParams &p, int dtype, hipStream_t s);
 
 // Updates of which each block holds some columns, at most 16 parts of four strips
-// of 128; one_product: the tiled form would take one (us, here and there: 60 x
-// 1,000 52 and 91, in one product 85; 750 of 905 x 33 613 and 1,012, 736; 128 x
-// 1,000 85 and 102, 94; 30 of 100 x 1,500 191 and 216, 167).
-inline bool ortho_columns(int64_t n, int64_t m, bool one_product) {
-    return n <= 64 ? m <= 8192 : n <= 128 && m <= 4096 && !one_product;
+// of 128 (us, here and in the tiled form: 60 x 1,000 52 and 91; 750 of 905 x 33 613
+// and 1,012; 128 x 1,000 85 and 102; 30 of 100 x 1,500 191 and 216).
+inline bool ortho_columns(int64_t n, int64_t m) {
+    return n <= 64 ? m <= 8192 : n <= 128 && m <= 4096;
 }
 void ortho_columns_layout(int64_t n, int64_t m, int32_t *parts, int32_t *part_cols, size_t *x_bytes,
                           size_t *part_bytes, size_t *plane_bytes);

@@ -157,6 +157,25 @@ def test_the_smallest_eps(rows, cols, dtype):
         check(out[i], g[i], eps=eps)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,rows,cols", [(3, 7, 30), (2, 30, 2000), (2, 64, 100), (2, 250, 90), (2, 100, 128), (2, 60, 1000),
+                                         (2, 1500, 100), (1, 128, 4096), (1, 64, 8193), (1, 97, 4097), (2, 129, 129),
+                                         (3, 200, 300), (40, 200, 300), (1, 1030, 1000), (1, 300, 9000)])
+def test_16_bits_are_the_rounding_of_32(n, rows, cols, dtype):
+    """A 16-bit update is the 32-bit one of the same numbers, rounded once, bit for bit: no form
+    multiplies in fewer bits for its type.  Smaller sides up to 32 are formed in 64 bits and
+    rounded from there; by way of 32 that differs only where the 32-bit number lies halfway
+    between two of 16, which are then equally far from it."""
+    for kind in ("random", "strong"):
+        g = matrices(n, rows, cols, dtype, 11, kind)
+        got, whole = run(g), run(g.float())
+        want = whole.to(dtype)
+        if min(rows, cols) > 32:
+            assert torch.equal(got, want)
+        else:
+            assert torch.equal((got.double() - whole.double()).abs(), (want.double() - whole.double()).abs())
+
+
 def test_orthogonal():
     """Steps that converge give the polar factor: U U^T = 1."""
     g = matrices(2, 60, 200, torch.float32, 9)
